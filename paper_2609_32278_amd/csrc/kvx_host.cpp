@@ -26,6 +26,7 @@ using kvx::check_align;
 using kvx::check_batch;
 using kvx::check_page_ids;
 using kvx::hip_fail;
+using kvx::inline_store_reqs;
 using kvx::Staging;
 using kvx::validate_mode;
 using kvx::Workspace;
@@ -853,32 +854,6 @@ std::vector<uint8_t> plan_blob(const std::vector<U>& units, const std::vector<M>
   if (mb) std::memcpy(blob.data() + ub, merges.data(), mb);
   if (db) std::memcpy(blob.data() + ub + mb, dec_merges.data(), db);
   return blob;
-}
-
-// The requests of a store batch in the kernel arguments when there are few enough
-// (returns false otherwise: the unit list is uploaded instead).  Workgroup order
-// matches the unit lists below: request by request, logical page by page.
-bool inline_store_reqs(const kvx_batch* b, const std::vector<int64_t>& qo, kvx::StoreReqs& rq) {
-  rq.n = 0;
-  int32_t wg = 0;
-  for (int r = 0; r < b->num_reqs; r++) {
-    const int64_t P = b->prefix_lens[r], E = b->extend_lens[r];
-    if (E == 0) continue;
-    if (rq.n == kvx::kStoreInlineReqs) {
-      rq.n = 0;
-      return false;
-    }
-    const int64_t pages = (P + E - 1) / kvx::kPageSize - P / kvx::kPageSize + 1;
-    rq.first[rq.n] = wg;
-    rq.qo[rq.n] = (int32_t)qo[(size_t)r];
-    rq.prefix[rq.n] = (int32_t)P;
-    rq.end[rq.n] = (int32_t)(P + E);
-    rq.page_base[rq.n] = b->page_indptr[r];
-    wg += (int32_t)pages;
-    rq.n++;
-  }
-  rq.first[rq.n] = wg;
-  return rq.n > 0;
 }
 
 // A decode batch that reads more K/V than the 256 MB Infinity Cache holds may use non-temporal

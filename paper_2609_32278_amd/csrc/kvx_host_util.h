@@ -182,4 +182,30 @@ inline int check_page_ids(int64_t num_pages, const kvx_batch* b, hipStream_t str
   return KVX_OK;
 }
 
+// The requests of a store batch in the kernel arguments when there are few enough
+// (returns false otherwise: the unit list is uploaded instead).  Workgroup order
+// matches the unit lists below: request by request, logical page by page.
+inline bool inline_store_reqs(const kvx_batch* b, const std::vector<int64_t>& qo, StoreReqs& rq) {
+  rq.n = 0;
+  int32_t wg = 0;
+  for (int r = 0; r < b->num_reqs; r++) {
+    const int64_t P = b->prefix_lens[r], E = b->extend_lens[r];
+    if (E == 0) continue;
+    if (rq.n == kStoreInlineReqs) {
+      rq.n = 0;
+      return false;
+    }
+    const int64_t pages = (P + E - 1) / kPageSize - P / kPageSize + 1;
+    rq.first[rq.n] = wg;
+    rq.qo[rq.n] = (int32_t)qo[(size_t)r];
+    rq.prefix[rq.n] = (int32_t)P;
+    rq.end[rq.n] = (int32_t)(P + E);
+    rq.page_base[rq.n] = b->page_indptr[r];
+    wg += (int32_t)pages;
+    rq.n++;
+  }
+  rq.first[rq.n] = wg;
+  return rq.n > 0;
+}
+
 }  // namespace kvx

@@ -1,0 +1,855 @@
+// Host side of latent attention: the C ABI declared in include/kvx_latent.h.
+//
+// Owns the pool, checks every argument before queuing work, plans the attention of ragged
+// (prefix, suffix) pairs over the 256 CUs and their 8 XCDs, and chooses the form of each
+// request.
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "kvx_host_util.h"
+#include "kvx_latent_internal.h"
+
+using kvx::ceil_div;
+using kvx::check_align;
+using kvx::check_batch;
+using kvx::check_page_ids;
+using kvx::hip_fail;
+using kvx::LatentExpandUnit;
+using kvx::LatentMerge;
+using kvx::LatentRows;
+using kvx::LatentTile;
+using kvx::LatentTileMerge;
+using kvx::LatentUnit;
+using kvx::report;
+using kvx::Staging;
+using kvx::Workspace;
+
+struct kvx_latent_pool {
+  int device = 0;
+  int64_t num_pages = 0;
+  int64_t page_bytes = 0;
+  int32_t latent_dim = 0;
+  int32_t dtype = KVX_LATENT_BF16;
+  int32_t split_keys = 0;
+  uint8_t* base = nullptr;
+  Staging st_rows, st_plan;
+  Workspace parts;     // partial results of split key ranges
+  Workspace absorbed;  // queries and sums in the latent space
+  Workspace expanded;  // keys and values of a group of heads
+};
+
+namespace {
+
+constexpr int kSlots = 256;  // CUs, one attention workgroup each
+constexpr int64_t kMaxPartBytes = 2ll << 30;
+constexpr int64_t kMaxExpandBytes = 2ll << 30;
+
+// Run an entry point's body: no exception crosses the ABI.
+template <typename F>
+int guarded(F&& body) {
+  report(KVX_OK, "%s", "");
+  try {
+    return body();
+  } catch (const std::bad_alloc&) {
+    return report(KVX_ENOMEM, "host memory for the plan of the call");
+  } catch (...) {
+    return report(KVX_EINVAL, "unexpected failure on the host");
+  }
+}
+
+// The pool's device for the length of a call.
+struct OnDevice {
+  int before = -1;
+  int enter(int device) {
+    KVX_HIP(hipGetDevice(&before));
+    if (before == device) before = -1;
+    else KVX_HIP(hipSetDevice(device));
+    return KVX_OK;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+int check_pool(const kvx_latent_pool* pool) {
+  if (pool == nullptr) return report(KVX_EINVAL, "pool is NULL");
+  return KVX_OK;
+}
+
+int check_stream(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  const hipError_t e = hipStreamIsCapturing(s, &st);
+  if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
+  if (st != hipStreamCaptureStatusNone)
+    return report(KVX_EUNSUPPORTED, "the stream is being captured: the plan of a call is made on the host");
+  return KVX_OK;
+}
+
+int check_scale(float sm_scale) {
+  if (!(sm_scale > 0.0f) || !std::isfinite(sm_scale)) return report(KVX_EINVAL, "sm_scale must be finite and > 0");
+  return KVX_OK;
+}
+
+// Heads, and rows of one request within an int32.
+int check_heads(const kvx_batch* b, int32_t Hq) {
+  if (Hq < 1 || Hq > 1024) return report(KVX_EINVAL, "num_q_heads = %d, must be in [1, 1024]", Hq);
+  for (int r = 0; r < b->num_reqs; r++)
+    if ((int64_t)b->extend_lens[r] * Hq > (int64_t)INT32_MAX - 1024)
+      return report(KVX_EUNSUPPORTED, "request %d: %d suffix tokens of %d heads are too many rows", r,
+                    b->extend_lens[r], Hq);
+  return KVX_OK;
+}
+
+// Byte ranges [a, a + n) and [b, b + n) that meet without being the same.
+bool overlap(const void* a, const void* b, size_t n) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x != y && x < y + n && y < x + n;
+}
+
+kvx::LatentPoolView view(const kvx_latent_pool* pool, const kvx_batch* batch) {
+  return {pool->base, pool->page_bytes, batch->page_ids};
+}
+
+// The touched pages of a batch's suffixes, request by request.
+std::vector<kvx::RopeUnit> page_units(const kvx_batch* batch, const std::vector<int64_t>& qo) {
+  std::vector<kvx::RopeUnit> units;
+  const int64_t S = kvx::kPageSize;
+  for (int r = 0; r < batch->num_reqs; r++) {
+    const int64_t P = batch->prefix_lens[r], E = batch->extend_lens[r], L = P + E;
+    if (E == 0) continue;
+    for (int64_t lp = P / S; lp <= (L - 1) / S; lp++) {
+      kvx::RopeUnit u;
+      u.row_slot0 = (int32_t)(qo[(size_t)r] + lp * S - P);
+      u.page_pos = (int32_t)(batch->page_indptr[r] + lp);
+      u.slot_begin = (int32_t)(std::max<int64_t>(P, lp * S) - lp * S);
+      u.slot_end = (int32_t)(std::min<int64_t>(L, lp * S + S) - lp * S);
+      u.pos_slot0 = (int32_t)(lp * S);
+      units.push_back(u);
+    }
+  }
+  return units;
+}
+
+// The units of a store or load call, in its arguments or uploaded.
+template <typename Params>
+int place_units(kvx_latent_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, hipStream_t s,
+                Params& p, int64_t& n_units) {
+  p.units = nullptr;
+  if (kvx::inline_store_reqs(batch, qo, p.reqs)) {
+    n_units = p.reqs.first[p.reqs.n];
+    return KVX_OK;
+  }
+  const std::vector<kvx::RopeUnit> units = page_units(batch, qo);
+  n_units = (int64_t)units.size();
+  void* dev = nullptr;
+  if (int rc = pool->st_rows.upload(units.data(), units.size() * sizeof(kvx::RopeUnit), s, &dev)) return rc;
+  p.units = (const kvx::RopeUnit*)dev;
+  return KVX_OK;
+}
+
+int check_stride(int64_t stride, int row, const char* name) {
+  if (stride < row || stride % 8 != 0 || stride > (int64_t)1 << 40)
+    return report(KVX_EINVAL, "%s = %lld: must be a multiple of 8, at least %d", name, (long long)stride, row);
+  return KVX_OK;
+}
+
+int store_call(kvx_latent_pool* pool, const kvx_batch* batch, const kvx_rope* rope, bool rotate, const void* q,
+               int32_t Hq, int32_t q_dim, void* q_out, const void* kv, int64_t kv_stride, hipStream_t s) {
+  if (int rc = check_pool(pool)) return rc;
+  std::vector<int64_t> qo;
+  if (int rc = check_batch(batch, qo)) return rc;
+  kvx::LatentStoreParams p{};
+  bool interleaved = false;
+  if (rotate) {
+    if (rope == nullptr) return report(KVX_EINVAL, "rope is NULL");
+    if (rope->rotary_dim != kvx::kLatRope)
+      return report(KVX_EINVAL, "rotary_dim = %d, must be the pool's rope_dim = %d", rope->rotary_dim, kvx::kLatRope);
+    if (rope->style != KVX_ROPE_HALF && rope->style != KVX_ROPE_INTERLEAVED)
+      return report(KVX_EINVAL, "style = %d", rope->style);
+    if (!(rope->norm_eps >= 0.0f) || !std::isfinite(rope->norm_eps))
+      return report(KVX_EINVAL, "norm_eps must be finite and >= 0");
+    if (rope->q_norm != nullptr) return report(KVX_EINVAL, "q_norm must be NULL");
+    if (int rc = check_align(rope->k_norm, "k_norm")) return rc;
+    for (int j = 0; j < kvx::kLatRope / 2; j++) {
+      double f;
+      if (rope->inv_freq) {
+        f = rope->inv_freq[j];
+        if (!(f >= 0.0) || !std::isfinite(f)) return report(KVX_EINVAL, "inv_freq[%d] must be finite and >= 0", j);
+      } else {
+        if (!(rope->theta > 0.0) || !std::isfinite(rope->theta))
+          return report(KVX_EINVAL, "theta must be finite and > 0");
+        f = std::pow(rope->theta, -2.0 * j / kvx::kLatRope);
+      }
+      p.rev_freq[j] = f / 6.283185307179586476925286766559;  // turns per position
+    }
+    interleaved = rope->style == KVX_ROPE_INTERLEAVED;
+    if (Hq < 0 || Hq > 1024) return report(KVX_EINVAL, "num_q_heads = %d, must be in [0, 1024]", Hq);
+    if (Hq > 0) {
+      if (!q || !q_out) return report(KVX_EINVAL, "q and q_out must be non-NULL");
+      if (q_dim < kvx::kLatRope || q_dim > 4096 || q_dim % 8 != 0)
+        return report(KVX_EINVAL, "q_dim = %d: must be a multiple of 8 in [%d, 4096]", q_dim, kvx::kLatRope);
+      if (int rc = check_align(q, "q")) return rc;
+      if (int rc = check_align(q_out, "q_out")) return rc;
+      if (overlap(q, q_out, (size_t)qo.back() * Hq * q_dim * 2))
+        return report(KVX_EINVAL, "q_out overlaps q without being q");
+    }
+    p.norm = (const uint16_t*)rope->k_norm;
+    p.norm_eps = rope->norm_eps;
+    p.rotate = 1;
+  }
+  if (int rc = check_stride(kv_stride, pool->latent_dim + kvx::kLatRope, "kv_stride")) return rc;
+  if (int rc = check_align(kv, "kv")) return rc;
+  if (qo.back() == 0) return KVX_OK;
+  if (!kv) return report(KVX_EINVAL, "kv is NULL");
+  OnDevice on;
+  if (int rc = on.enter(pool->device)) return rc;
+  if (int rc = check_stream(s)) return rc;
+  if (kvx::validate_mode())
+    if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
+  int64_t n_units = 0;
+  if (int rc = place_units(pool, batch, qo, s, p, n_units)) return rc;
+  p.pool = view(pool, batch);
+  p.kv = (const uint16_t*)kv;
+  p.kv_stride = kv_stride;
+  p.q = (const uint16_t*)q;
+  p.q_out = (uint16_t*)q_out;
+  p.num_q_heads = Hq;
+  p.q_dim = q_dim;
+  const hipError_t e =
+      kvx::launch_store_latent(p, n_units, pool->latent_dim, pool->dtype == KVX_LATENT_FP8, interleaved, s);
+  if (e != hipSuccess) return hip_fail(e, "store_latent kernel launch");
+  return p.units ? pool->st_rows.done(s) : KVX_OK;
+}
+
+// ------------------------------------------------------------------ plans
+
+// Host arrays of a call, uploaded in one piece.
+struct Blob {
+  std::vector<uint8_t> bytes;
+  template <typename U>
+  size_t add(const std::vector<U>& v) {
+    bytes.resize((bytes.size() + 15) / 16 * 16);
+    const size_t at = bytes.size();
+    bytes.resize(at + v.size() * sizeof(U));
+    if (!v.empty()) std::memcpy(bytes.data() + at, v.data(), v.size() * sizeof(U));
+    return at;
+  }
+};
+
+// Work that shares its keys, to run on one XCD: units [first, first + count).
+struct Group {
+  int64_t cost;
+  int32_t first, count;
+};
+
+// Units in launch order (workgroup i runs on XCD i % 8): groups, longest first, each to the
+// XCD with the least work so far; shorter queues are padded with empty units.
+template <typename U>
+std::vector<U> spread(const std::vector<U>& units, std::vector<Group>& groups) {
+  std::stable_sort(groups.begin(), groups.end(), [](const Group& a, const Group& b) { return a.cost > b.cost; });
+  std::vector<int32_t> queue[kvx::kNumXcd];
+  int64_t load[kvx::kNumXcd] = {};
+  for (const Group& g : groups) {
+    int x = 0;
+    for (int i = 1; i < kvx::kNumXcd; i++)
+      if (load[i] < load[x]) x = i;
+    load[x] += g.cost * g.count;
+    for (int32_t i = 0; i < g.count; i++) queue[x].push_back(g.first + i);
+  }
+  size_t most = 0;
+  for (const auto& q : queue) most = std::max(most, q.size());
+  std::vector<U> out(most * kvx::kNumXcd);  // value-initialised: padding
+  for (size_t x = 0; x < (size_t)kvx::kNumXcd; x++)
+    for (size_t i = 0; i < queue[x].size(); i++) out[i * kvx::kNumXcd + x] = units[(size_t)queue[x][i]];
+  while (!out.empty() && out.back().key_end == 0) out.pop_back();
+  return out;
+}
+
+// What a plan's length search sees of a request: `tiles` tiles of rows over about `len` steps
+// of 64 keys each.
+struct Span {
+  int64_t tiles, len;
+};
+
+// Steps of 64 keys that a part should have at most; 0: nothing is split.  Cost of a unit
+// besides its steps: kStart; of a part, its result written and read again: kPart.
+constexpr double kStart = 2.0, kPart = 1.0;
+int64_t choose_steps(const std::vector<Span>& spans) {
+  int64_t work = 0, longest = 0;
+  for (const Span& s : spans) {
+    work += s.tiles * s.len;
+    longest = std::max(longest, s.len);
+  }
+  if (work == 0) return 0;
+  auto estimate = [&](int64_t c) {
+    double total = 0.0, top = 0.0;
+    int64_t units = 0;
+    for (const Span& s : spans) {
+      const int64_t parts = c > 0 ? ceil_div(s.len, c) : 1;
+      const double each = (double)ceil_div(s.len, parts) + kStart + (parts > 1 ? kPart : 0.0);
+      total += (double)(s.tiles * parts) * each;
+      units += s.tiles * parts;
+      top = std::max(top, each);
+    }
+    const double merge = c > 0 && c < longest ? 3.0 : 0.0;
+    return (units <= kSlots ? top : std::max(top, total / kSlots + 0.5 * top)) + merge;
+  };
+  int64_t best = 0;
+  double at = estimate(0);
+  for (const double rounds : {0.25, 0.5, 0.75, 0.9, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0}) {
+    const int64_t c = std::max<int64_t>(1, (int64_t)std::ceil((double)work / (rounds * kSlots)));
+    if (c >= longest) continue;
+    const double e = estimate(c);
+    if (e < at) {
+      at = e;
+      best = c;
+    }
+  }
+  return best;
+}
+
+struct AbsorbedPlan {
+  std::vector<LatentUnit> units;
+  std::vector<LatentMerge> merges;
+  int64_t n_parts = 0;
+  int row_blocks = 1;
+};
+
+// One request of the absorbed form: its batch index and the row that its first suffix token
+// has in the arrays the attention works on.
+struct Member {
+  int32_t req;
+  int64_t row;
+};
+
+void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32_t Hq, int32_t latent_dim,
+                   int32_t split_keys, AbsorbedPlan& plan) {
+  int64_t most = 0;
+  for (const Member& m : members) most = std::max<int64_t>(most, (int64_t)b->extend_lens[m.req] * Hq);
+  plan.row_blocks = most <= 16 ? 1 : (most <= 32 ? 2 : 4);
+  const int64_t M = 16 * plan.row_blocks;
+  std::vector<Span> spans;
+  for (const Member& m : members) {
+    const int64_t E = b->extend_lens[m.req], L = b->prefix_lens[m.req] + E;
+    spans.push_back({ceil_div(E * Hq, M), ceil_div(L, kvx::kLatTileKeys)});
+  }
+  int64_t steps = split_keys > 0 ? split_keys / kvx::kLatTileKeys : choose_steps(spans);
+  const int64_t max_parts = kMaxPartBytes / (M * (latent_dim + 1) * 4);
+  auto parts_of = [&](const Span& s) { return steps > 0 ? ceil_div(s.len, steps) : 1; };
+  while (steps > 0) {
+    int64_t n = 0;
+    for (const Span& s : spans)
+      if (parts_of(s) > 1) n += s.tiles * parts_of(s);
+    if (n <= max_parts) break;
+    steps *= 2;
+  }
+  std::vector<LatentUnit> units;
+  std::vector<Group> groups;
+  for (size_t i = 0; i < members.size(); i++) {
+    const Member& m = members[i];
+    const int64_t P = b->prefix_lens[m.req], E = b->extend_lens[m.req], rows = E * Hq;
+    const int64_t parts = parts_of(spans[i]);
+    // equal parts, unless a length was asked for
+    const int64_t len = (split_keys > 0 && parts > 1 ? steps : ceil_div(spans[i].len, parts)) * kvx::kLatTileKeys;
+    const int64_t part0 = plan.n_parts;
+    const int64_t tiles = spans[i].tiles;
+    if (parts > 1) plan.n_parts += tiles * parts;
+    for (int64_t c = 0; c < parts; c++) {
+      Group g{0, (int32_t)units.size(), 0};
+      for (int64_t t = tiles - 1; t >= 0; t--) {
+        LatentUnit u{};
+        u.row0 = (int32_t)(t * M);
+        u.nrows = (int32_t)std::min<int64_t>(M, rows - t * M);
+        u.qo = (int32_t)m.row;
+        u.prefix = (int32_t)P;
+        u.page_base = b->page_indptr[m.req];
+        const int64_t end = P + (u.row0 + u.nrows - 1) / Hq + 1;  // keys that a row of the tile sees
+        if (c * len >= end) continue;
+        u.key_begin = (int32_t)(c * len);
+        u.key_end = (int32_t)std::min<int64_t>(end, (c + 1) * len);
+        u.part = end > len ? (int32_t)(part0 + t * parts + c) : -1;
+        g.cost = std::max<int64_t>(g.cost, ceil_div(u.key_end - u.key_begin, kvx::kLatTileKeys) + 2);
+        units.push_back(u);
+        g.count++;
+        if (c == 0 && end > len) {
+          const int64_t n = ceil_div(end, len);
+          plan.merges.push_back({u.row0, u.nrows, u.qo, (int32_t)(part0 + t * parts), (int32_t)n, 0});
+        }
+      }
+      if (g.count > 0) groups.push_back(g);
+    }
+  }
+  plan.units = spread(units, groups);
+}
+
+struct ExpandedPlan {
+  std::vector<LatentExpandUnit> expand;
+  std::vector<LatentTile> units;
+  std::vector<LatentTileMerge> merges;
+  int64_t n_parts = 0;
+};
+
+// Rows of the expanded buffers: requests side by side, each from a multiple of 64.
+int64_t expand_units(const kvx_batch* b, const std::vector<int32_t>& reqs, std::vector<LatentExpandUnit>& out,
+                     std::vector<int64_t>& x_row) {
+  int64_t at = 0;
+  for (int32_t r : reqs) {
+    const int64_t L = (int64_t)b->prefix_lens[r] + b->extend_lens[r];
+    x_row.push_back(at);
+    for (int64_t k = 0; k < L; k += 64) {
+      out.push_back({(int32_t)(at + k), b->page_indptr[r], (int32_t)k, (int32_t)L});
+    }
+    at += ceil_div(L, 64) * 64;
+  }
+  return at;
+}
+
+void plan_expanded(const kvx_batch* b, const std::vector<int64_t>& qo, const std::vector<int32_t>& reqs,
+                   const std::vector<int64_t>& x_row, int32_t heads, int32_t head_dim, ExpandedPlan& plan) {
+  const int64_t M = kvx::kLatTileTok;
+  std::vector<Span> spans;
+  for (int32_t r : reqs) {
+    const int64_t E = b->extend_lens[r], L = b->prefix_lens[r] + E;
+    spans.push_back({ceil_div(E, M) * heads, ceil_div(b->prefix_lens[r] + L, 128)});  // of its tiles on average
+  }
+  int64_t steps = choose_steps(spans);
+  const int64_t max_parts = kMaxPartBytes / (M * (head_dim + 1) * 4);
+  auto parts_of = [&](int64_t L) { return steps > 0 ? ceil_div(ceil_div(L, 64), steps) : 1; };
+  while (steps > 0) {
+    int64_t n = 0;
+    for (size_t i = 0; i < reqs.size(); i++) {
+      const int64_t p = parts_of((int64_t)b->prefix_lens[reqs[i]] + b->extend_lens[reqs[i]]);
+      if (p > 1) n += spans[i].tiles * p;
+    }
+    if (n <= max_parts) break;
+    steps *= 2;
+  }
+  std::vector<LatentTile> units;
+  std::vector<Group> groups;
+  for (size_t i = 0; i < reqs.size(); i++) {
+    const int32_t r = reqs[i];
+    const int64_t P = b->prefix_lens[r], E = b->extend_lens[r], tiles = ceil_div(E, M);
+    const int64_t parts = parts_of(P + E), len = ceil_div(ceil_div(P + E, 64), parts) * 64;
+    for (int32_t h = 0; h < heads; h++) {
+      const int64_t part0 = plan.n_parts;
+      if (parts > 1) plan.n_parts += tiles * parts;
+      for (int64_t c = 0; c < parts; c++) {
+        Group g{0, (int32_t)units.size(), 0};
+        for (int64_t t = tiles - 1; t >= 0; t--) {
+          const int64_t n = std::min<int64_t>(M, E - t * M), end = P + t * M + n;
+          if (c * len >= end) continue;
+          LatentTile u{};
+          u.qo_row = (int32_t)(qo[(size_t)r] + t * M);
+          u.head_ntok = (int32_t)(h << 16 | n);
+          u.pos0 = (int32_t)(P + t * M);
+          u.x_row = (int32_t)x_row[i];
+          u.key_begin = (int32_t)(c * len);
+          u.key_end = (int32_t)std::min<int64_t>(end, (c + 1) * len);
+          u.part = end > len ? (int32_t)(part0 + t * parts + c) : -1;
+          g.cost = std::max<int64_t>(g.cost, ceil_div(u.key_end - u.key_begin, 64) + 2);
+          units.push_back(u);
+          g.count++;
+          if (c == 0 && end > len)
+            plan.merges.push_back({u.qo_row, u.head_ntok, (int32_t)(part0 + t * parts), (int32_t)ceil_div(end, len)});
+        }
+        if (g.count > 0) groups.push_back(g);
+      }
+    }
+  }
+  if (groups.size() < 64) {  // too few to fill eight queues evenly: unit by unit
+    groups.clear();
+    for (size_t i = 0; i < units.size(); i++)
+      groups.push_back({ceil_div(units[i].key_end - units[i].key_begin, 64) + 2, (int32_t)i, 1});
+  }
+  plan.units = spread(units, groups);
+}
+
+// Whether a request is estimated to be faster in the absorbed form: products by its lengths.
+bool prefers_absorbed(int64_t P, int64_t E, int64_t latent, int64_t d) {
+  const double pairs = (double)E * P + 0.5 * (double)E * (E + 1);
+  const double ab = 2.0 * d * latent * E + (2.0 * latent + kvx::kLatRope) * pairs;
+  const double ex = 2.0 * d * latent * (P + E) + (2.0 * d + kvx::kLatRope) * pairs;
+  return ab <= ex;
+}
+
+// Attention on latents over `members`: launches its kernel and merge; the plan is at `dev`.
+int launch_absorbed(kvx_latent_pool* pool, const kvx_batch* batch, const AbsorbedPlan& plan, const uint8_t* dev,
+                    size_t units_at, size_t merges_at, const void* q, int32_t Hq, float sm_scale, void* out,
+                    float* lse, hipStream_t s) {
+  kvx::LatentAttnParams p{};
+  p.pool = view(pool, batch);
+  p.q = (const uint16_t*)q;
+  p.out = (uint16_t*)out;
+  p.lse = lse;
+  p.units = (const LatentUnit*)(dev + units_at);
+  const size_t per_part = (size_t)16 * plan.row_blocks * pool->latent_dim;
+  if (plan.n_parts > 0) {
+    if (int rc = pool->parts.ensure((size_t)plan.n_parts * (per_part + 16 * plan.row_blocks) * sizeof(float), s))
+      return rc;
+    p.o_part = (float*)pool->parts.ptr;
+    p.lse_part = p.o_part + (size_t)plan.n_parts * per_part;
+  }
+  p.num_q_heads = Hq;
+  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  hipError_t e = kvx::launch_latent_attention(p, (int64_t)plan.units.size(), pool->latent_dim,
+                                              pool->dtype == KVX_LATENT_FP8, plan.row_blocks, s);
+  if (e != hipSuccess) return hip_fail(e, "latent attention kernel launch");
+  if (!plan.merges.empty()) {
+    kvx::LatentMergeParams m{};
+    m.merges = (const LatentMerge*)(dev + merges_at);
+    m.o_part = p.o_part;
+    m.lse_part = p.lse_part;
+    m.out = p.out;
+    m.lse = lse;
+    m.num_q_heads = Hq;
+    e = kvx::launch_latent_merge(m, (int64_t)plan.merges.size(), pool->latent_dim, plan.row_blocks, s);
+    if (e != hipSuccess) return hip_fail(e, "latent merge kernel launch");
+  }
+  return pool->parts.done(s);
+}
+
+}  // namespace
+
+extern "C" {
+
+int latent_pool_create(int64_t num_pages, int32_t page_size, int32_t latent_dim, int32_t rope_dim, int32_t dtype,
+                       kvx_latent_pool** out) {
+  return guarded([&]() -> int {
+    if (out == nullptr) return report(KVX_EINVAL, "out is NULL");
+    *out = nullptr;
+    if (num_pages <= 0 || num_pages > (int64_t)INT32_MAX)
+      return report(KVX_EINVAL, "num_pages = %lld must be in [1, 2^31-1]", (long long)num_pages);
+    if (page_size != kvx::kPageSize) return report(KVX_EUNSUPPORTED, "page_size %d (supported: 16)", page_size);
+    if (latent_dim != 256 && latent_dim != 512)
+      return report(KVX_EUNSUPPORTED, "latent_dim %d (supported: 256, 512)", latent_dim);
+    if (rope_dim != kvx::kLatRope) return report(KVX_EUNSUPPORTED, "rope_dim %d (supported: 64)", rope_dim);
+    if (dtype != KVX_LATENT_BF16 && dtype != KVX_LATENT_FP8) return report(KVX_EINVAL, "dtype %d", dtype);
+    kvx_latent_pool* p = new kvx_latent_pool();
+    p->num_pages = num_pages;
+    p->latent_dim = latent_dim;
+    p->dtype = dtype;
+    p->page_bytes = kvx::kPageSize * (dtype == KVX_LATENT_FP8
+                                          ? (int64_t)latent_dim + 2 * rope_dim + latent_dim / kvx::kLatGroup
+                                          : 2 * ((int64_t)latent_dim + rope_dim));
+    hipError_t e = hipGetDevice(&p->device);
+    if (e == hipSuccess) e = hipMalloc((void**)&p->base, (size_t)num_pages * p->page_bytes);
+    if (e == hipSuccess) e = hipMemset(p->base, 0, (size_t)num_pages * p->page_bytes);
+    if (e == hipSuccess) e = hipDeviceSynchronize();
+    if (e != hipSuccess) {
+      if (p->base) (void)hipFree(p->base);
+      delete p;
+      return hip_fail(e, "latent pool allocation");
+    }
+    *out = p;
+    return KVX_OK;
+  });
+}
+
+int latent_pool_destroy(kvx_latent_pool* pool) {
+  return guarded([&]() -> int {
+    if (pool == nullptr) return KVX_OK;
+    OnDevice on;
+    (void)on.enter(pool->device);
+    const hipError_t e = hipDeviceSynchronize();
+    pool->st_rows.release();
+    pool->st_plan.release();
+    pool->parts.release();
+    pool->absorbed.release();
+    pool->expanded.release();
+    if (pool->base) (void)hipFree(pool->base);
+    delete pool;
+    if (e != hipSuccess) return hip_fail(e, "hipDeviceSynchronize");
+    return KVX_OK;
+  });
+}
+
+int latent_pool_layout(const kvx_latent_pool* pool, kvx_latent_layout* out) {
+  return guarded([&]() -> int {
+    if (int rc = check_pool(pool)) return rc;
+    if (out == nullptr) return report(KVX_EINVAL, "out is NULL");
+    std::memset(out, 0, sizeof *out);
+    out->base = pool->base;
+    out->num_pages = pool->num_pages;
+    out->page_bytes = pool->page_bytes;
+    out->page_size = kvx::kPageSize;
+    out->latent_dim = pool->latent_dim;
+    out->rope_dim = kvx::kLatRope;
+    out->dtype = pool->dtype;
+    const bool fp8 = pool->dtype == KVX_LATENT_FP8;
+    out->key_offset = fp8 ? kvx::kPageSize * pool->latent_dim : 2 * pool->latent_dim;
+    out->scale_offset = fp8 ? kvx::kPageSize * (pool->latent_dim + 2 * kvx::kLatRope) : 0;
+    return KVX_OK;
+  });
+}
+
+int latent_pool_set_split_keys(kvx_latent_pool* pool, int32_t keys) {
+  return guarded([&]() -> int {
+    if (int rc = check_pool(pool)) return rc;
+    if (keys < 0 || keys % kvx::kLatTileKeys != 0)
+      return report(KVX_EINVAL, "split keys %d: must be 0 or a positive multiple of %d", keys, kvx::kLatTileKeys);
+    pool->split_keys = keys;
+    return KVX_OK;
+  });
+}
+
+int store_latent(kvx_latent_pool* pool, const kvx_batch* batch, const void* kv, int64_t kv_stride,
+                 kvx_stream_t stream) {
+  return guarded([&]() -> int {
+    return store_call(pool, batch, nullptr, false, nullptr, 0, 0, nullptr, kv, kv_stride, (hipStream_t)stream);
+  });
+}
+
+int store_latent_rope(kvx_latent_pool* pool, const kvx_batch* batch, const kvx_rope* rope, const void* q,
+                      int32_t num_q_heads, int32_t q_dim, void* q_out, const void* kv, int64_t kv_stride,
+                      kvx_stream_t stream) {
+  return guarded([&]() -> int {
+    return store_call(pool, batch, rope, true, q, num_q_heads, q_dim, q_out, kv, kv_stride, (hipStream_t)stream);
+  });
+}
+
+int load_latent(kvx_latent_pool* pool, const kvx_batch* batch, void* out, int64_t out_stride, kvx_stream_t stream) {
+  return guarded([&]() -> int {
+    if (int rc = check_pool(pool)) return rc;
+    std::vector<int64_t> qo;
+    if (int rc = check_batch(batch, qo)) return rc;
+    if (int rc = check_stride(out_stride, pool->latent_dim + kvx::kLatRope, "out_stride")) return rc;
+    if (int rc = check_align(out, "out")) return rc;
+    if (qo.back() == 0) return KVX_OK;
+    if (!out) return report(KVX_EINVAL, "out is NULL");
+    hipStream_t s = (hipStream_t)stream;
+    OnDevice on;
+    if (int rc = on.enter(pool->device)) return rc;
+    if (int rc = check_stream(s)) return rc;
+    if (kvx::validate_mode())
+      if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
+    kvx::LatentLoadParams p{};
+    int64_t n_units = 0;
+    if (int rc = place_units(pool, batch, qo, s, p, n_units)) return rc;
+    p.pool = view(pool, batch);
+    p.out = (uint16_t*)out;
+    p.out_stride = out_stride;
+    const hipError_t e = kvx::launch_load_latent(p, n_units, pool->latent_dim, pool->dtype == KVX_LATENT_FP8, s);
+    if (e != hipSuccess) return hip_fail(e, "load_latent kernel launch");
+    return p.units ? pool->st_rows.done(s) : KVX_OK;
+  });
+}
+
+int latent_attention(kvx_latent_pool* pool, const kvx_batch* batch, const void* q, int32_t num_q_heads,
+                     float sm_scale, void* out, float* lse, kvx_stream_t stream) {
+  return guarded([&]() -> int {
+    if (int rc = check_pool(pool)) return rc;
+    std::vector<int64_t> qo;
+    if (int rc = check_batch(batch, qo)) return rc;
+    if (int rc = check_heads(batch, num_q_heads)) return rc;
+    if (int rc = check_scale(sm_scale)) return rc;
+    if (int rc = check_align(q, "q")) return rc;
+    if (int rc = check_align(out, "out")) return rc;
+    if (qo.back() == 0) return KVX_OK;
+    if (!q || !out) return report(KVX_EINVAL, "q and out must be non-NULL");
+    hipStream_t s = (hipStream_t)stream;
+    OnDevice on;
+    if (int rc = on.enter(pool->device)) return rc;
+    if (int rc = check_stream(s)) return rc;
+    if (kvx::validate_mode())
+      if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
+    std::vector<Member> members;
+    for (int32_t r = 0; r < batch->num_reqs; r++)
+      if (batch->extend_lens[r] > 0) members.push_back({r, qo[(size_t)r]});
+    AbsorbedPlan plan;
+    plan_absorbed(batch, members, num_q_heads, pool->latent_dim, pool->split_keys, plan);
+    Blob blob;
+    const size_t units_at = blob.add(plan.units), merges_at = blob.add(plan.merges);
+    void* dev = nullptr;
+    if (int rc = pool->st_plan.upload(blob.bytes.data(), blob.bytes.size(), s, &dev)) return rc;
+    if (int rc = launch_absorbed(pool, batch, plan, (const uint8_t*)dev, units_at, merges_at, q, num_q_heads, sm_scale,
+                                 out, lse, s))
+      return rc;
+    return pool->st_plan.done(s);
+  });
+}
+
+int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const kvx_latent_proj* proj,
+                            const void* q, float sm_scale, void* out, float* lse, int32_t form,
+                            kvx_stream_t stream) {
+  return guarded([&]() -> int {
+    if (int rc = check_pool(pool)) return rc;
+    std::vector<int64_t> qo;
+    if (int rc = check_batch(batch, qo)) return rc;
+    if (proj == nullptr) return report(KVX_EINVAL, "proj is NULL");
+    const int32_t Hq = proj->num_q_heads, D = proj->nope_dim, lat = pool->latent_dim;
+    if (int rc = check_heads(batch, Hq)) return rc;
+    if (D != 64 && D != 128) return report(KVX_EUNSUPPORTED, "nope_dim %d (supported: 64, 128)", D);
+    if (proj->v_dim != D) return report(KVX_EUNSUPPORTED, "v_dim %d (supported: nope_dim = %d)", proj->v_dim, D);
+    if (form != KVX_LATENT_AUTO && form != KVX_LATENT_ABSORBED && form != KVX_LATENT_EXPANDED)
+      return report(KVX_EINVAL, "form %d", form);
+    if (int rc = check_scale(sm_scale)) return rc;
+    if (int rc = check_align(q, "q")) return rc;
+    if (int rc = check_align(out, "out")) return rc;
+    if (int rc = check_align(proj->w_uk, "w_uk")) return rc;
+    if (int rc = check_align(proj->w_uv, "w_uv")) return rc;
+    if (qo.back() == 0) return KVX_OK;
+    if (!q || !out || !proj->w_uk || !proj->w_uv)
+      return report(KVX_EINVAL, "q, out, w_uk and w_uv must be non-NULL");
+
+    std::vector<Member> absorbed;
+    std::vector<int32_t> expanded;
+    int64_t own_rows = 0, x_tokens = 0;
+    for (int32_t r = 0; r < batch->num_reqs; r++) {
+      const int64_t P = batch->prefix_lens[r], E = batch->extend_lens[r];
+      if (E == 0) continue;
+      if (form == KVX_LATENT_ABSORBED || (form == KVX_LATENT_AUTO && prefers_absorbed(P, E, lat, D))) {
+        absorbed.push_back({r, own_rows});
+        own_rows += E;
+      } else {
+        expanded.push_back(r);
+        x_tokens += ceil_div(P + E, 64) * 64;
+      }
+    }
+    if (x_tokens > (int64_t)INT32_MAX)
+      return report(KVX_EUNSUPPORTED, "%lld tokens to expand in one call", (long long)x_tokens);
+
+    hipStream_t s = (hipStream_t)stream;
+    OnDevice on;
+    if (int rc = on.enter(pool->device)) return rc;
+    if (int rc = check_stream(s)) return rc;
+    if (kvx::validate_mode())
+      if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
+
+    // plans of everything, uploaded at once
+    Blob blob;
+    AbsorbedPlan ap;
+    std::vector<LatentRows> rows;
+    size_t a_units = 0, a_merges = 0, a_rows = 0;
+    if (!absorbed.empty()) {
+      plan_absorbed(batch, absorbed, Hq, lat, pool->split_keys, ap);
+      for (size_t i = 0; i < absorbed.size();) {  // neighbours in the batch run on together
+        size_t j = i;
+        int64_t n = 0;
+        const int64_t first = qo[(size_t)absorbed[i].req];
+        while (j < absorbed.size() && qo[(size_t)absorbed[j].req] == first + n)
+          n += batch->extend_lens[absorbed[j++].req];
+        for (int64_t t = 0; t < n; t += kvx::kLatProjTok)
+          rows.push_back({(int32_t)(first + t), (int32_t)(absorbed[i].row + t),
+                          (int32_t)std::min<int64_t>(kvx::kLatProjTok, n - t), 0});
+        i = j;
+      }
+      a_units = blob.add(ap.units);
+      a_merges = blob.add(ap.merges);
+      a_rows = blob.add(rows);
+    }
+    std::vector<LatentExpandUnit> x_units;
+    std::vector<int64_t> x_row;
+    int64_t x_rows = 0, per_head = 0;
+    int32_t heads = Hq, last = Hq;
+    ExpandedPlan xp, xl;  // of a group of heads, and of the last group where it is smaller
+    size_t x_at = 0, t_at[2] = {}, m_at[2] = {};
+    if (!expanded.empty()) {
+      x_rows = expand_units(batch, expanded, x_units, x_row);
+      per_head = 2 * x_rows * D * 2;
+      heads = (int32_t)std::min<int64_t>(Hq, std::max<int64_t>(1, kMaxExpandBytes / per_head));
+      heads = (int32_t)ceil_div(Hq, ceil_div(Hq, heads));
+      last = Hq - heads * (int32_t)(ceil_div(Hq, heads) - 1);
+      plan_expanded(batch, qo, expanded, x_row, heads, D, xp);
+      x_at = blob.add(x_units);
+      t_at[0] = t_at[1] = blob.add(xp.units);
+      m_at[0] = m_at[1] = blob.add(xp.merges);
+      if (last != heads) {
+        plan_expanded(batch, qo, expanded, x_row, last, D, xl);
+        t_at[1] = blob.add(xl.units);
+        m_at[1] = blob.add(xl.merges);
+      }
+    }
+    void* dev_v = nullptr;
+    if (int rc = pool->st_plan.upload(blob.bytes.data(), blob.bytes.size(), s, &dev_v)) return rc;
+    const uint8_t* dev = (const uint8_t*)dev_v;
+
+    if (!absorbed.empty()) {
+      const size_t q_bytes = (size_t)own_rows * Hq * (lat + kvx::kLatRope) * 2, o_bytes = (size_t)own_rows * Hq * lat * 2;
+      const size_t l_bytes = lse ? (size_t)own_rows * Hq * 4 : 0;
+      if (int rc = pool->absorbed.ensure(q_bytes + o_bytes + l_bytes, s)) return rc;
+      uint8_t* ws = (uint8_t*)pool->absorbed.ptr;
+      float* own_lse = lse ? (float*)(ws + q_bytes + o_bytes) : nullptr;
+      kvx::LatentProjParams p{};
+      p.in = (const uint16_t*)q;
+      p.w = (const uint16_t*)proj->w_uk;
+      p.out = (uint16_t*)ws;
+      p.rows = (const LatentRows*)(dev + a_rows);
+      p.num_q_heads = Hq;
+      hipError_t e = kvx::launch_latent_absorb(p, (int64_t)rows.size(), lat, D, s);
+      if (e != hipSuccess) return hip_fail(e, "latent query product launch");
+      if (int rc = launch_absorbed(pool, batch, ap, dev, a_units, a_merges, ws, Hq, sm_scale, ws + q_bytes, own_lse, s))
+        return rc;
+      p.in = (const uint16_t*)(ws + q_bytes);
+      p.w = (const uint16_t*)proj->w_uv;
+      p.out = (uint16_t*)out;
+      p.lse_in = own_lse;
+      p.lse_out = lse;
+      e = kvx::launch_latent_output(p, (int64_t)rows.size(), lat, D, s);
+      if (e != hipSuccess) return hip_fail(e, "latent output product launch");
+      if (int rc = pool->absorbed.done(s)) return rc;
+    }
+    if (!expanded.empty()) {
+      const size_t r_bytes = (size_t)x_rows * kvx::kLatRope * 2;
+      if (int rc = pool->expanded.ensure(r_bytes + (size_t)per_head * heads, s)) return rc;
+      const int64_t n_parts = std::max(xp.n_parts, xl.n_parts);
+      const size_t per_part = (size_t)kvx::kLatTileTok * D;
+      if (n_parts > 0)
+        if (int rc = pool->parts.ensure((size_t)n_parts * (per_part + kvx::kLatTileTok) * sizeof(float), s)) return rc;
+      uint8_t* ws = (uint8_t*)pool->expanded.ptr;
+      for (int32_t h0 = 0; h0 < Hq; h0 += heads) {
+        const int32_t n = std::min(heads, Hq - h0);
+        const bool tail = n != heads;
+        const ExpandedPlan& plan = tail ? xl : xp;
+        kvx::LatentExpandParams x{};
+        x.pool = view(pool, batch);
+        x.w_uk = (const uint16_t*)proj->w_uk + (size_t)h0 * D * lat;
+        x.w_uv = (const uint16_t*)proj->w_uv + (size_t)h0 * D * lat;
+        x.kx = (uint16_t*)(ws + r_bytes);
+        x.vx = x.kx + (size_t)n * x_rows * D;
+        x.rx = h0 == 0 ? (uint16_t*)ws : nullptr;
+        x.units = (const LatentExpandUnit*)(dev + x_at);
+        x.x_rows = x_rows;
+        x.heads = n;
+        hipError_t e = kvx::launch_latent_expand(x, (int64_t)x_units.size(), lat, D, pool->dtype == KVX_LATENT_FP8, s);
+        if (e != hipSuccess) return hip_fail(e, "latent expansion launch");
+        kvx::LatentPrefillParams p{};
+        p.q = (const uint16_t*)q;
+        p.out = (uint16_t*)out;
+        p.lse = lse;
+        p.kx = x.kx;
+        p.vx = x.vx;
+        p.rx = (const uint16_t*)ws;
+        p.units = (const LatentTile*)(dev + t_at[tail]);
+        p.o_part = (float*)pool->parts.ptr;
+        p.lse_part = n_parts ? p.o_part + (size_t)plan.n_parts * per_part : nullptr;
+        p.x_rows = x_rows;
+        p.num_q_heads = Hq;
+        p.head0 = h0;
+        p.scale_log2 = sm_scale * 1.4426950408889634f;
+        e = kvx::launch_latent_prefill(p, (int64_t)plan.units.size(), D, s);
+        if (e != hipSuccess) return hip_fail(e, "expanded attention launch");
+        if (!plan.merges.empty()) {
+          kvx::LatentTileMergeParams m{};
+          m.merges = (const LatentTileMerge*)(dev + m_at[tail]);
+          m.o_part = p.o_part;
+          m.lse_part = p.lse_part;
+          m.out = p.out;
+          m.lse = lse;
+          m.num_q_heads = Hq;
+          m.head0 = h0;
+          e = kvx::launch_latent_tile_merge(m, (int64_t)plan.merges.size(), D, s);
+          if (e != hipSuccess) return hip_fail(e, "expanded merge launch");
+        }
+      }
+      if (int rc = pool->expanded.done(s)) return rc;
+      if (int rc = pool->parts.done(s)) return rc;
+    }
+    return pool->st_plan.done(s);
+  });
+}
+
+}  // extern "C"

@@ -25,9 +25,11 @@ STATUS_NAMES = {0: "KVX_OK", 1: "KVX_EINVAL", 2: "KVX_ENOMEM", 3: "KVX_ERANGE",
 
 KVX_EVICT_LRU, KVX_EVICT_RR = 0, 1
 KVX_ROPE_HALF, KVX_ROPE_INTERLEAVED = 0, 1
+KVX_LATENT_BF16, KVX_LATENT_FP8 = 0, 1
+KVX_LATENT_AUTO, KVX_LATENT_ABSORBED, KVX_LATENT_EXPANDED = 0, 1, 2
 NOALLOC_PLAN_BYTES, NOALLOC_PARTS_BYTES = 8 << 20, 56 << 20  # KVX_NOALLOC_* in include/kvx.h
 
-# Every symbol include/kvx.h and include/kvx_cache.h declare.
+# Every symbol the headers in include/ declare.
 EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_pool_layout", "kv_pool_write_pages",
            "kv_pool_read_pages", "kv_pool_record_bytes", "kv_pool_spill", "kv_pool_reload", "store_kv", "store_kv_rope", "extend_attention", "extend_attention_noalloc", "extend_attention_plan",
            "kv_pool_set_split_keys", "kv_pool_set_scaled_q", "kvx_last_error",
@@ -35,7 +37,9 @@ EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_pool_layout", "kv_pool_write
            "kvx_cache_begin_turn_tiered", "kvx_cache_end_turn", "kvx_cache_complete", "kvx_cache_agent",
            "kvx_cache_agent_host", "kvx_cache_join", "kvx_cache_group", "kvx_cache_stats",
            "kvx_radix_create", "kvx_radix_destroy", "kvx_radix_begin", "kvx_radix_end", "kvx_radix_complete",
-           "kvx_radix_match", "kvx_radix_stats"]
+           "kvx_radix_match", "kvx_radix_stats",
+           "latent_pool_create", "latent_pool_destroy", "latent_pool_layout", "latent_pool_set_split_keys",
+           "store_latent", "store_latent_rope", "load_latent", "latent_attention", "latent_extend_attention"]
 
 
 class KvxNotBuilt(ImportError):
@@ -69,6 +73,17 @@ class kvx_rope(ctypes.Structure):
     _fields_ = [("theta", ctypes.c_double), ("inv_freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32),
                 ("style", ctypes.c_int32), ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p),
                 ("norm_eps", ctypes.c_float)]
+
+
+class kvx_latent_layout(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("num_pages", ctypes.c_int64), ("page_bytes", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("latent_dim", ctypes.c_int32), ("rope_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("key_offset", ctypes.c_int32), ("scale_offset", ctypes.c_int32)]
+
+
+class kvx_latent_proj(ctypes.Structure):
+    _fields_ = [("w_uk", ctypes.c_void_p), ("w_uv", ctypes.c_void_p), ("num_q_heads", ctypes.c_int32),
+                ("nope_dim", ctypes.c_int32), ("v_dim", ctypes.c_int32)]
 
 
 class kvx_work_item(ctypes.Structure):
@@ -146,6 +161,16 @@ def lib():
             "kvx_radix_complete": [P, i64],
             "kvx_radix_match": [P, P, i32, ctypes.POINTER(i32), P, i64],
             "kvx_radix_stats": [P, ctypes.POINTER(kvx_radix_counters)],
+            "latent_pool_create": [i64, i32, i32, i32, i32, ctypes.POINTER(P)],
+            "latent_pool_destroy": [P],
+            "latent_pool_layout": [P, ctypes.POINTER(kvx_latent_layout)],
+            "latent_pool_set_split_keys": [P, i32],
+            "store_latent": [P, ctypes.POINTER(kvx_batch), P, i64, P],
+            "store_latent_rope": [P, ctypes.POINTER(kvx_batch), ctypes.POINTER(kvx_rope), P, i32, i32, P, P, i64, P],
+            "load_latent": [P, ctypes.POINTER(kvx_batch), P, i64, P],
+            "latent_attention": [P, ctypes.POINTER(kvx_batch), P, i32, f32, P, P, P],
+            "latent_extend_attention": [P, ctypes.POINTER(kvx_batch), ctypes.POINTER(kvx_latent_proj), P, f32, P, P,
+                                        i32, P],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -380,6 +405,127 @@ def kv_pool_set_split_keys(pool, keys: int) -> None:
 
 def kv_pool_set_scaled_q(pool, enable: bool) -> None:
     _check(lib().kv_pool_set_scaled_q(pool, 1 if enable else 0), "kv_pool_set_scaled_q")
+
+
+# ------------------------------------------------------------------ latent attention (include/kvx_latent.h)
+
+def latent_pool_create(num_pages: int, page_size: int, latent_dim: int, rope_dim: int = 64,
+                       dtype: int = KVX_LATENT_BF16) -> ctypes.c_void_p:
+    out = ctypes.c_void_p()
+    _check(lib().latent_pool_create(int(num_pages), int(page_size), int(latent_dim), int(rope_dim), int(dtype),
+                                    ctypes.byref(out)), "latent_pool_create")
+    return out
+
+
+def latent_pool_destroy(pool) -> None:
+    _check(lib().latent_pool_destroy(pool), "latent_pool_destroy")
+
+
+def latent_pool_layout(pool) -> dict:
+    lay = kvx_latent_layout()
+    _check(lib().latent_pool_layout(pool, ctypes.byref(lay)), "latent_pool_layout")
+    return {name: getattr(lay, name) for name, _ in kvx_latent_layout._fields_}
+
+
+def latent_pool_set_split_keys(pool, keys: int) -> None:
+    _check(lib().latent_pool_set_split_keys(pool, int(keys)), "latent_pool_set_split_keys")
+
+
+def _latent_row(pool) -> tuple:
+    """(latent_dim, rope_dim) of a latent pool; an absent pool is the library's to report."""
+    lay = kvx_latent_layout()
+    _check(lib().latent_pool_layout(pool, ctypes.byref(lay)), "latent_pool_layout")
+    return lay.latent_dim, lay.rope_dim
+
+
+def _elems(t, size: int, name: str) -> None:
+    if t is not None and not isinstance(t, int) and t.element_size() != size:
+        raise ValueError(f"{name}: {t.dtype} elements; expected {'float32' if size == 4 else 'bf16'}")
+
+
+def _rows_ptr(t, rows: int, width: int, name: str) -> tuple:
+    """Address and row stride (elements) of a [rows, width] bf16 tensor whose rows are
+    contiguous: a slice of wider rows is taken as it is.  A raw address has packed rows."""
+    if t is None or isinstance(t, int):
+        return t, width
+    _elems(t, 2, name)
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a device (CUDA/HIP) tensor")
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < width or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {tuple(t.stride())}; the call needs [{rows}, "
+                         f"{width}] with contiguous rows")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else width)
+
+
+def store_latent(pool, batch: Batch, kv, stream=None) -> None:
+    """kv: [T, latent_dim + rope_dim] bf16, rows contiguous (the rows may be a slice of wider ones)."""
+    lat, rope = _latent_row(pool)
+    ptr, stride = _rows_ptr(kv, batch.total_extend, lat + rope, "kv")
+    _check(lib().store_latent(pool, ctypes.byref(batch.c), ptr, stride, _stream(stream)), "store_latent")
+
+
+def store_latent_rope(pool, batch: Batch, kv, *, theta: float = 10000.0, style: int = 0, norm=None,
+                      norm_eps: float = 1e-6, q=None, num_q_heads: int = 0, q_out=None, q_dim: Optional[int] = None,
+                      inv_freq=None, stream=None) -> None:
+    """store_latent with the latent's RMS norm (optional) and the rotation of the shared key
+    and of the queries' last rope_dim dims fused in.  q, q_out: [T, num_q_heads, q_dim]."""
+    lat, rope = _latent_row(pool)
+    t = batch.total_extend
+    ptr, stride = _rows_ptr(kv, t, lat + rope, "kv")
+    freqs = None if inv_freq is None else np.ascontiguousarray(inv_freq, dtype=np.float64)
+    if freqs is not None and freqs.size < rope // 2:
+        raise ValueError(f"inv_freq: {freqs.size} entries, the rotated dims need {rope // 2}")
+    if num_q_heads and q_dim is None:
+        if q is None or isinstance(q, int):
+            raise ValueError("q_dim is needed with a query address")
+        q_dim = q.shape[-1]
+    _elems(norm, 2, "norm")
+    _need(norm, 2 * lat, "norm")
+    if num_q_heads:
+        for name, buf in (("q", q), ("q_out", q_out)):
+            _elems(buf, 2, name)
+            _need(buf, 2 * t * int(num_q_heads) * int(q_dim), name)
+    r = kvx_rope(float(theta), None if freqs is None else freqs.ctypes.data, rope, int(style), None, _dptr(norm),
+                 float(norm_eps))
+    _check(lib().store_latent_rope(pool, ctypes.byref(batch.c), ctypes.byref(r), _dptr(q), int(num_q_heads),
+                                   int(q_dim or 0), _dptr(q_out), ptr, stride, _stream(stream)), "store_latent_rope")
+
+
+def load_latent(pool, batch: Batch, out, stream=None) -> None:
+    """out: [T, latent_dim + rope_dim] bf16, rows contiguous (the rows may be a slice of wider ones)."""
+    lat, rope = _latent_row(pool)
+    ptr, stride = _rows_ptr(out, batch.total_extend, lat + rope, "out")
+    _check(lib().load_latent(pool, ctypes.byref(batch.c), ptr, stride, _stream(stream)), "load_latent")
+
+
+def latent_attention(pool, batch: Batch, q, num_q_heads: int, sm_scale: float, out, lse=None, stream=None) -> None:
+    """q: [T, num_q_heads, latent_dim + rope_dim] (already multiplied by W_uk); out: [T, num_q_heads, latent_dim]."""
+    lat, rope = _latent_row(pool)
+    rows = batch.total_extend * int(num_q_heads)
+    for name, buf, size, width in (("q", q, 2, lat + rope), ("out", out, 2, lat), ("lse", lse, 4, 1)):
+        _elems(buf, size, name)
+        _need(buf, size * rows * width, name)
+    _check(lib().latent_attention(pool, ctypes.byref(batch.c), _dptr(q), int(num_q_heads), float(sm_scale),
+                                  _dptr(out), _dptr(lse), _stream(stream)), "latent_attention")
+
+
+def latent_extend_attention(pool, batch: Batch, q, w_uk, w_uv, sm_scale: float, out, lse=None,
+                            form: int = KVX_LATENT_AUTO, stream=None) -> None:
+    """q: [T, heads, nope_dim + rope_dim]; w_uk, w_uv: [heads, nope_dim | v_dim, latent_dim]; out: [T, heads, v_dim]."""
+    lat, rope = _latent_row(pool)
+    if w_uk.dim() != 3 or w_uv.dim() != 3 or w_uk.shape[0] != w_uv.shape[0] or w_uk.shape[2] != lat or w_uv.shape[2] != lat:
+        raise ValueError(f"w_uk {tuple(w_uk.shape)} and w_uv {tuple(w_uv.shape)}: expected [heads, dim, {lat}] each")
+    heads, nope, v = w_uk.shape[0], w_uk.shape[1], w_uv.shape[1]
+    rows = batch.total_extend * heads
+    for name, buf, size, width in (("q", q, 2, nope + rope), ("out", out, 2, v), ("lse", lse, 4, 1)):
+        _elems(buf, size, name)
+        _need(buf, size * rows * width, name)
+    _elems(w_uk, 2, "w_uk")
+    _elems(w_uv, 2, "w_uv")
+    proj = kvx_latent_proj(_dptr(w_uk), _dptr(w_uv), heads, nope, v)
+    _check(lib().latent_extend_attention(pool, ctypes.byref(batch.c), ctypes.byref(proj), _dptr(q), float(sm_scale),
+                                         _dptr(out), _dptr(lse), int(form), _stream(stream)),
+           "latent_extend_attention")
 
 
 # ------------------------------------------------------------------ prefix cache (include/kvx_cache.h)
