@@ -1,0 +1,419 @@
+"""Latent cache and attention on the GPU against a float64 reference (tests/latent_ref.py):
+stores with norm, rotation and 8-bit latents, read-back, both attention entry points and
+both forms, at the sizes and masks where they can go wrong."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import helpers
+import latent_ref as ref
+from paper_2609_32278_amd import kvx
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF16 = torch.bfloat16
+
+
+class Setup:
+    """A pool whose every slot holds NaN, a shuffled page table and the cached rows of a batch."""
+
+    def __init__(self, P, E, lat, fp8, seed=0, poison=True, extra_pages=5):
+        g = torch.Generator(DEV).manual_seed(seed)
+        self.P, self.E, self.lat, self.fp8, self.g = list(P), list(E), lat, fp8, g
+        need = [-(-(p + e) // 16) for p, e in zip(P, E)]
+        self.indptr = np.concatenate([[0], np.cumsum(need)]).astype(np.int32)
+        self.num_pages = int(self.indptr[-1]) + extra_pages
+        self.ids = torch.randperm(self.num_pages, device=DEV, generator=g).to(torch.int32)
+        self.pages = self.ids[: int(self.indptr[-1])].contiguous()
+        self.pool = kvx.latent_pool_create(self.num_pages, 16, lat, 64, kvx.KVX_LATENT_FP8 if fp8 else kvx.KVX_LATENT_BF16)
+        if poison:
+            n = self.num_pages * 16
+            self.store_all(torch.full((n, lat + 64), float("nan"), dtype=BF16, device=DEV))
+        self.batch = kvx.Batch(P, E, self.indptr, self.pages)
+        self.T = self.batch.total_extend
+
+    def store_all(self, rows):
+        n = self.num_pages
+        kvx.store_latent(self.pool, kvx.Batch([0], [n * 16], [0, n], self.ids), rows)
+
+    def load_all(self):
+        n = self.num_pages
+        out = torch.empty(n * 16, self.lat + 64, dtype=BF16, device=DEV)
+        kvx.load_latent(self.pool, kvx.Batch([0], [n * 16], [0, n], self.ids), out)
+        return out.view(n, 16, -1)
+
+    def normal(self, *shape, scale=1.0):
+        return torch.randn(shape, device=DEV, generator=self.g, dtype=BF16) * scale
+
+    def fill(self, scale=1.0, rows=None):
+        """Cache the whole sequences; returns the rows the pool then stands for (float64)."""
+        lens = [p + e for p, e in zip(self.P, self.E)]
+        rows = self.normal(sum(lens), self.lat + 64, scale=scale) if rows is None else rows
+        kvx.store_latent(self.pool, kvx.Batch([0] * len(lens), lens, self.indptr, self.pages), rows)
+        x = ref.f64(rows)
+        if self.fp8:
+            x[:, : self.lat] = ref.quantised(x[:, : self.lat])
+        cuts = np.cumsum([0] + lens)
+        return [x[cuts[i]:cuts[i + 1]] for i in range(len(lens))]
+
+    def close(self):
+        torch.cuda.synchronize()
+        kvx.latent_pool_destroy(self.pool)
+
+
+@pytest.fixture
+def setup():
+    made = []
+
+    def make(*a, **k):
+        made.append(Setup(*a, **k))
+        return made[-1]
+
+    yield make
+    for s in made:
+        s.close()
+
+
+# ------------------------------------------------------------------- store and load
+
+BATCHES = [
+    ([0], [1]),
+    ([5], [11]),                               # ends with the page
+    ([15], [2]),                               # across a page border
+    ([0, 37, 16, 100], [40, 0, 16, 3]),        # an empty request, whole pages, unaligned ends
+    (list(range(0, 130)), [1 + i % 3 for i in range(130)]),  # more requests than the arguments hold
+]
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lat", [256, 512])
+@pytest.mark.parametrize("P,E", BATCHES)
+def test_store_then_load(setup, P, E, lat, fp8):
+    s = setup(P, E, lat, fp8)
+    wide = s.normal(s.T, lat + 64 + 24, scale=3.0)  # rows inside wider rows
+    wide[:, : lat] *= torch.exp2(torch.randint(-20, 20, (s.T, lat), device=DEV, generator=s.g).float()).to(BF16)
+    wide[0, :64] = 0.0
+    rows = wide[:, 8:8 + lat + 64] if lat % 16 == 0 else wide
+    before = s.load_all()
+    kvx.store_latent(s.pool, s.batch, rows)
+    out = torch.full((s.T + 2, lat + 64 + 16), 7.0, dtype=BF16, device=DEV)
+    kvx.load_latent(s.pool, s.batch, out[1:1 + s.T, 8:8 + lat + 64])
+    want = ref.f64(rows)
+    if fp8:
+        want[:, :lat] = ref.quantised(want[:, :lat])
+    assert (ref.f64(out[1:1 + s.T, 8:8 + lat + 64]) == want).all()
+    # rows before and behind, and columns beside, are kept
+    assert (out[0] == 7).all() and (out[-1] == 7).all() and (out[:, :8] == 7).all() and (out[:, lat + 72:] == 7).all()
+    # so are all slots that the batch does not own
+    after = s.load_all()
+    touched = torch.zeros(s.num_pages, 16, dtype=torch.bool, device=DEV)
+    where = {int(p): i for i, p in enumerate(s.ids)}
+    for r, (p, e) in enumerate(zip(P, E)):
+        for t in range(p, p + e):
+            touched[where[int(s.pages[int(s.indptr[r]) + t // 16])], t % 16] = True
+    assert torch.equal(before.view(torch.int16)[~touched], after.view(torch.int16)[~touched])
+
+
+def test_store_special_values(setup):
+    """Infinities saturate an 8-bit group, NaN stays with its value, tiny groups reach the
+    smallest scale, the largest bf16 value stays finite."""
+    for fp8 in (False, True):
+        s = setup([0], [4], 256, fp8, poison=False)
+        x = torch.zeros(4, 320, dtype=BF16, device=DEV)
+        x[0, 3], x[0, 70], x[0, 130], x[0, 300] = math.inf, -math.inf, math.nan, math.nan
+        x[0, 131] = 2.0
+        x[1, :64] = 2.0 ** -126
+        x[1, 64:128] = 2.0 ** -133
+        x[2, :4] = torch.tensor([torch.finfo(BF16).max, -torch.finfo(BF16).max, 1.0, 2.0 ** 118])
+        kvx.store_latent(s.pool, s.batch, x)
+        out = torch.empty_like(x)
+        kvx.load_latent(s.pool, s.batch, out)
+        if not fp8:
+            assert torch.equal(out.view(torch.int16), x.view(torch.int16))
+            continue
+        top = 448 * 2.0 ** 119
+        assert out[0, 3] == top and out[0, 70] == -top and out[0, 131] == 2.0
+        assert out[0, 130].isnan() and out[0, 300].isnan()
+        assert (out[1, :64] == 2.0 ** -126).all()
+        assert (out[1, 64:128] == 0).all()  # below half of the smallest step, 2^-9 * 2^-117
+        assert out[2, 0] == top and out[2, 1] == -top and out[2, 3] == 2.0 ** 118
+
+
+@pytest.mark.parametrize("style", [0, 1])
+@pytest.mark.parametrize("lat,hd,heads,fp8,in_place", [
+    (512, 128, 3, False, False), (512, 128, 16, True, True), (256, 64, 1, True, False), (256, 0, 5, False, False),
+    (512, 72, 37, False, True), (256, 64, 0, False, False)])
+def test_store_rope(setup, style, lat, hd, heads, fp8, in_place):
+    P, E = [0, 250, 16, 1000], [17, 1, 0, 30]
+    s = setup(P, E, lat, fp8)
+    kv = s.normal(s.T, lat + 64, scale=2.0)
+    norm = 1.0 + s.normal(lat, scale=0.3)
+    q = s.normal(s.T, max(heads, 1), hd + 64)
+    given = q.clone()
+    q_out = q if in_place else torch.full_like(q, 9.0)
+    theta = 1e4 if style else 1e6
+    kvx.store_latent_rope(s.pool, s.batch, kv, theta=theta, style=style, norm=norm, norm_eps=1e-5, q=q,
+                          num_q_heads=heads, q_out=q_out)
+    out = torch.empty(s.T, lat + 64, dtype=BF16, device=DEV)
+    kvx.load_latent(s.pool, s.batch, out)
+    pos = np.concatenate([np.arange(p, p + e) for p, e in zip(P, E)])
+    freqs = theta ** (-2.0 * np.arange(32) / 64)
+    x = ref.f64(kv)
+    c = x[:, :lat] * ref.f64(norm) / np.sqrt((x[:, :lat] ** 2).mean(-1, keepdims=True) + 1e-5)
+    key = ref.rotated(x[:, lat:], pos, freqs, style)
+    helpers.check_nearest_bf16(out[:, lat:].contiguous().cpu().view(torch.int16).numpy().view(np.uint16), key,
+                               helpers.plane_scale(key, 64, style))
+    if fp8:
+        # float32 arithmetic: a value may land on the code next to it where it sits on a border
+        got, e = ref.f64(out[:, :lat]), ref.scale_exps(c)
+        lo = ref.quantised(c - np.abs(c) * 2.0 ** -20, e)
+        hi = ref.quantised(c + np.abs(c) * 2.0 ** -20, e)
+        assert ((np.minimum(lo, hi) <= got) & (got <= np.maximum(lo, hi))).all()
+        assert (got != ref.quantised(c, e)).mean() < 1e-3
+    else:
+        helpers.check_nearest_bf16(out[:, :lat].contiguous().cpu().view(torch.int16).numpy().view(np.uint16), c, np.abs(c))
+    if heads:
+        want = ref.rotated(ref.f64(given[..., hd:]), pos, freqs, style)
+        helpers.check_nearest_bf16(q_out[..., hd:].contiguous().cpu().view(torch.int16).numpy().view(np.uint16), want,
+                                   helpers.plane_scale(want, 64, style))
+        assert torch.equal(q_out[..., :hd], given[..., :hd])
+        if not in_place:
+            assert torch.equal(q, given)
+
+
+def test_store_rope_far_positions_and_given_rates(setup):
+    """Positions past 2^24, where an angle in float32 would have no digits left, with a rate table."""
+    far = (1 << 27) + 3
+    pages = torch.zeros(-(-(far + 2) // 16), dtype=torch.int32, device=DEV)
+    s = setup([0], [16], 256, False)
+    b = kvx.Batch([far], [2], [0, len(pages)], pages)
+    kv = s.normal(2, 320)
+    inv = np.random.default_rng(0).uniform(0, 1.5, 32)
+    kvx.store_latent_rope(s.pool, b, kv, inv_freq=inv, style=1)
+    out = torch.empty(2, 320, dtype=BF16, device=DEV)
+    kvx.load_latent(s.pool, b, out)
+    want = ref.rotated(ref.f64(kv[:, 256:]), np.array([far, far + 1]), inv, 1)
+    # the angle in float64 carries 2^-53 * 2^27 * 1.5 of a radian, far below float32's rounding
+    helpers.check_nearest_bf16(out[:, 256:].contiguous().cpu().view(torch.int16).numpy().view(np.uint16), want,
+                               helpers.plane_scale(want, 64, 1))
+    assert torch.equal(out[:, :256], kv[:, :256])
+
+
+# ------------------------------------------------------------------- attention on latents
+
+# rms: the weights' rounding and the output's, each at most 2^-8 / sqrt(3) of the value rms
+RMS_ATTEND = math.sqrt(2 / 3) * 2.0 ** -8 * 1.05
+
+
+def attend_and_check(s, rows, heads, scale, q=None, tag=""):
+    q = s.normal(s.T, heads, s.lat + 64) if q is None else q
+    out = torch.full((s.T + 1, heads, s.lat), 7.0, dtype=BF16, device=DEV)
+    lse = torch.full((s.T + 1, heads), 7.0, dtype=torch.float32, device=DEV)
+    kvx.latent_attention(s.pool, s.batch, q, heads, scale, out, lse)
+    at = 0
+    assert (out[s.T] == 7).all() and (lse[s.T] == 7).all()
+    for r, (p, e) in enumerate(zip(s.P, s.E)):
+        if e == 0:
+            continue
+        o, l, tol, ltol = ref.attend(ref.f64(q[at:at + e]), rows[r], rows[r][:, :s.lat], p, scale)
+        ref.check_rows(out[at:at + e], o, tol, RMS_ATTEND, f"{tag} request {r}")
+        assert (np.abs(ref.f64(lse[at:at + e]) - l) <= ltol).all(), f"{tag} request {r}: lse"
+        at += e
+    return out, lse
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lat,heads,P,E", [
+    (512, 1, [0], [1]),                        # one key, one row
+    (512, 16, [0, 62, 63, 64, 500], [1, 1, 1, 1, 1]),   # around a tile's end
+    (512, 5, [100, 3, 40], [2, 0, 3]),         # rows of two 16-row blocks, a request without any
+    (256, 33, [200, 17], [1, 2]),              # odd heads
+    (512, 128, [129, 300], [1, 2]),            # tiles that end inside a token
+    (256, 7, [0, 31], [70, 33]),               # the causal edge inside tiles
+    (512, 24, [1000], [9]),
+])
+def test_latent_attention(setup, lat, heads, P, E, fp8):
+    s = setup(P, E, lat, fp8)
+    attend_and_check(s, s.fill(), heads, (128 + 64) ** -0.5)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("split", [64, 192])
+def test_latent_attention_split(setup, split, fp8):
+    """Forced splits, the causal edge in several parts (some of which a tile's first rows do
+    not see at all)."""
+    for lat, heads, P, E in ((512, 16, [700, 10, 64], [1, 1, 1]), (256, 6, [40, 300], [150, 90])):
+        s = setup(P, E, lat, fp8)
+        kvx.latent_pool_set_split_keys(s.pool, split)
+        attend_and_check(s, s.fill(), heads, 0.07)
+
+
+@pytest.mark.parametrize("heads,E", [(16, 1), (20, 1), (16, 5)])
+def test_latent_attention_uneven_scores(setup, heads, E):
+    """Scores from very low to very high along the keys: a late key that outweighs all before
+    it by far more than float32's range of exponents, then the reverse."""
+    for order in (1, -1):
+        s = setup([400], [E], 512, False)
+        rows = s.normal(400 + E, 576)
+        rows[:, 0] = (torch.linspace(-30, 30, 400 + E, device=DEV) * order).to(BF16)
+        q = s.normal(E, heads, 576, scale=0.3)
+        q[..., 0] = 60.0
+        attend_and_check(s, s.fill(rows=rows), heads, 0.5, q=q)
+
+
+def test_latent_attention_equal_keys_and_zero_scale_rows(setup):
+    """All scores equal: the mean of the values, and the log of their number."""
+    s = setup([63], [1], 512, False)
+    rows = s.fill()
+    q = torch.zeros(1, 16, 576, dtype=BF16, device=DEV)
+    out, lse = attend_and_check(s, rows, 16, 0.1, q=q)
+    assert np.allclose(ref.f64(lse[0]), math.log(64), atol=1e-6)
+
+
+def test_latent_attention_long(setup):
+    """A cache whose slots lie past 2^31 bytes, by a page table that names its last pages."""
+    n = (1 << 31) // 18432 + 40
+    s = setup([500], [1], 512, False, poison=False, extra_pages=n)
+    s.pages = torch.arange(s.num_pages - 32, s.num_pages, dtype=torch.int32, device=DEV)
+    s.batch = kvx.Batch(s.P, s.E, s.indptr, s.pages)
+    attend_and_check(s, s.fill(), 16, 0.07)
+
+
+def test_latent_attention_matches_itself_on_another_stream(setup):
+    s = setup([300, 800], [1, 3], 512, True)
+    rows = s.fill()
+    q = s.normal(s.T, 16, 576)
+    a, _ = attend_and_check(s, rows, 16, 0.07, q=q)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    b = torch.empty_like(a[:s.T])
+    with torch.cuda.stream(other):
+        kvx.latent_attention(s.pool, s.batch, q, 16, 0.07, b)
+    other.synchronize()
+    assert torch.equal(a[:s.T], b)
+
+
+# ------------------------------------------------------------------- per-head attention
+
+# rms: roundings of the scores' operand, the weights, the sums or values, and the output, each
+# at most 2^-8 / sqrt(3); scores of about unit size pass theirs on one to one
+RMS_EXTEND = math.sqrt(4 / 3) * 2.0 ** -8 * 1.1
+
+
+def extend_and_check(s, rows, heads, hd, form, tag=""):
+    lat = s.lat
+    q = s.normal(s.T, heads, hd + 64)
+    w_uk = s.normal(heads, hd, lat, scale=lat ** -0.5)
+    w_uv = s.normal(heads, hd, lat, scale=lat ** -0.5)
+    scale = (hd + 64) ** -0.5
+    out = torch.full((s.T + 1, heads, hd), 7.0, dtype=BF16, device=DEV)
+    lse = torch.full((s.T + 1, heads), 7.0, dtype=torch.float32, device=DEV)
+    kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, scale, out, lse, form=form)
+    assert (out[s.T] == 7).all() and (lse[s.T] == 7).all()
+    at = 0
+    uk, uv = ref.f64(w_uk), ref.f64(w_uv)
+    for r, (p, e) in enumerate(zip(s.P, s.E)):
+        if e == 0:
+            continue
+        c, key = rows[r][:, :lat], rows[r][:, lat:]
+        x = ref.f64(q[at:at + e])
+        h = ref.HALF_BF16
+        k = np.concatenate([np.einsum("hdl,jl->hjd", uk, c), np.broadcast_to(key, (heads,) + key.shape)], -1)
+        v = np.einsum("hdl,jl->hjd", uv, c)
+        o, l, tol, ltol = ref.attend(x, k, v, p, scale, k_err=h, v_err=h)
+        # the absorbed form rounds q' = W_uk^T q and the sums in the latent space instead, where
+        # the products that meet those roundings are larger: bound both
+        ql = np.concatenate([np.einsum("hdl,ihd->ihl", uk, x[..., :hd]), x[..., hd:]], -1)
+        o2, l2, tol2, ltol2 = ref.attend(ql, rows[r], c, p, scale, q_err=h)
+        through = np.einsum("hdl,ihl->ihd", np.abs(uv), tol2 + h * (np.abs(o2) + tol2))
+        ref.check_rows(out[at:at + e], o, np.maximum(tol, through), RMS_EXTEND, f"{tag} request {r}")
+        assert (np.abs(ref.f64(lse[at:at + e]) - l) <= np.maximum(ltol, ltol2)).all(), f"{tag} request {r}: lse"
+        at += e
+    return out[:s.T]
+
+
+@pytest.mark.parametrize("form", [kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED, kvx.KVX_LATENT_AUTO])
+@pytest.mark.parametrize("lat,hd,heads,fp8,P,E", [
+    (512, 128, 2, False, [0], [1]),
+    (512, 128, 3, True, [100, 30, 0], [5, 0, 70]),
+    (256, 64, 4, False, [63, 64, 65], [65, 64, 63]),
+    (256, 128, 1, True, [10], [300]),          # more than one tile of tokens
+    (512, 64, 5, False, [700, 3, 200], [20, 130, 1]),
+])
+def test_latent_extend_attention(setup, lat, hd, heads, fp8, P, E, form):
+    s = setup(P, E, lat, fp8)
+    extend_and_check(s, s.fill(), heads, hd, form)
+
+
+def test_latent_extend_attention_split_keys(setup):
+    """A few rows over many keys: both forms split their key ranges."""
+    for form in (kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED):
+        s = setup([6000, 50], [40, 3], 256, False)
+        extend_and_check(s, s.fill(), 2, 64, form)
+
+
+def test_latent_extend_many_heads_in_groups(setup):
+    """Expanded keys and values of more tokens than one workspace holds for all heads at once:
+    three heads go two and one.  The tokens repeat 64 cached ones, so that a softmax over those
+    gives the result, and log of their number is added to lse."""
+    times = (2 << 30) // (2 * 128 * 2 * 64) // 2 - 40
+    L = 64 * times
+    s = setup([0], [64], 256, False)
+    rows = s.fill()[0]
+    pages = s.pages[:4].repeat(times)
+    b = kvx.Batch([L - 1], [1], [0, len(pages)], pages)
+    q = s.normal(1, 3, 192)
+    w_uk, w_uv = s.normal(3, 128, 256, scale=1 / 16), s.normal(3, 128, 256, scale=1 / 16)
+    out = torch.empty(1, 3, 128, dtype=BF16, device=DEV)
+    lse = torch.empty(1, 3, dtype=torch.float32, device=DEV)
+    kvx.latent_extend_attention(s.pool, b, q, w_uk, w_uv, 0.07, out, lse, form=kvx.KVX_LATENT_EXPANDED)
+    c, key, x = rows[:, :256], rows[:, 256:], ref.f64(q)
+    k = np.concatenate([np.einsum("hdl,jl->hjd", ref.f64(w_uk), c), np.broadcast_to(key, (3,) + key.shape)], -1)
+    v = np.einsum("hdl,jl->hjd", ref.f64(w_uv), c)
+    o, l, tol, ltol = ref.attend(x, k, v, 63, 0.07, k_err=ref.HALF_BF16, v_err=ref.HALF_BF16)
+    ref.check_rows(out, o, tol + np.abs(o) * L * 2.0 ** -24, RMS_EXTEND)
+    assert (np.abs(ref.f64(lse) - l - math.log(times)) <= ltol + L * 2.0 ** -24).all()
+
+
+# ------------------------------------------------------------------- together
+
+def test_turns_of_agents(setup):
+    """A prompt, a short turn and drafted tokens of several agents over one pool: each step
+    stores and attends as a layer does, in both forms, against attention over whole sequences."""
+    lat, hd, heads = 256, 64, 4
+    lens = [(90, 12, 3, 1), (33, 40, 1, 1), (7, 1, 2, 5)]
+    total = [sum(x) for x in lens]
+    s = setup([0] * 3, total, lat, False)
+    kv = s.normal(sum(total), lat + 64)
+    q = s.normal(sum(total), heads, hd + 64)
+    norm = 1.0 + s.normal(lat, scale=0.2)
+    w_uk, w_uv = s.normal(heads, hd, lat, scale=1 / 16), s.normal(heads, hd, lat, scale=1 / 16)
+    base = np.cumsum([0] + total)
+    scale = (hd + 64) ** -0.5
+    got = torch.empty(sum(total), heads, hd, dtype=BF16, device=DEV)
+    turned = torch.empty_like(q)
+    done = [0, 0, 0]
+    for step in range(4):
+        E = [x[step] for x in lens]
+        at = torch.cat([torch.arange(base[i] + done[i], base[i] + done[i] + E[i]) for i in range(3)]).to(DEV)
+        b = kvx.Batch(done, E, s.indptr, s.pages)
+        qs = torch.empty(len(at), heads, hd + 64, dtype=BF16, device=DEV)
+        kvx.store_latent_rope(s.pool, b, kv[at], norm=norm, q=q[at], num_q_heads=heads, q_out=qs)
+        o = torch.empty(len(at), heads, hd, dtype=BF16, device=DEV)
+        kvx.latent_extend_attention(s.pool, b, qs, w_uk, w_uv, scale, o)
+        got[at], turned[at] = o, qs
+        done = [d + e for d, e in zip(done, E)]
+    rows = torch.empty(sum(total), lat + 64, dtype=BF16, device=DEV)
+    kvx.load_latent(s.pool, kvx.Batch([0] * 3, total, s.indptr, s.pages), rows)
+    for i in range(3):
+        r = ref.f64(rows[base[i]:base[i + 1]])
+        k = np.concatenate([np.einsum("hdl,jl->hjd", ref.f64(w_uk), r[:, :lat]),
+                            np.broadcast_to(r[:, lat:], (heads, total[i], 64))], -1)
+        v = np.einsum("hdl,jl->hjd", ref.f64(w_uv), r[:, :lat])
+        o, _, tol, _ = ref.attend(ref.f64(turned[base[i]:base[i + 1]]), k, v, 0, scale, k_err=ref.HALF_BF16,
+                                  v_err=ref.HALF_BF16)
+        g = ref.f64(got[base[i]:base[i + 1]])
+        assert np.linalg.norm(g - o) <= RMS_EXTEND * np.linalg.norm(o)
