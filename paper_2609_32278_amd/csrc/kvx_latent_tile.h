@@ -37,6 +37,21 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
+// Keep an operand that is used throughout a unit in the accumulator half of the register
+// file, which the matrix instructions read as well.
+__device__ __forceinline__ void keep_in_acc(bf16x8& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm("" : "+a"(x));
+#endif
+}
+// An address offset that the compiler shall not take apart, so that one register and an
+// immediate make each address.
+__device__ __forceinline__ void opaque(uint32_t& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm("" : "+v"(x));
+#endif
+}
+
 // The transposing LDS read: lanes 4 j + i of 16 point at 4 values each of row j (16 values
 // side by side); lane i receives column i of the four rows.
 __device__ __forceinline__ s16x4 read_tr(const uint8_t* at) {
@@ -44,9 +59,58 @@ __device__ __forceinline__ s16x4 read_tr(const uint8_t* at) {
       (__attribute__((address_space(3))) s16x4*)(__attribute__((address_space(3))) void*)at);
 }
 
+typedef const __attribute__((address_space(3))) uint8_t* lds_ptr;
+__device__ __forceinline__ s16x4 read_tr(lds_ptr at) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
+}
+__device__ __forceinline__ bf16x8 read_b128(lds_ptr at) {
+  return *(const __attribute__((address_space(3))) bf16x8*)at;
+}
+
+__device__ __forceinline__ void write_b64(uint32_t at, uint32_t x, uint32_t y) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  *(__attribute__((address_space(3))) u32x2*)at = u32x2{x, y};
+}
+
 __device__ __forceinline__ bf16x8 join(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
+
+// Direct global -> LDS load of 1 KiB: lane l's 16 bytes at base + off land at LDS address
+// lds + 16 l.  Inline assembly, so that the compiler's wait counts, which cannot tell the
+// buffers apart, do not drain these loads; the kernels wait themselves.
+__device__ __forceinline__ void lds_load_1k(const uint8_t* base, int off, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(lds), "v"(off), "s"(base)
+      : "memory", "m0");
+}
+// ... with an address per lane
+__device__ __forceinline__ void lds_load_1k(const uint8_t* lane_address, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, off"
+      :
+      : "s"(lds), "v"(lane_address)
+      : "memory", "m0");
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p;
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  // s_waitcnt with only the vector-memory counter limited (expcnt, lgkmcnt at max)
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+
+typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;  // scalar-loaded
 
 // Stage tokens key0 .. key0 + 63 of a request (its page list at page_ids) as bf16 rows;
 // tokens at or past key_end are replaced by token `safe`, so that no slot that the request
