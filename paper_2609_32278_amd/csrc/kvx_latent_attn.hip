@@ -354,7 +354,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
       bf16x8 pb[2][RB];
       auto read_p = [&](int k2) {
 #pragma unroll
-        for (int rb = 0; rb < RB; rb++) pb[k2][rb] = read_b128((lds_ptr)pr_at[k2] + rb * 2048);
+        for (int rb = 0; rb < RB; rb++) pb[k2][rb] = read_b128(lds_at(pr_at[k2]) + rb * 2048);
       };
       read_p(0);
 #pragma unroll

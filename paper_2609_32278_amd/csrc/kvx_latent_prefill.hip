@@ -1,45 +1,66 @@
 // Attention of per-head queries to expanded keys and values, gfx950.
+#include <type_traits>
+
 #include "kvx_latent_tile.h"
 
 namespace kvx {
 namespace {
 
 constexpr int kThreads = 256;  // 4 waves x 64 tokens
-constexpr int kBN = 64;
+constexpr int kBN = 64;        // keys per tile
+constexpr int kStages = 3;     // tiles in LDS: one attended, one arriving, one being left
 
+// LDS layout of a tile: groups of 8 rows, in a group blocks of 128 bytes of the rows,
+// [group][block][8 rows][128 bytes]: K rows are the expanded part and then the shared rotated
+// key, V rows follow after the 64 K rows.  A wave-wide direct load of 1 KiB fills a block; the
+// 16-byte chunks of a row in a block are stored in the order c ^ swz(row), which keeps operand
+// reads (16 rows one chunk; 4 rows two chunks) free of bank conflicts.
 template <int D>
 struct PreGeom {
   static constexpr int QK = D + kLatRope;
-  static constexpr int KS = QK / 16;
-  static constexpr int DB = D / 32;
-  static constexpr int KROWB = QK * 2;
-  static constexpr int VROWB = D * 2;
+  static constexpr int KS = QK / 16;   // score product steps
+  static constexpr int DB = D / 32;    // 32-dim blocks of the sums
+  static constexpr int VB = D / 64;    // blocks of a V row
+  static constexpr int KB = VB + 1;    // blocks of a K row
+  static constexpr int V0 = 8 * KB * 1024;
+  static constexpr int STAGE = V0 + 8 * VB * 1024;
 };
-
-// Stored chunk of chunk c of a row.  K rows of 384 bytes are 32 banks apart modulo 64, those
-// of 256 bytes none; V rows of 256 bytes none, those of 128 bytes 32.
-template <int D>
-__device__ __forceinline__ int kswz(int r) {
-  if constexpr (D == 128) return swz(r);
-  else return r & 15;
-}
-template <int D>
-__device__ __forceinline__ int vswz(int r) {
-  if constexpr (D == 128) return ((r & 3) << 1) | ((r >> 2) & 1) | (r & 8);
-  else return (r & 2) | (r & 4) | ((r >> 3) & 1);
-}
 
 template <int D>
 __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefillParams p) {
   using G = PreGeom<D>;
-  __shared__ __attribute__((aligned(1024))) uint8_t kl[kBN * G::KROWB];
-  __shared__ __attribute__((aligned(1024))) uint8_t vl[kBN * G::VROWB];
+  constexpr int AK = 4, AV = 3;  // operand reads ahead of their products
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * G::STAGE];
   const LatentTile u = p.units[blockIdx.x];
   const int ntok = u.head_ntok & 0xFFFF, hd = u.head_ntok >> 16;
   if (ntok == 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
   const int Hq = p.num_q_heads;
+
+  const int n_tiles = (u.key_end - u.key_begin + kBN - 1) / kBN;
+  // this wave's loads: row groups 2 wave and 2 wave + 1 of a tile
+  const uint8_t* kx = (const uint8_t*)(p.kx + ((size_t)hd * p.x_rows + u.x_row + u.key_begin + wave * 16) * D);
+  const uint8_t* vx = (const uint8_t*)(p.vx + ((size_t)hd * p.x_rows + u.x_row + u.key_begin + wave * 16) * D);
+  const uint8_t* rx = (const uint8_t*)(p.rx + (size_t)(u.x_row + u.key_begin + wave * 16) * kLatRope);
+  const int chunk = ((lane & 7) ^ swz(lane >> 3)) << 4;
+  const int off_x = (lane >> 3) * (D * 2) + chunk, off_r = (lane >> 3) * (kLatRope * 2) + chunk;
+  const uint32_t lds0 = lds_address(lds) + wave * (2 * G::KB * 1024), lds0v = lds_address(lds) + G::V0 + wave * (2 * G::VB * 1024);
+  auto issue = [&](int t) {
+    const size_t at = (size_t)t * kBN;
+    const uint32_t st = (uint32_t)(t % kStages) * G::STAGE;
+#pragma unroll
+    for (int gr = 0; gr < 2; gr++) {
+      const int flip = gr ? 16 : 0;  // row bit 3 in swz
+#pragma unroll
+      for (int b = 0; b < G::VB; b++) {
+        lds_load_1k(kx + (at + gr * 8) * (D * 2) + b * 128, off_x ^ flip, lds0 + st + (gr * G::KB + b) * 1024);
+        lds_load_1k(vx + (at + gr * 8) * (D * 2) + b * 128, off_x ^ flip, lds0v + st + (gr * G::VB + b) * 1024);
+      }
+      lds_load_1k(rx + (at + gr * 8) * (kLatRope * 2), off_r ^ flip, lds0 + st + (gr * G::KB + G::VB) * 1024);
+    }
+  };
+
   bf16x8 qf[2][G::KS];
   int limit[2];
   int64_t flat[2];
@@ -50,107 +71,203 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
     limit[rb] = u.pos0 + t < u.key_end ? u.pos0 + t : u.key_end - 1;
     const uint4* src = (const uint4*)(p.q + flat[rb] * G::QK);
 #pragma unroll
-    for (int ks = 0; ks < G::KS; ks++) qf[rb][ks] = __builtin_bit_cast(bf16x8, src[ks * 2 + h]);
+    for (int ks = 0; ks < G::KS; ks++) {
+      qf[rb][ks] = __builtin_bit_cast(bf16x8, src[ks * 2 + h]);
+      keep_in_acc(qf[rb][ks]);
+    }
   }
-  const uint16_t* kx = p.kx + ((size_t)hd * p.x_rows + u.x_row) * D;
-  const uint16_t* vx = p.vx + ((size_t)hd * p.x_rows + u.x_row) * D;
-  const uint16_t* rx = p.rx + (size_t)u.x_row * kLatRope;
+  const int full_end = u.pos0 + 1 < u.key_end ? u.pos0 + 1 : u.key_end;  // keys before it are seen by every row
+
   f32x16 o[2][G::DB];
-  float m_run[2], l_run[2];
+  float m[2], ref[2], l[2];
+  const float scale = p.scale_log2;
+  uint32_t kat[4], vat[2][2];
 #pragma unroll
-  for (int rb = 0; rb < 2; rb++) {
-    m_run[rb] = -INFINITY;
-    l_run[rb] = 0.0f;
-#pragma unroll
-    for (int db = 0; db < G::DB; db++) o[rb][db] = f32x16{};
+  for (int i = 0; i < 4; i++) {
+    kat[i] = lds_address(lds) + (n >> 3) * (G::KB * 1024) + (n & 7) * 128 + (((2 * i + h) ^ swz(n)) << 4);
+    opaque(kat[i]);
   }
-  for (int k0 = u.key_begin; k0 < u.key_end; k0 += kBN) {
-    __syncthreads();
-    for (int i = tid; i < kBN * (D / 8); i += kThreads) {
-      const int r = i / (D / 8), c = i % (D / 8);
-      *(uint4*)(kl + r * G::KROWB + ((c ^ kswz<D>(r)) * 16)) = *(const uint4*)(kx + (size_t)(k0 + r) * D + c * 8);
-      *(uint4*)(vl + r * G::VROWB + ((c ^ vswz<D>(r)) * 16)) = *(const uint4*)(vx + (size_t)(k0 + r) * D + c * 8);
+#pragma unroll
+  for (int e = 0; e < 2; e++)
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+      const int r = 8 * e + 4 * h + (lane & 15) / 4;
+      vat[e][i] = lds_address(lds) + G::V0 + (r >> 3) * (G::VB * 1024) + (r & 7) * 128 +
+                  (((4 * i + 2 * (n >> 4) + (lane & 3) / 2) ^ swz(r)) << 4) + (lane & 1) * 8;
+      opaque(vat[e][i]);
     }
-    for (int i = tid; i < kBN * 8; i += kThreads) {
-      const int r = i / 8, c = i % 8;
-      *(uint4*)(kl + r * G::KROWB + (((D / 8 + c) ^ kswz<D>(r)) * 16)) =
-          *(const uint4*)(rx + (size_t)(k0 + r) * kLatRope + c * 8);
+
+  bf16x8 ka[AK + 1], va[AV + 1];
+  // 32 keys at a time: half `kb` of the tile in stage `st`
+  auto read_k = [&](uint32_t st, int kb, int ks) {
+    return read_b128(lds_at(kat[ks & 3] + st) + (ks >> 2) * 1024 + kb * (4 * G::KB * 1024));
+  };
+  auto read_v = [&](uint32_t st, int kb, int j) {  // step j: 16 keys (j / DB), dim block j % DB
+    const int db = j % G::DB, at = (2 * (2 * kb + j / G::DB)) * (G::VB * 1024) + (db >> 1) * 1024;
+    return join(read_tr(lds_at(vat[0][db & 1] + st) + at), read_tr(lds_at(vat[1][db & 1] + st) + at));
+  };
+  auto start_k = [&](uint32_t st, int kb) {
+#pragma unroll
+    for (int j = 0; j < AK; j++) ka[j] = read_k(st, kb, j);
+  };
+  auto start_v = [&](uint32_t st, int kb) {
+#pragma unroll
+    for (int j = 0; j < AV; j++) va[j] = read_v(st, kb, j);
+  };
+
+  uint32_t pk[2][8];  // weights of 32 keys, as pairs
+  // The i-th of the 32 scores of a lane (16 of each row): its weight, and pairs packed.
+  auto weigh = [&](f32x16 (&s)[2], int i) {
+    const int rb = i / 16, e = i % 16;
+    s[rb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][e], scale, -ref[rb]));
+    l[rb] += s[rb][e];
+    if (e & 1) {
+      pk[rb][e / 2] = pack_bf16(s[rb][e - 1], s[rb][e]);
+      formed(pk[rb][e / 2]);
+      formed(l[rb]);
     }
-    __syncthreads();
-    f32x16 s[2][2];  // [row block][key block]
+  };
+  // S of 32 keys into `s`, the weights of `w` formed between its steps; START_V: the first V
+  // operands of (vst, vkb) are read before the last steps.
+  auto scores = [&](f32x16 (&s)[2], uint32_t st, int kb, f32x16 (&w)[2], auto weights, uint32_t vst, int vkb) {
+    constexpr bool W = decltype(weights)::value;
+    s[0] = f32x16{};
+    s[1] = f32x16{};
 #pragma unroll
-    for (int rb = 0; rb < 2; rb++) s[rb][0] = s[rb][1] = f32x16{};
+    for (int ks = 0; ks < G::KS; ks++) {
+      if (ks + AK < G::KS) ka[(ks + AK) % (AK + 1)] = read_k(st, kb, ks + AK);
+      if (W && ks == G::KS - 3) start_v(vst, vkb);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int ks = 0; ks < G::KS; ks++)
+      for (int rb = 0; rb < 2; rb++) {
+        s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks % (AK + 1)], qf[rb][ks], s[rb], 0, 0, 0);
+        if constexpr (W) {
 #pragma unroll
-      for (int kb = 0; kb < 2; kb++) {
-        const int r = kb * 32 + n;
-        const bf16x8 a = *(const bf16x8*)(kl + r * G::KROWB + (((ks * 2 + h) ^ kswz<D>(r)) * 16));
-#pragma unroll
-        for (int rb = 0; rb < 2; rb++)
-          s[rb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[rb][ks], s[rb][kb], 0, 0, 0);
+          for (int i = 0; i < 32; i++)
+            if (i * 2 * G::KS / 32 == ks * 2 + rb) weigh(w, i);
+        }
       }
-    // accumulator i of a key block holds key 8 (i / 4) + 4 h + i % 4 of it
-    bf16x8 pb[2][4];
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto values = [&](uint32_t st, int kb) {
+#pragma unroll
+    for (int j = 0; j < 2 * G::DB; j++) {
+      if (j + AV < 2 * G::DB) va[(j + AV) % (AV + 1)] = read_v(st, kb, j + AV);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int rb = 0; rb < 2; rb++) {
+        const int half = j / G::DB * 4;
+        const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(pk[rb][half], pk[rb][half + 1], pk[rb][half + 2], pk[rb][half + 3]));
+        o[rb][j % G::DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j % (AV + 1)], b, o[rb][j % G::DB], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // accumulator i of a row holds key 8 (i / 4) + 4 h + i % 4 of the 32
+  auto mask = [&](f32x16 (&s)[2], int k0) {
+#pragma unroll
+    for (int rb = 0; rb < 2; rb++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) s[rb][i] = k0 + 8 * (i / 4) + 4 * h + i % 4 <= limit[rb] ? s[rb][i] : -INFINITY;
+  };
+  // the reference point moves to the maximum of these scores where that is larger
+  auto rereference = [&](f32x16 (&s)[2]) {
 #pragma unroll
     for (int rb = 0; rb < 2; rb++) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-          const int key = k0 + kb * 32 + 8 * (i / 4) + 4 * h + i % 4;
-          const float x = key <= limit[rb] ? s[rb][kb][i] * p.scale_log2 : -INFINITY;
-          s[rb][kb][i] = x;
-          mx = fmaxf(mx, x);
-        }
+      for (int i = 0; i < 16; i++) mx = fmaxf(mx, s[rb][i]);
+      mx *= scale;
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float m_new = fmaxf(m_run[rb], mx), m = m_new == -INFINITY ? 0.0f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m_run[rb] - m);
-      m_run[rb] = m_new;
-      float sum = 0.0f;
-#pragma unroll
-      for (int kb = 0; kb < 2; kb++)
-#pragma unroll
-        for (int half = 0; half < 2; half++) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            const float a = __builtin_amdgcn_exp2f(s[rb][kb][8 * half + 2 * e] - m);
-            const float b = __builtin_amdgcn_exp2f(s[rb][kb][8 * half + 2 * e + 1] - m);
-            sum += a + b;
-            w[e] = pack_bf16(a, b);
-          }
-          pb[rb][2 * kb + half] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-        }
-      l_run[rb] = l_run[rb] * alpha + sum;
+      const float m_new = fmaxf(m[rb], mx);
+      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[rb] - m_new);
+      l[rb] *= alpha;
 #pragma unroll
       for (int db = 0; db < G::DB; db++) o[rb][db] *= alpha;
+      m[rb] = m_new;
+      ref[rb] = m_new == -INFINITY ? 0.0f : m_new;
     }
-    // 16 keys a step: slot (h, j) of the step is key 8 (j / 4) + 4 h + j % 4, as P has them
+  };
+
+  // One pass over the keys.  FIXED: the reference point stays at the maximum of the first 32.
+  auto run = [&](auto fixed) {
+    constexpr bool FIXED = decltype(fixed)::value;
 #pragma unroll
-    for (int st = 0; st < 4; st++)
+    for (int rb = 0; rb < 2; rb++) {
+      m[rb] = -INFINITY;
+      l[rb] = 0.0f;
 #pragma unroll
-      for (int db = 0; db < G::DB; db++) {
-        s16x4 v[2];
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const int r = st * 16 + 8 * e + 4 * h + (lane & 15) / 4;
-          const int c = (db * 32 + (n & 16)) / 8 + (lane & 3) / 2;
-          v[e] = read_tr(vl + r * G::VROWB + ((c ^ vswz<D>(r)) * 16) + (lane & 1) * 8);
-        }
-        const bf16x8 a = join(v[0], v[1]);
-#pragma unroll
-        for (int rb = 0; rb < 2; rb++)
-          o[rb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[rb][st], o[rb][db], 0, 0, 0);
+      for (int db = 0; db < G::DB; db++) o[rb][db] = f32x16{};
+    }
+    issue(0);
+    if (n_tiles > 1) issue(1);
+    if (n_tiles > 1) wait_vmcnt<2 * (2 * G::VB + 1)>();
+    else wait_vmcnt<0>();
+    __syncthreads();
+    f32x16 sa[2], sb[2];
+    start_k(0, 0);
+    scores(sa, 0, 0, sb, std::false_type{}, 0, 0);
+    if (u.key_begin + 32 > full_end) mask(sa, u.key_begin);
+    rereference(sa);
+    start_k(0, 1);
+    uint32_t st = 0;
+    for (int t = 0; t < n_tiles; t++) {
+      const int k0 = u.key_begin + t * kBN;
+      const uint32_t next = st == (kStages - 1) * G::STAGE ? 0 : st + G::STAGE;
+      const bool more = t + 1 < n_tiles;
+      if constexpr (!FIXED) {
+        if (t > 0) rereference(sa);
       }
-  }
+      scores(sb, st, 1, sa, std::true_type{}, st, 0);
+      if (k0 + 64 > full_end) mask(sb, k0 + 32);
+      // tile t + 1 is whole, and every wave is past tile t - 1, whose stage tile t + 2 takes
+      if (more) {
+        wait_vmcnt<0>();
+        __syncthreads();
+        if (t + 2 < n_tiles) issue(t + 2);
+        start_k(next, 0);
+      }
+      values(st, 0);
+      if constexpr (!FIXED) rereference(sb);
+      if (more) {
+        scores(sa, next, 0, sb, std::true_type{}, st, 1);
+        if (k0 + 96 > full_end) mask(sa, k0 + 64);
+        start_k(next, 1);
+      } else {
+        start_v(st, 1);
+#pragma unroll
+        for (int i = 0; i < 32; i++) weigh(sb, i);
+      }
+      values(st, 1);
+      st = next;
+    }
+    __syncthreads();
+  };
+  // As in the attention on latents: only where an exponential or a sum overflows float32 are
+  // the keys gone over again with a reference that moves.
+  run(std::true_type{});
+  float acc = l[0] + l[1];
+#pragma unroll
+  for (int rb = 0; rb < 2; rb++)
+#pragma unroll
+    for (int db = 0; db < G::DB; db++)
+#pragma unroll
+      for (int i = 0; i < 16; i++) acc += o[rb][db][i];
+  const bool bad = __any(!__builtin_isfinite(acc));
+  volatile int* flags = (volatile int*)lds;
+  if (lane == 0) flags[wave] = bad;
+  __syncthreads();
+  const bool again = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+  __syncthreads();
+  if (again) run(std::false_type{});
+
 #pragma unroll
   for (int rb = 0; rb < 2; rb++) {
     const int tok = wave * 64 + rb * 32 + n;
-    const float l = l_run[rb] + __shfl_xor(l_run[rb], 32, 64);
-    const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
-    const float lse2 = l == 0.0f ? -INFINITY : m_run[rb] + __log2f(l);
+    const float lt = l[rb] + __shfl_xor(l[rb], 32, 64);
+    const float inv = lt > 0.0f ? 1.0f / lt : (lt == 0.0f ? 0.0f : lt);
+    const float lse2 = lt == 0.0f ? -INFINITY : m[rb] + __log2f(lt);
     if (tok >= ntok) continue;
     if (u.part < 0) {
       uint16_t* dst = p.out + flat[rb] * D + 4 * h;

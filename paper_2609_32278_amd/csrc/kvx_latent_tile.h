@@ -52,6 +52,14 @@ __device__ __forceinline__ void opaque(uint32_t& x) {
 #endif
 }
 
+// A value to be formed here, not where the compiler finds it used.
+template <typename T>
+__device__ __forceinline__ void formed(T& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(x));
+#endif
+}
+
 // The transposing LDS read: lanes 4 j + i of 16 point at 4 values each of row j (16 values
 // side by side); lane i receives column i of the four rows.
 __device__ __forceinline__ s16x4 read_tr(const uint8_t* at) {
@@ -60,6 +68,7 @@ __device__ __forceinline__ s16x4 read_tr(const uint8_t* at) {
 }
 
 typedef const __attribute__((address_space(3))) uint8_t* lds_ptr;
+__device__ __forceinline__ lds_ptr lds_at(uint32_t at) { return (lds_ptr)(uintptr_t)at; }
 __device__ __forceinline__ s16x4 read_tr(lds_ptr at) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
 }
@@ -69,7 +78,7 @@ __device__ __forceinline__ bf16x8 read_b128(lds_ptr at) {
 
 __device__ __forceinline__ void write_b64(uint32_t at, uint32_t x, uint32_t y) {
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  *(__attribute__((address_space(3))) u32x2*)at = u32x2{x, y};
+  *(__attribute__((address_space(3))) u32x2*)(uintptr_t)at = u32x2{x, y};
 }
 
 __device__ __forceinline__ bf16x8 join(s16x4 a, s16x4 b) {
