@@ -400,10 +400,11 @@ int64_t expand_units(const kvx_batch* b, const std::vector<int32_t>& reqs, std::
   for (int32_t r : reqs) {
     const int64_t L = (int64_t)b->prefix_lens[r] + b->extend_lens[r];
     x_row.push_back(at);
-    for (int64_t k = 0; k < L; k += 64) {
-      out.push_back({(int32_t)(at + k), b->page_indptr[r], (int32_t)k, (int32_t)L});
-    }
-    at += ceil_div(L, 64) * 64;
+    const int64_t rows = ceil_div(L, 64) * 64;
+    for (int64_t k = 0; k < rows; k += kvx::kLatExpandTok)
+      out.push_back({(int32_t)(at + k), b->page_indptr[r], (int32_t)k, (int32_t)L,
+                     (int32_t)std::min<int64_t>(kvx::kLatExpandTok, rows - k), 0});
+    at += rows;
   }
   return at;
 }

@@ -131,12 +131,15 @@ struct LatentProjParams {
   int32_t num_q_heads;
 };
 
-// 64 cached tokens of a request to the keys and values of `heads` heads.
+// Up to 256 cached tokens of a request, for the keys and values of all heads of a group.
+constexpr int kLatExpandTok = 256;
 struct LatentExpandUnit {
   int32_t x_row;      // first row in the expanded buffers (a multiple of 64)
   int32_t page_base;
-  int32_t key0;       // first token (a multiple of 64)
+  int32_t key0;       // first token (a multiple of kLatExpandTok)
   int32_t key_end;    // tokens of the request; rows past it repeat its last one
+  int32_t nrows;      // rows to write, a multiple of 64
+  int32_t pad;
 };
 
 struct LatentExpandParams {
@@ -149,6 +152,7 @@ struct LatentExpandParams {
   const LatentExpandUnit* units;
   int64_t x_rows;
   int32_t heads;
+  int32_t heads_per;     // per workgroup (set by the launcher)
 };
 
 // One workgroup of expanded attention: tokens of one request and head against a range of
