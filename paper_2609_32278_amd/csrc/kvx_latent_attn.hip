@@ -163,8 +163,56 @@ struct Loader<LAT, true> {
   }
 };
 
-template <int LAT, bool FP8, int RB>
-__global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnParams p) {
+// Where the units are: in memory, or in the arguments that follow the parameters.
+struct InMemory {};
+
+__device__ __forceinline__ LatentUnit unit_of(const LatentAttnParams& p, const InMemory&) { return p.units[blockIdx.x]; }
+__device__ __forceinline__ LatentUnit unit_of(const LatentAttnParams&, const LatentSmallPlan& plan) {
+  const uint32_t code = plan.code[blockIdx.x];
+  LatentUnit u{};
+  if (code == kLatNoUnit) return u;
+  const LatentSmallTile& t = plan.tile[code >> 10];
+  const int c = code & (kLatSmallParts - 1);
+  u.row0 = t.row0;
+  u.nrows = t.nrows;
+  u.qo = t.qo;
+  u.prefix = t.prefix;
+  u.page_base = t.page_base;
+  u.key_begin = c * t.len;
+  u.key_end = t.key_end < u.key_begin + t.len ? t.key_end : u.key_begin + t.len;
+  u.part = t.key_end > t.len ? t.part0 + c : -1;
+  return u;
+}
+__device__ __forceinline__ LatentUnit unit_of(const LatentAttnParams& p, const LatentRowPlan& plan) {
+  const int lane = threadIdx.x & 63, b = (int)blockIdx.x;
+  static_assert(kLatRowReqs == 128, "two requests a lane");
+  const int r = __popcll(__ballot(plan.first[lane] <= b)) + __popcll(__ballot(plan.first[64 + lane] <= b)) - 1;
+  LatentUnit u;
+  const int len = plan.len[r], c = b - plan.first[r], end = plan.prefix[r] + plan.extend[r];
+  u.row0 = 0;
+  u.nrows = plan.extend[r] * p.num_q_heads;
+  u.qo = plan.qo[r];
+  u.prefix = plan.prefix[r];
+  u.page_base = plan.page_base[r];
+  u.key_begin = c * len;
+  u.key_end = end < u.key_begin + len ? end : u.key_begin + len;
+  u.part = end > len ? plan.part0[r] + c : -1;
+  return u;
+}
+__device__ __forceinline__ LatentMerge merge_of(const LatentMergeParams& p, const LatentRowPlan& plan) {
+  const int r = blockIdx.x, len = plan.len[r], end = plan.prefix[r] + plan.extend[r];
+  return {0, plan.extend[r] * p.num_q_heads, plan.qo[r], plan.part0[r], end > len ? (end + len - 1) / len : 0, 0};
+}
+__device__ __forceinline__ LatentMerge merge_of(const LatentMergeParams& p, const InMemory&) {
+  return p.merges[blockIdx.x];
+}
+__device__ __forceinline__ LatentMerge merge_of(const LatentMergeParams&, const LatentSmallPlan& plan) {
+  const LatentSmallTile& t = plan.tile[blockIdx.x];
+  return {t.row0, t.nrows, t.qo, t.part0, t.key_end > t.len ? (t.key_end + t.len - 1) / t.len : 0, 0};
+}
+
+template <int LAT, bool FP8, int RB, class Plan>
+__global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnParams p, Plan plan) {
   using G = LatGeom<LAT>;
   constexpr int RW = RB == 4 ? 2 : 1, KW = 4 / RW;  // waves by rows and by keys in the score product
   constexpr int RBW = RB / RW, KBW = 4 / KW;        // 16-row and 16-key blocks of a wave in it
@@ -174,7 +222,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   __shared__ __attribute__((aligned(16))) uint8_t pl[RB * 16 * 128];  // softmax weights [row][key]
   float (*red)[RB * 16] = (float (*)[RB * 16])pl;  // between the waves, while no weights are there
   static_assert(sizeof pl >= 5 * RB * 16 * sizeof(float), "the waves' values fit");
-  const LatentUnit u = p.units[blockIdx.x];
+  const LatentUnit u = unit_of(p, plan);
   if (u.nrows == 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
@@ -430,89 +478,106 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
 }
 
 // Log-sum-exp combination of a tile's parts.  Workgroup (merge, row block, 16-dim block of
-// every wave's share): its four waves take every fourth part, with four of them in flight
-// each, for the 64 lanes' 4 sums per share, and add up through LDS.
-template <int LAT, int RB>
-__global__ __launch_bounds__(kThreads) void latent_merge_kernel(LatentMergeParams p) {
+// the latent): 64 lanes hold its 4 sums of 16 rows each; the four waves take every fourth
+// part, eight of them in flight, and add up through LDS.
+template <int LAT, int RB, class Plan>
+__global__ __launch_bounds__(kThreads) void latent_merge_kernel(LatentMergeParams p, Plan plan) {
   using G = LatGeom<LAT>;
-  const LatentMerge m = p.merges[blockIdx.x];
-  const int rb = blockIdx.y, db = blockIdx.z;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-  __shared__ f32x4 sums[4][4][64];
-  __shared__ float totals[4][16];
-  if (rb * 16 >= m.nrows) return;
+  const LatentMerge m = merge_of(p, plan);
+  const int rb = blockIdx.y, share = blockIdx.z / G::DB, db = blockIdx.z % G::DB;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+  __shared__ f32x4 sums[4][64];
+  __shared__ float totals[4][16], tops[16][16];
+  if (m.nparts == 0 || rb * 16 >= m.nrows) return;
   const int r = rb * 16 + n;
   const float* lse = p.lse_part + (size_t)m.part0 * (RB * 16) + r;
   float top = -INFINITY;
-  for (int i = g; i < m.nparts; i += 4) top = fmaxf(top, lse[(size_t)i * (RB * 16)]);
-  top = fmaxf(top, __shfl_xor(top, 16, 64));
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
-  const float ref = top == -INFINITY ? 0.0f : top;
-  f32x4 o[4];
+  for (int i = tid >> 4; i < m.nparts; i += 16) top = fmaxf(top, lse[(size_t)i * (RB * 16)]);
+  tops[tid >> 4][n] = top;
+  __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 4; w++) o[w] = f32x4{};
+  for (int i = 0; i < 16; i++) top = fmaxf(top, tops[i][n]);
+  const float ref = top == -INFINITY ? 0.0f : top;
+  f32x4 o{};
   float total = 0.0f;
-  const float* src = p.o_part + (size_t)m.part0 * (RB * 16 * LAT) + (size_t)(rb * G::DB + db) * 256 + lane * 4;
-#pragma unroll 2
+  const float* src = p.o_part + (size_t)m.part0 * (RB * 16 * LAT) + (size_t)((share * RB + rb) * G::DB + db) * 256 + lane * 4;
+#pragma unroll 8
   for (int i = wave; i < m.nparts; i += 4) {
     const float w = __builtin_amdgcn_exp2f(lse[(size_t)i * (RB * 16)] - ref);
     total += w;
-#pragma unroll
-    for (int k = 0; k < 4; k++)
-      o[k] += *(const f32x4*)(src + (size_t)i * (RB * 16 * LAT) + (size_t)k * (RB * G::DB * 256)) * w;
+    o += *(const f32x4*)(src + (size_t)i * (RB * 16 * LAT)) * w;
   }
-#pragma unroll
-  for (int k = 0; k < 4; k++) sums[wave][k][lane] = o[k];
+  sums[wave][lane] = o;
   if (g == 0) totals[wave][n] = total;
   __syncthreads();
-  // wave k finishes share k
-  const f32x4 s = (sums[0][wave][lane] + sums[1][wave][lane]) + (sums[2][wave][lane] + sums[3][wave][lane]);
+  if (wave != 0 || r >= m.nrows) return;
+  const f32x4 s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
   total = (totals[0][n] + totals[1][n]) + (totals[2][n] + totals[3][n]);
-  if (r >= m.nrows) return;
   const float inv = total > 0.0f ? 1.0f / total : (total == 0.0f ? 0.0f : total);
   const int64_t flat = (int64_t)m.qo * p.num_q_heads + m.row0 + r;
   uint2 w;
   w.x = pack_bf16(s[0] * inv, s[1] * inv);
   w.y = pack_bf16(s[2] * inv, s[3] * inv);
-  *(uint2*)(p.out + flat * LAT + wave * G::DW + db * 16 + 4 * g) = w;
-  if (p.lse != nullptr && wave == 0 && g == 0 && db == 0) p.lse[flat] = (ref + __log2f(total)) * kLn2;
+  *(uint2*)(p.out + flat * LAT + share * G::DW + db * 16 + 4 * g) = w;
+  if (p.lse != nullptr && blockIdx.z == 0 && g == 0) p.lse[flat] = (ref + __log2f(total)) * kLn2;
 }
 
-template <int LAT, bool FP8>
-void attn_by_blocks(const LatentAttnParams& p, unsigned n, int rb, hipStream_t s) {
-  if (rb == 1) hipLaunchKernelGGL((latent_attn_kernel<LAT, FP8, 1>), dim3(n), dim3(kThreads), 0, s, p);
-  else if (rb == 2) hipLaunchKernelGGL((latent_attn_kernel<LAT, FP8, 2>), dim3(n), dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL((latent_attn_kernel<LAT, FP8, 4>), dim3(n), dim3(kThreads), 0, s, p);
+template <int LAT, bool FP8, class Plan>
+void attn_by_blocks(const LatentAttnParams& p, unsigned n, const Plan& plan, int rb, hipStream_t s) {
+  if (rb == 1) hipLaunchKernelGGL((latent_attn_kernel<LAT, FP8, 1, Plan>), dim3(n), dim3(kThreads), 0, s, p, plan);
+  else if (rb == 2) hipLaunchKernelGGL((latent_attn_kernel<LAT, FP8, 2, Plan>), dim3(n), dim3(kThreads), 0, s, p, plan);
+  else hipLaunchKernelGGL((latent_attn_kernel<LAT, FP8, 4, Plan>), dim3(n), dim3(kThreads), 0, s, p, plan);
 }
 
-template <int LAT>
-void merge_by_blocks(const LatentMergeParams& p, unsigned n, int rb, hipStream_t s) {
-  if (rb == 1) hipLaunchKernelGGL((latent_merge_kernel<LAT, 1>), dim3(n, 1, LatGeom<LAT>::DB), dim3(kThreads), 0, s, p);
-  else if (rb == 2) hipLaunchKernelGGL((latent_merge_kernel<LAT, 2>), dim3(n, 2, LatGeom<LAT>::DB), dim3(kThreads), 0, s, p);
-  else hipLaunchKernelGGL((latent_merge_kernel<LAT, 4>), dim3(n, 4, LatGeom<LAT>::DB), dim3(kThreads), 0, s, p);
+template <class Plan>
+void attn_by_pool(const LatentAttnParams& p, unsigned n, const Plan& plan, int latent_dim, bool fp8, int rb,
+                  hipStream_t s) {
+  if (latent_dim == 512) {
+    if (fp8) attn_by_blocks<512, true>(p, n, plan, rb, s);
+    else attn_by_blocks<512, false>(p, n, plan, rb, s);
+  } else {
+    if (fp8) attn_by_blocks<256, true>(p, n, plan, rb, s);
+    else attn_by_blocks<256, false>(p, n, plan, rb, s);
+  }
+}
+
+template <int LAT, class Plan>
+void merge_by_blocks(const LatentMergeParams& p, unsigned n, const Plan& plan, int rb, hipStream_t s) {
+  const dim3 grid(n, rb, 4 * LatGeom<LAT>::DB), block(kThreads);
+  if (rb == 1) hipLaunchKernelGGL((latent_merge_kernel<LAT, 1, Plan>), grid, block, 0, s, p, plan);
+  else if (rb == 2) hipLaunchKernelGGL((latent_merge_kernel<LAT, 2, Plan>), grid, block, 0, s, p, plan);
+  else hipLaunchKernelGGL((latent_merge_kernel<LAT, 4, Plan>), grid, block, 0, s, p, plan);
 }
 
 }  // namespace
 
-hipError_t launch_latent_attention(const LatentAttnParams& p, int64_t n_units, int latent_dim, bool fp8, int row_blocks,
+hipError_t launch_latent_attention(const LatentAttnParams& p, int64_t n_units, const LatentSmallPlan* small,
+                                   const LatentRowPlan* rows, int latent_dim, bool fp8, int row_blocks,
                                    hipStream_t stream) {
-  if (n_units <= 0) return hipSuccess;
-  const unsigned n = (unsigned)n_units;
-  if (latent_dim == 512) {
-    if (fp8) attn_by_blocks<512, true>(p, n, row_blocks, stream);
-    else attn_by_blocks<512, false>(p, n, row_blocks, stream);
+  if (rows != nullptr) {
+    attn_by_pool(p, (unsigned)rows->n_units, *rows, latent_dim, fp8, row_blocks, stream);
+  } else if (small != nullptr) {
+    attn_by_pool(p, (unsigned)small->n_units, *small, latent_dim, fp8, row_blocks, stream);
   } else {
-    if (fp8) attn_by_blocks<256, true>(p, n, row_blocks, stream);
-    else attn_by_blocks<256, false>(p, n, row_blocks, stream);
+    if (n_units <= 0) return hipSuccess;
+    attn_by_pool(p, (unsigned)n_units, InMemory{}, latent_dim, fp8, row_blocks, stream);
   }
   return hipGetLastError();
 }
 
-hipError_t launch_latent_merge(const LatentMergeParams& p, int64_t n_merges, int latent_dim, int row_blocks,
-                               hipStream_t stream) {
-  if (n_merges <= 0) return hipSuccess;
-  if (latent_dim == 512) merge_by_blocks<512>(p, (unsigned)n_merges, row_blocks, stream);
-  else merge_by_blocks<256>(p, (unsigned)n_merges, row_blocks, stream);
+hipError_t launch_latent_merge(const LatentMergeParams& p, int64_t n_merges, const LatentSmallPlan* small,
+                               const LatentRowPlan* rows, int latent_dim, int row_blocks, hipStream_t stream) {
+  if (rows != nullptr) {
+    if (latent_dim == 512) merge_by_blocks<512>(p, (unsigned)rows->n, *rows, row_blocks, stream);
+    else merge_by_blocks<256>(p, (unsigned)rows->n, *rows, row_blocks, stream);
+  } else if (small != nullptr) {
+    if (latent_dim == 512) merge_by_blocks<512>(p, (unsigned)small->n_tiles, *small, row_blocks, stream);
+    else merge_by_blocks<256>(p, (unsigned)small->n_tiles, *small, row_blocks, stream);
+  } else {
+    if (n_merges <= 0) return hipSuccess;
+    if (latent_dim == 512) merge_by_blocks<512>(p, (unsigned)n_merges, InMemory{}, row_blocks, stream);
+    else merge_by_blocks<256>(p, (unsigned)n_merges, InMemory{}, row_blocks, stream);
+  }
   return hipGetLastError();
 }
 

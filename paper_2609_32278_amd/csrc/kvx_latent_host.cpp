@@ -246,10 +246,9 @@ struct Group {
   int32_t first, count;
 };
 
-// Units in launch order (workgroup i runs on XCD i % 8): groups, longest first, each to the
-// XCD with the least work so far; shorter queues are padded with empty units.
-template <typename U>
-std::vector<U> spread(const std::vector<U>& units, std::vector<Group>& groups) {
+// Launch order (workgroup i runs on XCD i % 8): groups, longest first, each to the XCD with
+// the least work so far; -1 pads the shorter queues.
+std::vector<int32_t> spread(std::vector<Group>& groups) {
   std::stable_sort(groups.begin(), groups.end(), [](const Group& a, const Group& b) { return a.cost > b.cost; });
   std::vector<int32_t> queue[kvx::kNumXcd];
   int64_t load[kvx::kNumXcd] = {};
@@ -262,10 +261,18 @@ std::vector<U> spread(const std::vector<U>& units, std::vector<Group>& groups) {
   }
   size_t most = 0;
   for (const auto& q : queue) most = std::max(most, q.size());
-  std::vector<U> out(most * kvx::kNumXcd);  // value-initialised: padding
+  std::vector<int32_t> out(most * kvx::kNumXcd, -1);
   for (size_t x = 0; x < (size_t)kvx::kNumXcd; x++)
-    for (size_t i = 0; i < queue[x].size(); i++) out[i * kvx::kNumXcd + x] = units[(size_t)queue[x][i]];
-  while (!out.empty() && out.back().key_end == 0) out.pop_back();
+    for (size_t i = 0; i < queue[x].size(); i++) out[i * kvx::kNumXcd + x] = queue[x][i];
+  while (!out.empty() && out.back() < 0) out.pop_back();
+  return out;
+}
+
+template <typename U>
+std::vector<U> in_order(const std::vector<U>& units, const std::vector<int32_t>& order) {
+  std::vector<U> out(order.size());  // value-initialised: padding
+  for (size_t i = 0; i < order.size(); i++)
+    if (order[i] >= 0) out[i] = units[(size_t)order[i]];
   return out;
 }
 
@@ -287,15 +294,16 @@ int64_t choose_steps(const std::vector<Span>& spans) {
   if (work == 0) return 0;
   auto estimate = [&](int64_t c) {
     double total = 0.0, top = 0.0;
-    int64_t units = 0;
+    int64_t units = 0, most = 1;
     for (const Span& s : spans) {
       const int64_t parts = c > 0 ? ceil_div(s.len, c) : 1;
       const double each = (double)ceil_div(s.len, parts) + kStart + (parts > 1 ? kPart : 0.0);
       total += (double)(s.tiles * parts) * each;
       units += s.tiles * parts;
       top = std::max(top, each);
+      most = std::max(most, parts);
     }
-    const double merge = c > 0 && c < longest ? 3.0 : 0.0;
+    const double merge = most > 1 ? 2.0 + 0.12 * (double)most : 0.0;
     return (units <= kSlots ? top : std::max(top, total / kSlots + 0.5 * top)) + merge;
   };
   int64_t best = 0;
@@ -317,6 +325,9 @@ struct AbsorbedPlan {
   std::vector<LatentMerge> merges;
   int64_t n_parts = 0;
   int row_blocks = 1;
+  bool in_args = false;  // `rows` (rows.n > 0) or `small` holds the plan instead
+  kvx::LatentRowPlan rows;
+  kvx::LatentSmallPlan small;
 };
 
 // One request of the absorbed form: its batch index and the row that its first suffix token
@@ -347,8 +358,49 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
     if (n <= max_parts) break;
     steps *= 2;
   }
+  const int32_t R = (int32_t)members.size();
+  plan.rows.n = 0;
+  if (R <= kvx::kLatRowReqs && std::all_of(spans.begin(), spans.end(), [](const Span& s) { return s.tiles == 1; })) {
+    // longest parts first
+    std::vector<int32_t> by(members.size());
+    std::vector<int64_t> len(members.size());
+    for (int32_t i = 0; i < R; i++) {
+      by[(size_t)i] = i;
+      const int64_t parts = parts_of(spans[(size_t)i]);
+      len[(size_t)i] = split_keys > 0 && parts > 1 ? steps : ceil_div(spans[(size_t)i].len, parts);
+    }
+    std::stable_sort(by.begin(), by.end(), [&](int32_t a, int32_t b) { return len[(size_t)a] > len[(size_t)b]; });
+    kvx::LatentRowPlan& rp = plan.rows;
+    int64_t at = 0;
+    bool merges = false;
+    for (int32_t i = 0; i < R; i++) {
+      const Member& m = members[(size_t)by[(size_t)i]];
+      const int64_t keys = (int64_t)b->prefix_lens[m.req] + b->extend_lens[m.req];
+      const int64_t l = len[(size_t)by[(size_t)i]] * kvx::kLatTileKeys, parts = ceil_div(keys, l);
+      rp.first[i] = (int32_t)at;
+      rp.qo[i] = (int32_t)m.row;
+      rp.extend[i] = b->extend_lens[m.req];
+      rp.prefix[i] = b->prefix_lens[m.req];
+      rp.page_base[i] = b->page_indptr[m.req];
+      rp.len[i] = (int32_t)l;
+      rp.part0[i] = (int32_t)plan.n_parts;
+      at += parts;
+      if (parts > 1) plan.n_parts += parts, merges = true;
+    }
+    std::fill(rp.first + R, rp.first + kvx::kLatRowReqs, INT32_MAX);
+    rp.n = R;
+    rp.n_units = (int32_t)at;
+    plan.in_args = true;
+    if (merges) plan.merges.resize(1);  // a merge launch is needed
+    return;
+  }
   std::vector<LatentUnit> units;
+  std::vector<uint16_t> codes;  // of the units, while the plan may be a small one
   std::vector<Group> groups;
+  int64_t all_tiles = 0, most_parts = 1;
+  for (const Span& s : spans) all_tiles += s.tiles, most_parts = std::max(most_parts, parts_of(s));
+  bool small = all_tiles <= kvx::kLatSmallTiles && most_parts <= kvx::kLatSmallParts;
+  int32_t n_tiles = 0;
   for (size_t i = 0; i < members.size(); i++) {
     const Member& m = members[i];
     const int64_t P = b->prefix_lens[m.req], E = b->extend_lens[m.req], rows = E * Hq;
@@ -358,6 +410,14 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
     const int64_t part0 = plan.n_parts;
     const int64_t tiles = spans[i].tiles;
     if (parts > 1) plan.n_parts += tiles * parts;
+    if (small) {
+      for (int64_t t = 0; t < tiles; t++) {
+        const int64_t n = std::min<int64_t>(M, rows - t * M);
+        plan.small.tile[n_tiles + t] = {(int32_t)(t * M), (int32_t)n, (int32_t)m.row, (int32_t)P,
+                                        b->page_indptr[m.req], (int32_t)(P + (t * M + n - 1) / Hq + 1), (int32_t)len,
+                                        (int32_t)(part0 + t * parts)};
+      }
+    }
     for (int64_t c = 0; c < parts; c++) {
       Group g{0, (int32_t)units.size(), 0};
       for (int64_t t = tiles - 1; t >= 0; t--) {
@@ -374,6 +434,7 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
         u.part = end > len ? (int32_t)(part0 + t * parts + c) : -1;
         g.cost = std::max<int64_t>(g.cost, ceil_div(u.key_end - u.key_begin, kvx::kLatTileKeys) + 2);
         units.push_back(u);
+        if (small) codes.push_back((uint16_t)((n_tiles + t) << 10 | c));
         g.count++;
         if (c == 0 && end > len) {
           const int64_t n = ceil_div(end, len);
@@ -382,8 +443,18 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
       }
       if (g.count > 0) groups.push_back(g);
     }
+    n_tiles += (int32_t)tiles;
   }
-  plan.units = spread(units, groups);
+  const std::vector<int32_t> order = spread(groups);
+  plan.in_args = small && order.size() <= (size_t)kvx::kLatSmallUnits;
+  if (!plan.in_args) {
+    plan.units = in_order(units, order);
+    return;
+  }
+  plan.small.n_units = (int32_t)order.size();
+  plan.small.n_tiles = n_tiles;
+  for (size_t i = 0; i < order.size(); i++)
+    plan.small.code[i] = order[i] < 0 ? kvx::kLatNoUnit : codes[(size_t)order[i]];
 }
 
 struct ExpandedPlan {
@@ -466,7 +537,7 @@ void plan_expanded(const kvx_batch* b, const std::vector<int64_t>& qo, const std
     for (size_t i = 0; i < units.size(); i++)
       groups.push_back({ceil_div(units[i].key_end - units[i].key_begin, 64) + 2, (int32_t)i, 1});
   }
-  plan.units = spread(units, groups);
+  plan.units = in_order(units, spread(groups));
 }
 
 // Whether a request is estimated to be faster in the absorbed form: products by its lengths.
@@ -496,7 +567,9 @@ int launch_absorbed(kvx_latent_pool* pool, const kvx_batch* batch, const Absorbe
   }
   p.num_q_heads = Hq;
   p.scale_log2 = sm_scale * 1.4426950408889634f;
-  hipError_t e = kvx::launch_latent_attention(p, (int64_t)plan.units.size(), pool->latent_dim,
+  const kvx::LatentRowPlan* rows = plan.in_args && plan.rows.n > 0 ? &plan.rows : nullptr;
+  const kvx::LatentSmallPlan* small = plan.in_args && !rows ? &plan.small : nullptr;
+  hipError_t e = kvx::launch_latent_attention(p, (int64_t)plan.units.size(), small, rows, pool->latent_dim,
                                               pool->dtype == KVX_LATENT_FP8, plan.row_blocks, s);
   if (e != hipSuccess) return hip_fail(e, "latent attention kernel launch");
   if (!plan.merges.empty()) {
@@ -507,10 +580,10 @@ int launch_absorbed(kvx_latent_pool* pool, const kvx_batch* batch, const Absorbe
     m.out = p.out;
     m.lse = lse;
     m.num_q_heads = Hq;
-    e = kvx::launch_latent_merge(m, (int64_t)plan.merges.size(), pool->latent_dim, plan.row_blocks, s);
+    e = kvx::launch_latent_merge(m, (int64_t)plan.merges.size(), small, rows, pool->latent_dim, plan.row_blocks, s);
     if (e != hipSuccess) return hip_fail(e, "latent merge kernel launch");
   }
-  return pool->parts.done(s);
+  return plan.n_parts > 0 ? pool->parts.done(s) : KVX_OK;
 }
 
 }  // namespace
@@ -663,13 +736,17 @@ int latent_attention(kvx_latent_pool* pool, const kvx_batch* batch, const void* 
     AbsorbedPlan plan;
     plan_absorbed(batch, members, num_q_heads, pool->latent_dim, pool->split_keys, plan);
     Blob blob;
-    const size_t units_at = blob.add(plan.units), merges_at = blob.add(plan.merges);
+    size_t units_at = 0, merges_at = 0;
     void* dev = nullptr;
-    if (int rc = pool->st_plan.upload(blob.bytes.data(), blob.bytes.size(), s, &dev)) return rc;
+    if (!plan.in_args) {
+      units_at = blob.add(plan.units);
+      merges_at = blob.add(plan.merges);
+      if (int rc = pool->st_plan.upload(blob.bytes.data(), blob.bytes.size(), s, &dev)) return rc;
+    }
     if (int rc = launch_absorbed(pool, batch, plan, (const uint8_t*)dev, units_at, merges_at, q, num_q_heads, sm_scale,
                                  out, lse, s))
       return rc;
-    return pool->st_plan.done(s);
+    return plan.in_args ? KVX_OK : pool->st_plan.done(s);
   });
 }
 
@@ -738,8 +815,10 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
                           (int32_t)std::min<int64_t>(kvx::kLatProjTok, n - t), 0});
         i = j;
       }
-      a_units = blob.add(ap.units);
-      a_merges = blob.add(ap.merges);
+      if (!ap.in_args) {
+        a_units = blob.add(ap.units);
+        a_merges = blob.add(ap.merges);
+      }
       a_rows = blob.add(rows);
     }
     std::vector<LatentExpandUnit> x_units;

@@ -76,6 +76,36 @@ struct LatentUnit {
 };
 static_assert(sizeof(LatentUnit) == 32, "LatentUnit is 32 bytes");
 
+// A small plan travels in the kernel arguments instead of through a copy: tiles of rows, and
+// for each unit in launch order a code word (tile << 10 | part), kLatNoUnit where there is
+// none.
+constexpr int kLatSmallTiles = 48, kLatSmallUnits = 1024, kLatSmallParts = 1 << 10;
+constexpr uint16_t kLatNoUnit = 0xFFFF;
+struct LatentSmallTile {
+  int32_t row0, nrows, qo, prefix, page_base;
+  int32_t key_end;  // keys that a row of the tile sees
+  int32_t len;      // keys per part (a multiple of kLatTileKeys)
+  int32_t part0;
+};
+struct LatentSmallPlan {
+  int32_t n_units;  // 0: the units are in memory
+  int32_t n_tiles;
+  LatentSmallTile tile[kLatSmallTiles];
+  uint16_t code[kLatSmallUnits];
+};
+
+// ... or, where every request is one tile of rows (a decode batch), the requests, longest
+// parts first: unit i is part i - first[r] of the last request r with first[r] <= i.
+constexpr int kLatRowReqs = 128;
+struct LatentRowPlan {
+  int32_t n;        // requests
+  int32_t n_units;
+  int32_t first[kLatRowReqs];  // INT32_MAX past the n-th
+  int32_t qo[kLatRowReqs], extend[kLatRowReqs], prefix[kLatRowReqs], page_base[kLatRowReqs];
+  int32_t len[kLatRowReqs];    // keys per part
+  int32_t part0[kLatRowReqs];
+};
+
 // The parts of one tile of rows.
 struct LatentMerge {
   int32_t row0, nrows, qo, part0, nparts, pad;
@@ -102,10 +132,13 @@ struct LatentMergeParams {
   int32_t num_q_heads;
 };
 
-hipError_t launch_latent_attention(const LatentAttnParams& p, int64_t n_units, int latent_dim, bool fp8,
-                                   int row_blocks, hipStream_t stream);
-hipError_t launch_latent_merge(const LatentMergeParams& p, int64_t n_merges, int latent_dim, int row_blocks,
-                               hipStream_t stream);
+// small, rows: the plan (in host memory) for the kernel arguments, or null; n_units and
+// n_merges are those of a plan in memory.
+hipError_t launch_latent_attention(const LatentAttnParams& p, int64_t n_units, const LatentSmallPlan* small,
+                                   const LatentRowPlan* rows, int latent_dim, bool fp8, int row_blocks,
+                                   hipStream_t stream);
+hipError_t launch_latent_merge(const LatentMergeParams& p, int64_t n_merges, const LatentSmallPlan* small,
+                               const LatentRowPlan* rows, int latent_dim, int row_blocks, hipStream_t stream);
 
 // ---- per-head weights
 
