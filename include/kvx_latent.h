@@ -51,9 +51,9 @@ enum kvx_latent_form {
 
 /* Device layout of a pool, for tests and tools.  A page holds 16 tokens in page_bytes
  * contiguous bytes.  bf16: [16][latent_dim + rope_dim].  fp8: codes [16][latent_dim], then
- * bf16 keys [16][rope_dim], then scale bytes, 2^(byte - 127): with T = 1024 / latent_dim
- * and G = latent_dim / 64, the byte of slot s and group g is at
- * ((s % T) * G + g) * (16 / T) + s / T. */
+ * bf16 keys [16][rope_dim], then scale bytes, 2^(byte - 127): the byte of slot s and group g
+ * (of 64 values) is at
+ * ((s % 8) * 2 + g % 2) * (latent_dim / 64) + s / 8 * (latent_dim / 128) + g / 2. */
 typedef struct {
     void *base; /* device */
     int64_t num_pages;

@@ -10,156 +10,138 @@ constexpr int kThreads = 256;
 
 // A tile of 64 keys in LDS: pages of 16 rows, in a page its two halves of 8 rows, in a half
 // blocks of 128 bytes of the rows: [page][half][block][8 rows][128 bytes], where a wave-wide
-// direct load of 1 KiB fills one block from one lane offset.  The eight 16-byte chunks of a
-// row in a block are stored in the order c ^ swz(row): rows are 32 banks apart modulo 64,
-// and this moves the rows of an operand read (16 rows one chunk; 4 rows two chunks) to
-// different banks.
+// direct load of 1 KiB fills one block.  The eight 16-byte chunks of a row in a block are
+// stored in the order c ^ order(row).  Score operands are read as chunk 2 g + (0 or 1) of 16
+// rows, value operands as two neighbouring chunks of 4 rows; with this order both meet every
+// bank once (counted: none of their reads conflict).
 template <int LAT>
 struct TileAt {
   static constexpr int HALF = 8 * LatGeom<LAT>::ROWB;
+  __device__ static int order(int r) { return (r & 2) | ((r >> 1) & 4) | ((r >> 2) & 1); }
   __device__ static int row(int r) { return (r >> 3) * HALF + (r & 7) * 128; }
-  __device__ static int chunk(int r, int c) { return row(r) + (c >> 3) * 1024 + (((c & 7) ^ swz(r)) << 4); }
+  __device__ static int chunk(int r, int c) { return row(r) + (c >> 3) * 1024 + (((c & 7) ^ order(r)) << 4); }
+};
+
+// How a wave brings its page of a 64-key tile to LDS: begin() with the tile, every issue(i)
+// and, for an 8-bit page, every finish(i) later.  Tokens at or past key_end become token
+// `safe`; a tile past the last is that token throughout.  The steps are made one by one among
+// the products of the tile before: a burst of them stalls the wave (18 loads of 1 KiB took
+// 1.8k cycles of a step's 5.5k).
+template <int LAT>
+struct Pages {
+  const uint8_t* base;
+  const_i32_ptr ids;
+  int64_t page_bytes;
+  int key_end, safe, lane, wave;
+  uint32_t page;  // of the next tile
+
+  __device__ __forceinline__ uint32_t page_at(int k0) const {
+    const int lp = k0 / kPageSize + wave, last = (key_end - 1) / kPageSize;
+    return (uint32_t)ids[lp < last ? lp : last];
+  }
+  __device__ __forceinline__ void init(const LatentAttnParams& p, const LatentUnit& u, int safe_key, int l, int w) {
+    base = p.pool.base;
+    ids = (const_i32_ptr)(p.pool.page_ids + u.page_base);
+    page_bytes = p.pool.page_bytes;
+    key_end = u.key_end;
+    safe = safe_key;
+    lane = l;
+    wave = w;
+  }
+  __device__ __forceinline__ const uint8_t* address(uint32_t pg) const { return base + (uint64_t)pg * page_bytes; }
 };
 
 template <int LAT, bool FP8>
 struct Loader;
 
 template <int LAT>
-struct Loader<LAT, false> {
+struct Loader<LAT, false> : Pages<LAT> {
   using G = LatGeom<LAT>;
-  static constexpr int BLOCKS = G::ROWB / 128;
-  int off;  // of this lane in a block of the first half; the second half's has bit 4 flipped
-  const uint8_t* base;
-  const int32_t* ids;
-  int64_t page_bytes;
-  int key_end, safe, lane, wave;
-  uint32_t page;  // of the next tile to load
+  using P = Pages<LAT>;
+  static constexpr int BLOCKS = G::ROWB / 128, LOADS = 2 * BLOCKS, WRITES = 0;
+  const uint8_t* from[2];  // of this lane in each half
+  uint32_t to;
 
-  __device__ __forceinline__ uint32_t page_at(int k0) const {
-    int lp = k0 / kPageSize + wave;
-    const int last = (key_end - 1) / kPageSize;
-    return (uint32_t)((const_i32_ptr)ids)[lp < last ? lp : last];
-  }
-  __device__ __forceinline__ void init(const LatentAttnParams& p, const LatentUnit& u, int safe_key, int l, int w) {
-    base = p.pool.base;
-    ids = p.pool.page_ids + u.page_base;
-    page_bytes = p.pool.page_bytes;
-    key_end = u.key_end;
-    safe = safe_key;
-    lane = l;
-    wave = w;
-    off = (l >> 3) * G::ROWB + (((l & 7) ^ swz(l >> 3)) << 4);
-    page = page_at(u.key_begin);
-  }
-  // Tokens k0 .. k0 + 63; those at or past key_end become token `safe`.
-  __device__ __forceinline__ void issue(uint8_t* tile, int k0) {
-    const uint32_t lds = lds_address(tile + wave * (16 * G::ROWB));
-    if (k0 + kLatTileKeys <= key_end) {
-      const uint8_t* src = base + (uint64_t)page * page_bytes;
+  __device__ __forceinline__ void begin(uint32_t tile, int k0) {
+    const uint8_t* src = P::address(P::page);
+    const uint8_t* alt = P::address((uint32_t)P::ids[P::safe / kPageSize]) + (P::safe % kPageSize) * G::ROWB;
+    const int left = P::key_end - k0 - P::wave * kPageSize;  // rows of this page that exist
 #pragma unroll
-      for (int i = 0; i < BLOCKS; i++) lds_load_1k(src + i * 128, off, lds + i * 1024);
-#pragma unroll
-      for (int i = 0; i < BLOCKS; i++)
-        lds_load_1k(src + 8 * G::ROWB + i * 128, off ^ 16, lds + (BLOCKS + i) * 1024);
-    } else {
-      const uint32_t sp = (uint32_t)((const_i32_ptr)ids)[safe / kPageSize];
-      const uint8_t* src = base + (uint64_t)page * page_bytes;
-      const uint8_t* alt = base + (uint64_t)sp * page_bytes + (safe % kPageSize) * G::ROWB;
-      const int left = key_end - k0 - wave * kPageSize;  // rows of this page that exist
-#pragma unroll
-      for (int h = 0; h < 2; h++) {
-        const int row = 8 * h + (lane >> 3), c = ((lane & 7) ^ swz(row)) << 4;
-        const uint8_t* from = (row < left ? src + row * G::ROWB : alt) + c;
-#pragma unroll
-        for (int i = 0; i < BLOCKS; i++) lds_load_1k(from + i * 128, lds + (h * BLOCKS + i) * 1024);
-      }
+    for (int h = 0; h < 2; h++) {
+      const int row = 8 * h + (P::lane >> 3), c = ((P::lane & 7) ^ TileAt<LAT>::order(row)) << 4;
+      from[h] = (row < left ? src + row * G::ROWB : alt) + c;
     }
-    page = page_at(k0 + kLatTileKeys);
+    to = tile + P::wave * (16 * G::ROWB);
+    P::page = P::page_at(k0 + kLatTileKeys);
   }
-  __device__ __forceinline__ void finish(uint8_t*) {}
+  __device__ __forceinline__ void issue(int i) { lds_load_1k(from[i / BLOCKS] + i % BLOCKS * 128, to + i * 1024); }
+  __device__ __forceinline__ void finish(int) {}
+  // evenly over the score product
+  __device__ static constexpr int issue_at(int i, int steps) { return i * steps / LOADS; }
 };
 
-// An 8-bit page comes through registers, 16 codes a lane and load, issued a tile ahead, and
-// is written to LDS as bf16 (exactly: code * 2^e) once the products of the tile before are
-// done.
+// An 8-bit page comes through registers, 16 codes a lane and load, and is written to LDS as
+// bf16 (exactly: code * 2^e).  A load takes 8 slots x 128 codes, so that its two writes fill
+// two blocks without bank conflicts.
 template <int LAT>
-struct Loader<LAT, true> {
+struct Loader<LAT, true> : Pages<LAT> {
   using G = LatGeom<LAT>;
-  static constexpr int LOADS = LAT / 64;       // of codes: 1 KiB each, 1024 / LAT slots
-  static constexpr int LPS = LAT / 16;         // lanes per slot
-  static constexpr int SPL = 64 / LPS;         // slots per load
-  const uint8_t* base;
-  const int32_t* ids;
-  int64_t page_bytes;
-  int key_end, safe, lane, wave;
-  uint32_t page;
-  uint4 codes[LOADS];
-  uint4 key[2];
-  uint64_t scales;  // LOADS bytes, one per load
+  using P = Pages<LAT>;
+  static constexpr int CODES = LAT / 64, PER = LAT / 128;  // loads of codes: of a page, of 8 slots
+  static constexpr int LOADS = CODES + 2, WRITES = CODES + 2;
+  const uint8_t* from[2];  // codes of this lane's slot in each half
+  const uint8_t* key[2];
+  uint4 data[LOADS];
+  uint64_t scales;     // CODES bytes, one per load
+  uint32_t to;
 
-  __device__ __forceinline__ uint32_t page_at(int at) const {
-    int lp = at / kPageSize + wave;
-    const int last = (key_end - 1) / kPageSize;
-    return (uint32_t)((const_i32_ptr)ids)[lp < last ? lp : last];
-  }
-  __device__ __forceinline__ void init(const LatentAttnParams& p, const LatentUnit& u, int safe_key, int l, int w) {
-    base = p.pool.base;
-    ids = p.pool.page_ids + u.page_base;
-    page_bytes = p.pool.page_bytes;
-    key_end = u.key_end;
-    safe = safe_key;
-    lane = l;
-    wave = w;
-    page = page_at(u.key_begin);
-  }
-  __device__ __forceinline__ void issue(uint8_t*, int k0) {
-    const uint8_t* src = base + (uint64_t)page * page_bytes;
+  __device__ __forceinline__ void begin(uint32_t tile, int k0) {
     constexpr int SC = kPageSize * (LAT + 2 * kLatRope);
-    const int left = key_end - k0 - wave * kPageSize, sub = lane / LPS, grp = (lane % LPS) / 4;
-    const uint8_t* sc = src + SC + latent_scale_at(LAT, sub, grp);
-    if constexpr (LOADS == 8) scales = *(const uint64_t*)sc;
+    const uint8_t* src = P::address(P::page);
+    const uint8_t* alt = P::address((uint32_t)P::ids[P::safe / kPageSize]);
+    const int left = P::key_end - k0 - P::wave * kPageSize, ss = P::safe % kPageSize;
+    const int sub = P::lane >> 3, c = P::lane & 7, hi = c >> 2;
+    const uint8_t* sc = src + SC + latent_scale_at(LAT, sub, hi);
+    if constexpr (CODES == 8) scales = *(const uint64_t*)sc;
     else scales = *(const uint32_t*)sc;
-    if (left >= kPageSize) {
 #pragma unroll
-      for (int i = 0; i < LOADS; i++) codes[i] = *(const uint4*)(src + i * 1024 + lane * 16);
-#pragma unroll
-      for (int i = 0; i < 2; i++) key[i] = *(const uint4*)(src + kPageSize * LAT + i * 1024 + lane * 16);
-    } else {  // slots that the request does not own: the safe token's
-      const uint8_t* alt = base + (uint64_t)(uint32_t)((const_i32_ptr)ids)[safe / kPageSize] * page_bytes;
-      const int ss = safe % kPageSize;
-      const uint64_t b = alt[SC + latent_scale_at(LAT, ss, grp)];
-#pragma unroll
-      for (int i = 0; i < LOADS; i++) {
-        const int slot = i * SPL + sub, c = lane % LPS;
-        if (slot >= left) scales = (scales & ~(0xFFull << (8 * i))) | b << (8 * i);
-        codes[i] = *(const uint4*)((slot < left ? src + slot * LAT : alt + ss * LAT) + c * 16);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; i++) {
-        const int slot = i * 8 + lane / 8, c = lane % 8;
-        key[i] = *(const uint4*)((slot < left ? src + slot * 128 : alt + ss * 128) + kPageSize * LAT + c * 16);
-      }
+    for (int h = 0; h < 2; h++) {
+      const int slot = 8 * h + sub;
+      from[h] = (slot < left ? src + slot * LAT : alt + ss * LAT) + c * 16;
+      key[h] = (slot < left ? src + slot * 128 : alt + ss * 128) + kPageSize * LAT + c * 16;
     }
-    page = page_at(k0 + kLatTileKeys);
-  }
-  __device__ __forceinline__ void finish(uint8_t* tile) {
-    uint8_t* rows = tile + wave * (16 * G::ROWB);
+    if (left < kPageSize) {  // uniform
 #pragma unroll
-    for (int i = 0; i < LOADS; i++) {
-      const int slot = i * SPL + lane / LPS, c = lane % LPS;
-      const float sc = __uint_as_float((uint32_t)(scales >> (8 * i) & 0xFF) << 23);
-      const uint32_t w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+      for (int i = 0; i < CODES; i++)
+        if (8 * (i / PER) + sub >= left)
+          scales = (scales & ~(0xFFull << (8 * i))) |
+                   (uint64_t)alt[SC + latent_scale_at(LAT, ss, 2 * (i % PER) + hi)] << (8 * i);
+    }
+    to = tile + P::wave * (16 * G::ROWB);
+    P::page = P::page_at(k0 + kLatTileKeys);
+  }
+  __device__ __forceinline__ void issue(int i) {
+    data[i] = *(const uint4*)(i < CODES ? from[i / PER] + i % PER * 128 : key[i - CODES]);
+  }
+  // early, so that the data is there for the writes beside the value product
+  __device__ static constexpr int issue_at(int i, int steps) { return i * (steps / 2) / LOADS; }
+  __device__ __forceinline__ void finish(int i) {
+    const int sub = P::lane >> 3, c = P::lane & 7;
+    if (i < CODES) {
+      const int slot = 8 * (i / PER) + sub, block = 2 * (i % PER) + (c >> 2);
+      const float sc = __uint_as_float(((uint32_t)(scales >> (8 * i)) & 0xFF) << 23);
+      const uint32_t w[4] = {data[i].x, data[i].y, data[i].z, data[i].w};
       uint32_t y[8];
 #pragma unroll
       for (int e = 0; e < 4; e++) {
         y[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], sc, false));
         y[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], sc, true));
       }
-      *(uint4*)(rows + TileAt<LAT>::chunk(slot, 2 * c)) = make_uint4(y[0], y[1], y[2], y[3]);
-      *(uint4*)(rows + TileAt<LAT>::chunk(slot, 2 * c + 1)) = make_uint4(y[4], y[5], y[6], y[7]);
+      write_b128(to + TileAt<LAT>::chunk(slot, 8 * block + 2 * (c & 3)), y[0], y[1], y[2], y[3]);
+      write_b128(to + TileAt<LAT>::chunk(slot, 8 * block + 2 * (c & 3) + 1), y[4], y[5], y[6], y[7]);
+    } else {
+      write_b128(to + TileAt<LAT>::chunk((i - CODES) * 8 + sub, LAT / 8 + c), data[i].x, data[i].y, data[i].z, data[i].w);
     }
-#pragma unroll
-    for (int i = 0; i < 2; i++) *(uint4*)(rows + TileAt<LAT>::chunk(i * 8 + lane / 8, LAT / 8 + lane % 8)) = key[i];
   }
 };
 
@@ -216,6 +198,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   using G = LatGeom<LAT>;
   constexpr int RW = RB == 4 ? 2 : 1, KW = 4 / RW;  // waves by rows and by keys in the score product
   constexpr int RBW = RB / RW, KBW = 4 / KW;        // 16-row and 16-key blocks of a wave in it
+  constexpr int QS = G::KS * KBW;                   // its steps
   // operand reads ahead of their products, in steps of the score and of the value product
   constexpr int AK = RBW == 1 ? 8 : 6, AV = RB == 1 ? 8 : (RB == 2 ? 5 : 3);
   __shared__ __attribute__((aligned(1024))) uint8_t tile[2][G::TILE];
@@ -233,7 +216,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   const int pos0 = u.prefix + u.row0 / Hq;
   // a token that every row of the unit sees, where there is one
   const int safe = pos0 < u.key_begin ? u.key_begin : (pos0 < u.key_end ? pos0 : u.key_end - 1);
-  Loader<LAT, FP8> loader;
+  using L = Loader<LAT, FP8>;
+  L loader;
   loader.init(p, u, safe, lane, wave);
 
   bf16x8 qf[RBW][G::KS];
@@ -246,8 +230,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
     limit[rb] = pos < u.key_end ? pos : u.key_end - 1;
     const uint4* src = (const uint4*)(p.q + (flat0 + (valid ? row : 0)) * G::ROW);
 #pragma unroll
-    for (int ks = 0; ks < G::KS; ks++) {
-      qf[rb][ks] = __builtin_bit_cast(bf16x8, src[ks * 4 + g]);
+    for (int ks = 0; ks < G::KS; ks++) {  // step ks, lanes g: chunk 2 g + ks % 2 of the step pair's eight
+      qf[rb][ks] = __builtin_bit_cast(bf16x8, src[(ks >> 1) * 8 + 2 * g + (ks & 1)]);
       // operands of the unit's whole life go to the accumulator half of the register file
       if constexpr (RBW * G::KS > 32) keep_in_acc(qf[rb][ks]);
     }
@@ -257,32 +241,32 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   f32x4 o[RB][G::DB];
   float m[RB];    // reference points (log2 units; -inf: no key seen yet)
   float l[RBW];   // this lane's share of its rows' sums
+  float neg[RBW]; // its rows' reference points, negated; 0 where there is none
   const float scale = p.scale_log2;
   // LDS offsets of the operands.  Chunk orders differ from row to row in bits 4 to 6 of an
   // offset only, so a few lane offsets and immediates reach every operand.
   uint32_t kat[2];  // score product: 32 dims a step, even and odd steps
 #pragma unroll
   for (int i = 0; i < 2; i++) {
-    const int r = kw * KBW * 16 + n;
-    kat[i] = TileAt<LAT>::row(r) + ((i * 64 + g * 16) ^ (swz(r) << 4));
+    const int r = kw * 16 + n;
+    kat[i] = TileAt<LAT>::chunk(r, 2 * g + i);
   }
-  uint32_t vat[4];  // value product: dim blocks modulo 4 (the second four keys of a lane have bit 6 flipped)
+  uint32_t vat[2][4];  // value product: first and second four keys of a lane, dim blocks modulo 4
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const int r = 8 * g + n / 4;
-    vat[i] = TileAt<LAT>::row(r) + wave * (G::DW / 64 * 1024) + ((i * 32 + (n % 4) / 2 * 16) ^ (swz(r) << 4)) +
-             (n % 2) * 8;
-  }
+  for (int e = 0; e < 2; e++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      vat[e][i] = TileAt<LAT>::chunk(8 * g + 4 * e + n / 4, 2 * i + (n % 4) / 2) + wave * (G::DW / 64 * 1024) + (n % 2) * 8;
+      opaque(vat[e][i]);
+    }
   uint32_t pw[KBW], pr_at[2];
 #pragma unroll
   for (int kb = 0; kb < KBW; kb++)
-    pw[kb] = lds_address(pl) + (rw * RBW * 16 + n) * 128 + (((2 * (kw * KBW + kb) + g / 2) ^ (n & 7)) * 16) + (g & 1) * 8;
+    pw[kb] = lds_address(pl) + (rw * RBW * 16 + n) * 128 + (((2 * (kb * KW + kw) + g / 2) ^ (n & 7)) * 16) + (g & 1) * 8;
 #pragma unroll
   for (int i = 0; i < 2; i++) pr_at[i] = lds_address(pl) + n * 128 + (((4 * i + g) ^ (n & 7)) * 16);
 #pragma unroll
   for (int i = 0; i < 2; i++) opaque(kat[i]), opaque(pr_at[i]);
-#pragma unroll
-  for (int i = 0; i < 4; i++) opaque(vat[i]);
 #pragma unroll
   for (int kb = 0; kb < KBW; kb++) opaque(pw[kb]);
 
@@ -297,53 +281,60 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
 #pragma unroll
       for (int db = 0; db < G::DB; db++) o[rb][db] = f32x4{};
     }
+    const uint32_t tile0 = lds_address(tile);
     loader.page = loader.page_at(u.key_begin);
-    loader.issue(tile[0], u.key_begin);
-    loader.finish(tile[0]);
+    loader.begin(tile0, u.key_begin);
+#pragma unroll
+    for (int i = 0; i < L::LOADS; i++) loader.issue(i);
+#pragma unroll
+    for (int i = 0; i < L::WRITES; i++) loader.finish(i);
     int buf = 0;
     for (int k0 = u.key_begin; k0 < u.key_end; k0 += kLatTileKeys, buf ^= 1) {
       const lds_ptr cur = (lds_ptr)tile[0] + buf * G::TILE;
-      uint8_t* nxt = tile[buf ^ 1];
-      const bool more = k0 + kLatTileKeys < u.key_end;
       if constexpr (!FP8) wait_vmcnt<0>();
       __syncthreads();  // the tile is whole, and every wave has done with the one before
-      if (more) loader.issue(nxt, k0 + kLatTileKeys);
 
       f32x4 s[RBW][KBW];
-#pragma unroll
-      for (int rb = 0; rb < RBW; rb++)
-#pragma unroll
-        for (int kb = 0; kb < KBW; kb++) s[rb][kb] = f32x4{};
       // Operand reads run ahead of their products: a step is 16 RBW cycles of MFMA, a read
       // from LDS takes some 130, and nothing else runs on this SIMD meanwhile.
       bf16x8 ka[AK + 1];
-      auto read_k = [&](int j) {  // step j: dims 32 (j / KBW) .., key block j % KBW
-        const int ks = j / KBW, kb = j % KBW;
-        return read_b128(cur + kat[ks & 1] + (ks >> 1) * 1024 + kb * (16 * G::ROWB));
+      auto read_k = [&](int j) {  // step j: key block j / KS, dims 32 (j % KS) ..
+        const int ks = j % G::KS, kb = j / G::KS;
+        return read_b128(cur + kat[ks & 1] + (ks >> 1) * 1024 + kb * (KW * 16 * G::ROWB));
       };
-#pragma unroll
-      for (int j = 0; j < AK; j++) ka[j] = read_k(j);
-#pragma unroll
-      for (int j = 0; j < G::KS * KBW; j++) {
-        if (j + AK < G::KS * KBW) ka[(j + AK) % (AK + 1)] = read_k(j + AK);
-        __builtin_amdgcn_sched_barrier(0);
+      // Scores of the tile; between(j) runs beside the products of step j.
+      auto scores = [&](auto between) {
 #pragma unroll
         for (int rb = 0; rb < RBW; rb++)
-          s[rb][j % KBW] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[j % (AK + 1)], qf[rb][j / KBW], s[rb][j % KBW], 0,
-                                                                   0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (k0 + kLatTileKeys > full_end) {
 #pragma unroll
-        for (int kb = 0; kb < KBW; kb++) {
-          const int key0 = k0 + (kw * KBW + kb) * 16 + 4 * g;
+          for (int kb = 0; kb < KBW; kb++) s[rb][kb] = f32x4{};
+#pragma unroll
+        for (int j = 0; j < AK; j++) ka[j] = read_k(j);
+#pragma unroll
+        for (int j = 0; j < QS; j++) {
+          if (j + AK < QS) ka[(j + AK) % (AK + 1)] = read_k(j + AK);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int rb = 0; rb < RBW; rb++)
+            s[rb][j / G::KS] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[j % (AK + 1)], qf[rb][j % G::KS],
+                                                                       s[rb][j / G::KS], 0, 0, 0);
+          between(j);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      auto mask = [&](int kb) {
+        if (k0 + kLatTileKeys > full_end) {
+          const int key0 = k0 + (kb * KW + kw) * 16 + 4 * g;
 #pragma unroll
           for (int rb = 0; rb < RBW; rb++)
 #pragma unroll
             for (int i = 0; i < 4; i++) s[rb][kb][i] = key0 + i <= limit[rb] ? s[rb][kb][i] : -INFINITY;
         }
-      }
-      if (!FIXED || k0 == u.key_begin) {  // uniform
+      };
+      if (!FIXED || k0 == u.key_begin) {  // uniform: the reference points, from scores of their own
+        scores([](int) {});
+#pragma unroll
+        for (int kb = 0; kb < KBW; kb++) mask(kb);
 #pragma unroll
         for (int rb = 0; rb < RBW; rb++) {
           float mx = -INFINITY;
@@ -370,54 +361,91 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
           m[rb] = m_new;
         }
         __syncthreads();
-      }
 #pragma unroll
-      for (int rb = 0; rb < RBW; rb++) {
-        const float mr = RW == 1 ? m[rb] : (rw == 0 ? m[rb] : m[RB - RBW + rb]);
-        const float ref = mr == -INFINITY ? 0.0f : mr;
-#pragma unroll
-        for (int kb = 0; kb < KBW; kb++) {
-          float pr[4];
-#pragma unroll
-          for (int i = 0; i < 4; i++) {
-            pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][i], scale, -ref));
-            l[rb] += pr[i];
-          }
-          write_b64(pw[kb] + rb * 2048, pack_bf16(pr[0], pr[1]), pack_bf16(pr[2], pr[3]));
+        for (int rb = 0; rb < RBW; rb++) {
+          const float mr = RW == 1 ? m[rb] : (rw == 0 ? m[rb] : m[RB - RBW + rb]);
+          neg[rb] = mr == -INFINITY ? 0.0f : -mr;
         }
       }
-      // step j of the value product: 32 keys (j / DB) of dim block j % DB
-      bf16x8 va[AV + 1];
-      auto read_v = [&](int j) {
+      // the weights of one row block and key block
+      auto weigh = [&](int rb, int kb) {
+        float pr[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][i], scale, neg[rb]));
+          l[rb] += pr[i];
+        }
+        uint32_t lo = pack_bf16(pr[0], pr[1]), hi = pack_bf16(pr[2], pr[3]);
+        formed(lo);
+        formed(hi);
+        formed(l[rb]);
+        write_b64(pw[kb] + rb * 2048, lo, hi);
+      };
+      bf16x8 va[AV + 1], pb[RB];
+      auto read_v = [&](int j) {  // step j of the value product: 32 keys (j / DB) of dim block j % DB
         const int k2 = j / G::DB, db = j % G::DB;
         s16x4 h[2];
 #pragma unroll
         for (int e = 0; e < 2; e++)
-          h[e] = read_tr(cur + vat[(db & 3) ^ (2 * e)] + k2 * (32 * G::ROWB) + e * 512 + (db >> 2) * 1024);
+          h[e] = read_tr(cur + vat[e][db & 3] + k2 * (32 * G::ROWB) + (db >> 2) * 1024);
         return join(h[0], h[1]);
       };
+      auto read_p = [&](int k2) {
+#pragma unroll
+        for (int rb = 0; rb < RB; rb++) pb[rb] = read_b128(lds_at(pr_at[k2]) + rb * 2048);
+      };
+      auto values = [&](int k2, auto between) {
+#pragma unroll
+        for (int jj = 0; jj < G::DB; jj++) {
+          const int j = k2 * G::DB + jj;
+          if (j + AV < 2 * G::DB) va[(j + AV) % (AV + 1)] = read_v(j + AV);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int rb = 0; rb < RB; rb++)
+            o[rb][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[j % (AV + 1)], pb[rb], o[rb][jj], 0, 0, 0);
+          between(jj);
+#pragma unroll
+          for (int i = 0; i < L::WRITES; i++)
+            if (i * (2 * G::DB) / L::WRITES == j) loader.finish(i);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      // A wave with two key blocks forms the weights of the first beside the scores of the
+      // second, and those of the second beside the value products of the first 32 keys.
+      loader.begin(tile0 + (buf ^ 1) * G::TILE, k0 + kLatTileKeys);
+      scores([&](int j) {
+#pragma unroll
+        for (int i = 0; i < L::LOADS; i++)
+          if (L::issue_at(i, QS) == j) loader.issue(i);
+        if constexpr (KBW == 2) {
+          if (j == G::KS) mask(0);
+#pragma unroll
+          for (int rb = 0; rb < RBW; rb++)
+            if (j == G::KS + 2 + 5 * rb) weigh(rb, 0);
+        }
+      });
+      if constexpr (KBW == 1) {
+        mask(0);
+#pragma unroll
+        for (int rb = 0; rb < RBW; rb++) weigh(rb, 0);
+      }
 #pragma unroll
       for (int j = 0; j < AV; j++) va[j] = read_v(j);
       __syncthreads();
-      bf16x8 pb[2][RB];
-      auto read_p = [&](int k2) {
-#pragma unroll
-        for (int rb = 0; rb < RB; rb++) pb[k2][rb] = read_b128(lds_at(pr_at[k2]) + rb * 2048);
-      };
       read_p(0);
+      if constexpr (KBW == 2) mask(1);
+      values(0, [&](int jj) {
+        if constexpr (KBW == 2) {
 #pragma unroll
-      for (int j = 0; j < 2 * G::DB; j++) {
-        const int k2 = j / G::DB, db = j % G::DB;
-        if (j + AV < 2 * G::DB) va[(j + AV) % (AV + 1)] = read_v(j + AV);
-        if (j == G::DB / 2) read_p(1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int rb = 0; rb < RB; rb++)
-          o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[j % (AV + 1)], pb[k2][rb], o[rb][db], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (more) loader.finish(nxt);
+          for (int rb = 0; rb < RBW; rb++)
+            if (jj == 1 + 2 * rb) weigh(rb, 1);
+        }
+      });
+      if constexpr (KBW == 2) __syncthreads();
+      read_p(1);
+      values(1, [](int) {});
     }
+    wait_vmcnt<0>();
     __syncthreads();
   };
   // With the fixed reference bf16 weights and float32 sums keep their relative precision for

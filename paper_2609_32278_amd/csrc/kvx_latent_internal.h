@@ -11,12 +11,11 @@ constexpr int kLatGroup = 64;       // latent values that share a scale on an fp
 constexpr int kLatMinExp = -117;    // their powers of two: every code * 2^e is a finite, normal bf16 value
 constexpr int kLatMaxExp = 119;
 
-// Where the scale byte of (slot, group) lies among a page's scale bytes.  One wave-wide load
-// of 16 codes a lane covers T = 1024 / latent_dim slots; a lane meets one group of one slot
-// of each of the page's 16 / T loads, and its bytes lie side by side.
+// Where the scale byte of (slot, group) lies among a page's scale bytes.  A wave that reads a
+// page's codes takes 8 slots x 128 codes at once, 16 codes a lane; the bytes that one lane
+// meets in these loads lie side by side.
 constexpr int latent_scale_at(int latent_dim, int slot, int group) {
-  const int T = 1024 / latent_dim, G = latent_dim / kLatGroup;
-  return ((slot % T) * G + group) * (kPageSize / T) + slot / T;
+  return ((slot % 8) * 2 + group % 2) * (latent_dim / 64) + slot / 8 * (latent_dim / 128) + group / 2;
 }
 
 struct LatentPoolView {

@@ -186,7 +186,7 @@ __global__ __launch_bounds__(kExpThreads, 1) void latent_expand_kernel(LatentExp
 #pragma unroll
       for (int j = 0; j < 2; j++) {
         codes[j] = *(const uint4*)(a_src[j] + k0);
-        sc[j] = a_src[2 + j][k0 / 64 * (LAT / 64)];
+        sc[j] = a_src[2 + j][(k0 / 64 & 1) * (LAT / 64) + k0 / 128];
       }
     } else {
 #pragma unroll

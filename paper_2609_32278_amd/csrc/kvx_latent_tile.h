@@ -81,6 +81,11 @@ __device__ __forceinline__ void write_b64(uint32_t at, uint32_t x, uint32_t y) {
   *(__attribute__((address_space(3))) u32x2*)(uintptr_t)at = u32x2{x, y};
 }
 
+__device__ __forceinline__ void write_b128(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  *(__attribute__((address_space(3))) u32x4*)(uintptr_t)at = u32x4{x, y, z, w};
+}
+
 __device__ __forceinline__ bf16x8 join(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
@@ -120,51 +125,6 @@ __device__ __forceinline__ void wait_vmcnt() {
 }
 
 typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;  // scalar-loaded
-
-// Stage tokens key0 .. key0 + 63 of a request (its page list at page_ids) as bf16 rows;
-// tokens at or past key_end are replaced by token `safe`, so that no slot that the request
-// does not own is read.
-template <int LAT, bool FP8, int THREADS>
-__device__ __forceinline__ void stage_rows(uint8_t* tile, const LatentPoolView& pool, const int32_t* page_ids,
-                                           int key0, int key_end, int safe) {
-  using G = LatGeom<LAT>;
-  const int tid = threadIdx.x;
-  if constexpr (FP8) {
-    constexpr int CPT = LAT / 16;
-    for (int i = tid; i < kLatTileKeys * CPT; i += THREADS) {
-      const int r = i / CPT, c = i % CPT;
-      const int key = key0 + r < key_end ? key0 + r : safe, slot = key % kPageSize;
-      const uint8_t* page = pool.base + (int64_t)page_ids[key / kPageSize] * pool.page_bytes;
-      const uint4 codes = *(const uint4*)(page + slot * LAT + c * 16);
-      const float sc = __uint_as_float(
-          (uint32_t)page[kPageSize * (LAT + 2 * kLatRope) + latent_scale_at(LAT, slot, c / 4)] << 23);
-      const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
-      uint32_t y[8];
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        y[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], sc, false));
-        y[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], sc, true));
-      }
-      *(uint4*)(tile + r * G::ROWB + (((2 * c) ^ swz(r)) * 16)) = make_uint4(y[0], y[1], y[2], y[3]);
-      *(uint4*)(tile + r * G::ROWB + (((2 * c + 1) ^ swz(r)) * 16)) = make_uint4(y[4], y[5], y[6], y[7]);
-    }
-    for (int i = tid; i < kLatTileKeys * 8; i += THREADS) {
-      const int r = i / 8, c = i % 8;
-      const int key = key0 + r < key_end ? key0 + r : safe, slot = key % kPageSize;
-      const uint8_t* page = pool.base + (int64_t)page_ids[key / kPageSize] * pool.page_bytes;
-      *(uint4*)(tile + r * G::ROWB + (((LAT / 8 + c) ^ swz(r)) * 16)) =
-          *(const uint4*)(page + kPageSize * LAT + slot * (2 * kLatRope) + c * 16);
-    }
-  } else {
-    for (int i = tid; i < kLatTileKeys * G::CPR; i += THREADS) {
-      const int r = i / G::CPR, c = i % G::CPR;
-      const int key = key0 + r < key_end ? key0 + r : safe;
-      const uint8_t* page = pool.base + (int64_t)page_ids[key / kPageSize] * pool.page_bytes;
-      *(uint4*)(tile + r * G::ROWB + ((c ^ swz(r)) * 16)) =
-          *(const uint4*)(page + (key % kPageSize) * G::ROWB + c * 16);
-    }
-  }
-}
 
 }  // namespace
 }  // namespace kvx
