@@ -22,18 +22,19 @@ struct TileAt {
   __device__ static int chunk(int r, int c) { return row(r) + (c >> 3) * 1024 + (((c & 7) ^ order(r)) << 4); }
 };
 
-// How a wave brings its page of a 64-key tile to LDS: begin() with the tile, every issue(i)
-// and, for an 8-bit page, every finish(i) later.  Tokens at or past key_end become token
-// `safe`; a tile past the last is that token throughout.  The steps are made one by one among
-// the products of the tile before: a burst of them stalls the wave (18 loads of 1 KiB took
-// 1.8k cycles of a step's 5.5k).
+// How a wave brings its page of a 64-key tile to LDS.  Tokens at or past key_end become token
+// `safe`; a tile past the last is that token throughout.  Loads and writes are made one by one
+// among the products of the tile before: a burst of them stalls the wave (18 loads of 1 KiB
+// took 1.8k cycles of a step's 5.5k).
 template <int LAT>
 struct Pages {
   const uint8_t* base;
   const_i32_ptr ids;
   int64_t page_bytes;
   int key_end, safe, lane, wave;
-  uint32_t page;  // of the next tile
+  const uint8_t* safe_page;
+  uint32_t page;  // of the next tile: read at the end of a step, as a scalar load under way
+                  // would make every wait for LDS a full drain
 
   __device__ __forceinline__ uint32_t page_at(int k0) const {
     const int lp = k0 / kPageSize + wave, last = (key_end - 1) / kPageSize;
@@ -47,6 +48,7 @@ struct Pages {
     safe = safe_key;
     lane = l;
     wave = w;
+    safe_page = address((uint32_t)ids[safe / kPageSize]);
   }
   __device__ __forceinline__ const uint8_t* address(uint32_t pg) const { return base + (uint64_t)pg * page_bytes; }
 };
@@ -58,13 +60,13 @@ template <int LAT>
 struct Loader<LAT, false> : Pages<LAT> {
   using G = LatGeom<LAT>;
   using P = Pages<LAT>;
-  static constexpr int BLOCKS = G::ROWB / 128, LOADS = 2 * BLOCKS, WRITES = 0;
+  static constexpr int BLOCKS = G::ROWB / 128, LOADS = 2 * BLOCKS;
   const uint8_t* from[2];  // of this lane in each half
   uint32_t to;
 
   __device__ __forceinline__ void begin(uint32_t tile, int k0) {
     const uint8_t* src = P::address(P::page);
-    const uint8_t* alt = P::address((uint32_t)P::ids[P::safe / kPageSize]) + (P::safe % kPageSize) * G::ROWB;
+    const uint8_t* alt = P::safe_page + (P::safe % kPageSize) * G::ROWB;
     const int left = P::key_end - k0 - P::wave * kPageSize;  // rows of this page that exist
 #pragma unroll
     for (int h = 0; h < 2; h++) {
@@ -72,63 +74,67 @@ struct Loader<LAT, false> : Pages<LAT> {
       from[h] = (row < left ? src + row * G::ROWB : alt) + c;
     }
     to = tile + P::wave * (16 * G::ROWB);
-    P::page = P::page_at(k0 + kLatTileKeys);
   }
   __device__ __forceinline__ void issue(int i) { lds_load_1k(from[i / BLOCKS] + i % BLOCKS * 128, to + i * 1024); }
-  __device__ __forceinline__ void finish(int) {}
-  // evenly over the score product
-  __device__ static constexpr int issue_at(int i, int steps) { return i * steps / LOADS; }
 };
 
 // An 8-bit page comes through registers, 16 codes a lane and load, and is written to LDS as
-// bf16 (exactly: code * 2^e).  A load takes 8 slots x 128 codes, so that its two writes fill
-// two blocks without bank conflicts.
+// bf16 (exactly: code * 2^e).  Beside the value product of a tile, the next tile's pieces are
+// written, each followed by the load of the same piece of the tile after that.
+//
+// A load takes 8 slots x 128 codes: lanes 8 i .. 8 i + 7 slots i % 4 and i % 4 + 4, whose chunk
+// orders differ in bit 0, so that the even (and the odd) chunks that eight lanes write fill
+// half a row of banks.
 template <int LAT>
 struct Loader<LAT, true> : Pages<LAT> {
   using G = LatGeom<LAT>;
   using P = Pages<LAT>;
   static constexpr int CODES = LAT / 64, PER = LAT / 128;  // loads of codes: of a page, of 8 slots
-  static constexpr int LOADS = CODES + 2, WRITES = CODES + 2;
+  static constexpr int LOADS = CODES + 2;
   const uint8_t* from[2];  // codes of this lane's slot in each half
   const uint8_t* key[2];
   uint4 data[LOADS];
-  uint64_t scales;     // CODES bytes, one per load
+  uint64_t scales, scales_next;  // CODES bytes, one per load
+  uint32_t at, key_at;           // this lane's first chunk, and its chunk of the key, in the first half
   uint32_t to;
 
-  __device__ __forceinline__ void begin(uint32_t tile, int k0) {
+  __device__ __forceinline__ int sub() const { return ((P::lane >> 3) & 3) | (P::lane & 4); }
+  __device__ __forceinline__ void init(const LatentAttnParams& p, const LatentUnit& u, int safe_key, int l, int w) {
+    P::init(p, u, safe_key, l, w);
+    at = w * (16 * G::ROWB) + TileAt<LAT>::chunk(sub(), 2 * (l & 3)) + (l >> 5) * 1024;
+    key_at = w * (16 * G::ROWB) + TileAt<LAT>::chunk(l >> 3, LAT / 8 + (l & 7));
+  }
+  __device__ __forceinline__ void begin(uint32_t tile, int k0) {  // `tile` is where finish() writes meanwhile
     constexpr int SC = kPageSize * (LAT + 2 * kLatRope);
     const uint8_t* src = P::address(P::page);
-    const uint8_t* alt = P::address((uint32_t)P::ids[P::safe / kPageSize]);
+    const uint8_t* alt = P::safe_page;
     const int left = P::key_end - k0 - P::wave * kPageSize, ss = P::safe % kPageSize;
-    const int sub = P::lane >> 3, c = P::lane & 7, hi = c >> 2;
-    const uint8_t* sc = src + SC + latent_scale_at(LAT, sub, hi);
-    if constexpr (CODES == 8) scales = *(const uint64_t*)sc;
-    else scales = *(const uint32_t*)sc;
+    const int c = (P::lane >> 5) * 4 + (P::lane & 3);
+    const uint8_t* sc = src + SC + latent_scale_at(LAT, sub(), P::lane >> 5);
+    if constexpr (CODES == 8) scales_next = *(const uint64_t*)sc;
+    else scales_next = *(const uint32_t*)sc;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-      const int slot = 8 * h + sub;
+      const int slot = 8 * h + sub(), ks = 8 * h + (P::lane >> 3);
       from[h] = (slot < left ? src + slot * LAT : alt + ss * LAT) + c * 16;
-      key[h] = (slot < left ? src + slot * 128 : alt + ss * 128) + kPageSize * LAT + c * 16;
+      key[h] = (ks < left ? src + ks * 128 : alt + ss * 128) + kPageSize * LAT + (P::lane & 7) * 16;
     }
     if (left < kPageSize) {  // uniform
 #pragma unroll
       for (int i = 0; i < CODES; i++)
-        if (8 * (i / PER) + sub >= left)
-          scales = (scales & ~(0xFFull << (8 * i))) |
-                   (uint64_t)alt[SC + latent_scale_at(LAT, ss, 2 * (i % PER) + hi)] << (8 * i);
+        if (8 * (i / PER) + sub() >= left)
+          scales_next = (scales_next & ~(0xFFull << (8 * i))) |
+                        (uint64_t)alt[SC + latent_scale_at(LAT, ss, 2 * (i % PER) + (P::lane >> 5))] << (8 * i);
     }
-    to = tile + P::wave * (16 * G::ROWB);
-    P::page = P::page_at(k0 + kLatTileKeys);
+    to = tile;
   }
   __device__ __forceinline__ void issue(int i) {
     data[i] = *(const uint4*)(i < CODES ? from[i / PER] + i % PER * 128 : key[i - CODES]);
   }
-  // early, so that the data is there for the writes beside the value product
-  __device__ static constexpr int issue_at(int i, int steps) { return i * (steps / 2) / LOADS; }
   __device__ __forceinline__ void finish(int i) {
-    const int sub = P::lane >> 3, c = P::lane & 7;
+    // slots 8 and up: the second half, where bit 2 of the chunk order is flipped
+    const uint32_t half = (i < CODES ? i / PER : i - CODES) ? TileAt<LAT>::HALF : 0, flip = half ? 64 : 0;
     if (i < CODES) {
-      const int slot = 8 * (i / PER) + sub, block = 2 * (i % PER) + (c >> 2);
       const float sc = __uint_as_float(((uint32_t)(scales >> (8 * i)) & 0xFF) << 23);
       const uint32_t w[4] = {data[i].x, data[i].y, data[i].z, data[i].w};
       uint32_t y[8];
@@ -137,10 +143,11 @@ struct Loader<LAT, true> : Pages<LAT> {
         y[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], sc, false));
         y[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], sc, true));
       }
-      write_b128(to + TileAt<LAT>::chunk(slot, 8 * block + 2 * (c & 3)), y[0], y[1], y[2], y[3]);
-      write_b128(to + TileAt<LAT>::chunk(slot, 8 * block + 2 * (c & 3) + 1), y[4], y[5], y[6], y[7]);
+      const uint32_t off = half + i % PER * 2048;
+      write_b128((at ^ flip) + to + off, y[0], y[1], y[2], y[3]);
+      write_b128((at ^ flip ^ 16) + to + off, y[4], y[5], y[6], y[7]);
     } else {
-      write_b128(to + TileAt<LAT>::chunk((i - CODES) * 8 + sub, LAT / 8 + c), data[i].x, data[i].y, data[i].z, data[i].w);
+      write_b128((key_at ^ flip) + to + half, data[i].x, data[i].y, data[i].z, data[i].w);
     }
   }
 };
@@ -199,6 +206,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   constexpr int RW = RB == 4 ? 2 : 1, KW = 4 / RW;  // waves by rows and by keys in the score product
   constexpr int RBW = RB / RW, KBW = 4 / KW;        // 16-row and 16-key blocks of a wave in it
   constexpr int QS = G::KS * KBW;                   // its steps
+  // Direct loads of the next tile: over the whole score product, or, where HBM and not the
+  // matrix unit is the bound, all at its start (128 requests on 16 heads: 382 us spread, 360 us).
+  constexpr int SPREAD = RB == 1 ? 1000 : 1;
   // operand reads ahead of their products, in steps of the score and of the value product
   constexpr int AK = RBW == 1 ? 8 : 6, AV = RB == 1 ? 8 : (RB == 2 ? 5 : 3);
   __shared__ __attribute__((aligned(1024))) uint8_t tile[2][G::TILE];
@@ -286,8 +296,16 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
     loader.begin(tile0, u.key_begin);
 #pragma unroll
     for (int i = 0; i < L::LOADS; i++) loader.issue(i);
+    loader.page = loader.page_at(u.key_begin + kLatTileKeys);
+    if constexpr (FP8) {
+      loader.scales = loader.scales_next;
 #pragma unroll
-    for (int i = 0; i < L::WRITES; i++) loader.finish(i);
+      for (int i = 0; i < L::LOADS; i++) loader.finish(i);
+      loader.begin(tile0, u.key_begin + kLatTileKeys);
+#pragma unroll
+      for (int i = 0; i < L::LOADS; i++) loader.issue(i);
+      loader.page = loader.page_at(u.key_begin + 2 * kLatTileKeys);
+    }
     int buf = 0;
     for (int k0 = u.key_begin; k0 < u.key_end; k0 += kLatTileKeys, buf ^= 1) {
       const lds_ptr cur = (lds_ptr)tile[0] + buf * G::TILE;
@@ -404,19 +422,27 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
           for (int rb = 0; rb < RB; rb++)
             o[rb][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[j % (AV + 1)], pb[rb], o[rb][jj], 0, 0, 0);
           between(jj);
+          if constexpr (FP8) {
 #pragma unroll
-          for (int i = 0; i < L::WRITES; i++)
-            if (i * (2 * G::DB) / L::WRITES == j) loader.finish(i);
+            for (int i = 0; i < L::LOADS; i++)
+              if (i * (2 * G::DB) / L::LOADS == j) {
+                loader.finish(i);
+                loader.issue(i);
+              }
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
       };
       // A wave with two key blocks forms the weights of the first beside the scores of the
       // second, and those of the second beside the value products of the first 32 keys.
-      loader.begin(tile0 + (buf ^ 1) * G::TILE, k0 + kLatTileKeys);
+      if constexpr (FP8) loader.scales = loader.scales_next;
+      loader.begin(tile0 + (buf ^ 1) * G::TILE, k0 + (FP8 ? 2 : 1) * kLatTileKeys);
       scores([&](int j) {
+        if constexpr (!FP8) {
 #pragma unroll
-        for (int i = 0; i < L::LOADS; i++)
-          if (L::issue_at(i, QS) == j) loader.issue(i);
+          for (int i = 0; i < L::LOADS; i++)
+            if (i * QS / SPREAD / L::LOADS == j) loader.issue(i);
+        }
         if constexpr (KBW == 2) {
           if (j == G::KS) mask(0);
 #pragma unroll
@@ -444,6 +470,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
       if constexpr (KBW == 2) __syncthreads();
       read_p(1);
       values(1, [](int) {});
+      loader.page = loader.page_at(k0 + (FP8 ? 3 : 2) * kLatTileKeys);
     }
     wait_vmcnt<0>();
     __syncthreads();
