@@ -13,8 +13,10 @@ constexpr int kStages = 3;     // tiles in LDS: one attended, one arriving, one 
 // LDS layout of a tile: groups of 8 rows, in a group blocks of 128 bytes of the rows,
 // [group][block][8 rows][128 bytes]: K rows are the expanded part and then the shared rotated
 // key, V rows follow after the 64 K rows.  A wave-wide direct load of 1 KiB fills a block; the
-// 16-byte chunks of a row in a block are stored in the order c ^ swz(row), which keeps operand
-// reads (16 rows one chunk; 4 rows two chunks) free of bank conflicts.
+// 16-byte chunks of a row in a block are stored in the order c ^ order(row), which keeps the
+// operand reads (32 rows one chunk; 4 rows four chunks) free of bank conflicts.
+__device__ __forceinline__ int order(int r) { return ((r & 2) << 1) | ((r & 4) >> 1) | ((r >> 3) & 1); }
+
 template <int D>
 struct PreGeom {
   static constexpr int QK = D + kLatRope;
@@ -43,22 +45,25 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
   const uint8_t* kx = (const uint8_t*)(p.kx + ((size_t)hd * p.x_rows + u.x_row + u.key_begin + wave * 16) * D);
   const uint8_t* vx = (const uint8_t*)(p.vx + ((size_t)hd * p.x_rows + u.x_row + u.key_begin + wave * 16) * D);
   const uint8_t* rx = (const uint8_t*)(p.rx + (size_t)(u.x_row + u.key_begin + wave * 16) * kLatRope);
-  const int chunk = ((lane & 7) ^ swz(lane >> 3)) << 4;
+  const int chunk = ((lane & 7) ^ order(lane >> 3)) << 4;
   const int off_x = (lane >> 3) * (D * 2) + chunk, off_r = (lane >> 3) * (kLatRope * 2) + chunk;
   const uint32_t lds0 = lds_address(lds) + wave * (2 * G::KB * 1024), lds0v = lds_address(lds) + G::V0 + wave * (2 * G::VB * 1024);
-  auto issue = [&](int t) {
-    const size_t at = (size_t)t * kBN;
-    const uint32_t st = (uint32_t)(t % kStages) * G::STAGE;
-#pragma unroll
-    for (int gr = 0; gr < 2; gr++) {
-      const int flip = gr ? 16 : 0;  // row bit 3 in swz
-#pragma unroll
-      for (int b = 0; b < G::VB; b++) {
-        lds_load_1k(kx + (at + gr * 8) * (D * 2) + b * 128, off_x ^ flip, lds0 + st + (gr * G::KB + b) * 1024);
-        lds_load_1k(vx + (at + gr * 8) * (D * 2) + b * 128, off_x ^ flip, lds0v + st + (gr * G::VB + b) * 1024);
-      }
-      lds_load_1k(rx + (at + gr * 8) * (kLatRope * 2), off_r ^ flip, lds0 + st + (gr * G::KB + G::VB) * 1024);
-    }
+  constexpr int PIECES = 2 * (G::KB + G::VB);
+  size_t aim_at = 0;
+  uint32_t aim_stage = 0;
+  auto aim = [&](int t) {  // the tile that the next pieces are of
+    aim_at = (size_t)(t < n_tiles ? t : n_tiles - 1) * kBN;
+    aim_stage = (uint32_t)(t % kStages) * G::STAGE;
+  };
+  auto piece = [&](int i) {
+    const int gr = i / (G::KB + G::VB), j = i % (G::KB + G::VB), flip = gr ? 16 : 0;  // row bit 3 in order
+    if (j < G::VB)
+      lds_load_1k(kx + (aim_at + gr * 8) * (D * 2) + j * 128, off_x ^ flip, lds0 + aim_stage + (gr * G::KB + j) * 1024);
+    else if (j == G::VB)
+      lds_load_1k(rx + (aim_at + gr * 8) * (kLatRope * 2), off_r ^ flip, lds0 + aim_stage + (gr * G::KB + j) * 1024);
+    else
+      lds_load_1k(vx + (aim_at + gr * 8) * (D * 2) + (j - G::KB) * 128, off_x ^ flip,
+                  lds0v + aim_stage + (gr * G::VB + j - G::KB) * 1024);
   };
 
   bf16x8 qf[2][G::KS];
@@ -84,7 +89,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
   uint32_t kat[4], vat[2][2];
 #pragma unroll
   for (int i = 0; i < 4; i++) {
-    kat[i] = lds_address(lds) + (n >> 3) * (G::KB * 1024) + (n & 7) * 128 + (((2 * i + h) ^ swz(n)) << 4);
+    kat[i] = lds_address(lds) + (n >> 3) * (G::KB * 1024) + (n & 7) * 128 + (((2 * i + h) ^ order(n)) << 4);
     opaque(kat[i]);
   }
 #pragma unroll
@@ -93,7 +98,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
     for (int i = 0; i < 2; i++) {
       const int r = 8 * e + 4 * h + (lane & 15) / 4;
       vat[e][i] = lds_address(lds) + G::V0 + (r >> 3) * (G::VB * 1024) + (r & 7) * 128 +
-                  (((4 * i + 2 * (n >> 4) + (lane & 3) / 2) ^ swz(r)) << 4) + (lane & 1) * 8;
+                  (((4 * i + 2 * (n >> 4) + (lane & 3) / 2) ^ order(r)) << 4) + (lane & 1) * 8;
       opaque(vat[e][i]);
     }
 
@@ -129,7 +134,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
   };
   // S of 32 keys into `s`, the weights of `w` formed between its steps; START_V: the first V
   // operands of (vst, vkb) are read before the last steps.
-  auto scores = [&](f32x16 (&s)[2], uint32_t st, int kb, f32x16 (&w)[2], auto weights, uint32_t vst, int vkb) {
+  // LOADS: the pieces of a later tile that the value product before left are loaded meanwhile.
+  constexpr int VP = PIECES * 2 / 5;  // pieces loaded beside a value product
+  auto scores = [&](f32x16 (&s)[2], uint32_t st, int kb, f32x16 (&w)[2], auto weights, auto loads, uint32_t vst,
+                    int vkb) {
     constexpr bool W = decltype(weights)::value;
     s[0] = f32x16{};
     s[1] = f32x16{};
@@ -147,10 +155,15 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
             if (i * 2 * G::KS / 32 == ks * 2 + rb) weigh(w, i);
         }
       }
+      if constexpr (decltype(loads)::value) {
+#pragma unroll
+        for (int i = VP; i < PIECES; i++)
+          if ((i - VP) * G::KS / (PIECES - VP) == ks) piece(i);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto values = [&](uint32_t st, int kb) {
+  auto values = [&](uint32_t st, int kb, auto loads) {
 #pragma unroll
     for (int j = 0; j < 2 * G::DB; j++) {
       if (j + AV < 2 * G::DB) va[(j + AV) % (AV + 1)] = read_v(st, kb, j + AV);
@@ -160,6 +173,11 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
         const int half = j / G::DB * 4;
         const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(pk[rb][half], pk[rb][half + 1], pk[rb][half + 2], pk[rb][half + 3]));
         o[rb][j % G::DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j % (AV + 1)], b, o[rb][j % G::DB], 0, 0, 0);
+      }
+      if constexpr (decltype(loads)::value) {
+#pragma unroll
+        for (int i = 0; i < VP; i++)
+          if (i * 2 * G::DB / VP == j) piece(i);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -200,14 +218,19 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
 #pragma unroll
       for (int db = 0; db < G::DB; db++) o[rb][db] = f32x16{};
     }
-    issue(0);
-    if (n_tiles > 1) issue(1);
-    if (n_tiles > 1) wait_vmcnt<2 * (2 * G::VB + 1)>();
-    else wait_vmcnt<0>();
+    using Yes = std::true_type;
+    using No = std::false_type;
+#pragma unroll
+    for (int t = 0; t < 2; t++) {
+      aim(t);
+#pragma unroll
+      for (int i = 0; i < PIECES; i++) piece(i);
+    }
+    wait_vmcnt<PIECES>();
     __syncthreads();
     f32x16 sa[2], sb[2];
     start_k(0, 0);
-    scores(sa, 0, 0, sb, std::false_type{}, 0, 0);
+    scores(sa, 0, 0, sb, No{}, No{}, 0, 0);
     if (u.key_begin + 32 > full_end) mask(sa, u.key_begin);
     rereference(sa);
     start_k(0, 1);
@@ -219,19 +242,17 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
       if constexpr (!FIXED) {
         if (t > 0) rereference(sa);
       }
-      scores(sb, st, 1, sa, std::true_type{}, st, 0);
+      scores(sb, st, 1, sa, Yes{}, No{}, st, 0);
       if (k0 + 64 > full_end) mask(sb, k0 + 32);
       // tile t + 1 is whole, and every wave is past tile t - 1, whose stage tile t + 2 takes
-      if (more) {
-        wait_vmcnt<0>();
-        __syncthreads();
-        if (t + 2 < n_tiles) issue(t + 2);
-        start_k(next, 0);
-      }
-      values(st, 0);
+      wait_vmcnt<0>();
+      __syncthreads();
+      aim(t + 2);
+      start_k(next, 0);
+      values(st, 0, Yes{});
       if constexpr (!FIXED) rereference(sb);
       if (more) {
-        scores(sa, next, 0, sb, std::true_type{}, st, 1);
+        scores(sa, next, 0, sb, Yes{}, Yes{}, st, 1);
         if (k0 + 96 > full_end) mask(sa, k0 + 64);
         start_k(next, 1);
       } else {
@@ -239,9 +260,10 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
 #pragma unroll
         for (int i = 0; i < 32; i++) weigh(sb, i);
       }
-      values(st, 1);
+      values(st, 1, No{});
       st = next;
     }
+    wait_vmcnt<0>();  // pieces past the last tile
     __syncthreads();
   };
   // As in the attention on latents: only where an exponential or a sum overflows float32 are
