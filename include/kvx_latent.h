@@ -44,7 +44,7 @@ enum kvx_latent_dtype {
 };
 
 enum kvx_latent_form {
-    KVX_LATENT_AUTO = 0,     /* per request, by its lengths: whichever is estimated to be faster */
+    KVX_LATENT_AUTO = 0,     /* by the batch's lengths, request by request: whichever is estimated to be faster */
     KVX_LATENT_ABSORBED = 1,
     KVX_LATENT_EXPANDED = 2
 };

@@ -240,6 +240,16 @@ struct Blob {
   }
 };
 
+// A list for the arguments of its kernel, or added to the blob; returns its offset there.
+template <typename U, int N>
+size_t place_list(const std::vector<U>& v, kvx::ShortList<U, N>& list, Blob& blob) {
+  list.n = 0;
+  if (v.size() > (size_t)N) return blob.add(v);
+  list.n = (int32_t)v.size();
+  std::copy(v.begin(), v.end(), list.at);
+  return 0;
+}
+
 // Work that shares its keys, to run on one XCD: units [first, first + count).
 struct Group {
   int64_t cost;
@@ -249,6 +259,18 @@ struct Group {
 // Launch order (workgroup i runs on XCD i % 8): groups, longest first, each to the XCD with
 // the least work so far; -1 pads the shorter queues.
 std::vector<int32_t> spread(std::vector<Group>& groups) {
+  // A group that is a large share of all would leave other XCDs idle: no more than a 64th of
+  // the units stay together.
+  int64_t units = 0;
+  for (const Group& g : groups) units += g.count;
+  const int32_t most_units = (int32_t)std::max<int64_t>(1, units / 64);
+  for (size_t i = 0, n = groups.size(); i < n; i++) {
+    while (groups[i].count > most_units) {
+      groups[i].count -= most_units;
+      const Group rest{groups[i].cost, groups[i].first + groups[i].count, most_units};
+      groups.push_back(rest);
+    }
+  }
   std::stable_sort(groups.begin(), groups.end(), [](const Group& a, const Group& b) { return a.cost > b.cost; });
   std::vector<int32_t> queue[kvx::kNumXcd];
   int64_t load[kvx::kNumXcd] = {};
@@ -532,20 +554,33 @@ void plan_expanded(const kvx_batch* b, const std::vector<int64_t>& qo, const std
       }
     }
   }
-  if (groups.size() < 64) {  // too few to fill eight queues evenly: unit by unit
-    groups.clear();
-    for (size_t i = 0; i < units.size(); i++)
-      groups.push_back({ceil_div(units[i].key_end - units[i].key_begin, 64) + 2, (int32_t)i, 1});
-  }
   plan.units = in_order(units, spread(groups));
 }
 
-// Whether a request is estimated to be faster in the absorbed form: products by its lengths.
-bool prefers_absorbed(int64_t P, int64_t E, int64_t latent, int64_t d) {
-  const double pairs = (double)E * P + 0.5 * (double)E * (E + 1);
-  const double ab = 2.0 * d * latent * E + (2.0 * latent + kvx::kLatRope) * pairs;
-  const double ex = 2.0 * d * latent * (P + E) + (2.0 * d + kvx::kLatRope) * pairs;
-  return ab <= ex;
+// The requests of a batch that take the absorbed form, by what each form costs: its products
+// at the rate they reach in large batches (the expanded form about 0.8 of the absorbed one's
+// 1.1 PFLOP/s, expansion and attention together) and its launches.  All of one form, or each
+// request its cheaper one.  Measured at 16, 32 and 128 heads, 2k to 30k tokens cached, both forms
+// per suffix length: 64 tokens 0.28-0.63 of the expanded form's time, 128 tokens 0.5-0.8,
+// 256 tokens 1.0-1.4, 512 tokens 1.5-2.0; four requests of 100 + 100 tokens 63 against 39 us.
+std::vector<bool> choose_forms(const kvx_batch* b, int32_t Hq, int64_t latent, int64_t d) {
+  constexpr double kRateAbsorbed = 1.1e9, kRateExpanded = 0.88e9;       // operations per us
+  constexpr double kLaunchAbsorbed = 30.0, kLaunchExpanded = 20.0;      // us
+  const int32_t R = b->num_reqs;
+  std::vector<bool> absorbed((size_t)R);
+  double all_a = kLaunchAbsorbed, all_e = kLaunchExpanded, mixed = kLaunchAbsorbed + kLaunchExpanded;
+  for (int32_t r = 0; r < R; r++) {
+    const double P = b->prefix_lens[r], E = b->extend_lens[r], pairs = E * P + 0.5 * E * (E + 1);
+    if (E == 0) continue;
+    const double a = 2.0 * Hq * (2.0 * d * latent * E + (2.0 * latent + kvx::kLatRope) * pairs) / kRateAbsorbed;
+    const double e = 2.0 * Hq * (2.0 * d * latent * (P + E) + (2.0 * d + kvx::kLatRope) * pairs) / kRateExpanded;
+    absorbed[(size_t)r] = a <= e;
+    all_a += a;
+    all_e += e;
+    mixed += std::min(a, e);
+  }
+  if (all_a <= mixed || all_e <= mixed) absorbed.assign((size_t)R, all_a <= all_e);
+  return absorbed;
 }
 
 // Attention on latents over `members`: launches its kernel and merge; the plan is at `dev`.
@@ -773,13 +808,15 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
     if (!q || !out || !proj->w_uk || !proj->w_uv)
       return report(KVX_EINVAL, "q, out, w_uk and w_uv must be non-NULL");
 
+    std::vector<bool> takes_absorbed((size_t)batch->num_reqs, form == KVX_LATENT_ABSORBED);
+    if (form == KVX_LATENT_AUTO) takes_absorbed = choose_forms(batch, Hq, lat, D);
     std::vector<Member> absorbed;
     std::vector<int32_t> expanded;
     int64_t own_rows = 0, x_tokens = 0;
     for (int32_t r = 0; r < batch->num_reqs; r++) {
       const int64_t P = batch->prefix_lens[r], E = batch->extend_lens[r];
       if (E == 0) continue;
-      if (form == KVX_LATENT_ABSORBED || (form == KVX_LATENT_AUTO && prefers_absorbed(P, E, lat, D))) {
+      if (takes_absorbed[(size_t)r]) {
         absorbed.push_back({r, own_rows});
         own_rows += E;
       } else {
@@ -801,6 +838,10 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
     Blob blob;
     AbsorbedPlan ap;
     std::vector<LatentRows> rows;
+    kvx::LatentProjParams ppar{};
+    kvx::LatentExpandParams xpar{};
+    kvx::LatentPrefillParams tpar[2] = {};
+    kvx::LatentTileMergeParams mpar[2] = {};
     size_t a_units = 0, a_merges = 0, a_rows = 0;
     if (!absorbed.empty()) {
       plan_absorbed(batch, absorbed, Hq, lat, pool->split_keys, ap);
@@ -819,7 +860,7 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
         a_units = blob.add(ap.units);
         a_merges = blob.add(ap.merges);
       }
-      a_rows = blob.add(rows);
+      a_rows = place_list(rows, ppar.list, blob);
     }
     std::vector<LatentExpandUnit> x_units;
     std::vector<int64_t> x_row;
@@ -834,17 +875,18 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
       heads = (int32_t)ceil_div(Hq, ceil_div(Hq, heads));
       last = Hq - heads * (int32_t)(ceil_div(Hq, heads) - 1);
       plan_expanded(batch, qo, expanded, x_row, heads, D, xp);
-      x_at = blob.add(x_units);
-      t_at[0] = t_at[1] = blob.add(xp.units);
-      m_at[0] = m_at[1] = blob.add(xp.merges);
+      x_at = place_list(x_units, xpar.list, blob);
+      t_at[0] = place_list(xp.units, tpar[0].list, blob);
+      m_at[0] = place_list(xp.merges, mpar[0].list, blob);
       if (last != heads) {
         plan_expanded(batch, qo, expanded, x_row, last, D, xl);
-        t_at[1] = blob.add(xl.units);
-        m_at[1] = blob.add(xl.merges);
+        t_at[1] = place_list(xl.units, tpar[1].list, blob);
+        m_at[1] = place_list(xl.merges, mpar[1].list, blob);
       }
     }
     void* dev_v = nullptr;
-    if (int rc = pool->st_plan.upload(blob.bytes.data(), blob.bytes.size(), s, &dev_v)) return rc;
+    if (!blob.bytes.empty())
+      if (int rc = pool->st_plan.upload(blob.bytes.data(), blob.bytes.size(), s, &dev_v)) return rc;
     const uint8_t* dev = (const uint8_t*)dev_v;
 
     if (!absorbed.empty()) {
@@ -853,7 +895,7 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
       if (int rc = pool->absorbed.ensure(q_bytes + o_bytes + l_bytes, s)) return rc;
       uint8_t* ws = (uint8_t*)pool->absorbed.ptr;
       float* own_lse = lse ? (float*)(ws + q_bytes + o_bytes) : nullptr;
-      kvx::LatentProjParams p{};
+      kvx::LatentProjParams& p = ppar;
       p.in = (const uint16_t*)q;
       p.w = (const uint16_t*)proj->w_uk;
       p.out = (uint16_t*)ws;
@@ -884,7 +926,7 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
         const int32_t n = std::min(heads, Hq - h0);
         const bool tail = n != heads;
         const ExpandedPlan& plan = tail ? xl : xp;
-        kvx::LatentExpandParams x{};
+        kvx::LatentExpandParams& x = xpar;
         x.pool = view(pool, batch);
         x.w_uk = (const uint16_t*)proj->w_uk + (size_t)h0 * D * lat;
         x.w_uv = (const uint16_t*)proj->w_uv + (size_t)h0 * D * lat;
@@ -896,7 +938,7 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
         x.heads = n;
         hipError_t e = kvx::launch_latent_expand(x, (int64_t)x_units.size(), lat, D, pool->dtype == KVX_LATENT_FP8, s);
         if (e != hipSuccess) return hip_fail(e, "latent expansion launch");
-        kvx::LatentPrefillParams p{};
+        kvx::LatentPrefillParams& p = tpar[tail];
         p.q = (const uint16_t*)q;
         p.out = (uint16_t*)out;
         p.lse = lse;
@@ -913,7 +955,7 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
         e = kvx::launch_latent_prefill(p, (int64_t)plan.units.size(), D, s);
         if (e != hipSuccess) return hip_fail(e, "expanded attention launch");
         if (!plan.merges.empty()) {
-          kvx::LatentTileMergeParams m{};
+          kvx::LatentTileMergeParams& m = mpar[tail];
           m.merges = (const LatentTileMerge*)(dev + m_at[tail]);
           m.o_part = p.o_part;
           m.lse_part = p.lse_part;
@@ -926,9 +968,10 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
         }
       }
       if (int rc = pool->expanded.done(s)) return rc;
-      if (int rc = pool->parts.done(s)) return rc;
+      if (n_parts > 0)
+        if (int rc = pool->parts.done(s)) return rc;
     }
-    return pool->st_plan.done(s);
+    return blob.bytes.empty() ? KVX_OK : pool->st_plan.done(s);
   });
 }
 

@@ -141,6 +141,13 @@ hipError_t launch_latent_merge(const LatentMergeParams& p, int64_t n_merges, con
 
 // ---- per-head weights
 
+// A short list travels in the arguments of the kernel that takes it.
+template <typename U, int N>
+struct ShortList {
+  int32_t n;  // 0: the list is in memory
+  U at[N];
+};
+
 // A run of suffix tokens of the batch, all heads, and where they are among the tokens that
 // take the absorbed form (whose latent-space rows are kept side by side).
 struct LatentRows {
@@ -150,6 +157,7 @@ struct LatentRows {
   int32_t pad;
 };
 constexpr int kLatProjTok = 64;
+using LatentRowList = ShortList<LatentRows, 64>;
 
 // Per-head products of the absorbed form.  Queries in: [T, Hq, nope + 64] and W_uk to
 // [T, Hq, latent + 64].  Sums out: [T, Hq, latent] and W_uv to [T, Hq, v].
@@ -161,6 +169,7 @@ struct LatentProjParams {
   float* lse_out;
   const LatentRows* rows;
   int32_t num_q_heads;
+  LatentRowList list;
 };
 
 // Up to 256 cached tokens of a request, for the keys and values of all heads of a group.
@@ -173,6 +182,7 @@ struct LatentExpandUnit {
   int32_t nrows;      // rows to write, a multiple of 64
   int32_t pad;
 };
+using LatentExpandList = ShortList<LatentExpandUnit, 96>;
 
 struct LatentExpandParams {
   LatentPoolView pool;
@@ -185,6 +195,7 @@ struct LatentExpandParams {
   int64_t x_rows;
   int32_t heads;
   int32_t heads_per;     // per workgroup (set by the launcher)
+  LatentExpandList list;
 };
 
 // One workgroup of expanded attention: tokens of one request and head against a range of
@@ -201,10 +212,12 @@ struct LatentTile {
 };
 static_assert(sizeof(LatentTile) == 32, "LatentTile is 32 bytes");
 constexpr int kLatTileTok = 256;
+using LatentTileList = ShortList<LatentTile, 96>;
 
 struct LatentTileMerge {
   int32_t qo_row, head_ntok, part0, nparts;
 };
+using LatentTileMergeList = ShortList<LatentTileMerge, 96>;
 
 struct LatentPrefillParams {
   const uint16_t* q;   // bf16 [T, Hq, head_dim + 64]
@@ -220,6 +233,7 @@ struct LatentPrefillParams {
   int32_t num_q_heads;
   int32_t head0;       // first head of the group
   float scale_log2;
+  LatentTileList list;
 };
 
 struct LatentTileMergeParams {
@@ -230,7 +244,11 @@ struct LatentTileMergeParams {
   float* lse;
   int32_t num_q_heads;
   int32_t head0;
+  LatentTileMergeList list;
 };
+static_assert(sizeof(LatentProjParams) <= 4096 && sizeof(LatentExpandParams) <= 4096 &&
+                  sizeof(LatentPrefillParams) <= 4096 && sizeof(LatentTileMergeParams) <= 4096,
+              "kernel arguments");
 
 hipError_t launch_latent_absorb(const LatentProjParams& p, int64_t n_rows, int latent_dim, int head_dim,
                                 hipStream_t stream);

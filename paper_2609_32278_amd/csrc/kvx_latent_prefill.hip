@@ -33,7 +33,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
   using G = PreGeom<D>;
   constexpr int AK = 4, AV = 3;  // operand reads ahead of their products
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * G::STAGE];
-  const LatentTile u = p.units[blockIdx.x];
+  const LatentTile u = listed(p, p.units);
   const int ntok = u.head_ntok & 0xFFFF, hd = u.head_ntok >> 16;
   if (ntok == 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
 template <int D>
 __global__ __launch_bounds__(kThreads) void latent_tile_merge_kernel(LatentTileMergeParams p) {
   constexpr int LPT = D / 8, TPW = kThreads / LPT;
-  const LatentTileMerge m = p.merges[blockIdx.x];
+  const LatentTileMerge m = listed(p, p.merges);
   const int tok = blockIdx.y * TPW + threadIdx.x / LPT, c = threadIdx.x % LPT;
   if (tok >= (m.head_ntok & 0xFFFF)) return;
   float top = -INFINITY;

@@ -15,7 +15,7 @@ __global__ __launch_bounds__(kThreads) void latent_absorb_kernel(LatentProjParam
   constexpr int IN = D + kLatRope, OUT = LAT + kLatRope;
   constexpr int WB = kSlice * 2 + 32;  // LDS row
   __shared__ __attribute__((aligned(16))) uint8_t wl[D * WB];
-  const LatentRows rows = p.rows[blockIdx.x];
+  const LatentRows rows = listed(p, p.rows);
   const int hd = blockIdx.y, s0 = blockIdx.z * kSlice;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
   const uint16_t* w = p.w + (size_t)hd * D * LAT + s0;
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void latent_absorb_kernel(LatentProjParam
 template <int LAT, int D>
 __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParams p) {
   constexpr int NB = D / 64;  // 16-row blocks of W per wave
-  const LatentRows rows = p.rows[blockIdx.x];
+  const LatentRows rows = listed(p, p.rows);
   const int hd = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
   const uint16_t* w = p.w + ((size_t)hd * D + wave * (D / 4) + n) * LAT + 8 * g;
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kExpThreads, 1) void latent_expand_kernel(LatentExp
   constexpr int A_BYTES = kExpTok * 128, W_BYTES = 2 * D * 128, STAGE = A_BYTES + W_BYTES;
   constexpr int WG = 2 * D / 64;           // groups of 8 weight rows per wave
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
-  const LatentExpandUnit u = p.units[blockIdx.x];
+  const LatentExpandUnit u = listed(p, p.units);
   const int head0 = blockIdx.y * p.heads_per, heads = p.heads - head0 < p.heads_per ? p.heads - head0 : p.heads_per;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;

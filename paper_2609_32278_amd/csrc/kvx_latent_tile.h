@@ -37,6 +37,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
+typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;  // scalar-loaded
+
+// This workgroup's element of the list in a kernel's parameters (its first argument), or of
+// the one in memory: scalar loads, so that what follows from it stays uniform.
+template <typename U, typename Params>
+__device__ __forceinline__ U listed(const Params& p, const U* memory) {
+  const const_i32_ptr in_args =
+      (const_i32_ptr)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() +
+                      offsetof(Params, list) + offsetof(decltype(p.list), at));
+  const const_i32_ptr w = (p.list.n > 0 ? in_args : (const_i32_ptr)memory) + (size_t)blockIdx.x * (sizeof(U) / 4);
+  int32_t words[sizeof(U) / 4];
+#pragma unroll
+  for (size_t i = 0; i < sizeof(U) / 4; i++) words[i] = w[i];
+  U u;
+  __builtin_memcpy(&u, words, sizeof u);
+  return u;
+}
+
 // Keep an operand that is used throughout a unit in the accumulator half of the register
 // file, which the matrix instructions read as well.
 __device__ __forceinline__ void keep_in_acc(bf16x8& x) {
@@ -124,7 +142,6 @@ __device__ __forceinline__ void wait_vmcnt() {
   __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
 
-typedef const __attribute__((address_space(4))) int32_t* const_i32_ptr;  // scalar-loaded
 
 }  // namespace
 }  // namespace kvx
