@@ -229,6 +229,14 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   using L = Loader<LAT, FP8>;
   L loader;
   loader.init(p, u, safe, lane, wave);
+  const uint32_t tile0 = lds_address(tile);
+  auto first_loads = [&]() {
+    loader.page = loader.page_at(u.key_begin);
+    loader.begin(tile0, u.key_begin);
+#pragma unroll
+    for (int i = 0; i < L::LOADS; i++) loader.issue(i);
+  };
+  first_loads();  // ahead of the queries', which then arrive with them
 
   bf16x8 qf[RBW][G::KS];
   int limit[RBW];  // last visible key of the lane's rows
@@ -291,21 +299,17 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
 #pragma unroll
       for (int db = 0; db < G::DB; db++) o[rb][db] = f32x4{};
     }
-    const uint32_t tile0 = lds_address(tile);
-    loader.page = loader.page_at(u.key_begin);
-    loader.begin(tile0, u.key_begin);
-#pragma unroll
-    for (int i = 0; i < L::LOADS; i++) loader.issue(i);
-    loader.page = loader.page_at(u.key_begin + kLatTileKeys);
+    if constexpr (!FIXED) first_loads();
     if constexpr (FP8) {
+      loader.page = loader.page_at(u.key_begin + kLatTileKeys);
       loader.scales = loader.scales_next;
 #pragma unroll
       for (int i = 0; i < L::LOADS; i++) loader.finish(i);
       loader.begin(tile0, u.key_begin + kLatTileKeys);
 #pragma unroll
       for (int i = 0; i < L::LOADS; i++) loader.issue(i);
-      loader.page = loader.page_at(u.key_begin + 2 * kLatTileKeys);
     }
+    loader.page = loader.page_at(u.key_begin + (FP8 ? 2 : 1) * kLatTileKeys);
     int buf = 0;
     for (int k0 = u.key_begin; k0 < u.key_end; k0 += kLatTileKeys, buf ^= 1) {
       const lds_ptr cur = (lds_ptr)tile[0] + buf * G::TILE;

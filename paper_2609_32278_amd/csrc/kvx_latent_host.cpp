@@ -7,7 +7,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "kvx_host_util.h"
@@ -250,14 +252,15 @@ size_t place_list(const std::vector<U>& v, kvx::ShortList<U, N>& list, Blob& blo
   return 0;
 }
 
-// Work that shares its keys, to run on one XCD: units [first, first + count).
+// Work that shares its keys, to run on one XCD: units [first, first + count), each of them
+// `cost` long at most.
 struct Group {
-  int64_t cost;
+  double cost;
   int32_t first, count;
 };
 
-// Launch order (workgroup i runs on XCD i % 8): groups, longest first, each to the XCD with
-// the least work so far; -1 pads the shorter queues.
+// Launch order (workgroup i runs on XCD i % 8): groups, longest first, each to the XCD that has
+// the CU which is free first; -1 pads the shorter queues.
 std::vector<int32_t> spread(std::vector<Group>& groups) {
   // A group that is a large share of all would leave other XCDs idle: no more than a 64th of
   // the units stay together.
@@ -272,20 +275,32 @@ std::vector<int32_t> spread(std::vector<Group>& groups) {
     }
   }
   std::stable_sort(groups.begin(), groups.end(), [](const Group& a, const Group& b) { return a.cost > b.cost; });
-  std::vector<int32_t> queue[kvx::kNumXcd];
-  int64_t load[kvx::kNumXcd] = {};
+  constexpr int kXcds = kvx::kNumXcd, kCus = kSlots / kXcds;
+  struct Xcd {
+    double free[kCus] = {};  // when its CUs are, a heap with the earliest first
+    std::vector<int32_t> queue;
+  };
+  Xcd xcd[kXcds];
   for (const Group& g : groups) {
-    int x = 0;
-    for (int i = 1; i < kvx::kNumXcd; i++)
-      if (load[i] < load[x]) x = i;
-    load[x] += g.cost * g.count;
-    for (int32_t i = 0; i < g.count; i++) queue[x].push_back(g.first + i);
+    // the XCD, and on it as many units as have a CU at about the time that its first has
+    for (int32_t at = 0; at < g.count;) {
+      Xcd* x = &xcd[0];
+      for (Xcd& y : xcd)
+        if (y.free[0] < x->free[0] || (y.free[0] == x->free[0] && y.queue.size() < x->queue.size())) x = &y;
+      const double limit = x->free[0] + 0.1 * g.cost;
+      do {
+        std::pop_heap(x->free, x->free + kCus, std::greater<double>());
+        x->free[kCus - 1] += g.cost;
+        std::push_heap(x->free, x->free + kCus, std::greater<double>());
+        x->queue.push_back(g.first + at++);
+      } while (at < g.count && x->free[0] <= limit);
+    }
   }
   size_t most = 0;
-  for (const auto& q : queue) most = std::max(most, q.size());
-  std::vector<int32_t> out(most * kvx::kNumXcd, -1);
-  for (size_t x = 0; x < (size_t)kvx::kNumXcd; x++)
-    for (size_t i = 0; i < queue[x].size(); i++) out[i * kvx::kNumXcd + x] = queue[x][i];
+  for (const Xcd& x : xcd) most = std::max(most, x.queue.size());
+  std::vector<int32_t> out(most * kXcds, -1);
+  for (size_t x = 0; x < (size_t)kXcds; x++)
+    for (size_t i = 0; i < xcd[x].queue.size(); i++) out[i * kXcds + x] = xcd[x].queue[i];
   while (!out.empty() && out.back() < 0) out.pop_back();
   return out;
 }
@@ -304,42 +319,102 @@ struct Span {
   int64_t tiles, len;
 };
 
-// Steps of 64 keys that a part should have at most; 0: nothing is split.  Cost of a unit
-// besides its steps: kStart; of a part, its result written and read again: kPart.
-constexpr double kStart = 2.0, kPart = 1.0;
-int64_t choose_steps(const std::vector<Span>& spans) {
+// Parts of at most `steps` steps of 64 keys (0: nothing is split): of equal length, or, where a
+// length was asked for, `cut` every `steps`.
+struct Split {
+  int64_t steps = 0;
+  bool cut = false;
+  int64_t parts(int64_t len) const { return steps > 0 ? ceil_div(len, steps) : 1; }
+  int64_t part_len(int64_t len) const { return cut && parts(len) > 1 ? steps : ceil_div(len, parts(len)); }
+};
+
+// What a unit costs besides its steps of 64 keys, in such steps: its first loads and its
+// epilogue; the result of a part, written and read again.  Fitted to four batches of 64-row
+// units timed at ten forced lengths each (a step is 1.8 us).  Smaller units have less to load
+// and to write.
+struct UnitCosts {
+  double start, part;
+};
+
+// Estimated time of a plan: units, longest first, each to the CU that is free first.  Equal CUs
+// are kept together, a plan of very many units counts as even, and the search stops beyond
+// `limit`, as planning is on the path of every call.
+double plan_time(const std::vector<Span>& spans, const Split& split, const UnitCosts& k, double limit) {
+  double total = 0.0, top = 0.0;
+  int64_t units = 0, most = 1;
+  auto cost = [&](const Span& s) {
+    return (double)split.part_len(s.len) + k.start + (split.parts(s.len) > 1 ? k.part : 0.0);
+  };
+  for (const Span& s : spans) {
+    const int64_t parts = split.parts(s.len);
+    total += cost(s) * (double)(s.tiles * parts);
+    units += s.tiles * parts;
+    top = std::max(top, cost(s));
+    most = std::max(most, parts);
+  }
+  const double merge = most > 1 ? 2.0 + 0.12 * (double)most : 0.0;
+  const double least = std::max(top, total / kSlots) + merge;
+  if (least >= limit || units <= kSlots) return least;
+  if (units > 3 * kSlots) return std::max(top, total / kSlots + 0.5 * top) + merge;
+  using Work = std::pair<double, int64_t>;  // cost, units; or free at, CUs
+  std::vector<Work> work;
+  for (const Span& s : spans) work.push_back({cost(s), s.tiles * split.parts(s.len)});
+  std::sort(work.begin(), work.end(), std::greater<Work>());
+  std::vector<Work> cus{{0.0, kSlots}};  // a heap with the earliest first
+  double end = 0.0;
+  for (Work& w : work) {
+    while (w.second > 0) {
+      std::pop_heap(cus.begin(), cus.end(), std::greater<Work>());
+      Work& c = cus.back();
+      const double from = c.first;
+      const int64_t n = std::min(w.second, c.second), left = c.second - n;
+      c = {from + w.first, n};
+      std::push_heap(cus.begin(), cus.end(), std::greater<Work>());
+      if (left > 0) {
+        cus.push_back({from, left});
+        std::push_heap(cus.begin(), cus.end(), std::greater<Work>());
+      }
+      end = std::max(end, from + w.first);
+      w.second -= n;
+    }
+    if (end + merge >= limit) break;
+  }
+  return end + merge;
+}
+
+// Forced lengths from 256 to 8192 keys against this choice, whole calls in us, best forced
+// length in brackets: decode of 128 requests on 16 heads 353 (352), 24 long requests on 128
+// heads 508 (473), drafts of 32 requests 203 (165, a length that fits this batch by chance).
+Split choose_split(const std::vector<Span>& spans, const UnitCosts& k) {
   int64_t work = 0, longest = 0;
   for (const Span& s : spans) {
     work += s.tiles * s.len;
     longest = std::max(longest, s.len);
   }
-  if (work == 0) return 0;
-  auto estimate = [&](int64_t c) {
-    double total = 0.0, top = 0.0;
-    int64_t units = 0, most = 1;
-    for (const Span& s : spans) {
-      const int64_t parts = c > 0 ? ceil_div(s.len, c) : 1;
-      const double each = (double)ceil_div(s.len, parts) + kStart + (parts > 1 ? kPart : 0.0);
-      total += (double)(s.tiles * parts) * each;
-      units += s.tiles * parts;
-      top = std::max(top, each);
-      most = std::max(most, parts);
-    }
-    const double merge = most > 1 ? 2.0 + 0.12 * (double)most : 0.0;
-    return (units <= kSlots ? top : std::max(top, total / kSlots + 0.5 * top)) + merge;
-  };
-  int64_t best = 0;
-  double at = estimate(0);
-  for (const double rounds : {0.25, 0.5, 0.75, 0.9, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0}) {
+  Split best;
+  if (work == 0) return best;
+  double at = plan_time(spans, best, k, HUGE_VAL);
+  for (const double rounds : {0.9, 1.0, 0.75, 0.5, 0.25, 1.2, 1.5, 1.75, 2.0, 2.5, 3.0, 4.0, 6.0}) {
     const int64_t c = std::max<int64_t>(1, (int64_t)std::ceil((double)work / (rounds * kSlots)));
     if (c >= longest) continue;
-    const double e = estimate(c);
-    if (e < at) {
-      at = e;
-      best = c;
+    const double t = plan_time(spans, Split{c}, k, at);
+    if (t < at) {
+      at = t;
+      best = Split{c};
     }
   }
   return best;
+}
+
+// Longer parts where there would be more of them than `most`.
+void bound_parts(const std::vector<Span>& spans, int64_t most, Split& split) {
+  while (split.steps > 0) {
+    int64_t n = 0;
+    for (const Span& s : spans)
+      if (split.parts(s.len) > 1) n += s.tiles * split.parts(s.len);
+    if (n <= most) return;
+    split.steps *= 2;
+  }
 }
 
 struct AbsorbedPlan {
@@ -370,16 +445,10 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
     const int64_t E = b->extend_lens[m.req], L = b->prefix_lens[m.req] + E;
     spans.push_back({ceil_div(E * Hq, M), ceil_div(L, kvx::kLatTileKeys)});
   }
-  int64_t steps = split_keys > 0 ? split_keys / kvx::kLatTileKeys : choose_steps(spans);
-  const int64_t max_parts = kMaxPartBytes / (M * (latent_dim + 1) * 4);
-  auto parts_of = [&](const Span& s) { return steps > 0 ? ceil_div(s.len, steps) : 1; };
-  while (steps > 0) {
-    int64_t n = 0;
-    for (const Span& s : spans)
-      if (parts_of(s) > 1) n += s.tiles * parts_of(s);
-    if (n <= max_parts) break;
-    steps *= 2;
-  }
+  Split split{split_keys / kvx::kLatTileKeys, true};
+  const UnitCosts costs = plan.row_blocks == 4 ? UnitCosts{6.0, 6.0} : UnitCosts{4.0, 2.0};
+  if (split_keys == 0) split = choose_split(spans, costs);
+  bound_parts(spans, kMaxPartBytes / (M * (latent_dim + 1) * 4), split);
   const int32_t R = (int32_t)members.size();
   plan.rows.n = 0;
   if (R <= kvx::kLatRowReqs && std::all_of(spans.begin(), spans.end(), [](const Span& s) { return s.tiles == 1; })) {
@@ -388,8 +457,7 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
     std::vector<int64_t> len(members.size());
     for (int32_t i = 0; i < R; i++) {
       by[(size_t)i] = i;
-      const int64_t parts = parts_of(spans[(size_t)i]);
-      len[(size_t)i] = split_keys > 0 && parts > 1 ? steps : ceil_div(spans[(size_t)i].len, parts);
+      len[(size_t)i] = split.part_len(spans[(size_t)i].len);
     }
     std::stable_sort(by.begin(), by.end(), [&](int32_t a, int32_t b) { return len[(size_t)a] > len[(size_t)b]; });
     kvx::LatentRowPlan& rp = plan.rows;
@@ -420,15 +488,13 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
   std::vector<uint16_t> codes;  // of the units, while the plan may be a small one
   std::vector<Group> groups;
   int64_t all_tiles = 0, most_parts = 1;
-  for (const Span& s : spans) all_tiles += s.tiles, most_parts = std::max(most_parts, parts_of(s));
+  for (const Span& s : spans) all_tiles += s.tiles, most_parts = std::max(most_parts, split.parts(s.len));
   bool small = all_tiles <= kvx::kLatSmallTiles && most_parts <= kvx::kLatSmallParts;
   int32_t n_tiles = 0;
   for (size_t i = 0; i < members.size(); i++) {
     const Member& m = members[i];
     const int64_t P = b->prefix_lens[m.req], E = b->extend_lens[m.req], rows = E * Hq;
-    const int64_t parts = parts_of(spans[i]);
-    // equal parts, unless a length was asked for
-    const int64_t len = (split_keys > 0 && parts > 1 ? steps : ceil_div(spans[i].len, parts)) * kvx::kLatTileKeys;
+    const int64_t parts = split.parts(spans[i].len), len = split.part_len(spans[i].len) * kvx::kLatTileKeys;
     const int64_t part0 = plan.n_parts;
     const int64_t tiles = spans[i].tiles;
     if (parts > 1) plan.n_parts += tiles * parts;
@@ -441,7 +507,7 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
       }
     }
     for (int64_t c = 0; c < parts; c++) {
-      Group g{0, (int32_t)units.size(), 0};
+      Group g{0.0, (int32_t)units.size(), 0};
       for (int64_t t = tiles - 1; t >= 0; t--) {
         LatentUnit u{};
         u.row0 = (int32_t)(t * M);
@@ -454,7 +520,8 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
         u.key_begin = (int32_t)(c * len);
         u.key_end = (int32_t)std::min<int64_t>(end, (c + 1) * len);
         u.part = end > len ? (int32_t)(part0 + t * parts + c) : -1;
-        g.cost = std::max<int64_t>(g.cost, ceil_div(u.key_end - u.key_begin, kvx::kLatTileKeys) + 2);
+        g.cost = std::max(g.cost, (double)ceil_div(u.key_end - u.key_begin, kvx::kLatTileKeys) + costs.start +
+                                      (u.part >= 0 ? costs.part : 0.0));
         units.push_back(u);
         if (small) codes.push_back((uint16_t)((n_tiles + t) << 10 | c));
         g.count++;
@@ -510,29 +577,24 @@ void plan_expanded(const kvx_batch* b, const std::vector<int64_t>& qo, const std
     const int64_t E = b->extend_lens[r], L = b->prefix_lens[r] + E;
     spans.push_back({ceil_div(E, M) * heads, ceil_div(b->prefix_lens[r] + L, 128)});  // of its tiles on average
   }
-  int64_t steps = choose_steps(spans);
-  const int64_t max_parts = kMaxPartBytes / (M * (head_dim + 1) * 4);
-  auto parts_of = [&](int64_t L) { return steps > 0 ? ceil_div(ceil_div(L, 64), steps) : 1; };
-  while (steps > 0) {
-    int64_t n = 0;
-    for (size_t i = 0; i < reqs.size(); i++) {
-      const int64_t p = parts_of((int64_t)b->prefix_lens[reqs[i]] + b->extend_lens[reqs[i]]);
-      if (p > 1) n += spans[i].tiles * p;
-    }
-    if (n <= max_parts) break;
-    steps *= 2;
-  }
+  const UnitCosts costs{6.0, 6.0};
+  Split split = choose_split(spans, costs);
+  // of the longest tiles, which the parts are made for
+  std::vector<Span> longest;
+  for (size_t i = 0; i < reqs.size(); i++)
+    longest.push_back({spans[i].tiles, ceil_div((int64_t)b->prefix_lens[reqs[i]] + b->extend_lens[reqs[i]], 64)});
+  bound_parts(longest, kMaxPartBytes / (M * (head_dim + 1) * 4), split);
   std::vector<LatentTile> units;
   std::vector<Group> groups;
   for (size_t i = 0; i < reqs.size(); i++) {
     const int32_t r = reqs[i];
     const int64_t P = b->prefix_lens[r], E = b->extend_lens[r], tiles = ceil_div(E, M);
-    const int64_t parts = parts_of(P + E), len = ceil_div(ceil_div(P + E, 64), parts) * 64;
+    const int64_t parts = split.parts(longest[i].len), len = split.part_len(longest[i].len) * 64;
     for (int32_t h = 0; h < heads; h++) {
       const int64_t part0 = plan.n_parts;
       if (parts > 1) plan.n_parts += tiles * parts;
       for (int64_t c = 0; c < parts; c++) {
-        Group g{0, (int32_t)units.size(), 0};
+        Group g{0.0, (int32_t)units.size(), 0};
         for (int64_t t = tiles - 1; t >= 0; t--) {
           const int64_t n = std::min<int64_t>(M, E - t * M), end = P + t * M + n;
           if (c * len >= end) continue;
@@ -544,7 +606,8 @@ void plan_expanded(const kvx_batch* b, const std::vector<int64_t>& qo, const std
           u.key_begin = (int32_t)(c * len);
           u.key_end = (int32_t)std::min<int64_t>(end, (c + 1) * len);
           u.part = end > len ? (int32_t)(part0 + t * parts + c) : -1;
-          g.cost = std::max<int64_t>(g.cost, ceil_div(u.key_end - u.key_begin, 64) + 2);
+          g.cost = std::max(g.cost, (double)ceil_div(u.key_end - u.key_begin, 64) + costs.start +
+                                        (u.part >= 0 ? costs.part : 0.0));
           units.push_back(u);
           g.count++;
           if (c == 0 && end > len)
