@@ -138,7 +138,7 @@ int load_latent(kvx_latent_pool *pool, const kvx_batch *batch, void *out, int64_
  * of their own.
  *   q            device bf16 [T, num_q_heads, latent_dim + rope_dim]
  *   num_q_heads  1 to 1024
- *   sm_scale     finite, > 0
+ *   sm_scale     > 0, at most 2e38
  *   out          device bf16 [T, num_q_heads, latent_dim] (round to nearest even)
  *   lse          device fp32 [T, num_q_heads] natural-log sum of exp of the scaled scores,
  *                or NULL
@@ -168,7 +168,9 @@ typedef struct {
  * Intermediate rows -- expanded keys and values, or queries and sums in the latent space --
  * are rounded to bf16 once each, so the two forms differ by such roundings, and the scores
  * behind lse carry one.  Uses library-owned device workspaces: for the expanded form the keys
- * and values of as many heads at a time as 2 GiB holds (at least one).
+ * and values of as many heads at a time as 2 GiB holds (at least one); for the absorbed form
+ * 2 (2 latent_dim + rope_dim) + 4 bytes for each of its suffix tokens and heads; for either up
+ * to 2 GiB of partial results.
  * Errors: as store_latent.  R = 0 or T = 0: no-op.
  */
 int latent_extend_attention(kvx_latent_pool *pool, const kvx_batch *batch, const kvx_latent_proj *proj,

@@ -47,15 +47,19 @@ struct kvx_latent_pool {
 namespace {
 
 constexpr int kSlots = 256;  // CUs, one attention workgroup each
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMaxPartBytes = 2ll << 30;
 constexpr int64_t kMaxExpandBytes = 2ll << 30;
 
-// Run an entry point's body: no exception crosses the ABI.
+// Run an entry point's body: no exception crosses the ABI, and an error of the runtime that is
+// returned is not left for the caller's next call to find.
 template <typename F>
 int guarded(F&& body) {
   report(KVX_OK, "%s", "");
   try {
-    return body();
+    const int rc = body();
+    if (rc == KVX_EHIP || rc == KVX_ENOMEM) (void)hipGetLastError();
+    return rc;
   } catch (const std::bad_alloc&) {
     return report(KVX_ENOMEM, "host memory for the plan of the call");
   } catch (...) {
@@ -92,7 +96,8 @@ int check_stream(hipStream_t s) {
 }
 
 int check_scale(float sm_scale) {
-  if (!(sm_scale > 0.0f) || !std::isfinite(sm_scale)) return report(KVX_EINVAL, "sm_scale must be finite and > 0");
+  if (!(sm_scale > 0.0f) || !std::isfinite(sm_scale * kLog2e))
+    return report(KVX_EINVAL, "sm_scale must be > 0 and at most 2e38");
   return KVX_OK;
 }
 
@@ -664,7 +669,7 @@ int launch_absorbed(kvx_latent_pool* pool, const kvx_batch* batch, const Absorbe
     p.lse_part = p.o_part + (size_t)plan.n_parts * per_part;
   }
   p.num_q_heads = Hq;
-  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  p.scale_log2 = sm_scale * kLog2e;
   const kvx::LatentRowPlan* rows = plan.in_args && plan.rows.n > 0 ? &plan.rows : nullptr;
   const kvx::LatentSmallPlan* small = plan.in_args && !rows ? &plan.small : nullptr;
   hipError_t e = kvx::launch_latent_attention(p, (int64_t)plan.units.size(), small, rows, pool->latent_dim,
@@ -1014,7 +1019,7 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
         p.x_rows = x_rows;
         p.num_q_heads = Hq;
         p.head0 = h0;
-        p.scale_log2 = sm_scale * 1.4426950408889634f;
+        p.scale_log2 = sm_scale * kLog2e;
         e = kvx::launch_latent_prefill(p, (int64_t)plan.units.size(), D, s);
         if (e != hipSuccess) return hip_fail(e, "expanded attention launch");
         if (!plan.merges.empty()) {

@@ -131,6 +131,10 @@ struct LatentMergeParams {
   int32_t num_q_heads;
 };
 
+static_assert(sizeof(LatentAttnParams) + sizeof(LatentSmallPlan) <= 4096 &&
+                  sizeof(LatentAttnParams) + sizeof(LatentRowPlan) <= 4096,
+              "kernel arguments");
+
 // small, rows: the plan (in host memory) for the kernel arguments, or null; n_units and
 // n_merges are those of a plan in memory.
 hipError_t launch_latent_attention(const LatentAttnParams& p, int64_t n_units, const LatentSmallPlan* small,

@@ -153,7 +153,7 @@ void refusals() {
   };
   CHECK(latent_attention(nullptr, one.get(), q, 16, 0.1f, qo, nullptr, nullptr) == KVX_EINVAL);
   for (int hq : {0, -1, 1025}) CHECK(attend(one.get(), q, hq, 0.1f, qo) == KVX_EINVAL);
-  for (float sc : {0.0f, -1.0f, INFINITY, NAN}) CHECK(attend(one.get(), q, 16, sc, qo) == KVX_EINVAL);
+  for (float sc : {0.0f, -1.0f, 3e38f, INFINITY, NAN}) CHECK(attend(one.get(), q, 16, sc, qo) == KVX_EINVAL);
   CHECK(attend(one.get(), nullptr, 16, 0.1f, qo) == KVX_EINVAL);
   CHECK(attend(one.get(), q, 16, 0.1f, nullptr) == KVX_EINVAL);
   CHECK(attend(one.get(), addr(0x100002), 16, 0.1f, qo) == KVX_EINVAL);

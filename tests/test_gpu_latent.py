@@ -378,6 +378,231 @@ def test_latent_extend_many_heads_in_groups(setup):
     assert (np.abs(ref.f64(lse) - l - math.log(times)) <= ltol + L * 2.0 ** -24).all()
 
 
+# ------------------------------------------------------------------- larger plans, other orders
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_decode_of_more_requests_than_arguments_hold(setup, fp8):
+    g = np.random.default_rng(3)
+    P = g.integers(0, 500, 150).tolist()
+    s = setup(P, [1] * 150, 256, fp8)
+    attend_and_check(s, s.fill(), 12, 0.07)
+
+
+def test_more_tiles_than_arguments_hold(setup):
+    s = setup([100, 0, 900], [40, 70, 9], 256, True)  # 64-row tiles: 25, 44 and 6
+    attend_and_check(s, s.fill(), 40, 0.07)
+    kvx.latent_pool_set_split_keys(s.pool, 128)
+    attend_and_check(s, s.fill(), 40, 0.07)
+
+
+def test_most_heads(setup):
+    s = setup([70, 5], [1, 2], 256, False)
+    attend_and_check(s, s.fill(), 1024, 0.07)
+
+
+def test_extend_of_more_tiles_than_arguments_hold(setup):
+    s = setup([64 * i for i in range(34)], [3] * 34, 256, True)
+    extend_and_check(s, s.fill(), 3, 64, kvx.KVX_LATENT_EXPANDED)
+    extend_and_check(s, s.fill(), 3, 64, kvx.KVX_LATENT_ABSORBED)
+
+
+def test_requests_that_share_pages(setup):
+    """Two requests whose prefix is the same pages, as a prefix cache hands them out."""
+    s = setup([96, 96], [5, 1], 512, True)
+    first = int(s.indptr[1])
+    s.pages[first:first + 6] = s.pages[:6]
+    rows = s.normal(int(sum(s.P) + sum(s.E)), 576)
+    rows[101:101 + 96] = rows[:96]
+    kvx.store_latent(s.pool, kvx.Batch([0, 96], [101, 1], s.indptr, s.pages), torch.cat([rows[:101], rows[197:]]))
+    x = ref.f64(rows)
+    x[:, :512] = ref.quantised(x[:, :512])
+    attend_and_check(s, [x[:101], x[101:]], 16, 0.07)
+    extend_and_check(s, [x[:101], x[101:]], 2, 128, kvx.KVX_LATENT_AUTO)
+
+
+@pytest.mark.parametrize("form", [kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_extend_uneven_scores(setup, fp8, form):
+    """Scores that rise along the keys past what float32 exponentials of a fixed reference
+    reach, and fall: the weights of all but a few keys vanish, the outputs stay those keys'."""
+    for order in (1, -1):
+        s = setup([300], [70], 256, fp8)
+        rows = s.normal(370, 320)
+        rows[:, 256] = (torch.linspace(-30, 30, 370, device=DEV) * order).to(BF16)
+        x = s.fill(rows=rows)[0]
+        q = s.normal(70, 2, 128, scale=0.3)
+        q[..., 64] = 60.0  # times the rotated key's first value, which no form rounds
+        w_uk, w_uv = s.normal(2, 64, 256, scale=1 / 16), s.normal(2, 64, 256, scale=1 / 16)
+        out = torch.empty(70, 2, 64, dtype=BF16, device=DEV)
+        lse = torch.empty(70, 2, dtype=torch.float32, device=DEV)
+        kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, 0.5, out, lse, form=form)
+        c, key, h = x[:, :256], x[:, 256:], ref.HALF_BF16
+        uk, uv, qq = ref.f64(w_uk), ref.f64(w_uv), ref.f64(q)
+        v = np.einsum("hdl,jl->hjd", uv, c)
+        # only the products with the expanded part (or with q') meet a rounding: bound those apart
+        k = np.concatenate([np.einsum("hdl,jl->hjd", uk, c), np.broadcast_to(key, (2,) + key.shape)], -1)
+        o, l, tol, ltol = ref.attend(qq, k, v, 300, 0.5, v_err=h)
+        ql = np.einsum("hdl,ihd->ihl", uk, qq[..., :64])
+        size = np.maximum(np.einsum("ihd,hjd->ihj", np.abs(qq[..., :64]), np.abs(k[..., :64])),
+                          np.einsum("ihl,jl->ihj", np.abs(ql), np.abs(c))).max(-1) * 0.5 * h
+        a = np.einsum("ihj,hjd->ihd", np.exp(np.where(np.arange(370)[None, None] <= 300 + np.arange(70)[:, None, None],
+                                                      np.einsum("ihd,hjd->ihj", qq, k) * 0.5, -np.inf) - l[..., None]),
+                      np.abs(v))
+        tol = tol + a * np.expm1(2 * size)[..., None]
+        if form == kvx.KVX_LATENT_ABSORBED:  # the sums in the latent space are rounded instead of the values
+            sums = np.einsum("ihj,jl->ihl", np.exp(np.where(np.arange(370)[None, None] <= 300 + np.arange(70)[:, None, None],
+                                                            np.einsum("ihd,hjd->ihj", qq, k) * 0.5, -np.inf) - l[..., None]),
+                             np.abs(c))
+            tol = tol + np.einsum("hdl,ihl->ihd", np.abs(uv), sums * (2 * h + np.expm1(2 * size)[..., None]))
+        got = ref.f64(out)
+        assert np.isfinite(got).all() and (np.abs(got - o) <= tol + h * (np.abs(o) + tol)).all()
+        assert (np.abs(ref.f64(lse) - l) <= ltol + size).all()
+
+
+def test_uneven_scores_of_8_bit_latents(setup):
+    for order, heads, E in ((1, 16, 1), (-1, 16, 1), (1, 33, 2), (1, 30, 1)):
+        s = setup([700], [E], 512, True)
+        rows = s.normal(700 + E, 576)
+        rows[:, 512] = (torch.linspace(-30, 30, 700 + E, device=DEV) * order).to(BF16)
+        q = s.normal(E, heads, 576, scale=0.3)
+        q[..., 512] = 60.0
+        attend_and_check(s, s.fill(rows=rows), heads, 0.5, q=q)
+
+
+def test_auto_takes_both_forms_in_one_call(setup):
+    """Decoding requests on both sides of a long prompt: the prompt goes expanded, the others
+    absorbed, and every row lands where it belongs."""
+    lat, hd, heads, n = 256, 64, 32, 2500
+    P, E = [3000] * 12 + [0] + [3000] * 12, [1] * 12 + [n] + [2] * 12
+    s = setup(P, E, lat, False)
+    rows = s.fill()
+    q = s.normal(s.T, heads, hd + 64)
+    w_uk, w_uv = s.normal(heads, hd, lat, scale=1 / 16), s.normal(heads, hd, lat, scale=1 / 16)
+    out = torch.full((s.T + 1, heads, hd), 7.0, dtype=BF16, device=DEV)
+    lse = torch.full((s.T + 1, heads), 7.0, dtype=torch.float32, device=DEV)
+    kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, 0.09, out, lse)
+    assert (out[s.T] == 7).all() and (lse[s.T] == 7).all()
+    uk, uv, at = ref.f64(w_uk), ref.f64(w_uv), 0
+    for r, (p, e) in enumerate(zip(P, E)):
+        take = 3  # of the prompt its last rows
+        first = at + max(e - take, 0)
+        x, c = ref.f64(q[first:at + e]), rows[r][:, :lat]
+        k = np.concatenate([np.einsum("hdl,jl->hjd", uk, c), np.broadcast_to(rows[r][:, lat:], (heads,) + rows[r][:, lat:].shape)], -1)
+        o, l, _, _ = ref.attend(x, k, np.einsum("hdl,jl->hjd", uv, c), p + max(e - take, 0), 0.09)
+        got = ref.f64(out[first:at + e])
+        assert np.linalg.norm(got - o) <= RMS_EXTEND * np.linalg.norm(o), r
+        # a score carries one rounding of 64 products' factor: of rms 2^-8 / sqrt(3) of its size
+        assert np.abs(ref.f64(lse[first:at + e]) - l).max() < 2.0 ** -8
+        at += e
+
+
+def test_forms_agree_and_calls_repeat(setup):
+    """The same call twice gives the same bits, with or without lse; the two forms differ by
+    their roundings only."""
+    s = setup([500, 0, 2000], [3, 90, 1], 512, True)
+    s.fill()
+    q = s.normal(s.T, 16, 192)
+    w_uk, w_uv = s.normal(16, 128, 512, scale=512 ** -0.5), s.normal(16, 128, 512, scale=512 ** -0.5)
+
+    def call(form, with_lse=True):
+        out = torch.empty(s.T, 16, 128, dtype=BF16, device=DEV)
+        lse = torch.empty(s.T, 16, dtype=torch.float32, device=DEV) if with_lse else None
+        kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, 0.07, out, lse, form=form)
+        return out, lse
+
+    got = {}
+    for form in (kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED, kvx.KVX_LATENT_AUTO):
+        got[form] = call(form)
+        again = call(form)
+        assert torch.equal(got[form][0], again[0]) and torch.equal(got[form][1], again[1])
+        assert torch.equal(got[form][0], call(form, False)[0])
+    a, b = (got[f][0].float() for f in (kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED))
+    assert (a - b).norm() <= 2 * RMS_EXTEND * b.norm()
+
+
+def test_two_pools_on_two_streams(setup):
+    pools = [setup([400 + 100 * i, 30], [1, 20], 256, bool(i), seed=i) for i in range(2)]
+    args = []
+    for s in pools:
+        s.fill()
+        args.append((s.normal(s.T, 24, 320), torch.empty(s.T, 24, 256, dtype=BF16, device=DEV)))
+        kvx.latent_attention(s.pool, s.batch, args[-1][0], 24, 0.07, args[-1][1])
+    torch.cuda.synchronize()
+    want = [o.clone() for _, o in args]
+    streams = [torch.cuda.Stream() for _ in pools]
+    for _ in range(3):
+        for s, (q, o), st in zip(pools, args, streams):
+            with torch.cuda.stream(st):
+                o.zero_()
+                kvx.latent_attention(s.pool, s.batch, q, 24, 0.07, o)
+        torch.cuda.synchronize()
+        for (_, o), w in zip(args, want):
+            assert torch.equal(o, w)
+
+
+def test_empty_batches(setup):
+    s = setup([20, 0], [0, 0], 256, False, poison=False)
+    nothing = kvx.Batch([], [], [0], torch.empty(0, dtype=torch.int32, device=DEV))
+    for b in (s.batch, nothing):
+        x = torch.empty(0, 320, dtype=BF16, device=DEV)
+        kvx.store_latent(s.pool, b, x)
+        kvx.load_latent(s.pool, b, x)
+        kvx.latent_attention(s.pool, b, torch.empty(0, 4, 320, dtype=BF16, device=DEV), 4, 0.1,
+                             torch.empty(0, 4, 256, dtype=BF16, device=DEV))
+
+
+# ------------------------------------------------------------------- refusals
+
+
+def test_capturing_stream_is_refused(setup):
+    s = setup([40], [2], 256, False)
+    s.fill()
+    q, o = s.normal(2, 4, 320), torch.empty(2, 4, 256, dtype=BF16, device=DEV)
+    row, x = s.normal(2, 320), torch.zeros(4, device=DEV)
+    w = s.normal(4, 64, 256)
+    qs, os_ = s.normal(2, 4, 128), torch.empty(2, 4, 64, dtype=BF16, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x += 1
+        for call in (lambda: kvx.store_latent(s.pool, s.batch, row), lambda: kvx.load_latent(s.pool, s.batch, row),
+                     lambda: kvx.store_latent_rope(s.pool, s.batch, row),
+                     lambda: kvx.latent_attention(s.pool, s.batch, q, 4, 0.1, o),
+                     lambda: kvx.latent_extend_attention(s.pool, s.batch, qs, w, w, 0.1, os_)):
+            with pytest.raises(kvx.KvxError) as e:
+                call()
+            assert e.value.status == kvx.KVX_EUNSUPPORTED
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert (x == 2).all()
+
+
+def test_validation_names_bad_pages(setup, monkeypatch):
+    s = setup([40], [2], 256, False)
+    monkeypatch.setenv("KVX_VALIDATE", "1")
+    row = s.normal(2, 320)
+    kvx.store_latent(s.pool, s.batch, row)
+    for bad in (s.num_pages, -1):
+        s.pages[1] = bad
+        b = kvx.Batch(s.P, s.E, s.indptr, s.pages)
+        w, q = s.normal(4, 64, 256), s.normal(2, 4, 320)
+        for call in (lambda: kvx.store_latent(s.pool, b, row), lambda: kvx.load_latent(s.pool, b, row),
+                     lambda: kvx.store_latent_rope(s.pool, b, row),
+                     lambda: kvx.latent_attention(s.pool, b, q, 4, 0.1, q.clone()),
+                     lambda: kvx.latent_extend_attention(s.pool, b, q, w, w, 0.1, q.clone())):
+            with pytest.raises(kvx.KvxError) as e:
+                call()
+            assert e.value.status == kvx.KVX_ERANGE
+
+
+def test_pool_that_does_not_fit():
+    with pytest.raises(kvx.KvxError) as e:
+        kvx.latent_pool_create((1 << 31) - 1, 16, 512, 64, kvx.KVX_LATENT_BF16)  # 39 TB
+    assert e.value.status == kvx.KVX_ENOMEM
+    assert (torch.ones(8, device=DEV) + 1).sum().item() == 16  # the failure is not found by other calls
+
 # ------------------------------------------------------------------- together
 
 def test_turns_of_agents(setup):
