@@ -1,5 +1,7 @@
 // Products with the per-head weights of latent attention, gfx950: queries into the latent
 // space and sums out of it (absorbed form), cached rows to keys and values (expanded form).
+#include <cmath>
+
 #include "kvx_latent_tile.h"
 
 namespace kvx {
@@ -120,25 +122,27 @@ __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParam
 }
 
 // Keys and values of cached tokens: (tokens x latent) times (latent x 2 head_dim) per head.
-// Workgroup = 8 waves: 256 tokens against the columns of W_uk and W_uv of one head after the
-// other, 64 latent dims a step, both operands double-buffered in LDS so that the loads of a
-// step (those of the next head's first step too) arrive under the products of the one before.
-// Waves 2 i and 2 i + 1 take 64 tokens, one W_uk, the other W_uv.
+// Workgroup = 4 waves of 64 tokens each, whose latents stay in registers (the accumulator
+// half) while the weights of one head after the other, W_uk and W_uv in turn, come through
+// LDS: 128 latent dims of one of them a stage, three stages, so that a stage is loaded under
+// the products of the one before and operand reads run on across the border.
 //
-// LDS layout of a step: groups of 8 rows of 64 values, [8 rows][128 bytes] each, filled by one
-// wave-wide direct load; 16-byte chunk c of row r is stored at c ^ x(r), x from row bits 1 to 3
-// for tokens and 1, 2, 4 for weights: the rows that 16 lanes read together differ in those.
-constexpr int kExpThreads = 512;
-constexpr int kExpTok = kLatExpandTok;
+// LDS layout of a stage: for each 64 of its dims, groups of 8 weight rows, [8 rows][128 bytes]
+// each, filled by one wave-wide direct load; 16-byte chunk c of row r is stored at
+// c ^ wswz(r): the rows that 16 lanes read together differ in row bits 1, 2 and 4.
+constexpr int kExpStages = 3;
 __device__ __forceinline__ int wswz(int r) { return ((r >> 1) & 3) | ((r >> 2) & 4); }
 
 template <int LAT, int D, bool FP8>
-__global__ __launch_bounds__(kExpThreads, 1) void latent_expand_kernel(LatentExpandParams p) {
-  constexpr int MB = D / 32;               // 32-row blocks of a wave's weights
-  constexpr int STEPS = LAT / 64;
-  constexpr int A_BYTES = kExpTok * 128, W_BYTES = 2 * D * 128, STAGE = A_BYTES + W_BYTES;
-  constexpr int WG = 2 * D / 64;           // groups of 8 weight rows per wave
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
+__global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentExpandParams p) {
+  constexpr int MB = D / 32;        // 32-row blocks of a weight
+  constexpr int KS = LAT / 16;      // steps of 16 latent dims
+  constexpr int SK = 8;             // ... of a stage
+  constexpr int STEPS = KS / SK;    // stages of a weight
+  constexpr int N = SK * MB;        // operand reads of a stage
+  constexpr int AK = 6;             // reads ahead of their products
+  constexpr int STAGE = D * 256, PIECES = D / 16;  // bytes; loads of a wave
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kExpStages * STAGE];
   const LatentExpandUnit u = listed(p, p.units);
   const int head0 = blockIdx.y * p.heads_per, heads = p.heads - head0 < p.heads_per ? p.heads - head0 : p.heads_per;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -146,8 +150,24 @@ __global__ __launch_bounds__(kExpThreads, 1) void latent_expand_kernel(LatentExp
   const int32_t* ids = p.pool.page_ids + u.page_base;
   const int last = u.key_end - 1;
 
+  const int w_off = (lane >> 3) * (LAT * 2) + (((lane & 7) ^ ((lane >> 4) & 3)) << 4);
+  const uint32_t base = lds_address(lds);
+  const int total = heads * 2 * STEPS;
+  // stage i: head head0 + i / (2 STEPS), W_uk or W_uv, latent dims 128 (i % STEPS) ..
+  auto issue = [&](int i, uint32_t to) {
+    const int hd = head0 + i / (2 * STEPS);
+    const uint16_t* w = (i / STEPS & 1 ? p.w_uv : p.w_uk) + (size_t)hd * D * LAT + i % STEPS * 128;
+#pragma unroll
+    for (int j = 0; j < PIECES; j++) {
+      const int q = wave * PIECES + j, sub = q / (D / 8), gr = q % (D / 8);
+      lds_load_1k((const uint8_t*)(w + gr * 8 * LAT + sub * 64), w_off ^ ((gr >> 1) & 1) << 6, to + q * 1024);
+    }
+  };
+  issue(0, base);
+  issue(1, base + STAGE);
+
   if (p.rx != nullptr && blockIdx.y == 0) {
-    for (int i = tid; i < u.nrows * 8; i += kExpThreads) {
+    for (int i = tid; i < u.nrows * 8; i += kThreads) {
       const int r = i / 8, c = i % 8, key = u.key0 + r < last ? u.key0 + r : last;
       const uint8_t* page = p.pool.base + (int64_t)ids[key / kPageSize] * p.pool.page_bytes;
       const uint8_t* src = FP8 ? page + kPageSize * LAT + (key % kPageSize) * (2 * kLatRope)
@@ -156,112 +176,98 @@ __global__ __launch_bounds__(kExpThreads, 1) void latent_expand_kernel(LatentExp
     }
   }
 
-  // tokens: wave w stages rows 32 w .. 32 w + 31
-  const uint8_t* a_src[4];
-  uint4 codes[2];
-  uint8_t sc[2];
-  if constexpr (FP8) {
+  // Latents: 8 values of step ks are chunk 4 (ks / 2) + 2 h + ks % 2, so that a lane's values of
+  // two steps are side by side (16 codes of an 8-bit pool).
+  bf16x8 x[2][KS];
 #pragma unroll
-    for (int i = 0; i < 2; i++) {  // 16 codes a lane: row 32 wave + 16 i + lane / 4
-      const int r = u.key0 + wave * 32 + i * 16 + lane / 4, key = r < last ? r : last;
-      a_src[i] = p.pool.base + (int64_t)ids[key / kPageSize] * p.pool.page_bytes + (key % kPageSize) * LAT + (lane % 4) * 16;
-      const int slot = key % kPageSize;
-      a_src[2 + i] = a_src[i] - (slot * LAT + (lane % 4) * 16) + kPageSize * (LAT + 2 * kLatRope) + latent_scale_at(LAT, slot, 0);
-    }
-  } else {
+  for (int t = 0; t < 2; t++) {
+    const int r = u.key0 + wave * 64 + t * 32 + n, key = r < last ? r : last, slot = key % kPageSize;
+    const uint8_t* page = p.pool.base + (int64_t)ids[key / kPageSize] * p.pool.page_bytes;
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int r = u.key0 + wave * 32 + i * 8 + lane / 8, key = r < last ? r : last;
-      a_src[i] = p.pool.base + (int64_t)ids[key / kPageSize] * p.pool.page_bytes +
-                 (key % kPageSize) * (2 * (LAT + kLatRope)) + (((lane & 7) ^ swz(i * 8 + lane / 8)) << 4);
-    }
-  }
-  const int w_off = (lane >> 3) * (LAT * 2) + (((lane & 7) ^ ((lane >> 4) & 3)) << 4);
-  const uint32_t base = lds_address(lds);
-  // step i of the workgroup: head head0 + i / STEPS, latent dims 64 (i % STEPS) ..
-  auto issue = [&](int i) {
-    const int hd = head0 + i / STEPS, k0 = i % STEPS * 64;
-    const uint32_t at = base + (i & 1) * STAGE;
-    if constexpr (FP8) {
-#pragma unroll
-      for (int j = 0; j < 2; j++) {
-        codes[j] = *(const uint4*)(a_src[j] + k0);
-        sc[j] = a_src[2 + j][(k0 / 64 & 1) * (LAT / 64) + k0 / 128];
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; j++) lds_load_1k(a_src[j] + k0 * 2, at + (wave * 4 + j) * 1024);
-    }
-#pragma unroll
-    for (int j = 0; j < WG; j++) {
-      const int gr = wave * WG + j;  // rows 8 gr ..: W_uk's, then W_uv's
-      const uint16_t* w = gr * 8 < D ? p.w_uk + ((size_t)hd * D + gr * 8) * LAT : p.w_uv + ((size_t)hd * D + gr * 8 - D) * LAT;
-      lds_load_1k((const uint8_t*)(w + k0), w_off ^ ((gr >> 1) & 1) << 6, at + A_BYTES + gr * 1024);
-    }
-  };
-  auto finish = [&](int i) {
-    if constexpr (FP8) {
-      uint8_t* at = lds + (i & 1) * STAGE;
-#pragma unroll
-      for (int j = 0; j < 2; j++) {
-        const int r = wave * 32 + j * 16 + lane / 4, c = (lane % 4) * 2;
-        const float s = __uint_as_float((uint32_t)sc[j] << 23);
-        const uint32_t w[4] = {codes[j].x, codes[j].y, codes[j].z, codes[j].w};
+    for (int j = 0; j < KS / 2; j++) {
+      if constexpr (FP8) {
+        const uint4 codes = *(const uint4*)(page + slot * LAT + j * 32 + h * 16);
+        const uint8_t sc = page[kPageSize * (LAT + 2 * kLatRope) + latent_scale_at(LAT, slot, j / 2)];
+        const float s = __uint_as_float((uint32_t)sc << 23);
+        const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
         uint32_t y[8];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
           y[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], s, false));
           y[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], s, true));
         }
-        *(uint4*)(at + r * 128 + ((c ^ swz(r)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-        *(uint4*)(at + r * 128 + (((c + 1) ^ swz(r)) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+        x[t][2 * j] = __builtin_bit_cast(bf16x8, make_uint4(y[0], y[1], y[2], y[3]));
+        x[t][2 * j + 1] = __builtin_bit_cast(bf16x8, make_uint4(y[4], y[5], y[6], y[7]));
+      } else {
+        const uint4* src = (const uint4*)(page + slot * (2 * (LAT + kLatRope)) + j * 64 + h * 32);
+        x[t][2 * j] = __builtin_bit_cast(bf16x8, src[0]);
+        x[t][2 * j + 1] = __builtin_bit_cast(bf16x8, src[1]);
       }
     }
-  };
+  }
+#pragma unroll
+  for (int t = 0; t < 2; t++)
+#pragma unroll
+    for (int ks = 0; ks < KS; ks++) keep_in_acc(x[t][ks]);
 
-  const int rows0 = (wave >> 1) * 64, is_v = wave & 1;
   // Weight row of MFMA row m: lane (n, h) of the result then holds 16 values side by side.
   const int mw = (n & 3) | ((n & 4) << 2) | ((n >> 1) & 12);
-  uint32_t aat[4], wat[4];
+  uint32_t wat[4];
 #pragma unroll
   for (int ks = 0; ks < 4; ks++) {
-    aat[ks] = base + (rows0 + n) * 128 + (((2 * ks + h) ^ swz(n)) << 4);
-    wat[ks] = base + A_BYTES + (is_v * D + mw) * 128 + (((2 * ks + h) ^ wswz(mw)) << 4);
-    opaque(aat[ks]);
+    wat[ks] = base + mw * 128 + (((4 * (ks / 2) + 2 * h + ks % 2) ^ wswz(mw)) << 4);
     opaque(wat[ks]);
   }
-  f32x16 acc[MB][2];
-  const int steps = heads * STEPS;
-  issue(0);
-  finish(0);
-  for (int i = 0; i < steps; i++) {
-    if (i % STEPS == 0) {
+  bf16x8 ka[AK + 1];
+  auto read = [&](uint32_t st, int j) {  // 32-row block j % MB of step j / MB
+    const int ks = j / MB;
+    return read_b128(lds_at(wat[ks & 3] + st) + (ks >> 2) * (D * 128) + j % MB * 4096);
+  };
+  wait_vmcnt<0>();
+  __syncthreads();
 #pragma unroll
-      for (int b = 0; b < MB; b++) acc[b][0] = acc[b][1] = f32x16{};
+  for (int j = 0; j < AK; j++) ka[j] = read(0, j);
+  uint32_t st = 0;
+  int i = 0;
+  for (int hv = 0; hv < heads * 2; hv++) {
+    f32x16 acc[MB][2];
+#pragma unroll
+    for (int b = 0; b < MB; b++) acc[b][0] = acc[b][1] = f32x16{};
+#pragma unroll
+    for (int s = 0; s < STEPS; s++, i++) {
+      const uint32_t next = st == (kExpStages - 1) * STAGE ? 0 : st + STAGE;
+#pragma unroll
+      for (int j = 0; j < N; j++) {
+        const int at = s * N + j;
+        if (j == N - AK) {
+          // stage i + 1 is whole, and every wave is past stage i - 1, whose place i + 2 takes
+          __builtin_amdgcn_sched_barrier(0);
+          wait_vmcnt<0>();
+          __syncthreads();
+          if (i + 2 < total) issue(i + 2, base + (next == (kExpStages - 1) * STAGE ? 0 : next + STAGE));
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        ka[(at + AK) % (AK + 1)] = j + AK < N ? read(st, j + AK) : read(next, j + AK - N);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+          acc[j % MB][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[at % (AK + 1)], x[t][s * SK + j / MB],
+                                                                   acc[j % MB][t], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      st = next;
     }
-    wait_vmcnt<0>();
-    __syncthreads();  // the step is whole, and every wave has done with the one before
-    if (i + 1 < steps) issue(i + 1);
-    const uint32_t st = (i & 1) * STAGE;
+    // the next weight's first operands keep their places whatever STEPS N modulo AK + 1 is
+    bf16x8 keep[AK];
 #pragma unroll
-    for (int ks = 0; ks < 4; ks++) {
-      bf16x8 a[MB], x[2];
+    for (int j = 0; j < AK; j++) keep[j] = ka[(STEPS * N + j) % (AK + 1)];
 #pragma unroll
-      for (int b = 0; b < MB; b++) a[b] = read_b128(lds_at(wat[ks] + st) + b * 4096);
+    for (int j = 0; j < AK; j++) ka[j] = keep[j];
+    const int hd = head0 + hv / 2;
+    uint16_t* out = (hv & 1 ? p.vx : p.kx) + ((size_t)hd * p.x_rows + u.x_row + wave * 64 + n) * D + 16 * h;
+    if (wave * 64 < u.nrows) {  // uniform: rows come in multiples of 64
 #pragma unroll
-      for (int t = 0; t < 2; t++) x[t] = read_b128(lds_at(aat[ks] + st) + t * 4096);
-#pragma unroll
-      for (int b = 0; b < MB; b++)
-#pragma unroll
-        for (int t = 0; t < 2; t++) acc[b][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[b], x[t], acc[b][t], 0, 0, 0);
-    }
-    if (i + 1 < steps) finish(i + 1);
-    if (i % STEPS == STEPS - 1) {
-      const int hd = head0 + i / STEPS;
-      uint16_t* out = (is_v ? p.vx : p.kx) + ((size_t)hd * p.x_rows + u.x_row + rows0 + n) * D + 16 * h;
-#pragma unroll
-      for (int t = 0; t < 2; t++) {
-        if (rows0 + t * 32 >= u.nrows) continue;  // uniform: rows come in multiples of 64
+      for (int t = 0; t < 2; t++)
 #pragma unroll
         for (int b = 0; b < MB; b++) {
           uint32_t y[8];
@@ -271,7 +277,6 @@ __global__ __launch_bounds__(kExpThreads, 1) void latent_expand_kernel(LatentExp
           dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
           dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
         }
-      }
     }
   }
 }
@@ -308,17 +313,25 @@ hipError_t launch_latent_output(const LatentProjParams& p, int64_t n_rows, int l
 
 template <int LAT, int D>
 static void expand_by_type(const LatentExpandParams& p, dim3 grid, bool fp8, hipStream_t stream) {
-  if (fp8) hipLaunchKernelGGL((latent_expand_kernel<LAT, D, true>), grid, dim3(kExpThreads), 0, stream, p);
-  else hipLaunchKernelGGL((latent_expand_kernel<LAT, D, false>), grid, dim3(kExpThreads), 0, stream, p);
+  if (fp8) hipLaunchKernelGGL((latent_expand_kernel<LAT, D, true>), grid, dim3(kThreads), 0, stream, p);
+  else hipLaunchKernelGGL((latent_expand_kernel<LAT, D, false>), grid, dim3(kThreads), 0, stream, p);
 }
 
 hipError_t launch_latent_expand(const LatentExpandParams& p0, int64_t n_units, int latent_dim, int head_dim, bool fp8,
                                 hipStream_t stream) {
   if (n_units <= 0) return hipSuccess;
   LatentExpandParams p = p0;
-  // Heads per workgroup: as many as leave at least two workgroups per CU
-  p.heads_per = (int32_t)(n_units * p.heads / 512);
-  p.heads_per = p.heads_per < 1 ? 1 : (p.heads_per > p.heads ? p.heads : p.heads_per);
+  // Heads per workgroup: the number that ends first, where one workgroup a CU takes a head at
+  // a time and half a head's time to load its tokens
+  double least = HUGE_VAL;
+  for (int32_t per = 1; per <= p.heads; per++) {
+    const int64_t wgs = n_units * ((p.heads + per - 1) / per);
+    const double t = (double)((wgs + 255) / 256) * (per + 0.5);
+    if (t <= least) {
+      least = t;
+      p.heads_per = per;
+    }
+  }
   const dim3 grid((unsigned)n_units, (unsigned)((p.heads + p.heads_per - 1) / p.heads_per));
   if (latent_dim == 512) {
     if (head_dim == 128) expand_by_type<512, 128>(p, grid, fp8, stream);

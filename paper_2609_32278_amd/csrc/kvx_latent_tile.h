@@ -26,10 +26,6 @@ struct LatGeom {
   static constexpr int TILE = kLatTileKeys * ROWB;
 };
 
-// Stored chunk of chunk c of key row r: rows are 32 banks apart modulo 64, and this moves
-// the rows of an operand read (16 rows one chunk; 4 rows two chunks) to different banks.
-__device__ __forceinline__ int swz(int r) { return (r & 2) | (r & 4) | ((r >> 3) & 1); }
-
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   bf16x2 v;
   v[0] = (__bf16)a;

@@ -194,7 +194,7 @@ def _check(status: int, func: str):
 def _stream(stream):
     if stream is None:
         import torch
-        if torch.cuda.is_available() and torch.cuda.is_initialized():
+        if torch.cuda.is_initialized():
             return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
         return None
     if isinstance(stream, int):
@@ -246,7 +246,7 @@ class Batch:
 
     @property
     def total_extend(self) -> int:
-        return int(self.extend_lens.astype(np.int64).sum())
+        return int(self.extend_lens.sum(dtype=np.int64))
 
 
 # ------------------------------------------------------------------------ pool
