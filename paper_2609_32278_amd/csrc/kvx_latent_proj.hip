@@ -227,9 +227,20 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentExpand
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < AK; j++) ka[j] = read(0, j);
+  // Results are packed at the end of a weight and stored, a piece at a time, beside the first
+  // products of the next.
+  constexpr int STORES = 4 * MB;
+  const bool stores = wave * 64 < u.nrows;  // uniform: rows come in multiples of 64
+  uint32_t y[2][MB][8];
+  uint16_t* out = nullptr;
+  auto store = [&](int k) {
+    const int t = k / (2 * MB), b = k / 2 % MB, e = k % 2 * 4;
+    *(uint4*)(out + (size_t)t * 32 * D + b * 32 + e * 2) = make_uint4(y[t][b][e], y[t][b][e + 1], y[t][b][e + 2], y[t][b][e + 3]);
+  };
   uint32_t st = 0;
   int i = 0;
   for (int hv = 0; hv < heads * 2; hv++) {
+    const bool pending = hv > 0 && stores;
     f32x16 acc[MB][2];
 #pragma unroll
     for (int b = 0; b < MB; b++) acc[b][0] = acc[b][1] = f32x16{};
@@ -242,7 +253,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentExpand
         if (j == N - AK) {
           // stage i + 1 is whole, and every wave is past stage i - 1, whose place i + 2 takes
           __builtin_amdgcn_sched_barrier(0);
-          wait_vmcnt<0>();
+          if (s == 0 && pending) wait_vmcnt<STORES>();  // what is newer than the stage's loads
+          else wait_vmcnt<0>();
           __syncthreads();
           if (i + 2 < total) issue(i + 2, base + (next == (kExpStages - 1) * STAGE ? 0 : next + STAGE));
           __builtin_amdgcn_sched_barrier(0);
@@ -253,6 +265,11 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentExpand
         for (int t = 0; t < 2; t++)
           acc[j % MB][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[at % (AK + 1)], x[t][s * SK + j / MB],
                                                                    acc[j % MB][t], 0, 0, 0);
+        if (s == 0) {
+#pragma unroll
+          for (int k = 0; k < STORES; k++)
+            if (k * (N - AK) / STORES == j && pending) store(k);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
       st = next;
@@ -264,21 +281,20 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentExpand
 #pragma unroll
     for (int j = 0; j < AK; j++) ka[j] = keep[j];
     const int hd = head0 + hv / 2;
-    uint16_t* out = (hv & 1 ? p.vx : p.kx) + ((size_t)hd * p.x_rows + u.x_row + wave * 64 + n) * D + 16 * h;
-    if (wave * 64 < u.nrows) {  // uniform: rows come in multiples of 64
+    out = (hv & 1 ? p.vx : p.kx) + ((size_t)hd * p.x_rows + u.x_row + wave * 64 + n) * D + 16 * h;
 #pragma unroll
-      for (int t = 0; t < 2; t++)
+    for (int t = 0; t < 2; t++)
 #pragma unroll
-        for (int b = 0; b < MB; b++) {
-          uint32_t y[8];
+      for (int b = 0; b < MB; b++)
 #pragma unroll
-          for (int e = 0; e < 8; e++) y[e] = pack_bf16(acc[b][t][2 * e], acc[b][t][2 * e + 1]);
-          uint4* dst = (uint4*)(out + (size_t)t * 32 * D + b * 32);
-          dst[0] = make_uint4(y[0], y[1], y[2], y[3]);
-          dst[1] = make_uint4(y[4], y[5], y[6], y[7]);
+        for (int e = 0; e < 8; e++) {
+          y[t][b][e] = pack_bf16(acc[b][t][2 * e], acc[b][t][2 * e + 1]);
+          formed(y[t][b][e]);
         }
-    }
   }
+  if (stores)
+#pragma unroll
+    for (int k = 0; k < STORES; k++) store(k);
 }
 
 }  // namespace
