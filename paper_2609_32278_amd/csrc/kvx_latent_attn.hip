@@ -1,4 +1,27 @@
 // Attention of (suffix token, head) rows to the latent cache entries themselves, gfx950.
+//
+//   o = sum_j w_j c_j / sum_j w_j,   w_j = exp(scale * q . (c_j, r_j)),
+// one pass over the keys with float32 scores, sums and reference points.  All heads of a token
+// see the same entries, so rows of any head and suffix token of a request share a tile of keys:
+// a row costs 2 (2 latent_dim + 64) operations a key, a key 2 (latent_dim + 64) bytes for all
+// rows (latent_dim + 128 and scales, 8-bit).
+//
+// Rows.  A unit holds 16, 32 or 64 rows, by the most that a request has: few rows are bound by
+// HBM, and fewer of them leave registers for more reads ahead; many by the matrix unit and by
+// LDS, from which each product's operands come once a wave.  A decode batch of 128 requests on
+// 16 heads: 339 us with 16 rows, 5.5 TB/s (3.7 TB/s is what a plain reduction of a large buffer
+// reaches here).  64 rows at latent_dim 512: the products of 64 keys are 2176 cycles of the
+// matrix unit, measured 3.9k a step (8-bit: 5k, with its conversions), 0.9 to 1.2 PFLOP/s by
+// how evenly a batch fills the CUs; a large library product reaches 1.2 to 1.3.
+//
+// Waves.  In the value product each of the 4 waves has a quarter of the latent dims and all rows.
+// In the score product it has a quarter of the keys and all rows, or, of 64 rows, half of the
+// keys and half of the rows: its queries then fit the register file (288 registers otherwise;
+// drafts of 32 requests on 64 heads 178 us against 194 with a quarter of the keys and the weights
+// formed after the products).
+//
+// Roundings: softmax weights to bf16, the operands the matrix unit takes (half a step, 2^-8, of
+// each weight; their sum adds the float32 weights); the result to bf16.
 #include <type_traits>
 
 #include "kvx_latent_tile.h"
@@ -479,7 +502,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
     wait_vmcnt<0>();
     __syncthreads();
   };
-  // With the fixed reference bf16 weights and float32 sums keep their relative precision for
+  // A reference that moves with every tile costs two barriers a tile (64-row units: 0.4k of 3.9k
+  // cycles).  With the fixed reference bf16 weights and float32 sums keep their relative precision for
   // scores far above it, unless an exponential or a sum overflows: then the keys are gone
   // over again with a reference that moves.
   run(std::true_type{});
@@ -536,7 +560,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   }
 }
 
-// Log-sum-exp combination of a tile's parts.  Workgroup (merge, row block, 16-dim block of
+// Log-sum-exp combination of a tile's parts, sums already divided by their totals: latency-bound
+// (5 to 17 us).  Workgroup (merge, row block, 16-dim block of
 // the latent): 64 lanes hold its 4 sums of 16 rows each; the four waves take every fourth
 // part, eight of them in flight, and add up through LDS.
 template <int LAT, int RB, class Plan>

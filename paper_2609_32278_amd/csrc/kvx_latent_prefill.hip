@@ -1,4 +1,16 @@
 // Attention of per-head queries to expanded keys and values, gfx950.
+//
+//   o = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale * q . (k_j, r_j)),
+// 2 (2 head_dim + 64) operations a visible pair: bound by the matrix unit.  A workgroup takes 256
+// tokens of one head, 64 a wave, so that an operand read from LDS feeds two products of 32 x 32;
+// queries sit in the accumulator half of the register file, and keys and values of 64 tokens come
+// through three LDS stages by direct loads.  The exponentials (as long as a third of the products)
+// are formed between the products of the next 32 keys, the loads issued one at a time among them:
+// apart they took 40% longer.  Measured: 8001 tokens of 128 heads in 2.4 ms, 1.1 PFLOP/s, the
+// matrix unit busy 64 to 68% of the cycles at the 2.0 GHz that the power limit leaves.
+//
+// Roundings: expanded keys and values to bf16 (the products' operands), weights to bf16, the result
+// to bf16; scores, sums and reference points are float32.
 #include <type_traits>
 
 #include "kvx_latent_tile.h"
@@ -319,7 +331,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
   }
 }
 
-// Workgroup (merge, 16 tokens): D / 8 lanes of 8 values per token.
+// Log-sum-exp combination of a tile's parts; each is read once (25 us for 16 turns of 16 heads).
+// Workgroup (merge, 16 or 32 tokens): D / 8 lanes of 8 values per token.
 template <int D>
 __global__ __launch_bounds__(kThreads) void latent_tile_merge_kernel(LatentTileMergeParams p) {
   constexpr int LPT = D / 8, TPW = kThreads / LPT;

@@ -1,5 +1,6 @@
 // Products with the per-head weights of latent attention, gfx950: queries into the latent
 // space and sums out of it (absorbed form), cached rows to keys and values (expanded form).
+// Operands are bf16, sums float32, each result is rounded once: to bf16, the operand of what follows.
 #include <cmath>
 
 #include "kvx_latent_tile.h"
@@ -11,7 +12,9 @@ constexpr int kThreads = 256;
 constexpr int kSlice = 128;  // latent dims per workgroup of the query product
 
 // q' = W_uk^T q, as (W_uk^T) q^T: W's rows run along the latent dims, so its operand is read
-// transposed from LDS.  Workgroup: 64 tokens, one head, 128 latent dims.
+// transposed from LDS.  Workgroup: 64 tokens, one head, 128 latent dims.  Bound by what it
+// writes, (latent_dim + 64) / (head_dim + 64) times what it reads: 900 tokens of 32 heads 30 us
+// (44 MB; 37 with results of 8 bytes a lane and loads of queries behind the barrier).
 template <int LAT, int D>
 __global__ __launch_bounds__(kThreads) void latent_absorb_kernel(LatentProjParams p) {
   constexpr int IN = D + kLatRope, OUT = LAT + kLatRope;
@@ -21,20 +24,31 @@ __global__ __launch_bounds__(kThreads) void latent_absorb_kernel(LatentProjParam
   const int hd = blockIdx.y, s0 = blockIdx.z * kSlice;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
   const uint16_t* w = p.w + (size_t)hd * D * LAT + s0;
-  for (int i = tid; i < D * (kSlice / 8); i += kThreads) {
-    const int k = i / (kSlice / 8), c = i % (kSlice / 8);
-    *(uint4*)(wl + k * WB + c * 16) = *(const uint4*)(w + (size_t)k * LAT + c * 8);
+  constexpr int WL = D * (kSlice / 8) / kThreads;
+  uint4 wr[WL];
+#pragma unroll
+  for (int j = 0; j < WL; j++) {
+    const int i = j * kThreads + tid;
+    wr[j] = *(const uint4*)(w + (size_t)(i / (kSlice / 8)) * LAT + i % (kSlice / 8) * 8);
+  }
+  const uint16_t* q[4];
+  bf16x8 x[4][D / 32];  // all on their way before the first is used
+#pragma unroll
+  for (int tb = 0; tb < 4; tb++) {
+    const int t = tb * 16 + n;
+    q[tb] = p.in + ((size_t)(rows.row0 + (t < rows.ntok ? t : 0)) * p.num_q_heads + hd) * IN;
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ks++) x[tb][ks] = *(const bf16x8*)(q[tb] + ks * 32 + 8 * g);
+  }
+#pragma unroll
+  for (int j = 0; j < WL; j++) {
+    const int i = j * kThreads + tid;
+    *(uint4*)(wl + i / (kSlice / 8) * WB + i % (kSlice / 8) * 16) = wr[j];
   }
   __syncthreads();
   f32x4 acc[4][2];
 #pragma unroll
   for (int tb = 0; tb < 4; tb++) acc[tb][0] = acc[tb][1] = f32x4{};
-  const uint16_t* q[4];
-#pragma unroll
-  for (int tb = 0; tb < 4; tb++) {
-    const int t = tb * 16 + n;
-    q[tb] = p.in + ((size_t)(rows.row0 + (t < rows.ntok ? t : 0)) * p.num_q_heads + hd) * IN;
-  }
 #pragma unroll
   for (int ks = 0; ks < D / 32; ks++) {
     bf16x8 a[2];
@@ -43,28 +57,24 @@ __global__ __launch_bounds__(kThreads) void latent_absorb_kernel(LatentProjParam
       s16x4 h[2];
 #pragma unroll
       for (int e = 0; e < 2; e++)
-        h[e] = read_tr(wl + (ks * 32 + 8 * g + 4 * e + n / 4) * WB + (wave * 32 + b * 16) * 2 + (n % 4) * 8);
+        h[e] = read_tr(wl + (ks * 32 + 8 * g + 4 * e + n / 4) * WB + (wave * 32 + (n % 4) * 8 + b * 4) * 2);
       a[b] = join(h[0], h[1]);
     }
 #pragma unroll
-    for (int tb = 0; tb < 4; tb++) {
-      const bf16x8 x = *(const bf16x8*)(q[tb] + ks * 32 + 8 * g);
+    for (int tb = 0; tb < 4; tb++)
 #pragma unroll
-      for (int b = 0; b < 2; b++) acc[tb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[b], x, acc[tb][b], 0, 0, 0);
-    }
+      for (int b = 0; b < 2; b++)
+        acc[tb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[b], x[tb][ks], acc[tb][b], 0, 0, 0);
   }
 #pragma unroll
   for (int tb = 0; tb < 4; tb++) {
     const int t = tb * 16 + n;
     if (t >= rows.ntok) continue;
     uint16_t* dst = p.out + ((size_t)(rows.own0 + t) * p.num_q_heads + hd) * OUT;
-#pragma unroll
-    for (int b = 0; b < 2; b++) {
-      uint2 y;
-      y.x = pack_bf16(acc[tb][b][0], acc[tb][b][1]);
-      y.y = pack_bf16(acc[tb][b][2], acc[tb][b][3]);
-      *(uint2*)(dst + s0 + wave * 32 + b * 16 + 4 * g) = y;
-    }
+    // the columns were read so that a lane's two blocks are 8 dims side by side
+    *(uint4*)(dst + s0 + wave * 32 + 8 * g) =
+        make_uint4(pack_bf16(acc[tb][0][0], acc[tb][0][1]), pack_bf16(acc[tb][0][2], acc[tb][0][3]),
+                   pack_bf16(acc[tb][1][0], acc[tb][1][1]), pack_bf16(acc[tb][1][2], acc[tb][1][3]));
     if (blockIdx.z == 0) {  // the rotated dims follow: 8 chunks, two of them per (wave, g) of waves 0
       if (wave == 0) {
 #pragma unroll
@@ -75,14 +85,15 @@ __global__ __launch_bounds__(kThreads) void latent_absorb_kernel(LatentProjParam
 }
 
 // o = W_uv (sum), as W_uv o^T; both operands run along the latent dims.  Workgroup: 64
-// tokens, one head.
+// tokens, one head.  Bound by reading the sums: 900 tokens of 32 heads 28 us.
 template <int LAT, int D>
 __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParams p) {
   constexpr int NB = D / 64;  // 16-row blocks of W per wave
   const LatentRows rows = listed(p, p.rows);
   const int hd = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
-  const uint16_t* w = p.w + ((size_t)hd * D + wave * (D / 4) + n) * LAT + 8 * g;
+  // rows of W so that a lane's results are 4 NB dims side by side
+  const uint16_t* w = p.w + ((size_t)hd * D + wave * (D / 4) + n / 4 * (4 * NB) + n % 4) * LAT + 8 * g;
   const uint16_t* x[4];
   f32x4 acc[4][NB];
 #pragma unroll
@@ -92,11 +103,11 @@ __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParam
 #pragma unroll
     for (int b = 0; b < NB; b++) acc[tb][b] = f32x4{};
   }
-#pragma unroll 4
+#pragma unroll 8
   for (int ks = 0; ks < LAT / 32; ks++) {
     bf16x8 a[NB];
 #pragma unroll
-    for (int b = 0; b < NB; b++) a[b] = *(const bf16x8*)(w + (size_t)b * 16 * LAT + ks * 32);
+    for (int b = 0; b < NB; b++) a[b] = *(const bf16x8*)(w + b * 4 * LAT + ks * 32);
 #pragma unroll
     for (int tb = 0; tb < 4; tb++) {
       const bf16x8 y = *(const bf16x8*)(x[tb] + ks * 32);
@@ -108,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParam
   for (int tb = 0; tb < 4; tb++) {
     const int t = tb * 16 + n;
     if (t >= rows.ntok) continue;
-    uint16_t* dst = p.out + ((size_t)(rows.row0 + t) * p.num_q_heads + hd) * D + wave * (D / 4) + 4 * g;
+    uint16_t* dst = p.out + ((size_t)(rows.row0 + t) * p.num_q_heads + hd) * D + wave * (D / 4) + 4 * NB * g;
     if (p.lse_out != nullptr && wave == 0 && g == 0)
       p.lse_out[(size_t)(rows.row0 + t) * p.num_q_heads + hd] = p.lse_in[(size_t)(rows.own0 + t) * p.num_q_heads + hd];
 #pragma unroll
@@ -116,7 +127,7 @@ __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParam
       uint2 y;
       y.x = pack_bf16(acc[tb][b][0], acc[tb][b][1]);
       y.y = pack_bf16(acc[tb][b][2], acc[tb][b][3]);
-      *(uint2*)(dst + b * 16) = y;
+      *(uint2*)(dst + b * 4) = y;
     }
   }
 }
@@ -125,7 +136,11 @@ __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParam
 // Workgroup = 4 waves of 64 tokens each, whose latents stay in registers (the accumulator
 // half) while the weights of one head after the other, W_uk and W_uv in turn, come through
 // LDS: 128 latent dims of one of them a stage, three stages, so that a stage is loaded under
-// the products of the one before and operand reads run on across the border.
+// the products of the one before and operand reads run on across the border.  A wave's results
+// are 32 x 32 blocks, four of a weight's rows by two of tokens: each operand read feeds two
+// products, half of what LDS can deliver (tokens through LDS as well, shared by two waves: reads
+// at the rate of the products, 1260 us where this takes 1071).  Bound by the matrix unit: 246k
+// tokens x 16 heads at 0.96 PFLOP/s.
 //
 // LDS layout of a stage: for each 64 of its dims, groups of 8 weight rows, [8 rows][128 bytes]
 // each, filled by one wave-wide direct load; 16-byte chunk c of row r is stored at
