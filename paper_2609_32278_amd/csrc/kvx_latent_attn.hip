@@ -502,8 +502,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
     wait_vmcnt<0>();
     __syncthreads();
   };
-  // A reference that moves with every tile costs two barriers a tile (64-row units: 0.4k of 3.9k
-  // cycles).  With the fixed reference bf16 weights and float32 sums keep their relative precision for
+  // A reference that moves with every tile would cost two more barriers and a rescaling of every
+  // sum a tile.  With the fixed reference bf16 weights and float32 sums keep their relative precision for
   // scores far above it, unless an exponential or a sum overflows: then the keys are gone
   // over again with a reference that moves.
   run(std::true_type{});

@@ -443,6 +443,10 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
                    int32_t split_keys, AbsorbedPlan& plan) {
   int64_t most = 0;
   for (const Member& m : members) most = std::max<int64_t>(most, (int64_t)b->extend_lens[m.req] * Hq);
+  // Rows of a unit, as many as the request with the most rows fills.  With 16, 32 and 64 rows:
+  // 128 requests of one token, 4k to 32k keys, 16 heads 481, 491, 515 us; 32 heads 527, 510, 535
+  // (8 bits 337, 342, 460); 4 such requests of 16 heads 18.6, 20.8, 23.4; 32 of 24 heads 44.5,
+  // 44.2, 47.2.  Requests of many rows read their keys once a unit.
   plan.row_blocks = most <= 16 ? 1 : (most <= 32 ? 2 : 4);
   const int64_t M = 16 * plan.row_blocks;
   std::vector<Span> spans;

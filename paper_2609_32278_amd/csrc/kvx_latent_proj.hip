@@ -135,17 +135,17 @@ __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParam
 // Keys and values of cached tokens: (tokens x latent) times (latent x 2 head_dim) per head.
 // Workgroup = 4 waves of 64 tokens each, whose latents stay in registers (the accumulator
 // half) while the weights of one head after the other, W_uk and W_uv in turn, come through
-// LDS: 128 latent dims of one of them a stage, three stages, so that a stage is loaded under
-// the products of the one before and operand reads run on across the border.  A wave's results
+// LDS: 128 latent dims of one of them a stage, four stages, so that a stage is loaded under
+// the products of the two before and operand reads run on across the border.  A wave's results
 // are 32 x 32 blocks, four of a weight's rows by two of tokens: each operand read feeds two
 // products, half of what LDS can deliver (tokens through LDS as well, shared by two waves: reads
-// at the rate of the products, 1260 us where this takes 1071).  Bound by the matrix unit: 246k
-// tokens x 16 heads at 0.96 PFLOP/s.
+// at the rate of the products, 1260 us where this takes 1044; three
+// stages 1071).  Bound by the matrix unit: 246k tokens x 16 heads at 0.99 PFLOP/s.
 //
 // LDS layout of a stage: for each 64 of its dims, groups of 8 weight rows, [8 rows][128 bytes]
 // each, filled by one wave-wide direct load; 16-byte chunk c of row r is stored at
 // c ^ wswz(r): the rows that 16 lanes read together differ in row bits 1, 2 and 4.
-constexpr int kExpStages = 3;
+constexpr int kExpStages = 4;
 __device__ __forceinline__ int wswz(int r) { return ((r >> 1) & 3) | ((r >> 2) & 4); }
 
 template <int LAT, int D, bool FP8>
@@ -180,6 +180,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentExpand
   };
   issue(0, base);
   issue(1, base + STAGE);
+  issue(2, base + 2 * STAGE);
 
   if (p.rx != nullptr && blockIdx.y == 0) {
     for (int i = tid; i < u.nrows * 8; i += kThreads) {
@@ -266,12 +267,14 @@ __global__ __launch_bounds__(kThreads, 1) void latent_expand_kernel(LatentExpand
       for (int j = 0; j < N; j++) {
         const int at = s * N + j;
         if (j == N - AK) {
-          // stage i + 1 is whole, and every wave is past stage i - 1, whose place i + 2 takes
+          // Stage i + 1 is whole, and every wave is past stage i - 1, whose place i + 3 takes.
+          // Newer than its loads are those of stage i + 2 and the stores since.
           __builtin_amdgcn_sched_barrier(0);
-          if (s == 0 && pending) wait_vmcnt<STORES>();  // what is newer than the stage's loads
-          else wait_vmcnt<0>();
+          if (i + 2 >= total) wait_vmcnt<0>();
+          else if (s < 2 && pending) wait_vmcnt<PIECES + STORES>();
+          else wait_vmcnt<PIECES>();
           __syncthreads();
-          if (i + 2 < total) issue(i + 2, base + (next == (kExpStages - 1) * STAGE ? 0 : next + STAGE));
+          if (i + 3 < total) issue(i + 3, base + (st == 0 ? (kExpStages - 1) * STAGE : st - STAGE));
           __builtin_amdgcn_sched_barrier(0);
         }
         ka[(at + AK) % (AK + 1)] = j + AK < N ? read(st, j + AK) : read(next, j + AK - N);
