@@ -642,3 +642,48 @@ def test_turns_of_agents(setup):
                                   v_err=ref.HALF_BF16)
         g = ref.f64(got[base[i]:base[i + 1]])
         assert np.linalg.norm(g - o) <= RMS_EXTEND * np.linalg.norm(o)
+
+
+def test_agents_through_the_prefix_cache():
+    """Agents whose histories the round-robin prefix cache keeps in a latent pool that is too small
+    for all: prefixes that stayed are attended where they lie, what was evicted is stored again."""
+    lat, hd, heads, num_pages = 256, 64, 3, 60
+    pool = kvx.latent_pool_create(num_pages, 16, lat, 64, kvx.KVX_LATENT_FP8)
+    cache = kvx.kvx_cache_create(num_pages, 16, 64, kvx.KVX_EVICT_RR)
+    g = torch.Generator(DEV).manual_seed(11)
+    rng = np.random.default_rng(11)
+    kv = [torch.randn(600, lat + 64, device=DEV, generator=g, dtype=BF16) for _ in range(4)]
+    w_uk, w_uv = (torch.randn(heads, hd, lat, device=DEV, generator=g, dtype=BF16) / 16 for _ in range(2))
+    uk, uv, scale = ref.f64(w_uk), ref.f64(w_uv), (hd + 64) ** -0.5
+    lens, reused, missed = [0] * 4, 0, 0
+    try:
+        for turn in range(5):
+            for agent in range(4):
+                before = lens[agent]
+                lens[agent] += int(rng.integers(40, 110))
+                prefix, table = kvx.kvx_cache_begin_turn(cache, agent, lens[agent])
+                reused, missed = reused + prefix, missed + before - min(prefix, before)
+                e = lens[agent] - prefix
+                b = kvx.Batch([prefix], [e], [0, len(table)], torch.from_numpy(table).to(DEV))
+                q = torch.randn(e, heads, hd + 64, device=DEV, generator=g, dtype=BF16)
+                out = torch.empty(e, heads, hd, dtype=BF16, device=DEV)
+                turned = torch.empty_like(q)
+                kvx.store_latent_rope(pool, b, kv[agent][prefix:lens[agent]], q=q, num_q_heads=heads, q_out=turned)
+                kvx.latent_extend_attention(pool, b, turned, w_uk, w_uv, scale, out)
+                kvx.kvx_cache_end_turn(cache, agent)
+                # the whole history from its own rows, not from the pool
+                x, pos = ref.f64(kv[agent][:lens[agent]]), np.arange(lens[agent])
+                freqs = 10000.0 ** (-2.0 * np.arange(32) / 64)
+                c = ref.quantised(x[:, :lat])
+                r = ref.rotated(x[:, lat:], pos, freqs, 0)
+                k = np.concatenate([np.einsum("hdl,jl->hjd", uk, c), np.broadcast_to(r, (heads,) + r.shape)], -1)
+                qr = ref.f64(q)
+                qr[..., hd:] = ref.rotated(qr[..., hd:], pos[prefix:], freqs, 0)
+                o, _, _, _ = ref.attend(qr, k, np.einsum("hdl,jl->hjd", uv, c), prefix, scale)
+                # RMS_EXTEND's four roundings and those of the rotated halves of keys and queries
+                assert np.linalg.norm(ref.f64(out) - o) <= RMS_EXTEND * math.sqrt(6 / 4) * np.linalg.norm(o), (turn, agent)
+        assert reused > 0 and missed > 0
+    finally:
+        torch.cuda.synchronize()
+        kvx.kvx_cache_destroy(cache)
+        kvx.latent_pool_destroy(pool)

@@ -73,3 +73,18 @@ def test_absent_pool_is_reported():
         with pytest.raises(kvx.KvxError) as e:
             call()
         assert e.value.status == kvx.KVX_EINVAL and "NULL" in kvx.kvx_last_error()
+
+
+def test_header_is_c(tmp_path):
+    if shutil.which("gcc") is None:
+        pytest.skip("gcc not installed")
+    src = tmp_path / "user.c"
+    src.write_text('#include "kvx_latent.h"\n'
+                   "int use(kvx_latent_pool *p, const kvx_batch *b, const kvx_latent_proj *w, void *x) {\n"
+                   "    kvx_latent_layout l;\n"
+                   "    return latent_pool_layout(p, &l) + store_latent(p, b, x, 576, 0) +\n"
+                   "           latent_extend_attention(p, b, w, x, 0.1f, x, 0, KVX_LATENT_AUTO, 0);\n"
+                   "}\n")
+    r = subprocess.run(["gcc", "-std=c99", "-pedantic", "-Wall", "-Wextra", "-Werror", "-fsyntax-only",
+                        "-I" + os.path.join(ROOT, "include"), str(src)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
