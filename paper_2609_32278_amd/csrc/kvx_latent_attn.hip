@@ -11,14 +11,15 @@
 // LDS, from which each product's operands come once a wave.  A decode batch of 128 requests on
 // 16 heads: 339 us with 16 rows, 5.5 TB/s (3.7 TB/s is what a plain reduction of a large buffer
 // reaches here).  64 rows at latent_dim 512: the products of 64 keys are 2176 cycles of the
-// matrix unit, measured 3.9k a step (8-bit: 5k, with its conversions), 0.9 to 1.2 PFLOP/s by
+// matrix unit, measured 3.8k a step (8-bit: 5k, with its conversions), 0.9 to 1.2 PFLOP/s by
 // how evenly a batch fills the CUs; a large library product reaches 1.2 to 1.3.
 //
 // Waves.  In the value product each of the 4 waves has a quarter of the latent dims and all rows.
 // In the score product it has a quarter of the keys and all rows, or, of 64 rows, half of the
 // keys and half of the rows: its queries then fit the register file (288 registers otherwise;
-// drafts of 32 requests on 64 heads 178 us against 194 with a quarter of the keys and the weights
-// formed after the products).
+// a quarter of the keys and all rows, half of the reads from LDS but the weights formed apart from
+// the products, is as fast on bf16 pools: drafts of 32 requests on 64 heads 176 and 174 us, short
+// turns 667 and 675).
 //
 // Roundings: softmax weights to bf16, the operands the matrix unit takes (half a step, 2^-8, of
 // each weight; their sum adds the float32 weights); the result to bf16.
@@ -45,35 +46,38 @@ struct TileAt {
   __device__ static int chunk(int r, int c) { return row(r) + (c >> 3) * 1024 + (((c & 7) ^ order(r)) << 4); }
 };
 
-// How a wave brings its page of a 64-key tile to LDS.  Tokens at or past key_end become token
-// `safe`; a tile past the last is that token throughout.  Loads and writes are made one by one
-// among the products of the tile before: a burst of them stalls the wave (18 loads of 1 KiB
-// took 1.8k cycles of a step's 5.5k).
+// How a wave brings its page of a 64-key tile to LDS.  Tokens at or past key_end become the
+// last one before it in the page (or, in a page past the last, the last of all).  Loads and
+// writes are made one by one among the products of the tile before: a burst of them stalls the
+// wave (18 loads of 1 KiB took 1.8k cycles of a step's 5.5k).
 template <int LAT>
 struct Pages {
   const uint8_t* base;
   const_i32_ptr ids;
   int64_t page_bytes;
-  int key_end, safe, lane, wave;
-  const uint8_t* safe_page;
-  uint32_t page;  // of the next tile: read at the end of a step, as a scalar load under way
-                  // would make every wait for LDS a full drain
+  int key_end, lane, wave;
+  uint32_t page;       // of the next tile: read at the end of a step, as a scalar load under way
+                       // would make every wait for LDS a full drain
+  const uint8_t* src;  // the page that is being loaded
 
   __device__ __forceinline__ uint32_t page_at(int k0) const {
     const int lp = k0 / kPageSize + wave, last = (key_end - 1) / kPageSize;
     return (uint32_t)ids[lp < last ? lp : last];
   }
-  __device__ __forceinline__ void init(const LatentAttnParams& p, const LatentUnit& u, int safe_key, int l, int w) {
+  __device__ __forceinline__ void init(const LatentAttnParams& p, const LatentUnit& u, int l, int w) {
     base = p.pool.base;
     ids = (const_i32_ptr)(p.pool.page_ids + u.page_base);
     page_bytes = p.pool.page_bytes;
     key_end = u.key_end;
-    safe = safe_key;
     lane = l;
     wave = w;
-    safe_page = address((uint32_t)ids[safe / kPageSize]);
   }
-  __device__ __forceinline__ const uint8_t* address(uint32_t pg) const { return base + (uint64_t)pg * page_bytes; }
+  // the page of tile k0, and its last slot that is read
+  __device__ __forceinline__ int enter(int k0) {
+    src = base + (uint64_t)page * page_bytes;
+    const int left = key_end - k0 - wave * kPageSize;
+    return left >= kPageSize ? kPageSize - 1 : (left > 0 ? left - 1 : (key_end - 1) % kPageSize);
+  }
 };
 
 template <int LAT, bool FP8>
@@ -84,21 +88,19 @@ struct Loader<LAT, false> : Pages<LAT> {
   using G = LatGeom<LAT>;
   using P = Pages<LAT>;
   static constexpr int BLOCKS = G::ROWB / 128, LOADS = 2 * BLOCKS;
-  const uint8_t* from[2];  // of this lane in each half
+  int from[2];  // of this lane in each half of the page
   uint32_t to;
 
   __device__ __forceinline__ void begin(uint32_t tile, int k0) {
-    const uint8_t* src = P::address(P::page);
-    const uint8_t* alt = P::safe_page + (P::safe % kPageSize) * G::ROWB;
-    const int left = P::key_end - k0 - P::wave * kPageSize;  // rows of this page that exist
+    const int last = P::enter(k0);
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int row = 8 * h + (P::lane >> 3), c = ((P::lane & 7) ^ TileAt<LAT>::order(row)) << 4;
-      from[h] = (row < left ? src + row * G::ROWB : alt) + c;
+      from[h] = (row < last ? row : last) * G::ROWB + c;
     }
     to = tile + P::wave * (16 * G::ROWB);
   }
-  __device__ __forceinline__ void issue(int i) { lds_load_1k(from[i / BLOCKS] + i % BLOCKS * 128, to + i * 1024); }
+  __device__ __forceinline__ void issue(int i) { lds_load_1k(P::src + i % BLOCKS * 128, from[i / BLOCKS], to + i * 1024); }
 };
 
 // An 8-bit page comes through registers, 16 codes a lane and load, and is written to LDS as
@@ -114,45 +116,43 @@ struct Loader<LAT, true> : Pages<LAT> {
   using P = Pages<LAT>;
   static constexpr int CODES = LAT / 64, PER = LAT / 128;  // loads of codes: of a page, of 8 slots
   static constexpr int LOADS = CODES + 2;
-  const uint8_t* from[2];  // codes of this lane's slot in each half
-  const uint8_t* key[2];
+  uint32_t from[2];  // codes of this lane's slot in each half
+  uint32_t key[2];
   uint4 data[LOADS];
   uint64_t scales, scales_next;  // CODES bytes, one per load
   uint32_t at, key_at;           // this lane's first chunk, and its chunk of the key, in the first half
   uint32_t to;
 
   __device__ __forceinline__ int sub() const { return ((P::lane >> 3) & 3) | (P::lane & 4); }
-  __device__ __forceinline__ void init(const LatentAttnParams& p, const LatentUnit& u, int safe_key, int l, int w) {
-    P::init(p, u, safe_key, l, w);
+  __device__ __forceinline__ void init(const LatentAttnParams& p, const LatentUnit& u, int l, int w) {
+    P::init(p, u, l, w);
     at = w * (16 * G::ROWB) + TileAt<LAT>::chunk(sub(), 2 * (l & 3)) + (l >> 5) * 1024;
     key_at = w * (16 * G::ROWB) + TileAt<LAT>::chunk(l >> 3, LAT / 8 + (l & 7));
   }
   __device__ __forceinline__ void begin(uint32_t tile, int k0) {  // `tile` is where finish() writes meanwhile
     constexpr int SC = kPageSize * (LAT + 2 * kLatRope);
-    const uint8_t* src = P::address(P::page);
-    const uint8_t* alt = P::safe_page;
-    const int left = P::key_end - k0 - P::wave * kPageSize, ss = P::safe % kPageSize;
+    const int last = P::enter(k0);
     const int c = (P::lane >> 5) * 4 + (P::lane & 3);
-    const uint8_t* sc = src + SC + latent_scale_at(LAT, sub(), P::lane >> 5);
+    const uint8_t* sc = P::src + (uint32_t)(SC + latent_scale_at(LAT, sub(), P::lane >> 5));
     if constexpr (CODES == 8) scales_next = *(const uint64_t*)sc;
     else scales_next = *(const uint32_t*)sc;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int slot = 8 * h + sub(), ks = 8 * h + (P::lane >> 3);
-      from[h] = (slot < left ? src + slot * LAT : alt + ss * LAT) + c * 16;
-      key[h] = (ks < left ? src + ks * 128 : alt + ss * 128) + kPageSize * LAT + (P::lane & 7) * 16;
+      from[h] = (slot < last ? slot : last) * LAT + c * 16;
+      key[h] = kPageSize * LAT + (ks < last ? ks : last) * 128 + (P::lane & 7) * 16;
     }
-    if (left < kPageSize) {  // uniform
+    if (last < kPageSize - 1) {  // uniform
 #pragma unroll
       for (int i = 0; i < CODES; i++)
-        if (8 * (i / PER) + sub() >= left)
+        if (8 * (i / PER) + sub() > last)
           scales_next = (scales_next & ~(0xFFull << (8 * i))) |
-                        (uint64_t)alt[SC + latent_scale_at(LAT, ss, 2 * (i % PER) + (P::lane >> 5))] << (8 * i);
+                        (uint64_t)P::src[SC + latent_scale_at(LAT, last, 2 * (i % PER) + (P::lane >> 5))] << (8 * i);
     }
     to = tile;
   }
   __device__ __forceinline__ void issue(int i) {
-    data[i] = *(const uint4*)(i < CODES ? from[i / PER] + i % PER * 128 : key[i - CODES]);
+    data[i] = *(const uint4*)(P::src + (i < CODES ? from[i / PER] + i % PER * 128 : key[i - CODES]));
   }
   __device__ __forceinline__ void finish(int i) {
     // slots 8 and up: the second half, where bit 2 of the chunk order is flipped
@@ -229,9 +229,12 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   constexpr int RW = RB == 4 ? 2 : 1, KW = 4 / RW;  // waves by rows and by keys in the score product
   constexpr int RBW = RB / RW, KBW = 4 / KW;        // 16-row and 16-key blocks of a wave in it
   constexpr int QS = G::KS * KBW;                   // its steps
-  // Direct loads of the next tile: over the whole score product, or, where HBM and not the
-  // matrix unit is the bound, all at its start (128 requests on 16 heads: 382 us spread, 360 us).
-  constexpr int SPREAD = RB == 1 ? 1000 : 1;
+  // Direct loads of the next tile, as positions in score steps (half value steps from QS on): over
+  // the score product and, of 64 rows, a quarter of the value product (drafts of 32 requests on 64
+  // heads 182 us over three quarters of the scores, 178 over the scores, 174 so), or, where HBM and
+  // not the matrix unit is the bound, all at its start (128 requests on 16 heads: 382 us spread,
+  // 360 us).
+  constexpr int SPAN = RB == 1 ? 0 : (RB == 4 ? QS * 11 / 9 : QS);
   // operand reads ahead of their products, in steps of the score and of the value product
   constexpr int AK = RBW == 1 ? 8 : 6, AV = RB == 1 ? 8 : (RB == 2 ? 5 : 3);
   __shared__ __attribute__((aligned(1024))) uint8_t tile[2][G::TILE];
@@ -247,11 +250,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   const int64_t flat0 = (int64_t)u.qo * Hq + u.row0;
 
   const int pos0 = u.prefix + u.row0 / Hq;
-  // a token that every row of the unit sees, where there is one
-  const int safe = pos0 < u.key_begin ? u.key_begin : (pos0 < u.key_end ? pos0 : u.key_end - 1);
   using L = Loader<LAT, FP8>;
   L loader;
-  loader.init(p, u, safe, lane, wave);
+  loader.init(p, u, lane, wave);
   const uint32_t tile0 = lds_address(tile);
   auto first_loads = [&]() {
     loader.page = loader.page_at(u.key_begin);
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
         if constexpr (!FP8) {
 #pragma unroll
           for (int i = 0; i < L::LOADS; i++)
-            if (i * QS / SPREAD / L::LOADS == j) loader.issue(i);
+            if (i * SPAN / L::LOADS == j) loader.issue(i);
         }
         if constexpr (KBW == 2) {
           if (j == G::KS) mask(0);
@@ -492,6 +493,11 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
 #pragma unroll
           for (int rb = 0; rb < RBW; rb++)
             if (jj == 1 + 2 * rb) weigh(rb, 1);
+        }
+        if constexpr (!FP8) {
+#pragma unroll
+          for (int i = 0; i < L::LOADS; i++)
+            if (i * SPAN / L::LOADS >= QS && (i * SPAN / L::LOADS - QS) / 2 == jj) loader.issue(i);
         }
       });
       if constexpr (KBW == 2) __syncthreads();
