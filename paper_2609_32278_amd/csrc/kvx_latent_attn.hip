@@ -11,7 +11,7 @@
 // LDS, from which each product's operands come once a wave.  A decode batch of 128 requests on
 // 16 heads: 339 us with 16 rows, 5.5 TB/s (3.7 TB/s is what a plain reduction of a large buffer
 // reaches here).  64 rows at latent_dim 512: the products of 64 keys are 2176 cycles of the
-// matrix unit, measured 3.8k a step (8-bit: 5k, with its conversions), 0.9 to 1.2 PFLOP/s by
+// matrix unit, measured 3.8k a step (8-bit: 4.8k, with its conversions), 0.9 to 1.2 PFLOP/s by
 // how evenly a batch fills the CUs; a large library product reaches 1.2 to 1.3.
 //
 // Waves.  In the value product each of the 4 waves has a quarter of the latent dims and all rows.
@@ -154,22 +154,20 @@ struct Loader<LAT, true> : Pages<LAT> {
   __device__ __forceinline__ void issue(int i) {
     data[i] = *(const uint4*)(P::src + (i < CODES ? from[i / PER] + i % PER * 128 : key[i - CODES]));
   }
-  __device__ __forceinline__ void finish(int i) {
+  // A quarter of a piece's conversion, and its writes.
+  uint32_t y[4];
+  __device__ __forceinline__ void finish(int i, int e) {
     // slots 8 and up: the second half, where bit 2 of the chunk order is flipped
     const uint32_t half = (i < CODES ? i / PER : i - CODES) ? TileAt<LAT>::HALF : 0, flip = half ? 64 : 0;
     if (i < CODES) {
       const float sc = __uint_as_float(((uint32_t)(scales >> (8 * i)) & 0xFF) << 23);
-      const uint32_t w[4] = {data[i].x, data[i].y, data[i].z, data[i].w};
-      uint32_t y[8];
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        y[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], sc, false));
-        y[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], sc, true));
-      }
-      const uint32_t off = half + i % PER * 2048;
-      write_b128((at ^ flip) + to + off, y[0], y[1], y[2], y[3]);
-      write_b128((at ^ flip ^ 16) + to + off, y[4], y[5], y[6], y[7]);
-    } else {
+      const uint32_t w = e == 0 ? data[i].x : (e == 1 ? data[i].y : (e == 2 ? data[i].z : data[i].w));
+      y[2 * e % 4] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, sc, false));
+      y[2 * e % 4 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, sc, true));
+      formed(y[2 * e % 4]);
+      formed(y[2 * e % 4 + 1]);
+      if (e % 2) write_b128((at ^ flip ^ (e == 3 ? 16 : 0)) + to + half + i % PER * 2048, y[0], y[1], y[2], y[3]);
+    } else if (e == 0) {
       write_b128((key_at ^ flip) + to + half, data[i].x, data[i].y, data[i].z, data[i].w);
     }
   }
@@ -328,7 +326,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
       loader.page = loader.page_at(u.key_begin + kLatTileKeys);
       loader.scales = loader.scales_next;
 #pragma unroll
-      for (int i = 0; i < L::LOADS; i++) loader.finish(i);
+      for (int i = 0; i < L::LOADS; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) loader.finish(i, e);
       loader.begin(tile0, u.key_begin + kLatTileKeys);
 #pragma unroll
       for (int i = 0; i < L::LOADS; i++) loader.issue(i);
@@ -413,19 +413,13 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
           neg[rb] = mr == -INFINITY ? 0.0f : -mr;
         }
       }
-      // the weights of one row block and key block
-      auto weigh = [&](int rb, int kb) {
-        float pr[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][i], scale, neg[rb]));
-          l[rb] += pr[i];
-        }
-        uint32_t lo = pack_bf16(pr[0], pr[1]), hi = pack_bf16(pr[2], pr[3]);
-        formed(lo);
-        formed(hi);
+      // the i-th of a lane's four weights of one row block and key block
+      auto weigh = [&](int rb, int kb, int i) {
+        s[rb][kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rb][kb][i], scale, neg[rb]));
+        l[rb] += s[rb][kb][i];
         formed(l[rb]);
-        write_b64(pw[kb] + rb * 2048, lo, hi);
+        if (i == 3)
+          write_b64(pw[kb] + rb * 2048, pack_bf16(s[rb][kb][0], s[rb][kb][1]), pack_bf16(s[rb][kb][2], s[rb][kb][3]));
       };
       bf16x8 va[AV + 1], pb[RB];
       auto read_v = [&](int j) {  // step j of the value product: 32 keys (j / DB) of dim block j % DB
@@ -447,16 +441,21 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
           if (j + AV < 2 * G::DB) va[(j + AV) % (AV + 1)] = read_v(j + AV);
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int rb = 0; rb < RB; rb++)
+          for (int rb = 0; rb < RB; rb++) {
             o[rb][jj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[j % (AV + 1)], pb[rb], o[rb][jj], 0, 0, 0);
-          between(jj);
-          if constexpr (FP8) {
+            if (rb == (FP8 ? 0 : RB - 1)) between(jj);
+            // a quarter of a piece beside each product (a whole one behind a step's products: 24
+            // long requests on 128 heads 461 us, so 445)
+            if constexpr (FP8) {
 #pragma unroll
-            for (int i = 0; i < L::LOADS; i++)
-              if (i * (2 * G::DB) / L::LOADS == j) {
-                loader.finish(i);
-                loader.issue(i);
-              }
+              for (int i = 0; i < L::LOADS; i++)
+                if (i * (2 * G::DB) / L::LOADS == j) {
+#pragma unroll
+                  for (int e = rb * 4 / RB; e < (rb + 1) * 4 / RB; e++) loader.finish(i, e);
+                  if (rb == RB - 1) loader.issue(i);
+                }
+              __builtin_amdgcn_sched_barrier(0);
+            }
           }
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -474,14 +473,14 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
         if constexpr (KBW == 2) {
           if (j == G::KS) mask(0);
 #pragma unroll
-          for (int rb = 0; rb < RBW; rb++)
-            if (j == G::KS + 2 + 5 * rb) weigh(rb, 0);
+          for (int e = 0; e < 4 * RBW; e++)
+            if (j == G::KS + 2 + 5 * (e / 4)) weigh(e / 4, 0, e % 4);
         }
       });
       if constexpr (KBW == 1) {
         mask(0);
 #pragma unroll
-        for (int rb = 0; rb < RBW; rb++) weigh(rb, 0);
+        for (int e = 0; e < 4 * RBW; e++) weigh(e / 4, 0, e % 4);
       }
 #pragma unroll
       for (int j = 0; j < AV; j++) va[j] = read_v(j);
@@ -491,8 +490,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
       values(0, [&](int jj) {
         if constexpr (KBW == 2) {
 #pragma unroll
-          for (int rb = 0; rb < RBW; rb++)
-            if (jj == 1 + 2 * rb) weigh(rb, 1);
+          for (int e = 0; e < 4 * RBW; e++)
+            if (jj == 1 + 2 * (e / 4)) weigh(e / 4, 1, e % 4);
         }
         if constexpr (!FP8) {
 #pragma unroll
