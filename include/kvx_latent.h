@@ -137,7 +137,8 @@ int load_latent(kvx_latent_pool *pool, const kvx_batch *batch, void *out, int64_
  * stream).  The core of the absorbed form, for callers who keep W_uk and W_uv in weights
  * of their own.
  *   q            device bf16 [T, num_q_heads, latent_dim + rope_dim]
- *   num_q_heads  1 to 1024
+ *   num_q_heads  1 to 1024; a request's E_r * num_q_heads is at most 2^31 - 1025, its P_r + E_r at
+ *                most 2^31 - 2^23 (EUNSUPPORTED)
  *   sm_scale     > 0, at most 2e38
  *   out          device bf16 [T, num_q_heads, latent_dim] (round to nearest even)
  *   lse          device fp32 [T, num_q_heads] natural-log sum of exp of the scaled scores,
@@ -151,7 +152,7 @@ int latent_attention(kvx_latent_pool *pool, const kvx_batch *batch, const void *
 typedef struct {
     const void *w_uk;    /* device bf16 [num_q_heads][nope_dim][latent_dim] */
     const void *w_uv;    /* device bf16 [num_q_heads][v_dim][latent_dim] */
-    int32_t num_q_heads; /* 1 to 1024 */
+    int32_t num_q_heads; /* 1 to 1024, with the limits of latent_attention */
     int32_t nope_dim;    /* 64 or 128 */
     int32_t v_dim;       /* equal to nope_dim */
 } kvx_latent_proj;

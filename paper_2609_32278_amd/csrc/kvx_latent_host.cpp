@@ -101,13 +101,18 @@ int check_scale(float sm_scale) {
   return KVX_OK;
 }
 
-// Heads, and rows of one request within an int32.
+// Heads, rows of one request within an int32, and keys with room for what equal parts, rounded
+// up to 64 keys each, go past the last of them (64 keys a part, at most 130560 parts).
+constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - ((int64_t)1 << 23);
 int check_heads(const kvx_batch* b, int32_t Hq) {
   if (Hq < 1 || Hq > 1024) return report(KVX_EINVAL, "num_q_heads = %d, must be in [1, 1024]", Hq);
-  for (int r = 0; r < b->num_reqs; r++)
+  for (int r = 0; r < b->num_reqs; r++) {
+    if ((int64_t)b->prefix_lens[r] + b->extend_lens[r] > kMaxKeys)
+      return report(KVX_EUNSUPPORTED, "request %d: more than %lld tokens", r, (long long)kMaxKeys);
     if ((int64_t)b->extend_lens[r] * Hq > (int64_t)INT32_MAX - 1024)
       return report(KVX_EUNSUPPORTED, "request %d: %d suffix tokens of %d heads are too many rows", r,
                     b->extend_lens[r], Hq);
+  }
   return KVX_OK;
 }
 

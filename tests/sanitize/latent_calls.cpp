@@ -162,6 +162,10 @@ void refusals() {
   huge.add(0, 1 << 22);
   CHECK(attend(huge.get(), q, 1024, 0.1f, qo) == KVX_EUNSUPPORTED);
 
+  TestBatch far;
+  far.add((1ll << 31) - (1 << 23), 1);
+  CHECK(attend(far.get(), q, 1, 0.1f, qo) == KVX_EUNSUPPORTED);
+
   kvx_latent_proj proj{addr(0x300000), addr(0x400000), 16, 128, 128};
   auto extend = [&](const kvx_latent_proj* p, int form) {
     return latent_extend_attention(&pool, one.get(), p, q, 0.1f, qo, nullptr, form, nullptr);
