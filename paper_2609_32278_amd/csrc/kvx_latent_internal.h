@@ -59,7 +59,6 @@ hipError_t launch_load_latent(const LatentLoadParams& p, int64_t n_units, int la
 // ---- attention to the latents themselves
 
 constexpr int kLatTileKeys = 64;     // keys staged in LDS at once; parts start at multiples of it
-constexpr int kLatMaxRowBlocks = 4;  // 16-row blocks of a unit
 
 // One workgroup: rows [row0, row0 + nrows) of a request's (suffix token, head) rows, token
 // by token, against keys [key_begin, key_end) of its sequence.

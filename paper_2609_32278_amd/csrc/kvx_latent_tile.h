@@ -19,7 +19,6 @@ template <int LAT>
 struct LatGeom {
   static constexpr int ROW = LAT + kLatRope;          // values of an entry
   static constexpr int ROWB = ROW * 2;                // bytes of its bf16 row in LDS
-  static constexpr int CPR = ROW / 8;                 // 16-byte chunks per row
   static constexpr int KS = ROW / 32;                 // k-steps of the score product
   static constexpr int DW = LAT / 4;                  // latent dims of a wave's sums
   static constexpr int DB = DW / 16;
@@ -116,16 +115,6 @@ __device__ __forceinline__ void lds_load_1k(const uint8_t* base, int off, uint32
       : "s"(lds), "v"(off), "s"(base)
       : "memory", "m0");
 }
-// ... with an address per lane
-__device__ __forceinline__ void lds_load_1k(const uint8_t* lane_address, uint32_t lds) {
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, off"
-      :
-      : "s"(lds), "v"(lane_address)
-      : "memory", "m0");
-}
 
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)p;
@@ -137,7 +126,6 @@ __device__ __forceinline__ void wait_vmcnt() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
   __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
-
 
 }  // namespace
 }  // namespace kvx
