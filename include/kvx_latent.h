@@ -23,6 +23,9 @@
  *   - A call runs on the pool's device and leaves the caller's current device as it was.
  *   - A stream that is being captured into a HIP graph is refused (KVX_EUNSUPPORTED): the
  *     plan of a call is made on the host, from the lengths of its batch.
+ *   - Scores are float32, those that are scaled too: one below -3.4e38 counts as -inf, a weight
+ *     of zero, and one above 3.4e38 makes its row's result and lse NaN.  A row whose scores are
+ *     all -inf gives zeros and an lse of -inf.
  *   - Cache rows that attention reads are finite.  A row that is not may reach any query
  *     row of its request, those before it too.  Slots past a request's P_r + E_r tokens
  *     reach none, whatever they hold.

@@ -509,12 +509,16 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   };
   // A reference that moves with every tile would cost two more barriers and a rescaling of every
   // sum a tile.  With the fixed reference bf16 weights and float32 sums keep their relative precision for
-  // scores far above it, unless an exponential or a sum overflows: then the keys are gone
-  // over again with a reference that moves.
+  // scores far above it, unless an exponential or a sum overflows, or the first tile held no
+  // score above -inf for a row that sees some of it: then the keys are gone over again with a
+  // reference that moves.
   run(std::true_type{});
   float acc = 0.0f;
 #pragma unroll
-  for (int rb = 0; rb < RBW; rb++) acc += l[rb];
+  for (int rb = 0; rb < RBW; rb++) {
+    const float mr = RW == 1 ? m[rb] : (rw == 0 ? m[rb] : m[RB - RBW + rb]);
+    acc += mr == -INFINITY && limit[rb] >= u.key_begin ? INFINITY : l[rb];
+  }
 #pragma unroll
   for (int rb = 0; rb < RB; rb++)
 #pragma unroll
@@ -542,6 +546,7 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
     float lt = red[0][r];
 #pragma unroll
     for (int k = 1; k < KW; k++) lt += red[k][r];
+    if (m[rb] == INFINITY) lt = NAN;  // inf - inf; the weights against such a reference are 0
     const float inv = lt > 0.0f ? 1.0f / lt : (lt == 0.0f ? 0.0f : lt);
     const float lse2 = lt == 0.0f ? -INFINITY : m[rb] + __log2f(lt);
     if (u.part < 0) {

@@ -280,16 +280,19 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
     wait_vmcnt<0>();  // pieces past the last tile
     __syncthreads();
   };
-  // As in the attention on latents: only where an exponential or a sum overflows float32 are
-  // the keys gone over again with a reference that moves.
+  // As in the attention on latents: only where an exponential or a sum overflows float32, or
+  // a row sees some of the first 32 keys but no score above -inf there, are the keys gone over
+  // again with a reference that moves.
   run(std::true_type{});
-  float acc = l[0] + l[1];
+  float acc = 0.0f;
 #pragma unroll
-  for (int rb = 0; rb < 2; rb++)
+  for (int rb = 0; rb < 2; rb++) {
+    acc += m[rb] == -INFINITY && limit[rb] >= u.key_begin ? INFINITY : l[rb];
 #pragma unroll
     for (int db = 0; db < G::DB; db++)
 #pragma unroll
       for (int i = 0; i < 16; i++) acc += o[rb][db][i];
+  }
   const bool bad = __any(!__builtin_isfinite(acc));
   volatile int* flags = (volatile int*)lds;
   if (lane == 0) flags[wave] = bad;
@@ -301,7 +304,8 @@ __global__ __launch_bounds__(kThreads, 1) void latent_prefill_kernel(LatentPrefi
 #pragma unroll
   for (int rb = 0; rb < 2; rb++) {
     const int tok = wave * 64 + rb * 32 + n;
-    const float lt = l[rb] + __shfl_xor(l[rb], 32, 64);
+    float lt = l[rb] + __shfl_xor(l[rb], 32, 64);
+    if (m[rb] == INFINITY) lt = NAN;  // inf - inf; the weights against such a reference are 0
     const float inv = lt > 0.0f ? 1.0f / lt : (lt == 0.0f ? 0.0f : lt);
     const float lse2 = lt == 0.0f ? -INFINITY : m[rb] + __log2f(lt);
     if (tok >= ntok) continue;

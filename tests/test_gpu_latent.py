@@ -687,3 +687,92 @@ def test_agents_through_the_prefix_cache():
         torch.cuda.synchronize()
         kvx.kvx_cache_destroy(cache)
         kvx.latent_pool_destroy(pool)
+
+
+# ------------------------------------------------------------------- scores past float32
+
+
+def overflowing(s, heads, dim, low, scale=0.3):
+    """Cached rows and queries whose first 64 scores lie below float32's range (-1.2e39, from the
+    first rotated dim), the others `low` (from the second) plus what the rest of the dims give."""
+    rows = s.normal(sum(s.P) + sum(s.E), s.lat + 64)
+    rows[:64, s.lat], rows[64:, s.lat] = -4.0, 0.0
+    rows[:, s.lat + 1] = -low / 16
+    q = s.normal(s.T, heads, dim, scale=scale)
+    q[..., -64], q[..., -63] = 3e38, 16.0
+    return rows, q
+
+
+@pytest.mark.parametrize("low", [0, 4096])
+@pytest.mark.parametrize("split", [0, 64, 192, 1024])
+@pytest.mark.parametrize("heads,E,fp8", [(16, 1, False), (20, 1, True), (16, 5, False), (33, 3, True)])
+def test_latent_attention_after_scores_below_float32(setup, heads, E, fp8, split, low):
+    """Keys whose scores overflow to -inf have no weight; the keys after them count in full, also
+    where they lie so low that exponentials against a reference of zero would vanish."""
+    s = setup([400], [E], 256, fp8)
+    kvx.latent_pool_set_split_keys(s.pool, split)
+    rows, q = overflowing(s, heads, 320, low)
+    x = s.fill(rows=rows)[0]
+    out = torch.empty(E, heads, 256, dtype=BF16, device=DEV)
+    lse = torch.empty(E, heads, dtype=torch.float32, device=DEV)
+    kvx.latent_attention(s.pool, s.batch, q, heads, 0.07, out, lse)
+    o, l, tol, ltol = ref.attend(ref.f64(q), x[64:], x[64:, :256], 400 - 64, 0.07)
+    # scores of 4096 * 0.07 carry float32 steps of 2^-15, which the rms of the roundings does not see
+    ref.check_rows(out, o, tol, RMS_ATTEND)
+    assert (np.abs(ref.f64(lse) - l) <= ltol).all()
+
+
+@pytest.mark.parametrize("low", [0, 4096])
+@pytest.mark.parametrize("form", [kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED])
+@pytest.mark.parametrize("hd,P,E", [(64, 400, 70), (128, 6000, 40)])  # the second splits its keys
+def test_extend_after_scores_below_float32(setup, hd, P, E, form, low):
+    s = setup([P], [E], 256, False)
+    rows, q = overflowing(s, 2, hd + 64, low)
+    x = s.fill(rows=rows)[0][64:]
+    w_uk, w_uv = s.normal(2, hd, 256, scale=1 / 16), s.normal(2, hd, 256, scale=1 / 16)
+    out = torch.empty(E, 2, hd, dtype=BF16, device=DEV)
+    lse = torch.empty(E, 2, dtype=torch.float32, device=DEV)
+    kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, 0.07, out, lse, form=form)
+    uk, uv, qq, c = ref.f64(w_uk), ref.f64(w_uv), ref.f64(q), x[:, :256]
+    k = np.concatenate([np.einsum("hdl,jl->hjd", uk, c), np.broadcast_to(x[:, 256:], (2, len(x), 64))], -1)
+    o, l, _, _ = ref.attend(qq, k, np.einsum("hdl,jl->hjd", uv, c), P - 64, 0.07)
+    got = ref.f64(out)
+    assert np.isfinite(got).all() and np.linalg.norm(got - o) <= RMS_EXTEND * np.linalg.norm(o)
+    # half a bf16 step of every term of the products that meet a rounding (the rotated dims meet none)
+    ql = np.einsum("hdl,ihd->ihl", uk, qq[..., :hd])
+    size = np.maximum(np.einsum("ihd,hjd->ihj", np.abs(qq[..., :hd]), np.abs(k[..., :hd])),
+                      np.einsum("ihl,jl->ihj", np.abs(ql), np.abs(c))).max(-1) * 0.07 * ref.HALF_BF16
+    rest = (np.abs(l) + low * 0.07 + 30.0) * (320 + P) * ref.F32  # float32 sums of up to 320 terms and P weights
+    assert (np.abs(ref.f64(lse) - l) <= size + rest).all()
+
+
+@pytest.mark.parametrize("split", [0, 64])
+@pytest.mark.parametrize("key", [5, 170])
+def test_scores_above_float32_give_nan(setup, split, key):
+    """A scaled score past float32's largest value: NaN in its row, as inf - inf is, and in no other."""
+    s = setup([300], [1], 256, False)
+    kvx.latent_pool_set_split_keys(s.pool, split)
+    rows = s.normal(301, 320)
+    rows[:, 256] = 0.0
+    rows[key, 256] = 1e10
+    x = s.fill(rows=rows)[0]
+    w_uk, w_uv = s.normal(4, 64, 256, scale=1 / 16), s.normal(4, 64, 256, scale=1 / 16)
+
+    def check(dim, width, v, call, rms):
+        q = torch.zeros(1, 4, dim, dtype=BF16, device=DEV)
+        q[0, 2, -64] = 1e10
+        out = torch.zeros(1, 4, width, dtype=BF16, device=DEV)
+        lse = torch.zeros(1, 4, dtype=torch.float32, device=DEV)
+        call(q, out, lse)
+        got, l = ref.f64(out)[0], ref.f64(lse)[0]
+        assert np.isnan(got[2]).all() and np.isnan(l[2])
+        others = [0, 1, 3]
+        want = (v if v.ndim == 3 else np.broadcast_to(v, (4,) + v.shape)).mean(1)
+        assert np.linalg.norm(got[others] - want[others]) <= rms * np.linalg.norm(want[others])
+        assert np.abs(l[others] - math.log(301)).max() < 1e-5
+
+    check(320, 256, x[:, :256], lambda q, o, l: kvx.latent_attention(s.pool, s.batch, q, 4, 1e20, o, l), RMS_ATTEND)
+    v = np.einsum("hdl,jl->hjd", ref.f64(w_uv), x[:, :256])
+    for form in (kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED):
+        check(128, 64, v, lambda q, o, l: kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, 1e20, o, l, form=form),
+              RMS_EXTEND)
