@@ -439,7 +439,11 @@ def _latent_row(pool) -> tuple:
 
 
 def _elems(t, size: int, name: str) -> None:
-    if t is not None and not isinstance(t, int) and t.element_size() != size:
+    """Size 4 is float32; size 2 is bf16, or its bits as 16-bit integers."""
+    if t is None or isinstance(t, int):
+        return
+    want = ("float32",) if size == 4 else ("bfloat16", "int16", "uint16")
+    if str(t.dtype) not in ["torch." + w for w in want]:
         raise ValueError(f"{name}: {t.dtype} elements; expected {'float32' if size == 4 else 'bf16'}")
 
 

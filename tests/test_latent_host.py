@@ -88,3 +88,25 @@ def test_header_is_c(tmp_path):
     r = subprocess.run(["gcc", "-std=c99", "-pedantic", "-Wall", "-Wextra", "-Werror", "-fsyntax-only",
                         "-I" + os.path.join(ROOT, "include"), str(src)], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
+
+
+def test_binding_refuses_types_of_the_same_width(monkeypatch):
+    """16-bit floats that are not bf16, and 32-bit integers for lse, are not taken for their bits."""
+    monkeypatch.setattr(kvx, "_latent_row", lambda pool: (512, 64))
+    b = kvx.Batch([16], [4], [0, 2], 0x1000)
+    half, ints = torch.zeros(4, 576, dtype=torch.float16), torch.zeros(4, 16, dtype=torch.int32)
+    w, q = torch.zeros(16, 128, 512, dtype=torch.bfloat16), torch.zeros(4, 16, 192, dtype=torch.float16)
+    for call in (lambda: kvx.store_latent(None, b, half), lambda: kvx.load_latent(None, b, half),
+                 lambda: kvx.store_latent_rope(None, b, half), lambda: kvx.store_latent_rope(None, b, 1, norm=half),
+                 lambda: kvx.store_latent_rope(None, b, 1, q=q, q_out=q, num_q_heads=16),
+                 lambda: kvx.latent_attention(None, b, half, 1, 0.1, 1), lambda: kvx.latent_attention(None, b, 1, 1, 0.1, half),
+                 lambda: kvx.latent_extend_attention(None, b, q, w, w, 0.1, 1),
+                 lambda: kvx.latent_extend_attention(None, b, 1, w.half(), w, 0.1, 1),
+                 lambda: kvx.latent_extend_attention(None, b, 1, w, w.half(), 0.1, 1)):
+        with pytest.raises(ValueError, match="float16 elements; expected bf16"):
+            call()
+    with pytest.raises(ValueError, match="int32 elements; expected float32"):
+        kvx.latent_attention(None, b, 1, 16, 0.1, 1, ints)
+    # the bits of bf16 as integers pass (and are then not on the device)
+    with pytest.raises(ValueError, match="device"):
+        kvx.store_latent(None, b, half.view(torch.int16))
