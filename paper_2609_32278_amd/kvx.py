@@ -438,12 +438,17 @@ def _latent_row(pool) -> tuple:
     return lay.latent_dim, lay.rope_dim
 
 
+_DTYPES: dict = {}  # by element size, filled when a tensor is first checked: torch may not be imported yet
+
+
 def _elems(t, size: int, name: str) -> None:
     """Size 4 is float32; size 2 is bf16, or its bits as 16-bit integers."""
     if t is None or isinstance(t, int):
         return
-    want = ("float32",) if size == 4 else ("bfloat16", "int16", "uint16")
-    if str(t.dtype) not in ["torch." + w for w in want]:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({4: {torch.float32}, 2: {torch.bfloat16, torch.int16, torch.uint16}})
+    if t.dtype not in _DTYPES[size]:
         raise ValueError(f"{name}: {t.dtype} elements; expected {'float32' if size == 4 else 'bf16'}")
 
 
