@@ -20,7 +20,8 @@
  * kvx_radix.h serve a latent pool as they serve a KV pool.  The conventions at the head of
  * kvx.h hold here too (status codes, checks before any work, streams, one pool's calls in
  * order, scratch that grows, page ids and KVX_VALIDATE).  Besides:
- *   - A call runs on the pool's device and leaves the caller's current device as it was.
+ *   - A call runs on the pool's device and leaves the caller's current device as it was.  A
+ *     stream of another device is refused (KVX_EINVAL).
  *   - A stream that is being captured into a HIP graph is refused (KVX_EUNSUPPORTED): the
  *     plan of a call is made on the host, from the lengths of its batch.
  *   - Scores are float32, those that are scaled too: one below -3.4e38 counts as -inf, a weight

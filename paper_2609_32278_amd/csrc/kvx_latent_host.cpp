@@ -86,12 +86,16 @@ int check_pool(const kvx_latent_pool* pool) {
   return KVX_OK;
 }
 
-int check_stream(hipStream_t s) {
+int check_stream(hipStream_t s, int device) {
   hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
   const hipError_t e = hipStreamIsCapturing(s, &st);
   if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
   if (st != hipStreamCaptureStatusNone)
     return report(KVX_EUNSUPPORTED, "the stream is being captured: the plan of a call is made on the host");
+  if (s == nullptr || s == hipStreamLegacy || s == hipStreamPerThread) return KVX_OK;  // the current device's
+  hipDevice_t of = device;
+  KVX_HIP(hipStreamGetDevice(s, &of));
+  if (of != device) return report(KVX_EINVAL, "the stream is of device %d, the pool of device %d", of, device);
   return KVX_OK;
 }
 
@@ -219,7 +223,7 @@ int store_call(kvx_latent_pool* pool, const kvx_batch* batch, const kvx_rope* ro
   if (!kv) return report(KVX_EINVAL, "kv is NULL");
   OnDevice on;
   if (int rc = on.enter(pool->device)) return rc;
-  if (int rc = check_stream(s)) return rc;
+  if (int rc = check_stream(s, pool->device)) return rc;
   if (kvx::validate_mode())
     if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
   int64_t n_units = 0;
@@ -809,7 +813,7 @@ int load_latent(kvx_latent_pool* pool, const kvx_batch* batch, void* out, int64_
     hipStream_t s = (hipStream_t)stream;
     OnDevice on;
     if (int rc = on.enter(pool->device)) return rc;
-    if (int rc = check_stream(s)) return rc;
+    if (int rc = check_stream(s, pool->device)) return rc;
     if (kvx::validate_mode())
       if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
     kvx::LatentLoadParams p{};
@@ -839,7 +843,7 @@ int latent_attention(kvx_latent_pool* pool, const kvx_batch* batch, const void* 
     hipStream_t s = (hipStream_t)stream;
     OnDevice on;
     if (int rc = on.enter(pool->device)) return rc;
-    if (int rc = check_stream(s)) return rc;
+    if (int rc = check_stream(s, pool->device)) return rc;
     if (kvx::validate_mode())
       if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
     std::vector<Member> members;
@@ -907,7 +911,7 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
     hipStream_t s = (hipStream_t)stream;
     OnDevice on;
     if (int rc = on.enter(pool->device)) return rc;
-    if (int rc = check_stream(s)) return rc;
+    if (int rc = check_stream(s, pool->device)) return rc;
     if (kvx::validate_mode())
       if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
 

@@ -191,11 +191,14 @@ def _check(status: int, func: str):
         raise KvxError(status, func, kvx_last_error())
 
 
-def _stream(stream):
+def _stream(stream, *tensors):
+    """The stream of a call.  None: the current one of the device that the first of `tensors` is
+    on, or, where none is a tensor, of the current device."""
     if stream is None:
         import torch
         if torch.cuda.is_initialized():
-            return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+            dev = next((t.device for t in tensors if t is not None and not isinstance(t, int)), None)
+            return ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
         return None
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
@@ -470,7 +473,7 @@ def store_latent(pool, batch: Batch, kv, stream=None) -> None:
     """kv: [T, latent_dim + rope_dim] bf16, rows contiguous (the rows may be a slice of wider ones)."""
     lat, rope = _latent_row(pool)
     ptr, stride = _rows_ptr(kv, batch.total_extend, lat + rope, "kv")
-    _check(lib().store_latent(pool, ctypes.byref(batch.c), ptr, stride, _stream(stream)), "store_latent")
+    _check(lib().store_latent(pool, ctypes.byref(batch.c), ptr, stride, _stream(stream, kv)), "store_latent")
 
 
 def store_latent_rope(pool, batch: Batch, kv, *, theta: float = 10000.0, style: int = 0, norm=None,
@@ -497,14 +500,15 @@ def store_latent_rope(pool, batch: Batch, kv, *, theta: float = 10000.0, style: 
     r = kvx_rope(float(theta), None if freqs is None else freqs.ctypes.data, rope, int(style), None, _dptr(norm),
                  float(norm_eps))
     _check(lib().store_latent_rope(pool, ctypes.byref(batch.c), ctypes.byref(r), _dptr(q), int(num_q_heads),
-                                   int(q_dim or 0), _dptr(q_out), ptr, stride, _stream(stream)), "store_latent_rope")
+                                   int(q_dim or 0), _dptr(q_out), ptr, stride, _stream(stream, kv, q)),
+           "store_latent_rope")
 
 
 def load_latent(pool, batch: Batch, out, stream=None) -> None:
     """out: [T, latent_dim + rope_dim] bf16, rows contiguous (the rows may be a slice of wider ones)."""
     lat, rope = _latent_row(pool)
     ptr, stride = _rows_ptr(out, batch.total_extend, lat + rope, "out")
-    _check(lib().load_latent(pool, ctypes.byref(batch.c), ptr, stride, _stream(stream)), "load_latent")
+    _check(lib().load_latent(pool, ctypes.byref(batch.c), ptr, stride, _stream(stream, out)), "load_latent")
 
 
 def latent_attention(pool, batch: Batch, q, num_q_heads: int, sm_scale: float, out, lse=None, stream=None) -> None:
@@ -515,7 +519,7 @@ def latent_attention(pool, batch: Batch, q, num_q_heads: int, sm_scale: float, o
         _elems(buf, size, name)
         _need(buf, size * rows * width, name)
     _check(lib().latent_attention(pool, ctypes.byref(batch.c), _dptr(q), int(num_q_heads), float(sm_scale),
-                                  _dptr(out), _dptr(lse), _stream(stream)), "latent_attention")
+                                  _dptr(out), _dptr(lse), _stream(stream, q, out)), "latent_attention")
 
 
 def latent_extend_attention(pool, batch: Batch, q, w_uk, w_uv, sm_scale: float, out, lse=None,
@@ -533,7 +537,7 @@ def latent_extend_attention(pool, batch: Batch, q, w_uk, w_uv, sm_scale: float, 
     _elems(w_uv, 2, "w_uv")
     proj = kvx_latent_proj(_dptr(w_uk), _dptr(w_uv), heads, nope, v)
     _check(lib().latent_extend_attention(pool, ctypes.byref(batch.c), ctypes.byref(proj), _dptr(q), float(sm_scale),
-                                         _dptr(out), _dptr(lse), int(form), _stream(stream)),
+                                         _dptr(out), _dptr(lse), int(form), _stream(stream, q, out)),
            "latent_extend_attention")
 
 

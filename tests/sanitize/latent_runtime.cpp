@@ -1,0 +1,180 @@
+// Checks of latent attention's host code (csrc/kvx_latent_host.cpp) over a stand-in for the HIP
+// runtime with two devices, whose allocations can be made to fail: what a call does with streams,
+// devices and errors.  Built by tests/test_latent_runtime.py with the sanitizers; kernels are not
+// launched but counted.  The argument names the check.
+
+#include "kvx_latent_host.cpp"
+
+#include <cstdarg>
+#include <cstdio>
+#include <cstdlib>
+#include <set>
+#include <string>
+
+struct ihipStream_t {
+  int device;
+};
+
+namespace fake {
+int current = 0;
+int fail_host = 0, fail_device = 0;  // how many of the next allocations fail
+hipError_t last = hipSuccess;
+std::vector<std::string> launched;
+std::vector<int> launched_on;
+std::set<void*> host;  // live pinned buffers
+
+hipError_t done(hipError_t e) {
+  if (e != hipSuccess) last = e;
+  return e;
+}
+}  // namespace fake
+
+extern "C" {
+hipError_t hipGetDevice(int* d) { return *d = fake::current, hipSuccess; }
+hipError_t hipSetDevice(int d) { return fake::current = d, hipSuccess; }
+hipError_t hipGetLastError() {
+  const hipError_t e = fake::last;
+  fake::last = hipSuccess;
+  return e;
+}
+const char* hipGetErrorString(hipError_t) { return "stand-in error"; }
+hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* st) {
+  return *st = hipStreamCaptureStatusNone, hipSuccess;
+}
+hipError_t hipStreamGetDevice(hipStream_t s, hipDevice_t* d) { return *d = s->device, hipSuccess; }
+hipError_t hipStreamSynchronize(hipStream_t) { return hipSuccess; }
+hipError_t hipStreamWaitEvent(hipStream_t, hipEvent_t, unsigned) { return hipSuccess; }
+hipError_t hipEventCreateWithFlags(hipEvent_t* e, unsigned) { return *e = (hipEvent_t)std::malloc(1), hipSuccess; }
+hipError_t hipEventRecord(hipEvent_t, hipStream_t) { return hipSuccess; }
+hipError_t hipEventSynchronize(hipEvent_t) { return hipSuccess; }
+hipError_t hipEventDestroy(hipEvent_t e) { return std::free((void*)e), hipSuccess; }
+hipError_t hipDeviceSynchronize() { return hipSuccess; }
+hipError_t hipHostMalloc(void** p, size_t n, unsigned) {
+  if (fake::fail_host > 0) return fake::fail_host--, fake::done(hipErrorOutOfMemory);
+  *p = std::malloc(n);
+  fake::host.insert(*p);
+  return hipSuccess;
+}
+hipError_t hipHostFree(void* p) { return fake::host.erase(p), std::free(p), hipSuccess; }
+hipError_t hipMalloc(void** p, size_t n) { return *p = std::malloc(n), hipSuccess; }
+hipError_t hipFree(void* p) { return std::free(p), hipSuccess; }
+hipError_t hipMallocAsync(void** p, size_t n, hipStream_t) {
+  if (fake::fail_device > 0) return fake::fail_device--, fake::done(hipErrorOutOfMemory);
+  // workspaces are never touched here: their size is not reserved
+  return *p = std::malloc(n < (1 << 20) ? n : 64), hipSuccess;
+}
+hipError_t hipFreeAsync(void* p, hipStream_t) { return std::free(p), hipSuccess; }
+hipError_t hipMemset(void* p, int v, size_t n) { return std::memset(p, v, n), hipSuccess; }
+hipError_t hipMemcpy(void* d, const void* s, size_t n, hipMemcpyKind) { return std::memcpy(d, s, n), hipSuccess; }
+hipError_t hipMemcpyAsync(void* d, const void* s, size_t n, hipMemcpyKind, hipStream_t) {
+  return std::memcpy(d, s, n), hipSuccess;
+}
+}
+
+namespace kvx {
+static std::string g_message;
+int report(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_message = buf;
+  return code;
+}
+static hipError_t count(const char* name) {
+  fake::launched.push_back(name);
+  fake::launched_on.push_back(fake::current);
+  return hipSuccess;
+}
+hipError_t launch_store_latent(const LatentStoreParams&, int64_t, int, bool, bool, hipStream_t) { return count("store"); }
+hipError_t launch_load_latent(const LatentLoadParams&, int64_t, int, bool, hipStream_t) { return count("load"); }
+hipError_t launch_latent_attention(const LatentAttnParams&, int64_t, const LatentSmallPlan*, const LatentRowPlan*, int,
+                                   bool, int, hipStream_t) {
+  return count("attention");
+}
+hipError_t launch_latent_merge(const LatentMergeParams&, int64_t, const LatentSmallPlan*, const LatentRowPlan*, int, int,
+                               hipStream_t) {
+  return count("merge");
+}
+hipError_t launch_latent_absorb(const LatentProjParams&, int64_t, int, int, hipStream_t) { return count("absorb"); }
+hipError_t launch_latent_output(const LatentProjParams&, int64_t, int, int, hipStream_t) { return count("output"); }
+hipError_t launch_latent_expand(const LatentExpandParams&, int64_t, int, int, bool, hipStream_t) { return count("expand"); }
+hipError_t launch_latent_prefill(const LatentPrefillParams&, int64_t, int, hipStream_t) { return count("prefill"); }
+hipError_t launch_latent_tile_merge(const LatentTileMergeParams&, int64_t, int, hipStream_t) { return count("tiles"); }
+}  // namespace kvx
+
+#define CHECK(cond)                                                                                        \
+  do {                                                                                                     \
+    if (!(cond)) {                                                                                         \
+      std::fprintf(stderr, "check failed at line %d: %s (%s)\n", __LINE__, #cond, kvx::g_message.c_str()); \
+      std::exit(3);                                                                                        \
+    }                                                                                                      \
+  } while (0)
+
+namespace {
+
+struct TestBatch {
+  std::vector<int32_t> P, E, indptr{0};
+  int32_t ids = 0;
+  kvx_batch b{};
+  void add(int32_t p, int32_t e) {
+    P.push_back(p);
+    E.push_back(e);
+    indptr.push_back(indptr.back() + (int32_t)(((int64_t)p + e + 15) / 16));
+  }
+  const kvx_batch* get() {
+    b = kvx_batch{(int32_t)P.size(), P.data(), E.data(), indptr.data(), &ids};
+    return &b;
+  }
+};
+
+void* addr(uintptr_t a) { return (void*)a; }
+
+kvx_latent_pool* make_pool(int device) {
+  const int before = fake::current;
+  fake::current = device;
+  kvx_latent_pool* p = nullptr;
+  CHECK(latent_pool_create(4, 16, 256, 64, KVX_LATENT_BF16, &p) == KVX_OK);
+  fake::current = before;
+  return p;
+}
+
+// Every call on a pool of device 1, with device 0 current.
+std::vector<int> all_calls(kvx_latent_pool* pool, const kvx_batch* b, hipStream_t s) {
+  const kvx_rope rope{10000.0, nullptr, 64, KVX_ROPE_HALF, nullptr, nullptr, 1e-6f};
+  const kvx_latent_proj proj{addr(0x300000), addr(0x400000), 4, 64, 64};
+  void *x = addr(0x10000), *q = addr(0x100000), *o = addr(0x200000);
+  return {store_latent(pool, b, x, 320, s),
+          store_latent_rope(pool, b, &rope, nullptr, 0, 0, nullptr, x, 320, s),
+          load_latent(pool, b, x, 320, s),
+          latent_attention(pool, b, q, 4, 0.1f, o, nullptr, s),
+          latent_extend_attention(pool, b, &proj, q, 0.1f, o, nullptr, KVX_LATENT_ABSORBED, s),
+          latent_extend_attention(pool, b, &proj, q, 0.1f, o, nullptr, KVX_LATENT_EXPANDED, s)};
+}
+
+// A stream of another device than the pool's is refused; the pool's own and the null stream run
+// there, and the caller's device stays current.
+void streams() {
+  kvx_latent_pool* pool = make_pool(1);
+  TestBatch t;
+  t.add(20, 3);
+  ihipStream_t other{0}, own{1};
+  for (int rc : all_calls(pool, t.get(), &other)) CHECK(rc == KVX_EINVAL);
+  CHECK(fake::launched.empty() && fake::current == 0);
+  for (hipStream_t s : {&own, (ihipStream_t*)nullptr})
+    for (int rc : all_calls(pool, t.get(), s)) CHECK(rc == KVX_OK);
+  CHECK(!fake::launched.empty() && fake::current == 0);
+  for (int d : fake::launched_on) CHECK(d == 1);
+  CHECK(latent_pool_destroy(pool) == KVX_OK && fake::current == 0);
+}
+
+}  // namespace
+
+int main(int argc, char** argv) {
+  const std::string what = argc > 1 ? argv[1] : "";
+  if (what == "streams") streams();
+  else return 2;
+  std::printf("%s passed\n", what.c_str());
+  return 0;
+}
