@@ -70,6 +70,7 @@ struct Staging {
     if (bytes > host_cap) {
       if (host) KVX_HIP(hipHostFree(host));
       host = nullptr;
+      host_cap = 0;
       size_t cap = std::max<size_t>(bytes + bytes / 2, 4096);
       KVX_HIP(hipHostMalloc(&host, cap, hipHostMallocDefault));
       host_cap = cap;

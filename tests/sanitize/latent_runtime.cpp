@@ -169,11 +169,31 @@ void streams() {
   CHECK(latent_pool_destroy(pool) == KVX_OK && fake::current == 0);
 }
 
+// After an upload whose buffers could not be had, on the host or on the device, the pool works on.
+void staging() {
+  kvx_latent_pool* pool = make_pool(0);
+  TestBatch some, more;
+  for (int i = 0; i < kvx::kStoreInlineReqs + 1; i++) some.add(i, 1);
+  for (int i = 0; i < 4000; i++) more.add(i, 1);
+  void* x = addr(0x10000);
+  CHECK(store_latent(pool, some.get(), x, 320, nullptr) == KVX_OK);
+  for (int* failing : {&fake::fail_host, &fake::fail_device}) {
+    *failing = 1;
+    fake::launched.clear();
+    CHECK(store_latent(pool, more.get(), x, 320, nullptr) == KVX_ENOMEM && fake::launched.empty());
+    CHECK(*failing == 0 && fake::last == hipSuccess);
+    CHECK(store_latent(pool, some.get(), x, 320, nullptr) == KVX_OK && fake::launched.size() == 1);
+  }
+  CHECK(store_latent(pool, more.get(), x, 320, nullptr) == KVX_OK);
+  CHECK(latent_pool_destroy(pool) == KVX_OK && fake::host.empty());
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
   const std::string what = argc > 1 ? argv[1] : "";
   if (what == "streams") streams();
+  else if (what == "staging") staging();
   else return 2;
   std::printf("%s passed\n", what.c_str());
   return 0;

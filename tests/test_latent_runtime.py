@@ -43,6 +43,10 @@ def test_streams_and_devices(driver, tmp_path):
     run_check(driver, "streams", tmp_path)
 
 
+def test_uploads_that_find_no_memory(driver, tmp_path):
+    run_check(driver, "staging", tmp_path)
+
+
 class OnSecond:
     """What the binding asks of a tensor, of one on the second device."""
 
