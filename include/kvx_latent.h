@@ -169,11 +169,13 @@ typedef struct {
  *   q     device bf16 [T, num_q_heads, nope_dim + rope_dim] (the last rope_dim rotated)
  *   out   device bf16 [T, num_q_heads, v_dim] (round to nearest even)
  *   lse   device fp32 [T, num_q_heads], or NULL
- *   form  enum kvx_latent_form
+ *   form  enum kvx_latent_form.  The expanded form takes at most 2^31 - 1 tokens P_r + E_r in
+ *         all, each request's rounded up to 64 (EUNSUPPORTED); past that the automatic choice is
+ *         the absorbed form for every request
  * Intermediate rows -- expanded keys and values, or queries and sums in the latent space --
  * are rounded to bf16 once each, so the two forms differ by such roundings, and the scores
  * behind lse carry one.  Uses library-owned device workspaces: for the expanded form the keys
- * and values of as many heads at a time as 2 GiB holds (at least one); for the absorbed form
+ * and values of as many heads at a time as 2 GiB holds (at least one), and the rotated keys; for the absorbed form
  * 2 (2 latent_dim + rope_dim) + 4 bytes for each of its suffix tokens and heads; for either up
  * to 2 GiB of partial results.
  * Errors: as store_latent.  R = 0 or T = 0: no-op.

@@ -638,6 +638,15 @@ void plan_expanded(const kvx_batch* b, const std::vector<int64_t>& qo, const std
   plan.units = in_order(units, spread(groups));
 }
 
+// Rows of the expanded buffers for the requests that do not take the absorbed form.
+int64_t tokens_to_expand(const kvx_batch* b, const std::vector<bool>& absorbed) {
+  int64_t n = 0;
+  for (int32_t r = 0; r < b->num_reqs; r++)
+    if (b->extend_lens[r] > 0 && !absorbed[(size_t)r])
+      n += ceil_div((int64_t)b->prefix_lens[r] + b->extend_lens[r], 64) * 64;
+  return n;
+}
+
 // The requests of a batch that take the absorbed form, by what each form costs: its products
 // at the rate they reach in large batches (the expanded form about 0.8 of the absorbed one's
 // 1.1 PFLOP/s, expansion and attention together) and its launches.  All of one form, or each
@@ -661,6 +670,7 @@ std::vector<bool> choose_forms(const kvx_batch* b, int32_t Hq, int64_t latent, i
     mixed += std::min(a, e);
   }
   if (all_a <= mixed || all_e <= mixed) absorbed.assign((size_t)R, all_a <= all_e);
+  if (tokens_to_expand(b, absorbed) > INT32_MAX) absorbed.assign((size_t)R, true);
   return absorbed;
 }
 
@@ -893,18 +903,18 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
     if (form == KVX_LATENT_AUTO) takes_absorbed = choose_forms(batch, Hq, lat, D);
     std::vector<Member> absorbed;
     std::vector<int32_t> expanded;
-    int64_t own_rows = 0, x_tokens = 0;
+    int64_t own_rows = 0;
     for (int32_t r = 0; r < batch->num_reqs; r++) {
-      const int64_t P = batch->prefix_lens[r], E = batch->extend_lens[r];
+      const int64_t E = batch->extend_lens[r];
       if (E == 0) continue;
       if (takes_absorbed[(size_t)r]) {
         absorbed.push_back({r, own_rows});
         own_rows += E;
       } else {
         expanded.push_back(r);
-        x_tokens += ceil_div(P + E, 64) * 64;
       }
     }
+    const int64_t x_tokens = tokens_to_expand(batch, takes_absorbed);
     if (x_tokens > (int64_t)INT32_MAX)
       return report(KVX_EUNSUPPORTED, "%lld tokens to expand in one call", (long long)x_tokens);
 

@@ -188,12 +188,30 @@ void staging() {
   CHECK(latent_pool_destroy(pool) == KVX_OK && fake::host.empty());
 }
 
+// Tokens whose expansion one call cannot index: the expanded form is refused, the automatic
+// choice takes the other.
+void many_tokens() {
+  kvx_latent_pool* pool = make_pool(0);
+  TestBatch t;
+  for (int i = 0; i < 2; i++) t.add(1100000000, 600);
+  const kvx_latent_proj proj{addr(0x300000), addr(0x400000), 4, 64, 64};
+  auto call = [&](int form) {
+    fake::launched.clear();
+    return latent_extend_attention(pool, t.get(), &proj, addr(0x100000), 0.1f, addr(0x200000), nullptr, form, nullptr);
+  };
+  CHECK(call(KVX_LATENT_EXPANDED) == KVX_EUNSUPPORTED && fake::launched.empty());
+  CHECK(call(KVX_LATENT_AUTO) == KVX_OK);
+  CHECK(fake::launched == (std::vector<std::string>{"absorb", "attention", "merge", "output"}));
+  CHECK(latent_pool_destroy(pool) == KVX_OK);
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
   const std::string what = argc > 1 ? argv[1] : "";
   if (what == "streams") streams();
   else if (what == "staging") staging();
+  else if (what == "tokens") many_tokens();
   else return 2;
   std::printf("%s passed\n", what.c_str());
   return 0;

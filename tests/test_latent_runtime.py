@@ -47,6 +47,10 @@ def test_uploads_that_find_no_memory(driver, tmp_path):
     run_check(driver, "staging", tmp_path)
 
 
+def test_more_tokens_than_one_call_expands(driver, tmp_path):
+    run_check(driver, "tokens", tmp_path)
+
+
 class OnSecond:
     """What the binding asks of a tensor, of one on the second device."""
 
