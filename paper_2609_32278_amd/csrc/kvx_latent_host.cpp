@@ -647,23 +647,52 @@ int64_t tokens_to_expand(const kvx_batch* b, const std::vector<bool>& absorbed) 
   return n;
 }
 
-// The requests of a batch that take the absorbed form, by what each form costs: its products
-// at the rate they reach in large batches (the expanded form about 0.8 of the absorbed one's
-// 1.1 PFLOP/s, expansion and attention together) and its launches.  All of one form, or each
-// request its cheaper one.  Measured at 16, 32 and 128 heads, 2k to 30k tokens cached, both forms
-// per suffix length: 64 tokens 0.28-0.63 of the expanded form's time, 128 tokens 0.5-0.8,
-// 256 tokens 1.0-1.4, 512 tokens 1.5-2.0; four requests of 100 + 100 tokens 63 against 39 us.
-std::vector<bool> choose_forms(const kvx_batch* b, int32_t Hq, int64_t latent, int64_t d) {
-  constexpr double kRateAbsorbed = 1.1e9, kRateExpanded = 0.88e9;       // operations per us
-  constexpr double kLaunchAbsorbed = 30.0, kLaunchExpanded = 20.0;      // us
+// The requests of a batch that take the absorbed form, by the estimated time of each form: what
+// its kernels compute (suffixes in whole units of 16, 32 or 64 rows, or tiles of 256 tokens,
+// cached tokens expanded 256 at a time) at the rates that they reach, what a unit costs besides,
+// and the launches with one unit's walk along its keys, which few units do not hide.  All of one
+// form, or each request its cheaper one.
+// Fitted to both forms' times at 14 suffix lengths from 1 to 700 of 32 batches (latent 256 and 512,
+// heads of 64 and 128, both pool types), in us absorbed / expanded: 12 requests of 8000 cached
+// tokens and 16 heads, latent 512, heads of 128, 128 new tokens 471 / 674, 257 956 / 935, 512
+// 1545 / 980; 8 bits 519 / 652, 1138 / 906, 1775 / 954; latent 256, heads of 64 288 / 339, 604 / 486,
+// 932 / 512; and of 550 random batches.  400 other random batches: on average 1.6% above the
+// faster of the two, at most 1.4 times, where both are some 25 us (by the pairs alone, without
+// whole tiles and units, their start and steps: 17%, 4.7 times; 23 short requests of 102 heads
+// 112 us where 42 do).
+std::vector<bool> choose_forms(const kvx_batch* b, int32_t Hq, int64_t latent, int64_t d, bool fp8 = false) {
+  // operations a us
+  const double rate_a = (latent == 512 ? 1.28e9 : 1.0e9) * (fp8 ? 0.84 : 1.0), rate_weights = 0.45e9;
+  const double rate_e = d == 128 ? 1.06e9 : 0.85e9, rate_expand = 1.28e9;
+  // what a unit costs besides, in steps of 64 keys
+  constexpr double kUnitA = 14.0, kUnitE = 4.3;
+  constexpr int64_t T = kvx::kLatTileTok;
   const int32_t R = b->num_reqs;
+  int64_t most = 0, longest = 0;
+  for (int32_t r = 0; r < R; r++)
+    if (b->extend_lens[r] > 0) {
+      most = std::max<int64_t>(most, (int64_t)b->extend_lens[r] * Hq);
+      longest = std::max<int64_t>(longest, (int64_t)b->prefix_lens[r] + b->extend_lens[r]);
+    }
+  const int64_t M = most <= 16 ? 16 : (most <= 32 ? 32 : 64);  // rows of the absorbed form's units
+  // us of launches and of the steps of one unit (a longer walk is split between more units)
+  const double steps = (double)ceil_div(std::min<int64_t>(longest, 1024), kvx::kLatTileKeys);
+  const double wide = latent / 512.0;
+  const double start_a = 21.0 + (M == 64 ? 9.0 * wide : 0.0) + 1.1 * wide * (M == 64 && fp8 ? 1.2 : 1.0) * steps;
+  const double start_e = 16.0 + 3.0 * wide + 2.4 * d / 128.0 * steps;
   std::vector<bool> absorbed((size_t)R);
-  double all_a = kLaunchAbsorbed, all_e = kLaunchExpanded, mixed = kLaunchAbsorbed + kLaunchExpanded;
+  double all_a = start_a, all_e = start_e, mixed = start_a + start_e;
   for (int32_t r = 0; r < R; r++) {
-    const double P = b->prefix_lens[r], E = b->extend_lens[r], pairs = E * P + 0.5 * E * (E + 1);
+    const int64_t P = b->prefix_lens[r], E = b->extend_lens[r];
     if (E == 0) continue;
-    const double a = 2.0 * Hq * (2.0 * d * latent * E + (2.0 * latent + kvx::kLatRope) * pairs) / kRateAbsorbed;
-    const double e = 2.0 * Hq * (2.0 * d * latent * (P + E) + (2.0 * d + kvx::kLatRope) * pairs) / kRateExpanded;
+    // pairs: a unit's or tile's rows see the keys up to its last token's
+    const double keys_a = P + 0.5 * (E + (double)M / Hq) + kUnitA * kvx::kLatTileKeys;
+    const double keys_e = P + 0.5 * (E + std::min(E, T)) + kUnitE * kvx::kLatTileKeys;
+    const double pairs_a = (double)(ceil_div(E * Hq, M) * M) * keys_a, pairs_e = (double)(ceil_div(E, T) * T * Hq) * keys_e;
+    const double weights = 4.0 * d * latent * Hq;  // operations a token
+    const double a = 2.0 * (2.0 * latent + kvx::kLatRope) * pairs_a / rate_a + weights * E / rate_weights;
+    const double e = 2.0 * (2.0 * d + kvx::kLatRope) * pairs_e / rate_e +
+                     weights * (double)(ceil_div(P + E, kvx::kLatExpandTok) * kvx::kLatExpandTok) / rate_expand;
     absorbed[(size_t)r] = a <= e;
     all_a += a;
     all_e += e;
@@ -900,7 +929,7 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
       return report(KVX_EINVAL, "q, out, w_uk and w_uv must be non-NULL");
 
     std::vector<bool> takes_absorbed((size_t)batch->num_reqs, form == KVX_LATENT_ABSORBED);
-    if (form == KVX_LATENT_AUTO) takes_absorbed = choose_forms(batch, Hq, lat, D);
+    if (form == KVX_LATENT_AUTO) takes_absorbed = choose_forms(batch, Hq, lat, D, pool->dtype == KVX_LATENT_FP8);
     std::vector<Member> absorbed;
     std::vector<int32_t> expanded;
     int64_t own_rows = 0;

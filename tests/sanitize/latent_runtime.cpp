@@ -205,6 +205,35 @@ void many_tokens() {
   CHECK(latent_pool_destroy(pool) == KVX_OK);
 }
 
+// The automatic choice takes the form that was measured to be faster by a fifth or more (us,
+// absorbed and expanded): whole tiles, units and pool types count.
+void choices() {
+  struct Timed {
+    int lat, hd, heads;
+    bool fp8;
+    int reqs, prefix, extend;
+    double absorbed, expanded;
+  };
+  const Timed timed[] = {
+      {512, 128, 16, false, 12, 8000, 128, 470.8, 673.7},  {512, 128, 16, false, 12, 8000, 512, 1545.3, 979.6},
+      {512, 128, 16, true, 12, 8000, 180, 821.1, 662.3},   {512, 128, 16, true, 12, 8000, 300, 1158.7, 911.2},
+      {256, 128, 64, false, 4, 3000, 400, 507.3, 412.1},   {256, 128, 64, true, 4, 3000, 400, 601.5, 409.2},
+      {256, 128, 16, false, 12, 8000, 257, 617.8, 772.0},  {256, 128, 16, true, 2, 30000, 400, 687.3, 446.8},
+      {256, 64, 16, false, 12, 8000, 300, 614.7, 484.2},   {512, 64, 16, false, 12, 8000, 257, 938.2, 578.5},
+      {512, 128, 4, false, 6, 500, 1, 28.8, 45.5},         {256, 128, 4, true, 6, 500, 1, 25.4, 37.3},
+      {512, 128, 96, true, 9, 562, 136, 473.0, 317.0},     {256, 128, 37, true, 22, 126, 2, 28.0, 71.0},
+  };
+  for (const Timed& t : timed) {
+    TestBatch b;
+    for (int i = 0; i < t.reqs; i++) b.add(t.prefix, t.extend);
+    for (bool absorbed : choose_forms(b.get(), t.heads, t.lat, t.hd, t.fp8))
+      if (absorbed != (t.absorbed < t.expanded)) {
+        std::fprintf(stderr, "latent %d, %d heads of %d, %d + %d tokens\n", t.lat, t.heads, t.hd, t.prefix, t.extend);
+        std::exit(3);
+      }
+  }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -212,6 +241,7 @@ int main(int argc, char** argv) {
   if (what == "streams") streams();
   else if (what == "staging") staging();
   else if (what == "tokens") many_tokens();
+  else if (what == "choices") choices();
   else return 2;
   std::printf("%s passed\n", what.c_str());
   return 0;

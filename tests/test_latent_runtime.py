@@ -51,6 +51,10 @@ def test_more_tokens_than_one_call_expands(driver, tmp_path):
     run_check(driver, "tokens", tmp_path)
 
 
+def test_automatic_form_is_the_faster_one(driver, tmp_path):
+    run_check(driver, "choices", tmp_path)
+
+
 class OnSecond:
     """What the binding asks of a tensor, of one on the second device."""
 
