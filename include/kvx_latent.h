@@ -16,16 +16,18 @@
  * suits single tokens, drafted tokens and short turns; long suffixes suit the other.
  *
  * The pages, the page table and the batch are those of kvx.h: pages of 16 tokens, request r
- * with a prefix of P_r tokens in the pool and a suffix of E_r tokens; kvx_cache.h and
- * kvx_radix.h serve a latent pool as they serve a KV pool.  The conventions at the head of
- * kvx.h hold here too (status codes, checks before any work, streams, one pool's calls in
- * order, scratch that grows, page ids and KVX_VALIDATE).  Besides:
+ * with a prefix of P_r tokens in the pool and a suffix of E_r tokens.  kvx_cache.h and
+ * kvx_radix.h serve a latent pool as they serve a KV pool, except for the host tier of a cache:
+ * a latent pool has no spill, reload or raw page moves, so its cache is one without
+ * (kvx_cache_create).  The conventions at the head of kvx.h hold here too (status codes, checks
+ * before any work, streams, one pool's calls in order, scratch that grows, page ids and
+ * KVX_VALIDATE).  Besides:
  *   - A call runs on the pool's device and leaves the caller's current device as it was.  A
  *     stream of another device is refused (KVX_EINVAL).
  *   - A stream that is being captured into a HIP graph is refused (KVX_EUNSUPPORTED): the
  *     plan of a call is made on the host, from the lengths of its batch.
- *   - Scores are float32, those that are scaled too: one below -3.4e38 counts as -inf, a weight
- *     of zero, and one above 3.4e38 makes its row's result and lse NaN.  A row whose scores are
+ *   - Scores are float32, also times sm_scale and log2 e: one below -3.4e38 counts as -inf, a
+ *     weight of zero, and one above 3.4e38 makes its row's result and lse NaN.  A row whose scores are
  *     all -inf gives zeros and an lse of -inf.
  *   - Cache rows that attention reads are finite.  A row that is not may reach any query
  *     row of its request, those before it too.  Slots past a request's P_r + E_r tokens
