@@ -26,6 +26,8 @@
  *     stream of another device is refused (KVX_EINVAL).
  *   - A stream that is being captured into a HIP graph is refused (KVX_EUNSUPPORTED): the
  *     plan of a call is made on the host, from the lengths of its batch.
+ *   - Results (q_out, out, lse) overlap no input of their call and not each other (KVX_EINVAL),
+ *     but for q_out in place of q.
  *   - Scores are float32, also times sm_scale and log2 e: one below -3.4e38 counts as -inf, a
  *     weight of zero, and one above 3.4e38 makes its row's result and lse NaN.  A row whose scores are
  *     all -inf gives zeros and an lse of -inf.

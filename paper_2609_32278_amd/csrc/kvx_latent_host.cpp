@@ -120,10 +120,30 @@ int check_heads(const kvx_batch* b, int32_t Hq) {
   return KVX_OK;
 }
 
-// Byte ranges [a, a + n) and [b, b + n) that meet without being the same.
-bool overlap(const void* a, const void* b, size_t n) {
+// Byte ranges [a, a + n) and [b, b + m) that meet.
+bool meet(const void* a, size_t n, const void* b, size_t m) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x != y && x < y + n && y < x + n;
+  return x < y + m && y < x + n;
+}
+
+// Whether [a, a + n) meets one of `rows` rows of `width` bytes, `stride` apart, from b on.
+bool meets_rows(const void* a, size_t n, const void* b, int64_t rows, size_t width, size_t stride) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  const uintptr_t i = x < y + width ? 0 : (x - y - width) / stride + 1;  // the first row that ends behind x
+  return i < (uintptr_t)rows && y + i * stride < x + n;
+}
+
+// The results of attention, over rows of `row` bytes each, against what it reads and each other.
+int check_results(const void* out, size_t row, const float* lse, size_t rows, const void* q, size_t q_row,
+                  const void* w_uk = nullptr, const void* w_uv = nullptr, size_t w_bytes = 0) {
+  if (meet(out, rows * row, q, rows * q_row) || meet(out, rows * row, w_uk, w_bytes) || meet(out, rows * row, w_uv, w_bytes))
+    return report(KVX_EINVAL, "out overlaps an input");
+  if (lse == nullptr) return KVX_OK;
+  const size_t n = rows * sizeof(float);
+  if (meet(lse, n, q, rows * q_row) || meet(lse, n, w_uk, w_bytes) || meet(lse, n, w_uv, w_bytes))
+    return report(KVX_EINVAL, "lse overlaps an input");
+  if (meet(lse, n, out, rows * row)) return report(KVX_EINVAL, "lse overlaps out");
+  return KVX_OK;
 }
 
 kvx::LatentPoolView view(const kvx_latent_pool* pool, const kvx_batch* batch) {
@@ -210,7 +230,8 @@ int store_call(kvx_latent_pool* pool, const kvx_batch* batch, const kvx_rope* ro
         return report(KVX_EINVAL, "q_dim = %d: must be a multiple of 8 in [%d, 4096]", q_dim, kvx::kLatRope);
       if (int rc = check_align(q, "q")) return rc;
       if (int rc = check_align(q_out, "q_out")) return rc;
-      if (overlap(q, q_out, (size_t)qo.back() * Hq * q_dim * 2))
+      const size_t q_bytes = (size_t)qo.back() * Hq * q_dim * 2;
+      if (q != q_out && meet(q, q_bytes, q_out, q_bytes))
         return report(KVX_EINVAL, "q_out overlaps q without being q");
     }
     p.norm = (const uint16_t*)rope->k_norm;
@@ -221,6 +242,9 @@ int store_call(kvx_latent_pool* pool, const kvx_batch* batch, const kvx_rope* ro
   if (int rc = check_align(kv, "kv")) return rc;
   if (qo.back() == 0) return KVX_OK;
   if (!kv) return report(KVX_EINVAL, "kv is NULL");
+  if (rotate && Hq > 0 && meets_rows(q_out, (size_t)qo.back() * Hq * q_dim * 2, kv, qo.back(),
+                                     (size_t)(pool->latent_dim + kvx::kLatRope) * 2, (size_t)kv_stride * 2))
+    return report(KVX_EINVAL, "q_out overlaps kv");
   OnDevice on;
   if (int rc = on.enter(pool->device)) return rc;
   if (int rc = check_stream(s, pool->device)) return rc;
@@ -879,6 +903,9 @@ int latent_attention(kvx_latent_pool* pool, const kvx_batch* batch, const void* 
     if (int rc = check_align(out, "out")) return rc;
     if (qo.back() == 0) return KVX_OK;
     if (!q || !out) return report(KVX_EINVAL, "q and out must be non-NULL");
+    if (int rc = check_results(out, (size_t)pool->latent_dim * 2, lse, (size_t)qo.back() * num_q_heads, q,
+                               (size_t)(pool->latent_dim + kvx::kLatRope) * 2))
+      return rc;
     hipStream_t s = (hipStream_t)stream;
     OnDevice on;
     if (int rc = on.enter(pool->device)) return rc;
@@ -927,6 +954,9 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
     if (qo.back() == 0) return KVX_OK;
     if (!q || !out || !proj->w_uk || !proj->w_uv)
       return report(KVX_EINVAL, "q, out, w_uk and w_uv must be non-NULL");
+    if (int rc = check_results(out, (size_t)D * 2, lse, (size_t)qo.back() * Hq, q, (size_t)(D + kvx::kLatRope) * 2,
+                               proj->w_uk, proj->w_uv, (size_t)Hq * D * lat * 2))
+      return rc;
 
     std::vector<bool> takes_absorbed((size_t)batch->num_reqs, form == KVX_LATENT_ABSORBED);
     if (form == KVX_LATENT_AUTO) takes_absorbed = choose_forms(batch, Hq, lat, D, pool->dtype == KVX_LATENT_FP8);

@@ -197,7 +197,7 @@ void many_tokens() {
   const kvx_latent_proj proj{addr(0x300000), addr(0x400000), 4, 64, 64};
   auto call = [&](int form) {
     fake::launched.clear();
-    return latent_extend_attention(pool, t.get(), &proj, addr(0x100000), 0.1f, addr(0x200000), nullptr, form, nullptr);
+    return latent_extend_attention(pool, t.get(), &proj, addr(0x100000), 0.1f, addr(0x800000), nullptr, form, nullptr);
   };
   CHECK(call(KVX_LATENT_EXPANDED) == KVX_EUNSUPPORTED && fake::launched.empty());
   CHECK(call(KVX_LATENT_AUTO) == KVX_OK);
@@ -234,6 +234,45 @@ void choices() {
   }
 }
 
+// Outputs that overlap an input, which other workgroups may still read, or each other.
+void overlaps() {
+  kvx_latent_pool* pool = make_pool(0);
+  TestBatch t;
+  t.add(20, 3);
+  const kvx_batch* b = t.get();
+  const kvx_rope rope{10000.0, nullptr, 64, KVX_ROPE_HALF, nullptr, nullptr, 1e-6f};
+  const uintptr_t q = 0x100000, kv = 0x300000;
+  const uintptr_t q_bytes = 3 * 4 * 128 * 2;
+  auto store = [&](uintptr_t q_out, int64_t stride) {
+    return store_latent_rope(pool, b, &rope, addr(q), 4, 128, addr(q_out), addr(kv), stride, nullptr);
+  };
+  CHECK(store(kv, 320) == KVX_EINVAL);
+  CHECK(store(kv - q_bytes + 16, 320) == KVX_EINVAL && store(kv - q_bytes, 320) == KVX_OK);
+  CHECK(store(kv + 3 * 640 - 16, 320) == KVX_EINVAL && store(kv + 3 * 640, 320) == KVX_OK);
+  CHECK(store(kv + 640, 4096) == KVX_OK);            // between two rows: 3072 bytes of 7552
+  CHECK(store(kv + 8192 - q_bytes, 4096) == KVX_OK);
+  CHECK(store(kv + 624, 4096) == KVX_EINVAL && store(kv + 8192 - q_bytes + 16, 4096) == KVX_EINVAL);
+  CHECK(store(kv + 2 * 8192 + 640, 4096) == KVX_OK && store(kv + 2 * 8192 + 624, 4096) == KVX_EINVAL);
+  auto attend = [&](uintptr_t out, uintptr_t lse) {
+    return latent_attention(pool, b, addr(q), 4, 0.1f, addr(out), (float*)lse, nullptr);
+  };
+  const uintptr_t rows = 3 * 4, o = 0x200000;
+  CHECK(attend(q, 0) == KVX_EINVAL && attend(q + rows * 640 - 16, 0) == KVX_EINVAL);
+  CHECK(attend(q - rows * 512 + 16, 0) == KVX_EINVAL && attend(q - rows * 512, 0) == KVX_OK);
+  CHECK(attend(q + rows * 640, 0) == KVX_OK);
+  CHECK(attend(o, q + 64) == KVX_EINVAL && attend(o, o) == KVX_EINVAL && attend(o, o + rows * 512 - 4) == KVX_EINVAL);
+  CHECK(attend(o, o + rows * 512) == KVX_OK && attend(o, o - rows * 4) == KVX_OK);
+  const uintptr_t uk = 0x400000, uv = 0x500000, w_bytes = 4 * 64 * 256 * 2;
+  const kvx_latent_proj proj{addr(uk), addr(uv), 4, 64, 64};
+  auto extend = [&](uintptr_t out, uintptr_t lse) {
+    return latent_extend_attention(pool, b, &proj, addr(q), 0.1f, addr(out), (float*)lse, KVX_LATENT_AUTO, nullptr);
+  };
+  CHECK(extend(q + 16, 0) == KVX_EINVAL && extend(uk + w_bytes - 16, 0) == KVX_EINVAL && extend(uv, 0) == KVX_EINVAL);
+  CHECK(extend(o, uk) == KVX_EINVAL && extend(o, uv + 16) == KVX_EINVAL && extend(o, o + 16) == KVX_EINVAL);
+  CHECK(extend(o, q) == KVX_EINVAL && extend(o, o + rows * 128) == KVX_OK && extend(q + rows * 256, uv + w_bytes) == KVX_OK);
+  CHECK(latent_pool_destroy(pool) == KVX_OK);
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
@@ -242,6 +281,7 @@ int main(int argc, char** argv) {
   else if (what == "staging") staging();
   else if (what == "tokens") many_tokens();
   else if (what == "choices") choices();
+  else if (what == "overlaps") overlaps();
   else return 2;
   std::printf("%s passed\n", what.c_str());
   return 0;

@@ -55,6 +55,10 @@ def test_automatic_form_is_the_faster_one(driver, tmp_path):
     run_check(driver, "choices", tmp_path)
 
 
+def test_outputs_over_inputs_are_refused(driver, tmp_path):
+    run_check(driver, "overlaps", tmp_path)
+
+
 class OnSecond:
     """What the binding asks of a tensor, of one on the second device."""
 
