@@ -776,3 +776,74 @@ def test_scores_above_float32_give_nan(setup, split, key):
     for form in (kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED):
         check(128, 64, v, lambda q, o, l: kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, 1e20, o, l, form=form),
               RMS_EXTEND)
+
+
+# ------------------------------------------------------------------- many heads of one expansion
+
+
+def heads_a_workgroup(units, heads):
+    """Heads that a workgroup of the expansion takes one after the other: the number that ends
+    first on 256 CUs at a head's time each and half a head's time for the tokens, the largest such."""
+    return min(range(heads, 0, -1), key=lambda per: -(-units * -(-heads // per) // 256) * (per + 0.5))
+
+
+@pytest.mark.parametrize("lat,hd,heads,fp8", [
+    (512, 128, 17, False), (512, 128, 17, True), (512, 64, 23, True), (512, 64, 17, False), (256, 128, 17, True),
+    (256, 64, 29, False)])
+def test_expansion_of_several_heads_a_workgroup(setup, lat, hd, heads, fp8):
+    """Each workgroup forms the keys and values of three heads or more, the last of them of fewer:
+    operands, stores and waits run on from one head to the next."""
+    g = np.random.default_rng(lat + hd + heads)
+    E = g.integers(1, 4, 36).tolist()
+    P = [int(x) - e for x, e in zip(g.integers(4, 120, 36), E)]
+    P[3], P[4] = 256 - E[3], 256  # a whole unit, and one token or a few past it
+    units = sum(-(-(p + e) // 256) for p, e in zip(P, E))
+    per = heads_a_workgroup(units, heads)
+    assert per >= 3 and heads % per != 0
+    s = setup(P, E, lat, fp8)
+    rows = s.fill()
+    q = s.normal(s.T, heads, hd + 64)
+    w_uk, w_uv = (s.normal(heads, hd, lat, scale=lat ** -0.5) for _ in range(2))
+    out = torch.full((s.T + 1, heads, hd), 7.0, dtype=BF16, device=DEV)
+    lse = torch.full((s.T + 1, heads), 7.0, dtype=torch.float32, device=DEV)
+    scale = (hd + 64) ** -0.5
+    kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, scale, out, lse, form=kvx.KVX_LATENT_EXPANDED)
+    assert (out[s.T] == 7).all() and (lse[s.T] == 7).all()
+    qq, uk, uv, at = ref.f64(q), ref.f64(w_uk).reshape(-1, lat), ref.f64(w_uv).reshape(-1, lat), 0
+    for r, (p, e) in enumerate(zip(P, E)):
+        c, key = rows[r][:, :lat], rows[r][:, lat:]
+        k = (c @ uk.T).reshape(-1, heads, hd).transpose(1, 0, 2)
+        k = np.concatenate([k, np.broadcast_to(key, (heads,) + key.shape)], -1)
+        v = (c @ uv.T).reshape(-1, heads, hd).transpose(1, 0, 2)
+        o, l, tol, ltol = ref.attend(qq[at:at + e], k, v, p, scale, k_err=ref.HALF_BF16, v_err=ref.HALF_BF16)
+        ref.check_rows(out[at:at + e], o, tol, RMS_EXTEND, f"request {r}")
+        assert (np.abs(ref.f64(lse[at:at + e]) - l) <= ltol).all(), f"request {r}: lse"
+        at += e
+
+
+@pytest.mark.parametrize("lat,hd,fp8", [(512, 128, True), (256, 64, False)])
+def test_rows_throughout_a_long_suffix(setup, lat, hd, fp8):
+    """A suffix of several tiles of tokens, split keys and several heads a workgroup: the first and
+    last rows, those around every tile's border and some in between."""
+    P, n, heads = 1500, 2300, 35
+    s = setup([P], [n], lat, fp8)
+    rows = s.fill()[0]
+    per = heads_a_workgroup(-(-(P + n) // 256), heads)
+    assert per >= 2
+    q = s.normal(n, heads, hd + 64)
+    w_uk, w_uv = (s.normal(heads, hd, lat, scale=lat ** -0.5) for _ in range(2))
+    out = torch.empty(n, heads, hd, dtype=BF16, device=DEV)
+    lse = torch.empty(n, heads, dtype=torch.float32, device=DEV)
+    scale = (hd + 64) ** -0.5
+    kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, scale, out, lse, form=kvx.KVX_LATENT_EXPANDED)
+    picks = sorted({0, 1, n - 1} | {t + i for t in range(256, n, 256) for i in (-1, 0)} |
+                   set(np.random.default_rng(1).integers(0, n, 12).tolist()))
+    c, key = rows[:, :lat], rows[:, lat:]
+    k = (c @ ref.f64(w_uk).reshape(-1, lat).T).reshape(-1, heads, hd).transpose(1, 0, 2)
+    k = np.concatenate([k, np.broadcast_to(key, (heads,) + key.shape)], -1)
+    v = (c @ ref.f64(w_uv).reshape(-1, lat).T).reshape(-1, heads, hd).transpose(1, 0, 2)
+    for i in picks:
+        o, l, tol, ltol = ref.attend(ref.f64(q[i:i + 1]), k[:, :P + i + 1], v[:, :P + i + 1], P + i, scale,
+                                     k_err=ref.HALF_BF16, v_err=ref.HALF_BF16)
+        ref.check_rows(out[i:i + 1], o, tol, RMS_EXTEND, f"row {i}")
+        assert (np.abs(ref.f64(lse[i:i + 1]) - l) <= ltol).all(), f"row {i}: lse"
