@@ -9,8 +9,8 @@
 // Rows.  A unit holds 16, 32 or 64 rows, by the most that a request has: few rows are bound by
 // HBM, and fewer of them leave registers for more reads ahead; many by the matrix unit and by
 // LDS, from which each product's operands come once a wave.  A decode batch of 128 requests on
-// 16 heads: 339 us with 16 rows, 5.5 TB/s (3.7 TB/s is what a plain reduction of a large buffer
-// reaches here).  64 rows at latent_dim 512: the products of 64 keys are 2176 cycles of the
+// 16 heads: 339 us with 16 rows, 5.5 TB/s read (a large copy reads and writes 5.0 in all, a
+// library's sum of 4 GiB reads 3.7 to 4.0).  64 rows at latent_dim 512: the products of 64 keys are 2176 cycles of the
 // matrix unit, measured 3.8k a step (8-bit: 4.8k, with its conversions), 0.9 to 1.2 PFLOP/s by
 // how evenly a batch fills the CUs; a large library product reaches 1.2 to 1.3.
 //
@@ -229,9 +229,9 @@ __global__ __launch_bounds__(kThreads, 1) void latent_attn_kernel(LatentAttnPara
   constexpr int QS = G::KS * KBW;                   // its steps
   // Direct loads of the next tile, as positions in score steps (half value steps from QS on): over
   // the score product and, of 64 rows, a quarter of the value product (drafts of 32 requests on 64
-  // heads 182 us over three quarters of the scores, 178 over the scores, 174 so), or, where HBM and
-  // not the matrix unit is the bound, all at its start (128 requests on 16 heads: 382 us spread,
-  // 360 us).
+  // heads 182 us over three quarters of the scores, 178 over the scores, 174 so), or, of 16 rows,
+  // where HBM and not the matrix unit is the bound, all at its start (4 requests on 16 heads 18.7 us,
+  // spread 19.0; 128 requests 339 either way).
   constexpr int SPAN = RB == 1 ? 0 : (RB == 4 ? QS * 11 / 9 : QS);
   // operand reads ahead of their products, in steps of the score and of the value product
   constexpr int AK = RBW == 1 ? 8 : 6, AV = RB == 1 ? 8 : (RB == 2 ? 5 : 3);

@@ -420,9 +420,10 @@ double plan_time(const std::vector<Span>& spans, const Split& split, const UnitC
   return end + merge;
 }
 
-// Forced lengths from 256 to 8192 keys against this choice, whole calls in us, best forced
-// length in brackets: decode of 128 requests on 16 heads 353 (352), 24 long requests on 128
-// heads 508 (473), drafts of 32 requests 203 (165, a length that fits this batch by chance).
+// A dozen forced lengths from 512 to 16384 keys against this choice, whole calls in us, best forced
+// length in brackets: decode of 128 requests on 16 heads 339 (352), 24 long requests on 128
+// heads 442 (434), drafts of 32 requests 175 (162, a length that fits this batch by chance),
+// short turns 655 (675).
 Split choose_split(const std::vector<Span>& spans, const UnitCosts& k) {
   int64_t work = 0, longest = 0;
   for (const Span& s : spans) {
@@ -477,9 +478,9 @@ void plan_absorbed(const kvx_batch* b, const std::vector<Member>& members, int32
   int64_t most = 0;
   for (const Member& m : members) most = std::max<int64_t>(most, (int64_t)b->extend_lens[m.req] * Hq);
   // Rows of a unit, as many as the request with the most rows fills.  With 16, 32 and 64 rows:
-  // 128 requests of one token, 4k to 32k keys, 16 heads 481, 491, 515 us; 32 heads 527, 510, 535
-  // (8 bits 337, 342, 460); 4 such requests of 16 heads 18.6, 20.8, 23.4; 32 of 24 heads 44.5,
-  // 44.2, 47.2.  Requests of many rows read their keys once a unit.
+  // 128 requests of one token, 4k to 32k keys, 16 heads 361, 373, 391 us; 32 heads 520, 378, 396
+  // (8 bits 344, 241, 306); 4 requests on 1k to 8k keys, 16 heads 19.8, 21.8, 24.5; 32 of them, 24
+  // heads 48.7, 34.9, 37.8.  Requests of many rows read their keys once a unit.
   plan.row_blocks = most <= 16 ? 1 : (most <= 32 ? 2 : 4);
   const int64_t M = 16 * plan.row_blocks;
   std::vector<Span> spans;

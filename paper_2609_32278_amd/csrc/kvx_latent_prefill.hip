@@ -6,7 +6,7 @@
 // queries sit in the accumulator half of the register file, and keys and values of 64 tokens come
 // through three LDS stages by direct loads.  The exponentials (as long as a third of the products)
 // are formed between the products of the next 32 keys, the loads issued one at a time among them
-// (all at once at the start of a tile: 16 turns of 16 heads 4.66 ms a call against 4.43).
+// (all at once at the start of a tile: calls of 16 turns of 16 heads take 5% more).
 // Measured: 8001 tokens of 128 heads in 2.4 ms, 1.1 PFLOP/s (32 tokens a wave, staged through
 // registers and with nothing overlapped: 7.4 ms), the matrix unit busy 64 to 68% of the cycles at
 // the 2.0 GHz that the power limit leaves.

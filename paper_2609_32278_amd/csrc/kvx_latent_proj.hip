@@ -12,9 +12,11 @@ constexpr int kThreads = 256;
 constexpr int kSlice = 128;  // latent dims per workgroup of the query product
 
 // q' = W_uk^T q, as (W_uk^T) q^T: W's rows run along the latent dims, so its operand is read
-// transposed from LDS.  Workgroup: 64 tokens, one head, 128 latent dims.  Bound by what it
-// writes, (latent_dim + 64) / (head_dim + 64) times what it reads: 900 tokens of 32 heads 30 us
-// (44 MB; 37 with results of 8 bytes a lane and loads of queries behind the barrier).
+// transposed from LDS.  Workgroup: 64 tokens, one head, 128 latent dims.  Bound by latency (its
+// waves wait 61% of their cycles): a workgroup is one chain of loads, a barrier, few products and
+// stores, and every wave of every 128-dim slice reads the queries again.  900 tokens of 32 heads
+// 30 us, 1.6 TB/s of the 48 MB that have to go in and out; counted, 189 MB of requests to L2 and
+// 81 MB to HBM (37 us with results of 8 bytes a lane and loads of queries behind the barrier).
 template <int LAT, int D>
 __global__ __launch_bounds__(kThreads) void latent_absorb_kernel(LatentProjParams p) {
   constexpr int IN = D + kLatRope, OUT = LAT + kLatRope;
@@ -85,7 +87,9 @@ __global__ __launch_bounds__(kThreads) void latent_absorb_kernel(LatentProjParam
 }
 
 // o = W_uv (sum), as W_uv o^T; both operands run along the latent dims.  Workgroup: 64
-// tokens, one head.  Bound by reading the sums: 900 tokens of 32 heads 28 us.
+// tokens, one head.  Bound by latency: 900 tokens of 32 heads are 480 workgroups, two a CU, each
+// a chain of loads and products whose four waves all read the sums.  28 us, 1.5 TB/s of the 41 MB
+// that have to go in and out; counted, 112 MB of requests to L2 and 69 MB to HBM.
 template <int LAT, int D>
 __global__ __launch_bounds__(kThreads) void latent_output_kernel(LatentProjParams p) {
   constexpr int NB = D / 64;  // 16-row blocks of W per wave
