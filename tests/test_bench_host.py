@@ -60,3 +60,14 @@ def test_more_than_one_gpu_is_refused():
                        timeout=300, cwd=ROOT)
     assert r.returncode != 0
     assert "one GPU" in (r.stdout + r.stderr)
+
+
+def test_committed_summaries_are_of_the_present_code():
+    """The benchmark drops the traffic of a summary that is older than the code without a word, so
+    that is found here: take the counters again after a change to those sources."""
+    import glob
+    paths = glob.glob(os.path.join(ROOT, "profiles", "*_hbm_counters.md"))
+    assert paths
+    for path in paths:
+        config = os.path.basename(path)[:-len("_hbm_counters.md")].replace("extend_attn_", "").replace("decode_kernel_", "")
+        assert bench.traffic_from_profiles(config) is not None, path
