@@ -778,6 +778,41 @@ def test_scores_above_float32_give_nan(setup, split, key):
               RMS_EXTEND)
 
 
+@pytest.mark.parametrize("split", [0, 64])
+def test_rows_without_a_score_and_nan_queries(setup, split):
+    """A head whose scores are all -inf gives zeros and an lse of -inf, one with a NaN in its query
+    NaN; the heads beside them in the same unit are what they are without."""
+    s = setup([300], [2], 256, True)
+    kvx.latent_pool_set_split_keys(s.pool, split)
+    rows = s.normal(302, 320)
+    rows[:, 256] = -4.0
+    s.fill(rows=rows)
+    w_uk, w_uv = s.normal(5, 64, 256, scale=1 / 16), s.normal(5, 64, 256, scale=1 / 16)
+
+    def check(dim, width, call):
+        q = s.normal(2, 5, dim)
+        got = []
+        for spoil in (False, True):
+            if spoil:
+                q[:, 1, -64], q[:, 3, 7] = 3e38, math.nan
+            out = torch.full((2, 5, width), 7.0, dtype=BF16, device=DEV)
+            lse = torch.full((2, 5), 7.0, dtype=torch.float32, device=DEV)
+            call(q, out, lse)
+            got.append((ref.f64(out), ref.f64(lse)))
+        (o, l), (po, pl) = got
+        assert (po[:, 1] == 0).all() and (pl[:, 1] == -math.inf).all()
+        assert np.isnan(po[:, 3]).all() and np.isnan(pl[:, 3]).all()
+        # a unit that is run again has another reference point: the roundings of the weights differ
+        for h in (0, 2, 4):
+            assert np.linalg.norm(po[:, h] - o[:, h]) <= 2 * RMS_EXTEND * np.linalg.norm(o[:, h])
+            # two float32 sums of 302 weights
+            assert np.abs(pl[:, h] - l[:, h]).max() <= 2 * (302 + 16) * ref.F32
+
+    check(320, 256, lambda q, o, l: kvx.latent_attention(s.pool, s.batch, q, 5, 0.07, o, l))
+    for form in (kvx.KVX_LATENT_ABSORBED, kvx.KVX_LATENT_EXPANDED):
+        check(128, 64, lambda q, o, l: kvx.latent_extend_attention(s.pool, s.batch, q, w_uk, w_uv, 0.09, o, l, form=form))
+
+
 # ------------------------------------------------------------------- many heads of one expansion
 
 
