@@ -72,8 +72,19 @@ enum kvx_status {
 
 enum kvx_kv_dtype {
     KVX_KV_BF16 = 0,     /* K/V stored as bf16 */
-    KVX_KV_FP8_E4M3 = 1  /* K/V stored as OCP e4m3 (fp8, max 448, no inf) with per-head scales */
+    KVX_KV_FP8_E4M3 = 1, /* K/V stored as OCP e4m3 (fp8, max 448, no inf) with per-head scales */
+    KVX_KV_FP8_PAGE = 2  /* K/V stored as e4m3 with a power of two for every page and KV head, one of
+                            K and one of V, which the stores find ("page-scaled") */
 };
+
+/* Page-scaled pools.  A page and KV head holds code * 2^e, one e for its K and one for its V:
+ * the smallest integer with max|x| <= 448 * 2^e over the values that the page then holds, kept
+ * within [-117, 119].  A store that begins in the middle of a page takes the page's tokens
+ * before it, as the page holds them, into that maximum, and where e moves they are rounded
+ * again (only values below 2^-6 * 2^e can change).  Each new value is stored as
+ * e4m3(clamp(x * 2^-e, -448, 448)), rounded to nearest even, NaN as NaN (it counts for no
+ * maximum).  The slots of a written page past the batch's last token of the request become
+ * zero.  Every stored value is a bf16 number: the attention and load_kv read it exactly. */
 
 /* ------------------------------------------------------------------ the pool */
 
@@ -93,8 +104,8 @@ typedef struct {
     int32_t reserved;
     int64_t k_stride_page, k_stride_head, k_stride_slot, k_stride_dim;
     int64_t v_stride_page, v_stride_head, v_stride_slot, v_stride_dim;
-    const float *k_scale;  /* device [num_kv_heads], NULL for bf16 */
-    const float *v_scale;  /* device [num_kv_heads], NULL for bf16 */
+    const float *k_scale;  /* device [num_kv_heads], NULL for bf16.  Page-scaled pool: the power of */
+    const float *v_scale;  /* two of (page, head) is entry 2 * (page * num_kv_heads + head) */
 } kvx_pool_layout;
 
 /*
@@ -104,9 +115,10 @@ typedef struct {
  *   page_size     must be 16.
  *   num_kv_heads  >= 1.
  *   head_dim      64 or 128.
- *   kv_dtype      KVX_KV_BF16 or KVX_KV_FP8_E4M3.
+ *   kv_dtype      KVX_KV_BF16, KVX_KV_FP8_E4M3 or KVX_KV_FP8_PAGE.
  *   k_scale, v_scale  host [num_kv_heads] positive finite dequantisation scales
- *                 for the fp8 pool (stored value = code * scale); NULL for bf16.
+ *                 for the fp8 pool (stored value = code * scale); NULL for bf16 and for
+ *                 a page-scaled pool.
  *   out           receives the handle.
  * The pool's contents are zero after creation.  Synchronous.  Errors: EINVAL,
  * EUNSUPPORTED (page_size != 16, head_dim not 64/128), ENOMEM, EHIP.
@@ -125,7 +137,9 @@ int kv_pool_layout(const kvx_pool *pool, kvx_pool_layout *out);
  * for both K and V, in the pool's element type (bf16 bits or fp8 codes); the
  * library converts to and from its own V layout.  Neither call converts values.
  *   page_ids   host [n] physical page ids (each in [0, num_pages); always checked)
- *   k_*, v_*   device buffers of n * num_kv_heads * page_size * head_dim elements
+ *   k_*, v_*   device buffers of n * num_kv_heads * page_size * head_dim elements; on a
+ *              page-scaled pool each goes on with the pages' scales, float [n][num_kv_heads]
+ *              (to be written as they were read: powers of two, 2^-117 to 2^119, or 0)
  * Asynchronous on `stream`.  Errors: EINVAL, ERANGE, ENOMEM, EHIP.
  */
 int kv_pool_write_pages(kvx_pool *pool, const int32_t *page_ids, int64_t n, const void *k_src,
@@ -138,7 +152,7 @@ int kv_pool_read_pages(const kvx_pool *pool, const int32_t *page_ids, int64_t n,
  * (the paper's stated future work, Section 6: keep evicted KV in a slower tier
  * and bring it back).  A spill record holds one page exactly as the pool holds
  * it -- its K block then its V block, kv_pool_record_bytes() bytes, raw (bf16 or
- * fp8 codes; the scales stay with the pool) -- so spill + reload is a bit-exact
+ * fp8 codes; the scales of heads stay with the pool, those of a page are in its record) -- so spill + reload is a bit-exact
  * round trip into any page of a pool of the same shape and dtype.
  *   kv_pool_spill:  record slots[i] of host := page page_ids[i]
  *   kv_pool_reload: page page_ids[i] := record slots[i] of host
@@ -176,13 +190,25 @@ typedef struct {
  * the token at absolute position t = P_r + i goes to slot t % 16 of logical page
  * t / 16.  bf16 pool: the bits are copied.  fp8 pool: each element is stored as
  * e4m3(clamp(float(x) * float(1/scale_h), -448, 448)), rounded to nearest even.
- * Slots not written by the batch keep their contents.
+ * Slots not written by the batch keep their contents.  Page-scaled pool: see there.
  *   k_ext, v_ext  device bf16 [T, num_kv_heads, head_dim], T = sum E_r.
  * Must precede extend_attention of the same batch on the same stream.
  * Errors: EINVAL, ERANGE (validation mode), ENOMEM, EHIP.  R = 0 or T = 0: no-op.
  */
 int store_kv(kvx_pool *pool, const kvx_batch *batch, const void *k_ext, const void *v_ext,
              kvx_stream_t stream);
+
+/*
+ * Read tokens back: row i of request r's E_r rows is token P_r + i of its sequence in the pool,
+ * as bf16 [num_kv_heads][head_dim]: the bits of a bf16 pool, code * scale of an fp8 pool rounded to
+ * nearest even, the stored values of a page-scaled pool exactly.
+ *   k_out, v_out  device bf16 [T, num_kv_heads, head_dim], T = sum E_r; they do not overlap
+ * Runs on the pool's device and leaves the caller's current device as it was; a stream of
+ * another device is refused (EINVAL), and one that is being captured into a HIP graph
+ * (EUNSUPPORTED).  Errors: EINVAL, EUNSUPPORTED, ERANGE (validation mode), ENOMEM, EHIP.
+ * R = 0 or T = 0: no-op.
+ */
+int load_kv(const kvx_pool *pool, const kvx_batch *batch, void *k_out, void *v_out, kvx_stream_t stream);
 
 /* Layout of the rotation planes of a head (see store_kv_rope). */
 enum {
@@ -211,8 +237,8 @@ typedef struct {
  *   (mean over all head_dim dims), then rotated: each plane (a, b) of the first
  *   rotary_dim dims turns by t * f_j:  (a cos - b sin, a sin + b cos).
  * The rotated K is stored as store_kv stores K (bf16 round-to-nearest-even, or
- * e4m3 of float(y) * float(1/scale) on an fp8 pool); V is stored exactly as by
- * store_kv; the rotated Q goes to q_out as bf16 (round to nearest even).
+ * e4m3 of float(y) * float(1/scale) on an fp8 pool, or from float(y) as a page-scaled pool
+ * has it); V is stored exactly as by store_kv; the rotated Q goes to q_out as bf16 (round to nearest even).
  * Arithmetic is float32, with every angle reduced to one turn in float64 first,
  * and each result is rounded once.
  *   q, q_out     device bf16 [T, num_q_heads, head_dim]; q_out may be q itself
@@ -282,6 +308,27 @@ int extend_attention(kvx_pool *pool, const kvx_batch *batch, const void *q, int3
 int extend_attention_noalloc(kvx_pool *pool, const kvx_batch *batch, const void *q, int32_t num_q_heads,
                              float sm_scale, void *out, float *lse, kvx_stream_t stream);
 
+/*
+ * Cross attention: queries that are not in the pool themselves attend to every token that
+ * their request holds there -- an encoder's states, stored by store_kv, of another length than
+ * the queries.  For each request r, query row i and query head hq,
+ *   o = softmax_j(sm_scale * q . k_j) v_j   over tokens j = 0 .. L_r - 1,
+ * without a causal mask.
+ *   batch   prefix_lens[r] is L_r, the tokens in the pool, and extend_lens[r] the request's
+ *           queries E_r; its pages are ceil(L_r / 16) (more may be listed)
+ *   q, num_q_heads, sm_scale, out, lse   as for extend_attention, T = sum E_r
+ * A request without tokens (L_r = 0) gives zeros, and an lse of -inf.
+ * The queries' number has no part in how a row is computed beyond the order of its sums.
+ * All pool types; kv_pool_set_split_keys and kv_pool_set_scaled_q (for the requests with more
+ * queries than a few) hold here too.  out and lse overlap neither q nor each other (EINVAL).
+ * Runs on the pool's device and leaves the caller's current device as it was; a stream of
+ * another device is refused (EINVAL), and one that is being captured into a HIP graph
+ * (EUNSUPPORTED).  Errors: EINVAL, EUNSUPPORTED, ERANGE (validation mode), ENOMEM, EHIP.
+ * R = 0 or T = 0: no-op.
+ */
+int cross_attention(kvx_pool *pool, const kvx_batch *batch, const void *q, int32_t num_q_heads, float sm_scale,
+                    void *out, float *lse, kvx_stream_t stream);
+
 /* ---------------------------------------------------------- planning, tuning */
 
 /* One work item of extend_attention: a tile of suffix tokens of one request and
@@ -326,7 +373,7 @@ int extend_attention_plan(const kvx_batch *batch, int32_t num_q_heads, int32_t n
 int kv_pool_set_split_keys(kvx_pool *pool, int32_t keys);
 
 /*
- * Scaled-Q softmax of extend_attention's prefill launches on a bf16 pool (0 =
+ * Scaled-Q softmax of extend_attention's prefill launches on a bf16 or page-scaled pool (0 =
  * off, the default; 1 = on).  When on, each query is multiplied by
  * c = float32(sm_scale * float32(log2 e)) in float32 and rounded to bf16 (round to
  * nearest even) when it is loaded, and the scores of those queries are taken in
@@ -334,7 +381,7 @@ int kv_pool_set_split_keys(kvx_pool *pool, int32_t keys);
  * instruction per (query, key) pair, about 5% of the kernel time on long key
  * ranges, and adds one more bf16 rounding of q (2^-9 relative per element): the
  * error against the exact attention grows where scores are large (about twice
- * the default's at query scale 4).  The prefill kernel of an fp8 pool always takes
+ * the default's at query scale 4).  extend_attention's prefill kernel of an fp8 pool with a scale a head always takes
  * this form (its e4m3 keys dominate the error), and decode steps (and one-token
  * suffixes that take the decode code) are always exact.  The softmax itself (Section 2's prefill over the uncached suffix) is
  * unchanged.  A setting of the pool: takes effect for calls queued after it, from

@@ -73,6 +73,11 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeParams p) {
 hipError_t launch_extend_attention(const AttnParams& p, int64_t n_units, int head_dim, bool fp8, bool scaled_q,
                                    hipStream_t stream) {
   if (n_units <= 0) return hipSuccess;
+  if (p.cross) {
+    if (p.page_scaled) return launch_cross_page_attention(p, n_units, head_dim, scaled_q, stream);
+    return launch_cross_attention(p, n_units, head_dim, fp8, scaled_q, stream);
+  }
+  if (p.page_scaled) return launch_page_attention(p, n_units, head_dim, scaled_q, stream);
   if (p.compact != nullptr) return launch_small_attention(p, n_units, head_dim, fp8, scaled_q, stream);
   if (p.mixed) return launch_mixed_attention(p, n_units, head_dim, fp8, scaled_q, stream);
   launch_attn<false>(p, UnitsInMemory{}, n_units, head_dim, fp8, scaled_q, stream);

@@ -108,14 +108,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// 8 fp8 e4m3 codes -> 8 bf16, two per instruction with a unit scale (exact: every
+// 8 fp8 e4m3 codes -> 8 bf16, two per instruction, times a power of two (exact: every
 // e4m3 value is a bf16 value)
-__device__ __forceinline__ uint4 fp8x8_to_bf16x8(uint2 c) {
+__device__ __forceinline__ uint4 fp8x8_to_bf16x8(uint2 c, float by = 1.0f) {
   uint4 r;
-  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, 1.0f, false));
-  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, 1.0f, true));
-  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, 1.0f, false));
-  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, 1.0f, true));
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, by, false));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, by, true));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, by, false));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, by, true));
   return r;
 }
 
@@ -205,6 +205,17 @@ __device__ __forceinline__ void lds_dma_16(const char* sbase, int voff, uint32_t
       "s_mov_b32 m0, %0\n\t"
       "s_nop 0\n\t"
       "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(lds), "v"(voff), "s"(sbase)
+      : "memory", "m0");
+}
+
+// The same for one word a lane, at LDS address lds + 4 l.
+__device__ __forceinline__ void lds_dma_4(const char* sbase, int voff, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %1, %2"
       :
       : "s"(lds), "v"(voff), "s"(sbase)
       : "memory", "m0");
@@ -410,6 +421,19 @@ __device__ __forceinline__ void folded_rescale(f32x16 (&st)[kKB], f32x16 (&o)[Ge
   }
 }
 
+// The same for the exact form, before a tile of maximum m_tile (log2 units) is exponentiated.
+template <int D>
+__device__ __forceinline__ void exact_rescale(f32x16 (&o)[Geom<D>::DB], float m_tile, float& m_run, float& l_run) {
+  if (__any(m_tile > m_run + kRescaleThreshold)) {
+    const float m_new = fmaxf(m_run, m_tile);
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+    l_run *= alpha;
+#pragma unroll
+    for (int b = 0; b < Geom<D>::DB; b++) o[b] *= alpha;
+    m_run = m_new;
+  }
+}
+
 // The work item of this workgroup (scalar loads: every index derived from it stays
 // uniform) and the lane's query row within it.
 struct Rows {
@@ -424,13 +448,16 @@ struct Rows {
 };
 
 // Where the units are: in memory (AttnParams::units), or written out from the compact plan
-// in the kernel's arguments, which follow AttnParams there.
+// in the kernel's arguments, which follow AttnParams there.  Of a cross attention: every row
+// of a unit sees the keys up to q_pos0.
 struct UnitsInMemory {};
+struct CrossUnitsInMemory {};
+struct CrossCompactPlan : CompactPlan {};
 
 template <class Plan>
 __device__ __forceinline__ Rows rows_of(const AttnParams& p, const Plan& plan) {
   Rows r;
-  if constexpr (std::is_same_v<Plan, CompactPlan>) {
+  if constexpr (std::is_base_of_v<CompactPlan, Plan>) {
     const const_i32_ptr words =
         (const_i32_ptr)((const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() +
                         sizeof(AttnParams) + offsetof(CompactPlan, words));
@@ -456,7 +483,8 @@ __device__ __forceinline__ Rows rows_of(const AttnParams& p, const Plan& plan) {
   r.tok = r.rho / p.group;
   r.hq = r.kv_head * p.group + (r.rho - r.tok * p.group);
   r.valid = r.tok < r.ntok;
-  r.qpos = r.u.q_pos0 + r.tok;
+  constexpr bool kCross = std::is_same_v<Plan, CrossUnitsInMemory> || std::is_same_v<Plan, CrossCompactPlan>;
+  r.qpos = kCross ? r.u.q_pos0 : r.u.q_pos0 + r.tok;
   return r;
 }
 
@@ -552,7 +580,7 @@ __device__ __forceinline__ void write_result(const AttnParams& p, const Rows& r,
 // 427 us, the decoding ones 308 us.
 
 // Run the workgroup's unit if it is a decode unit.
-template <int D, bool FP8>
+template <int D, bool FP8, bool PAGE = false>
 __device__ __forceinline__ bool run_decode_unit(const AttnParams& p, uint8_t* o_lds, uint8_t* ml_lds) {
   const const_i32_ptr w = (const_i32_ptr)(p.units + blockIdx.x);
   const int head_ntok = w[5];
@@ -580,7 +608,7 @@ __device__ __forceinline__ bool run_decode_unit(const AttnParams& p, uint8_t* o_
   d.group = p.group;
   d.scale_log2 = p.scale_log2;
   const decode::CombineShared<D, kWaves> sm{(float*)o_lds, (float*)ml_lds, (float*)ml_lds + kWaves * decode::kRows};
-  if constexpr (FP8) decode::decode_unit_fp8<D, kWaves, true>(d, u, sm, decode::PlainLoads{});
+  if constexpr (FP8) decode::decode_unit_fp8<D, kWaves, true, PAGE>(d, u, sm, decode::PlainLoads{});
   else decode::decode_unit<D, kWaves, true>(d, u, sm, decode::PlainLoads{});
   return true;
 }
@@ -882,6 +910,8 @@ struct Geom8 {
   static_assert(NDMA >= 1 && (2 * KINSTR) % kWaves == 0, "direct loads must spread evenly over waves");
 };
 
+constexpr int kScaleBytes = 256;  // of a wave's scales in a staging slot: a word a lane
+
 // One wave's direct load of a pair: load g = wave + 8 * it is K load g (g < KINSTR)
 // or V load g - KINSTR; lane l of load j moves 16 codes to staging byte
 // 1024 j + 16 l of the tile's region.
@@ -921,7 +951,9 @@ struct CodeLoad {
 //      s = h ^ ((d >> 3) & 1): codes at byte 16 d + 8 s of the V codes.
 // Chunk Q + 512 sits 4096 code bytes further in both (the row swizzle repeats), and
 // its V slots 4096 / D keys later.
-template <int D>
+// PAGE: chunks Q = 64 (wave * NCONV + k) + lane instead, all in page wave / 2 of the tile.  K's
+// next 64 chunks are four rows on, which turns bit 2 of the swizzle.
+template <int D, bool PAGE = false>
 struct ConvLane {
   static constexpr int NCONV = Geom<D>::TILE_BYTES / 16 / kAttnThreads;  // chunks per lane and tile
   static_assert(NCONV >= 1 && Geom<D>::TILE_BYTES % (16 * kAttnThreads) == 0, "conversion must spread evenly");
@@ -929,6 +961,12 @@ struct ConvLane {
   int ksrc;  // byte offset of the lane's K codes in the K codes of a staging slot
   int vsrc;  // byte offset of the lane's V codes in the V codes
   int vkey;  // key offset of the lane's first V slot in the tile
+  __device__ __forceinline__ static int first_chunk(int wave, int lane) { return 64 * (PAGE ? wave * NCONV : wave) + lane; }
+  // chunk k of the lane, from its first one: bytes of the bf16 tile; of the K codes, of the V codes
+  __device__ __forceinline__ static constexpr int step(int k) { return (PAGE ? 1024 : 8192) * k; }
+  __device__ __forceinline__ int k_at(int k) const { return PAGE ? (ksrc ^ (32 * k)) + 4 * D * k : ksrc + 4096 * k; }
+  __device__ __forceinline__ int v_at(int k) const { return vsrc + (PAGE ? 512 : 4096) * k; }
+  __device__ __forceinline__ int v_key(int k) const { return vkey + (PAGE ? 0 : (4096 / D) * k); }
   __device__ __forceinline__ void init(int L) {
     using G = Geom<D>;
     const int r = L / G::CPR, pch = L % G::CPR;
@@ -951,20 +989,30 @@ __device__ __forceinline__ uint4 zero_past(uint4 x, int key, int key_end) {
   return x;
 }
 
-template <int D, bool MIXED, class Plan>
+// PAGE: a page-scaled pool.  The powers of two go into the conversion, which takes one anyway, and
+// neither into Q nor into the result: scores and outputs are of the values themselves.  A wave
+// converts codes of one page of a tile only (ConvLane), and fetches that page's two scales with
+// the codes, by one more direct load into LDS per pair.  (As scalar loads they miss the scalar
+// cache, pages being anywhere, and each LDS wait after them waits for them too: 16 turns of 18155
+// tokens in all on 249k, 32/8/128 heads, 4430 us with those.)
+// SQ: the folded form (always in the causal kernels of a pool with a scale a head).  Without it Q
+// goes in as it is and the scores are scaled in float32, as in the bf16 kernel.
+template <int D, bool MIXED, class Plan, bool PAGE = false, bool SQ = true>
 __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnParams p, Plan plan) {
   using G = Geom<D>;
   using G8 = Geom8<D>;
   // one block, bf16 buffers first: every MFMA operand read and conversion write then
   // lies below 64 KiB and addresses with an immediate offset
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * G8::NBUF * G::TILE_BYTES + G8::NSTG * G8::PAIR];
+  constexpr int SLOT = G8::PAIR + (PAGE ? kWaves * kScaleBytes : 0);  // a staging slot, with each wave's scales
+  constexpr int LOADS = G8::NDMA + (PAGE ? 1 : 0);                    // direct loads per wave and pair
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * G8::NBUF * G::TILE_BYTES + G8::NSTG * SLOT];
   uint8_t(*k_lds)[G::TILE_BYTES] = (uint8_t(*)[G::TILE_BYTES])lds;
   uint8_t(*v_lds)[G::TILE_BYTES] = (uint8_t(*)[G::TILE_BYTES])(lds + G8::NBUF * G::TILE_BYTES);
-  uint8_t(*stg)[G8::PAIR] = (uint8_t(*)[G8::PAIR])(lds + 2 * G8::NBUF * G::TILE_BYTES);
+  uint8_t(*stg)[SLOT] = (uint8_t(*)[SLOT])(lds + 2 * G8::NBUF * G::TILE_BYTES);
   if constexpr (MIXED) {
     constexpr int O_BYTES = sizeof(float) * kWaves * decode::kRows * D;
     static_assert(sizeof lds >= O_BYTES + 2 * sizeof(float) * kWaves * decode::kRows, "the decode combine fits");
-    if (run_decode_unit<D, true>(p, lds, lds + O_BYTES)) return;
+    if (run_decode_unit<D, true, PAGE>(p, lds, lds + O_BYTES)) return;
   }
 
   const Rows r = rows_of(p, plan);
@@ -975,9 +1023,10 @@ __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnPa
               r.kv_head};
   // Q times softmax scale (log2 units) times k_scale: the products come out in the
   // exponent's units
-  const float vscale = p.v_scale[r.kv_head];
+  const float vscale = PAGE ? 1.0f : p.v_scale[r.kv_head];
+  const float scale = PAGE ? p.scale_log2 : p.scale_log2 * p.k_scale[r.kv_head];
   bf16x8 qf[G::KSTEPS];
-  load_q<D, true>(qf, p, r, p.scale_log2 * p.k_scale[r.kv_head]);
+  load_q<D, SQ>(qf, p, r, scale);
   int koff[G::KSTEPS];
   k_offsets<D>(koff, r.n, h);
   const int vbase = v_offset(r.n, h);
@@ -1006,8 +1055,9 @@ __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnPa
     head_base[it] = (const char*)(ld[it].is_v ? p.v_pool : p.k_pool) + (size_t)r.kv_head * (kPageSize * D);
   }
   // the bf16 chunks this lane converts: 16 L (+ 8192 k) of each tile
-  const int L = wave * 64 + lane;
-  ConvLane<D> cv;
+  using Conv = ConvLane<D, PAGE>;
+  const int L = Conv::first_chunk(wave, lane);
+  Conv cv;
   cv.init(L);
   const int lp0 = (int)((uint32_t)kb0 / kPageSize);
   // tile of pair s that load `it` fetches: K(s+1) or V(s)
@@ -1021,8 +1071,29 @@ __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnPa
     lds_dma_16(block, ld[it].off, lds);
   };
   // load pair s (tiles that do not exist are skipped); returns the loads issued
+  // PAGE: the scales of K(s+1) and V(s) of the page that this wave converts, K's in the slot's even
+  // words and V's in its odd ones; scale_page: that page of the two tiles
+  uint32_t scale_page_k = 0, scale_page_v = 0;
+  const char* const scales = PAGE ? (const char*)p.k_scale + 8 * (size_t)r.kv_head : nullptr;
+  auto scale_off = [&]() -> int {
+    return (int)(((lane & 1) ? scale_page_v : scale_page_k) * (8u * (uint32_t)p.num_kv_heads)) + 4 * (lane & 1);
+  };
+  auto scale_dma = [&](uint8_t* slot, int off) {
+    lds_dma_4(scales, off, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)(slot + G8::PAIR + wave * kScaleBytes));
+  };
+  auto next_scale_page = [&](int tt) {  // tile of the next pair's K
+    scale_page_v = scale_page_k;
+    scale_page_k = (uint32_t)page_of(c, lp0 + tt * (kBN / kPageSize) + wave / 2);
+  };
   auto issue = [&](int s) -> int {
     int n = 0;
+    if constexpr (PAGE) {
+      if (s < n_tiles) {
+        scale_dma(stg[s & 3], scale_off());
+        next_scale_page(s + 2);
+        n++;
+      }
+    }
 #pragma unroll
     for (int it = 0; it < G8::NDMA; it++) {
       const int tt = tile_of(it, s);
@@ -1039,17 +1110,19 @@ __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnPa
     constexpr bool WHOLE = decltype(whole)::value;
     const bool k_in = WHOLE || (s + 1 >= 0 && s + 1 < n_tiles);  // K(s+1) exists
     const bool v_in = WHOLE || (s >= 0 && s < n_tiles);          // V(s) exists
+    float2 by = make_float2(1.0f, 1.0f);
+    if constexpr (PAGE) by = *(const float2*)(src + G8::PAIR + wave * kScaleBytes);
 #pragma unroll
-    for (int k = 0; k < ConvLane<D>::NCONV; k++) {
+    for (int k = 0; k < Conv::NCONV; k++) {
       if (k_in) {
-        const uint2 c = *(const uint2*)(src + cv.ksrc + 4096 * k);
-        *(uint4*)(kdst + 16 * L + 8192 * k) = fp8x8_to_bf16x8(c);
+        const uint2 c = *(const uint2*)(src + cv.k_at(k));
+        *(uint4*)(kdst + 16 * L + Conv::step(k)) = fp8x8_to_bf16x8(c, by.x);
       }
       if (v_in) {
-        const uint2 c = *(const uint2*)(src + G8::TILE_CODES + cv.vsrc + 4096 * k);
-        uint4 x = fp8x8_to_bf16x8(c);
-        if (!WHOLE && s >= last_whole) x = zero_past(x, kb0 + s * kBN + cv.vkey + (4096 / D) * k, u.key_end);
-        *(uint4*)(vdst + 16 * L + 8192 * k) = x;
+        const uint2 c = *(const uint2*)(src + G8::TILE_CODES + cv.v_at(k));
+        uint4 x = fp8x8_to_bf16x8(c, by.y);
+        if (!WHOLE && s >= last_whole) x = zero_past(x, kb0 + s * kBN + cv.v_key(k), u.key_end);
+        *(uint4*)(vdst + 16 * L + Conv::step(k)) = x;
       }
     }
   };
@@ -1060,18 +1133,19 @@ __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnPa
     constexpr bool FIXED = decltype(fixed)::value;
 #pragma unroll
     for (int b = 0; b < G::DB; b++) o[b] = f32x16{};
-    m_run = 0.0f;
+    m_run = SQ ? 0.0f : -1e30f;
     l_run = 0.0f;
     cneg = f32x16{};
     // ---- prologue: pairs -1 = {K(0)}, 0, 1, 2 loaded; -1 and 0 converted (K(0), K(1),
     // V(0) in bf16), 1 resident, 2 in flight
 #pragma unroll
     for (int it = 0; it < G8::NDMA; it++) pid[it] = page_for(it, 0);
+    if constexpr (PAGE) next_scale_page(0);
     issue(-1);
     issue(0);
     issue(1);
     const int in_flight = issue(2);
-    wait_issued<G8::NDMA>(in_flight);
+    wait_issued<LOADS>(in_flight);
     __syncthreads();
     convert(-1, False{}, stg[3], k_lds[0], v_lds[1]);
     convert(0, False{}, stg[0], k_lds[1], v_lds[0]);
@@ -1081,9 +1155,10 @@ __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnPa
     bf16x8 pb[2 * kKB];
     qk_tile<D>(sa, k_lds[0], koff, qf, cneg);
     mx = n_full > 0 ? row_max<false>(sa, kb0, qpos, h) : row_max<true>(sa, kb0, qpos, h);
-    set_reference(sa, mx, m_run, cneg);
+    if constexpr (SQ) set_reference(sa, mx, m_run, cneg);
+    else if constexpr (FIXED) m_run = mx * scale;
+    if constexpr (FIXED && !SQ) prescale(sa, scale, m_run);
     __syncthreads();  // every wave has read K(0) before iteration 0 converts K(2) into its buffer
-
 
     // One pipelined iteration: consumes S(t), produces S(t+1) from bf16 K(t+1) (in the
     // second pass with its maximum), accumulates P(t) V(t), loads pair t+3 and
@@ -1104,40 +1179,50 @@ __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnPa
       const int k0 = kb0 + t * kBN;
       const bool has_next = MASKED ? t + 1 < n_tiles : true;
       constexpr bool SPREAD = WHOLE && !MASKED;
-      int issued = G8::NDMA;
+      int issued = LOADS;
       const char* blk[G8::NDMA];
+      int scale_at = 0;
       if constexpr (SPREAD) {
+        if constexpr (PAGE) scale_at = scale_off();
 #pragma unroll
         for (int it = 0; it < G8::NDMA; it++) blk[it] = page_block(head_base[it], pid[it], page_bytes);
       } else {
         issued = issue(t + 3);
       }
-      if constexpr (!FIXED) folded_rescale<D>(s_cur, o, mx, m_run, l_run, cneg);
+      if constexpr (!FIXED) {
+        if constexpr (SQ) folded_rescale<D>(s_cur, o, mx, m_run, l_run, cneg);
+        else exact_rescale<D>(o, mx * scale, m_run, l_run);
+      }
+      constexpr bool PRE = FIXED && !SQ;  // the exponents are formed beside the PV products, as in the bf16 kernel
       if constexpr (SPREAD) {
         qk_tile<D>(s_nxt, k_lds[buf(1)], koff, qf, cneg, [&](int i) {
           if (i < G8::NDMA) dma(i, stg[slot_of(3)], blk[i]);
+          if (PAGE && i == G8::NDMA) scale_dma(stg[slot_of(3)], scale_at);
         });
       } else {
         if (!MASKED || has_next) qk_tile<D>(s_nxt, k_lds[buf(1)], koff, qf, cneg);
       }
       convert(t + 1, whole, stg[slot_of(1)], k_lds[buf(2)], v_lds[buf(1)]);
-      l_run = exp_pack<true>(s_cur, pb, l_run, m_run, 0.0f);
+      l_run = exp_pack<SQ || PRE>(s_cur, pb, l_run, m_run, scale);
       pv_tile<D>(o, v_lds[buf(0)], vbase, pb);
       if constexpr (MASKED) {
         if (has_next) {
           if constexpr (FIXED) causal_mask(s_nxt, k0 + kBN, qpos, h);
           else mx = row_max<true>(s_nxt, k0 + kBN, qpos, h);
+          if constexpr (PRE) prescale(s_nxt, scale, m_run);
         }
-      } else if constexpr (!FIXED) {
-        mx = row_max<false>(s_nxt, k0 + kBN, qpos, h);
+      } else {
+        if constexpr (!FIXED) mx = row_max<false>(s_nxt, k0 + kBN, qpos, h);
+        if constexpr (PRE) prescale(s_nxt, scale, m_run);
       }
       if constexpr (SPREAD) {
 #pragma unroll
         for (int it = 0; it < G8::NDMA; it++) pid[it] = page_for(it, tile_of(it, t + 4));
+        if constexpr (PAGE) next_scale_page(t + 5);
       }
       // pair t+2 (loaded one iteration ago) is converted in the next iteration
-      if constexpr (WHOLE) wait_vmcnt<G8::NDMA>();
-      else wait_issued<G8::NDMA>(issued);
+      if constexpr (WHOLE) wait_vmcnt<LOADS>();
+      else wait_issued<LOADS>(issued);
       // each iteration keeps its own softmax work (as in the bf16 kernel's folded form)
       __builtin_amdgcn_sched_barrier(0);
       __syncthreads();
@@ -1208,6 +1293,20 @@ void launch_attn(const AttnParams& p, const Plan& plan, int64_t n_units, int hea
     if (fp8) hipLaunchKernelGGL((extend_attn_fp8_kernel<64, MIXED, Plan>), grid, block, 0, stream, p, plan);
     else if (scaled_q) hipLaunchKernelGGL((extend_attn_kernel<64, true, MIXED, Plan>), grid, block, 0, stream, p, plan);
     else hipLaunchKernelGGL((extend_attn_kernel<64, false, MIXED, Plan>), grid, block, 0, stream, p, plan);
+  }
+}
+
+// The 8-bit kernel in either form.
+template <bool PAGE, bool MIXED, class Plan>
+void launch_attn8(const AttnParams& p, const Plan& plan, int64_t n_units, int head_dim, bool scaled_q,
+                      hipStream_t stream) {
+  const dim3 grid((unsigned)n_units), block(kAttnThreads);
+  if (head_dim == 128) {
+    if (scaled_q) hipLaunchKernelGGL((extend_attn_fp8_kernel<128, MIXED, Plan, PAGE, true>), grid, block, 0, stream, p, plan);
+    else hipLaunchKernelGGL((extend_attn_fp8_kernel<128, MIXED, Plan, PAGE, false>), grid, block, 0, stream, p, plan);
+  } else {
+    if (scaled_q) hipLaunchKernelGGL((extend_attn_fp8_kernel<64, MIXED, Plan, PAGE, true>), grid, block, 0, stream, p, plan);
+    else hipLaunchKernelGGL((extend_attn_fp8_kernel<64, MIXED, Plan, PAGE, false>), grid, block, 0, stream, p, plan);
   }
 }
 

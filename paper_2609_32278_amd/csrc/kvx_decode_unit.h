@@ -50,12 +50,19 @@ __device__ __forceinline__ float group_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// 8 fp8 e4m3 codes -> 8 bf16 (exact: e4m3 values are bf16 values)
-__device__ __forceinline__ uint4 fp8x8_bf16(uint2 c) {
-  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, 1.0f, false)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, 1.0f, true)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, 1.0f, false)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, 1.0f, true)));
+// 8 fp8 e4m3 codes -> 8 bf16, times a power of two (exact: e4m3 values are bf16 values)
+__device__ __forceinline__ uint4 fp8x8_bf16(uint2 c, float by = 1.0f) {
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, by, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, by, true)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, by, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, by, true)));
+}
+
+// Row n of a unit's queries among all of them (see combine_waves).
+template <bool CROSS>
+__device__ __forceinline__ size_t query_row(const DecodeArgs& p, const DecodeUnit& u, int n) {
+  if constexpr (CROSS) return (size_t)(u.qo_row + n / p.group) * p.num_q_heads + u.head * p.group + n % p.group;
+  else return (size_t)u.qo_row * p.num_q_heads + u.head * p.group + n;
 }
 
 // Shared memory of a workgroup's combine: every wave's O [NW][kRows][D], row maxima and
@@ -73,12 +80,13 @@ struct CombineShared {
 // NaN (a NaN or an infinite score) is written as zeros, and as NaN with NANS, which is
 // what a prefill tile gives: one-token requests beside longer ones keep that.  They also
 // get a tile's `none` where no score is above -inf: 0, on an fp8 pool NaN.
-template <int D, int NW, bool NANS>
+// CROSS: the unit's rows are u.ntok tokens of G heads each (row = token * G + head).
+template <int D, int NW, bool NANS, bool CROSS = false>
 __device__ __forceinline__ void combine_waves(const DecodeArgs& p, const DecodeUnit& u, CombineShared<D, NW> sm,
                                               const f32x4 (&o)[D / 16], float m_run, float l_run, float vscale,
                                               float none) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n = lane & 15, g = lane >> 4, G = p.group;
+  const int n = lane & 15, g = lane >> 4, G = p.group, rows = CROSS ? u.ntok * G : G;
   const float l_row = group_sum(l_run);
   if (g == 0) {
     sm.m[wave * kRows + n] = m_run;
@@ -89,7 +97,7 @@ __device__ __forceinline__ void combine_waves(const DecodeArgs& p, const DecodeU
 #pragma unroll
     for (int i = 0; i < 4; i++) sm.o[(wave * kRows + n) * D + 16 * b + 4 * g + i] = o[b][i];
   __syncthreads();
-  for (int idx = threadIdx.x; idx < G * D; idx += 64 * NW) {
+  for (int idx = threadIdx.x; idx < rows * D; idx += 64 * NW) {
     const int row = idx / D, d = idx - row * D;
     float M = -INFINITY;
 #pragma unroll
@@ -106,7 +114,8 @@ __device__ __forceinline__ void combine_waves(const DecodeArgs& p, const DecodeU
     const float val = wsum > 0.f ? acc * vscale / wsum : !NANS ? 0.f : wsum == 0.f ? none : acc * 0.f;
     const float lse_v = wsum > 0.f ? (M + __log2f(wsum)) * kLn2 : -INFINITY;
     if (u.part < 0) {
-      const size_t orow = (size_t)u.qo_row * p.num_q_heads + u.head * G + row;
+      const size_t orow = CROSS ? (size_t)(u.qo_row + row / G) * p.num_q_heads + u.head * G + row % G
+                                : (size_t)u.qo_row * p.num_q_heads + u.head * G + row;
       p.out[orow * D + d] = __builtin_bit_cast(uint16_t, (__bf16)val);
       if (p.lse != nullptr && d == 0) p.lse[orow] = lse_v;
     } else {
@@ -131,7 +140,7 @@ struct PlainLoads {
 
 // One unit on NW waves; wave w takes page pairs w, w + NW, ...  nt: asked once the first
 // (plain) loads are on their way, whether to read the further pages non-temporally; uniform.
-template <int D, int NW, bool NANS, class Nt>
+template <int D, int NW, bool NANS, bool CROSS = false, class Nt>
 __device__ __forceinline__ void decode_unit(const DecodeArgs& p, const DecodeUnit& u, CombineShared<D, NW> sm, Nt&& nt) {
   constexpr int QS = D / 32;   // QK reduction steps
   constexpr int DB = D / 16;   // PV output blocks
@@ -145,8 +154,8 @@ __device__ __forceinline__ void decode_unit(const DecodeArgs& p, const DecodeUni
   // Q^T B-operands: dims 32 s + 8 g .. +8 of query row n (zero past the group)
   bf16x8 qf[QS];
   {
-    const bool valid = n < G;
-    const uint4* src = (const uint4*)(p.q + ((size_t)u.qo_row * p.num_q_heads + u.head * G + (valid ? n : 0)) * D + 8 * g);
+    const bool valid = n < (CROSS ? u.ntok * G : G);
+    const uint4* src = (const uint4*)(p.q + query_row<CROSS>(p, u, valid ? n : 0) * D + 8 * g);
 #pragma unroll
     for (int s = 0; s < QS; s++) qf[s] = __builtin_bit_cast(bf16x8, valid ? src[4 * s] : make_uint4(0, 0, 0, 0));
   }
@@ -280,7 +289,7 @@ __device__ __forceinline__ void decode_unit(const DecodeArgs& p, const DecodeUni
   else
     for (int j = wave; j < n_pairs; j += NW) compute(j, j + NW, r, std::false_type{});
 
-  combine_waves<D, NW, NANS>(p, u, sm, o, m_run, l_run, 1.0f, 0.f);
+  combine_waves<D, NW, NANS, CROSS>(p, u, sm, o, m_run, l_run, 1.0f, 0.f);
 }
 
 // ---------------------------------------------------------------- fp8 pool
@@ -303,9 +312,12 @@ template <int D>
 struct QuadRegs {
   uint4 k[4][D / 64];  // K codes: MFMA j, 64-dim step i
   uint4 v[D / 16];     // V^T codes: all 16 slots of the lane's dim of page g
+  float kby, vby;      // page-scaled pool: the powers of two of the lane's K page and V page
 };
 
-template <int D, int NW, bool NANS, class Nt>
+// PAGE: a page-scaled pool, whose powers of two the conversions take (k_scale: all of them, K
+// and V of every page and head side by side).
+template <int D, int NW, bool NANS, bool PAGE = false, bool CROSS = false, class Nt>
 __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const DecodeUnit& u, CombineShared<D, NW> sm,
                                                 Nt&& nt) {
   constexpr int KS = D / 64;  // K loads per MFMA row block
@@ -319,9 +331,8 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
   // Q^T B-operands: k-step (i, h) takes dims 64 i + 16 g + 8 h .. +8 of query row n
   bf16x8 qf[KS][2];
   {
-    const bool valid = n < G;
-    const uint4* src =
-        (const uint4*)(p.q + ((size_t)u.qo_row * p.num_q_heads + u.head * G + (valid ? n : 0)) * D + 16 * g);
+    const bool valid = n < (CROSS ? u.ntok * G : G);
+    const uint4* src = (const uint4*)(p.q + query_row<CROSS>(p, u, valid ? n : 0) * D + 16 * g);
 #pragma unroll
     for (int i = 0; i < KS; i++)
 #pragma unroll
@@ -353,7 +364,9 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
   const bool k_odd = n & 4, k_high = n & 8, v_odd = g & 1, v_high = g & 2;
   auto load_k = [&](const ids_t& w, QuadRegs<D>& r, auto nt_flag) {
     constexpr bool NT = decltype(nt_flag)::value;
-    const char* src = kbase + (uint64_t)pick(w, k_odd, k_high) * page_bytes;
+    const uint32_t page = pick(w, k_odd, k_high);
+    const char* src = kbase + (uint64_t)page * page_bytes;
+    if constexpr (PAGE) r.kby = p.k_scale[2 * ((uint64_t)page * (uint32_t)p.num_kv_heads + (uint32_t)u.head)];
 #pragma unroll
     for (int j = 0; j < 4; j++)
 #pragma unroll
@@ -361,7 +374,9 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
   };
   auto load_v = [&](const ids_t& w, QuadRegs<D>& r, auto nt_flag) {
     constexpr bool NT = decltype(nt_flag)::value;
-    const char* src = vbase + (uint64_t)pick(w, v_odd, v_high) * page_bytes;
+    const uint32_t page = pick(w, v_odd, v_high);
+    const char* src = vbase + (uint64_t)page * page_bytes;
+    if constexpr (PAGE) r.vby = p.k_scale[2 * ((uint64_t)page * (uint32_t)p.num_kv_heads + (uint32_t)u.head) + 1];
 #pragma unroll
     for (int b = 0; b < DB; b++) r.v[b] = load16<NT>(src + 256 * b);
   };
@@ -370,7 +385,7 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
 #pragma unroll
   for (int b = 0; b < DB; b++) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
-  const float scale = p.scale_log2 * p.k_scale[u.head];
+  const float scale = PAGE ? p.scale_log2 : p.scale_log2 * p.k_scale[u.head];
 
   // Quad `quad` from r; its registers are refilled with quad `next` (if < n_quads) as
   // soon as the products have read them.  TAIL: the quad reaches past key_end.  (A template
@@ -382,15 +397,16 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
     ids_t nx{};
     if (more) nx = ids_of(next);
     f32x4 s[4];
+    const float kby = PAGE ? r.kby : 1.0f;
 #pragma unroll
     for (int j = 0; j < 4; j++) {
       s[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < KS; i++) {
         const uint4 c = r.k[j][i];
-        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.x, c.y))),
+        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.x, c.y), kby)),
                                                        qf[i][0], s[j], 0, 0, 0);
-        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.z, c.w))),
+        s[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.z, c.w), kby)),
                                                        qf[i][1], s[j], 0, 0, 0);
       }
     }
@@ -430,6 +446,7 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
     }
     const bf16x8 pa = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
     const bf16x8 pb = __builtin_bit_cast(bf16x8, make_uint4(pw[4], pw[5], pw[6], pw[7]));
+    const float vby = PAGE ? r.vby : 1.0f;
     uint32_t mask[4];  // zeroes V of keys past the end: unwritten slots may hold NaN codes
     if constexpr (TAIL) {
 #pragma unroll
@@ -442,9 +459,9 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
     for (int b = 0; b < DB; b++) {
       uint4 c = r.v[b];
       if constexpr (TAIL) c = make_uint4(c.x & mask[0], c.y & mask[1], c.z & mask[2], c.w & mask[3]);
-      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.x, c.y))), pa,
+      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.x, c.y), vby)), pa,
                                                      o[b], 0, 0, 0);
-      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.z, c.w))), pb,
+      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.z, c.w), vby)), pb,
                                                      o[b], 0, 0, 0);
     }
     if (more) load_v(nx, r, nt_flag);
@@ -463,7 +480,8 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
   else
     for (; j < n_full; j += NW) compute(j, j + NW, r, std::false_type{}, std::false_type{});
   if (j < n_quads) compute(j, j + NW, r, std::true_type{}, std::false_type{});
-  combine_waves<D, NW, NANS>(p, u, sm, o, m_run, l_run, p.v_scale[u.head], __builtin_nanf(""));
+  combine_waves<D, NW, NANS, CROSS>(p, u, sm, o, m_run, l_run, PAGE ? 1.0f : p.v_scale[u.head],
+                                    PAGE ? 0.f : __builtin_nanf(""));
 }
 
 

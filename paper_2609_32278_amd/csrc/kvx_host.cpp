@@ -20,14 +20,16 @@
 
 #include "kvx_host_util.h"
 #include "kvx_internal.h"
+#include "kvx_pool.h"
 
 using kvx::ceil_div;
 using kvx::check_align;
 using kvx::check_batch;
 using kvx::check_page_ids;
+using kvx::check_pool;
 using kvx::hip_fail;
 using kvx::inline_store_reqs;
-using kvx::Staging;
+using kvx::use_device;
 using kvx::validate_mode;
 using kvx::Workspace;
 using kvx::AttnUnit;
@@ -69,36 +71,7 @@ constexpr int64_t kMaxParts = 16384;
 
 }  // namespace
 
-struct kvx_pool {
-  int device = 0;
-  int64_t num_pages = 0;
-  int32_t page_size = 16;
-  int32_t num_kv_heads = 0;
-  int32_t head_dim = 0;
-  int32_t kv_dtype = KVX_KV_BF16;
-  int32_t elem_bytes = 2;
-  void* k = nullptr;
-  void* v = nullptr;
-  float* scales_d = nullptr;  // [k_scale | v_scale | k_inv | v_inv], each num_kv_heads
-  Staging st_store, st_attn, st_io, st_move;
-  Workspace parts;
-  int32_t split_keys = 0;  // key-range split length of extend_attention; 0 = automatic
-  int32_t scaled_q = 0;    // 1: prefill attention on a bf16 pool takes the folded softmax
-};
-
 namespace {
-
-int check_pool(const kvx_pool* pool) {
-  if (pool == nullptr) return fail(KVX_EINVAL, "pool is NULL");
-  return KVX_OK;
-}
-
-int use_device(const kvx_pool* pool) {
-  int cur = -1;
-  KVX_HIP(hipGetDevice(&cur));
-  if (cur != pool->device) KVX_HIP(hipSetDevice(pool->device));
-  return KVX_OK;
-}
 
 struct Plan {
   std::vector<AttnUnit> units;  // in launch order (position i runs on XCD i % 8)
@@ -368,10 +341,12 @@ bool is_mixed_batch(const kvx_batch* b, int32_t Hq, int32_t Hkv) {
 //     total work of the request, a request of few long tiles came last: 16 agents with
 //     4k-32k prefixes, 3.19 -> 2.85 ms.)
 //   * mixed: one-token suffixes become decode units, key chunks of the (request, KV head).
+//   * cross: every row of a request sees its P tokens in the pool, which the suffix is not among.
 //   * packed: the smallest plan there is, without padding and with no split but a forced one; a
 //     unit then runs on whatever XCD its place gives it.
 int make_plan(const kvx_batch* b, const std::vector<int64_t>& qo, int32_t Hq, int32_t Hkv, int32_t D,
-              int32_t split_keys, const PartLimits& limits, bool mixed, Plan& plan, bool packed = false) {
+              int32_t split_keys, const PartLimits& limits, bool mixed, Plan& plan, bool packed = false,
+              bool cross = false) {
   const int G = Hq / Hkv;
   const int tile_tok = kvx::kTileRows / G;
   const int BN = kvx::kTileKeys;
@@ -381,15 +356,15 @@ int make_plan(const kvx_batch* b, const std::vector<int64_t>& qo, int32_t Hq, in
   std::vector<int32_t> order;
   for (int r = 0; r < b->num_reqs; r++)
     if (b->extend_lens[r] > (plan.mixed ? 1 : 0)) order.push_back(r);
-  std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) {
-    return (int64_t)b->prefix_lens[x] + b->extend_lens[x] > (int64_t)b->prefix_lens[y] + b->extend_lens[y];
-  });
+  auto keys_of = [&](int32_t r) { return (int64_t)b->prefix_lens[r] + (cross ? 0 : b->extend_lens[r]); };
+  std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return keys_of(x) > keys_of(y); });
   std::vector<Tile> tiles;  // request by request, a request's longest tile first
   for (const int32_t r : order) {
     const int64_t P = b->prefix_lens[r], E = b->extend_lens[r];
     for (int64_t t0 = (E - 1) / tile_tok * tile_tok; t0 >= 0; t0 -= tile_tok) {
       const int64_t ntok = std::min<int64_t>(tile_tok, E - t0);
-      tiles.push_back(Tile{r, (int32_t)t0, (int32_t)ntok, P + t0 + ntok, P + t0});
+      if (cross) tiles.push_back(Tile{r, (int32_t)t0, (int32_t)ntok, P, P - 1});
+      else tiles.push_back(Tile{r, (int32_t)t0, (int32_t)ntok, P + t0 + ntok, P + t0});
     }
   }
 
@@ -657,17 +632,30 @@ bool is_decode_batch(const kvx_batch* b, int32_t Hq, int32_t Hkv) {
   return any;
 }
 
-// Work plan of a decode step: each (request, KV head) key range [0, P] is cut into
+// Rows that the decode code takes at once: the query heads of one token (ntok 0), or of the
+// ntok tokens of a cross attention, over keys [0, keys) of request r.
+struct StepRows {
+  int32_t r, qo_row, ntok;
+  int64_t keys;
+};
+
+std::vector<StepRows> decode_rows(const kvx_batch* b, const std::vector<int64_t>& qo) {
+  std::vector<StepRows> rows;
+  for (int r = 0; r < b->num_reqs; r++)
+    if (b->extend_lens[r] == 1) rows.push_back(StepRows{r, (int32_t)qo[(size_t)r], 0, (int64_t)b->prefix_lens[r] + 1});
+  return rows;
+}
+
+// Work plan of a decode step: the key range of each rows and KV head is cut into
 // chunks of a common length, a multiple of 64 keys chosen so that the batch yields
 // about 2048 chunks (8 per CU, of which two to four run at a time), at
 // least 512 keys each; a range of more than one chunk becomes parts merged by
 // log-sum-exp.  Chunks are dispatched longest first.
-int make_decode_plan(const kvx_batch* b, const std::vector<int64_t>& qo, int32_t Hkv, int32_t split_keys,
-                     int64_t max_parts, DecodePlan& plan) {
+int make_step_plan(const kvx_batch* b, const std::vector<StepRows>& rows, int32_t Hkv, int32_t split_keys,
+                   int64_t max_parts, DecodePlan& plan) {
   const int64_t A = kvx::kDecodeChunkAlign;
   int64_t total = 0;
-  for (int r = 0; r < b->num_reqs; r++)
-    if (b->extend_lens[r] == 1) total += (int64_t)Hkv * ((int64_t)b->prefix_lens[r] + 1);
+  for (const StepRows& w : rows) total += (int64_t)Hkv * w.keys;
   int64_t chunk;
   if (split_keys > 0) {
     chunk = split_keys;
@@ -677,35 +665,33 @@ int make_decode_plan(const kvx_batch* b, const std::vector<int64_t>& qo, int32_t
   }
   for (;;) {  // bound the partial results like the prefill planner does
     int64_t parts = 0;
-    for (int r = 0; r < b->num_reqs; r++) {
-      if (b->extend_lens[r] != 1) continue;
-      const int64_t n = ((int64_t)b->prefix_lens[r] + 1 + chunk - 1) / chunk;
+    for (const StepRows& w : rows) {
+      const int64_t n = (w.keys + chunk - 1) / chunk;
       if (n > 1) parts += n * Hkv;
     }
     if (parts <= max_parts) break;
     chunk *= 2;
   }
-  for (int r = 0; r < b->num_reqs; r++) {
-    if (b->extend_lens[r] != 1) continue;
-    const int64_t L = (int64_t)b->prefix_lens[r] + 1;
-    const int64_t nc = (L + chunk - 1) / chunk;
+  for (const StepRows& w : rows) {
+    const int64_t nc = std::max<int64_t>(1, (w.keys + chunk - 1) / chunk);
     const int64_t part0 = plan.n_parts;
     for (int64_t c = 0; c < nc; c++) {
       for (int32_t h = 0; h < Hkv; h++) {  // heads side by side (see InlinePlan)
         DecodeUnit u{};
-        u.qo_row = (int32_t)qo[(size_t)r];
-        u.page_base = b->page_indptr[r];
+        u.qo_row = w.qo_row;
+        u.page_base = b->page_indptr[w.r];
         u.key_begin = (int32_t)(c * chunk);
-        u.key_end = (int32_t)std::min<int64_t>(L, (c + 1) * chunk);
+        u.key_end = (int32_t)std::min<int64_t>(w.keys, (c + 1) * chunk);
         u.head = h;
         u.part = nc > 1 ? (int32_t)(part0 + h * nc + c) : -1;
-        u.req = r;
+        u.req = w.r;
+        u.ntok = w.ntok;
         plan.units.push_back(u);
       }
     }
     if (nc > 1) {
       for (int32_t h = 0; h < Hkv; h++)
-        plan.merges.push_back(DecodeMerge{(int32_t)qo[(size_t)r], h, (int32_t)(part0 + h * nc), (int32_t)nc});
+        plan.merges.push_back(DecodeMerge{w.qo_row, h | w.ntok << 16, (int32_t)(part0 + h * nc), (int32_t)nc});
       plan.n_parts += nc * Hkv;
     }
   }
@@ -718,6 +704,11 @@ int make_decode_plan(const kvx_batch* b, const std::vector<int64_t>& qo, int32_t
     plan.items.push_back(it);
   }
   return KVX_OK;
+}
+
+int make_decode_plan(const kvx_batch* b, const std::vector<int64_t>& qo, int32_t Hkv, int32_t split_keys,
+                     int64_t max_parts, DecodePlan& plan) {
+  return make_step_plan(b, decode_rows(b, qo), Hkv, split_keys, max_parts, plan);
 }
 
 int check_heads(int32_t Hq, int32_t Hkv, int32_t D) {
@@ -862,13 +853,15 @@ std::vector<uint8_t> plan_blob(const std::vector<U>& units, const std::vector<M>
 // every page list would cost each unit more than these loads give.
 constexpr int64_t kStreamBytes = 256ll << 20;
 
-int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, const void* q,
-                     int32_t num_q_heads, float sm_scale, void* out, float* lse, hipStream_t s, CallBuffers& buf) {
+// The rows of a decode step, or of a cross attention.
+int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<StepRows>& rows, bool cross,
+                     const void* q, int32_t num_q_heads, float sm_scale, void* out, float* lse, hipStream_t s,
+                     CallBuffers& buf) {
   const int D = pool->head_dim;
   constexpr int R = kvx::kDecodeMaxGroup;
   DecodePlan plan;
-  if (int rc = make_decode_plan(batch, qo, pool->num_kv_heads, pool->split_keys,
-                                buf.max_parts((size_t)R * (D + 1) * sizeof(float)), plan))
+  if (int rc = make_step_plan(batch, rows, pool->num_kv_heads, pool->split_keys,
+                              buf.max_parts((size_t)R * (D + 1) * sizeof(float)), plan))
     return rc;
   kvx::DecodeParams dp;
   kvx::DecodeMergeParams m;
@@ -880,12 +873,14 @@ int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<i
   }
   int64_t kv_bytes = 0;  // K and V, page lists that share pages counted each
   std::vector<int32_t> lists;
-  for (int r = 0; r < batch->num_reqs; r++) {
-    if (batch->extend_lens[r] != 1) continue;
-    kv_bytes += 2 * ((int64_t)batch->prefix_lens[r] + 1) * pool->num_kv_heads * D * pool->elem_bytes;
-    lists.push_back(batch->page_indptr[r]);
+  bool again = false;  // a request's keys are read for several rows
+  for (const StepRows& w : rows) {
+    if (w.keys == 0) continue;
+    kv_bytes += 2 * w.keys * pool->num_kv_heads * D * pool->elem_bytes;
+    again |= !lists.empty() && lists.back() == batch->page_indptr[w.r];
+    lists.push_back(batch->page_indptr[w.r]);
   }
-  const bool streams = kv_bytes > kStreamBytes && lists.size() <= (size_t)kvx::kShareReqs;
+  const bool streams = kv_bytes > kStreamBytes && lists.size() <= (size_t)kvx::kShareReqs && !again;
   dp.lists.base = nullptr;
   dp.lists.n = streams ? (int32_t)lists.size() : 0;
   const size_t lists_at = blob.size();
@@ -922,12 +917,14 @@ int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<i
   dp.units = (const DecodeUnit*)dev;
   p.o_part = plan.n_parts ? parts : nullptr;
   p.lse_part = plan.n_parts ? parts + (size_t)plan.n_parts * R * D : nullptr;
-  p.k_scale = pool->scales_d;
-  p.v_scale = pool->scales_d ? pool->scales_d + pool->num_kv_heads : nullptr;
+  p.k_scale = pool->k_scales();
+  p.v_scale = pool->v_scales();
   p.num_q_heads = num_q_heads;
   p.num_kv_heads = pool->num_kv_heads;
   p.group = num_q_heads / pool->num_kv_heads;
   p.scale_log2 = sm_scale * 1.4426950408889634f;
+  p.page_scaled = pool->page_scaled() ? 1 : 0;
+  p.cross = cross ? 1 : 0;
   if (!in_args && dp.lists.n > 0) dp.lists.base = (const int32_t*)((const uint8_t*)dev + lists_at);
   hipError_t e = kvx::launch_decode(dp, (int64_t)plan.units.size(), D, pool->kv_dtype == KVX_KV_FP8_E4M3, s);
   if (e != hipSuccess) return hip_fail(e, "decode kernel launch");
@@ -939,11 +936,17 @@ int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<i
     m.lse = lse;
     m.num_q_heads = num_q_heads;
     m.group = p.group;
+    m.cross = 0;
+    if (cross)
+      for (const DecodeMerge& x : plan.merges) m.cross = std::max(m.cross, x.head >> 16);
     e = kvx::launch_decode_merge(m, (int64_t)plan.merges.size(), D, s);
     if (e != hipSuccess) return hip_fail(e, "decode merge kernel launch");
   }
   return buf.done(s, !in_args);
 }
+
+int tile_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, bool cross, const void* q,
+                   int32_t num_q_heads, float sm_scale, void* out, float* lse, hipStream_t s, CallBuffers& buf);
 
 }  // namespace
 
@@ -979,7 +982,10 @@ int kv_pool_create(int64_t num_pages, int32_t page_size, int32_t num_kv_heads, i
   if (num_kv_heads >= (1 << 15)) return fail(KVX_EUNSUPPORTED, "num_kv_heads too large");
   if (page_size != kvx::kPageSize) return fail(KVX_EUNSUPPORTED, "page_size %d (supported: 16)", page_size);
   if (head_dim != 64 && head_dim != 128) return fail(KVX_EUNSUPPORTED, "head_dim %d (supported: 64, 128)", head_dim);
-  if (kv_dtype != KVX_KV_BF16 && kv_dtype != KVX_KV_FP8_E4M3) return fail(KVX_EINVAL, "kv_dtype %d", kv_dtype);
+  if (kv_dtype != KVX_KV_BF16 && kv_dtype != KVX_KV_FP8_E4M3 && kv_dtype != KVX_KV_FP8_PAGE)
+    return fail(KVX_EINVAL, "kv_dtype %d", kv_dtype);
+  if (kv_dtype == KVX_KV_FP8_PAGE && (k_scale || v_scale))
+    return fail(KVX_EINVAL, "a page-scaled pool finds its scales itself: k_scale and v_scale must be NULL");
   if (kv_dtype == KVX_KV_FP8_E4M3) {
     if (!k_scale || !v_scale) return fail(KVX_EUNSUPPORTED, "an fp8 pool needs k_scale and v_scale");
     for (int h = 0; h < num_kv_heads; h++)
@@ -1001,6 +1007,7 @@ int kv_pool_create(int64_t num_pages, int32_t page_size, int32_t num_kv_heads, i
     if (p->k) (void)hipFree(p->k);
     if (p->v) (void)hipFree(p->v);
     if (p->scales_d) (void)hipFree(p->scales_d);
+    if (p->page_scales) (void)hipFree(p->page_scales);
     delete p;
     return rc;
   };
@@ -1025,6 +1032,15 @@ int kv_pool_create(int64_t num_pages, int32_t page_size, int32_t num_kv_heads, i
     if (e == hipSuccess) e = hipMemcpy(p->scales_d, s.data(), s.size() * sizeof(float), hipMemcpyHostToDevice);
     if (e != hipSuccess) return cleanup(hip_fail(e, "fp8 scales"));
   }
+  if (kv_dtype == KVX_KV_FP8_PAGE) {
+    const size_t scale_bytes = (size_t)num_pages * num_kv_heads * 2 * sizeof(float);
+    void* ptr = nullptr;
+    e = hipMalloc(&ptr, scale_bytes);
+    if (e != hipSuccess) return cleanup(hip_fail(e, "hipMalloc(page scales)"));
+    p->page_scales = (float*)ptr;
+    e = hipMemset(ptr, 0, scale_bytes);
+    if (e != hipSuccess) return cleanup(hip_fail(e, "hipMemset(page scales)"));
+  }
   e = hipDeviceSynchronize();
   if (e != hipSuccess) return cleanup(hip_fail(e, "hipDeviceSynchronize"));
   *out = p;
@@ -1037,6 +1053,7 @@ int kv_pool_destroy(kvx_pool* pool) {
   (void)use_device(pool);
   hipError_t e = hipDeviceSynchronize();
   pool->st_store.release();
+  pool->st_load.release();
   pool->st_attn.release();
   pool->st_io.release();
   pool->st_move.release();
@@ -1044,6 +1061,7 @@ int kv_pool_destroy(kvx_pool* pool) {
   if (pool->k) (void)hipFree(pool->k);
   if (pool->v) (void)hipFree(pool->v);
   if (pool->scales_d) (void)hipFree(pool->scales_d);
+  if (pool->page_scales) (void)hipFree(pool->page_scales);
   delete pool;
   if (e != hipSuccess) return hip_fail(e, "hipDeviceSynchronize");
   return KVX_OK;
@@ -1071,8 +1089,8 @@ int kv_pool_layout(const kvx_pool* pool, kvx_pool_layout* out) {
   out->v_stride_head = S * D;
   out->v_stride_slot = 1;
   out->v_stride_dim = S;
-  out->k_scale = pool->scales_d;
-  out->v_scale = pool->scales_d ? pool->scales_d + H : nullptr;
+  out->k_scale = pool->k_scales();
+  out->v_scale = pool->v_scales();
   return KVX_OK;
 }
 
@@ -1093,7 +1111,7 @@ static int page_io(kvx_pool* pool, const int32_t* page_ids, int64_t n, void* k_l
   hipStream_t s = (hipStream_t)stream;
   // Up to a few launches' worth of ids travel in kernel arguments instead of through a
   // copy and its wait (2000 pages out and in on new pools: 181 us with copies, 151 us without).
-  const bool in_args = n <= 8 * kvx::kInlinePages;
+  const bool in_args = n <= 8 * kvx::kInlinePages && !pool->page_scaled();
   void* ids_d = nullptr;
   if (!in_args)
     if (int rc = pool->st_io.upload(page_ids, (size_t)n * sizeof(int32_t), s, &ids_d)) return rc;
@@ -1106,6 +1124,7 @@ static int page_io(kvx_pool* pool, const int32_t* page_ids, int64_t n, void* k_l
   p.v_lin = v_lin;
   p.num_kv_heads = pool->num_kv_heads;
   p.to_pool = to_pool;
+  p.page_scale = pool->page_scales;
   hipError_t e = kvx::launch_page_io(p, n, pool->head_dim, pool->elem_bytes, s);
   if (e != hipSuccess) return hip_fail(e, "page io kernel launch");
   return in_args ? KVX_OK : pool->st_io.done(s);
@@ -1123,8 +1142,14 @@ int kv_pool_read_pages(const kvx_pool* pool, const int32_t* page_ids, int64_t n,
   return page_io(const_cast<kvx_pool*>(pool), page_ids, n, k_dst, v_dst, 0, stream);
 }
 
+static int64_t block_bytes(const kvx_pool* pool) {
+  return (int64_t)pool->num_kv_heads * kvx::kPageSize * pool->head_dim * pool->elem_bytes;
+}
+
+// A page's K block, V block and, on a page-scaled pool, scales, up to 16 bytes.
 static int64_t record_bytes(const kvx_pool* pool) {
-  return 2 * (int64_t)pool->num_kv_heads * kvx::kPageSize * pool->head_dim * pool->elem_bytes;
+  const int64_t scales = pool->page_scaled() ? 2 * (int64_t)pool->num_kv_heads * (int64_t)sizeof(float) : 0;
+  return 2 * block_bytes(pool) + (scales + 15) / 16 * 16;
 }
 
 int kv_pool_record_bytes(const kvx_pool* pool, int64_t* bytes) {
@@ -1177,7 +1202,10 @@ static int page_move(kvx_pool* pool, const int32_t* page_ids, const int32_t* slo
   p.k_pool = (uint8_t*)pool->k;
   p.v_pool = (uint8_t*)pool->v;
   p.host = (uint8_t*)attr.devicePointer + (attr.hostPointer ? off : 0);
-  p.block_bytes = record_bytes(pool) / 2;
+  p.block_bytes = block_bytes(pool);
+  p.record_bytes = record_bytes(pool);
+  p.page_scale = pool->page_scales;
+  p.num_kv_heads = pool->num_kv_heads;
   p.to_host = to_host;
   hipError_t e = kvx::launch_page_move(p, n, s);
   if (e != hipSuccess) return hip_fail(e, "page move kernel launch");
@@ -1196,6 +1224,27 @@ int kv_pool_reload(kvx_pool* pool, const int32_t* page_ids, const int32_t* slots
   return page_move(pool, page_ids, slots, n, host, host_slots, 0, stream);
 }
 
+// The launch of store_kv_rope, and of store_kv into a page-scaled pool: the call's arguments
+// checked, its rotation and queries in p, the pool's device current.
+static int rope_store(kvx_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, kvx::RopeParams& p,
+                      bool interleaved, const void* k_ext, const void* v_ext, hipStream_t s) {
+  int64_t n_units = 0;
+  if (int rc = kvx::place_units(pool->st_store, batch, qo, s, p, n_units)) return rc;
+  p.k_ext = (const uint16_t*)k_ext;
+  p.v_ext = (const uint16_t*)v_ext;
+  p.k_pool = pool->k;
+  p.v_pool = pool->v;
+  p.page_ids = batch->page_ids;
+  p.k_inv_scale = pool->scales_d ? pool->scales_d + 2 * pool->num_kv_heads : nullptr;
+  p.v_inv_scale = pool->scales_d ? pool->scales_d + 3 * pool->num_kv_heads : nullptr;
+  p.page_scale = pool->page_scales;
+  p.num_kv_heads = pool->num_kv_heads;
+  const hipError_t e =
+      kvx::launch_store_kv_rope(p, n_units, pool->head_dim, pool->kv_dtype == KVX_KV_FP8_E4M3, interleaved, s);
+  if (e != hipSuccess) return hip_fail(e, p.rotary_dim > 0 ? "store_kv_rope kernel launch" : "store_kv kernel launch");
+  return p.units ? pool->st_store.done(s) : KVX_OK;
+}
+
 int store_kv(kvx_pool* pool, const kvx_batch* batch, const void* k_ext, const void* v_ext, kvx_stream_t stream) {
   g_last_error.clear();
   if (int rc = check_pool(pool)) return rc;
@@ -1209,6 +1258,10 @@ int store_kv(kvx_pool* pool, const kvx_batch* batch, const void* k_ext, const vo
   hipStream_t s = (hipStream_t)stream;
   if (validate_mode())
     if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
+  if (pool->page_scaled()) {
+    kvx::RopeParams p{};
+    return rope_store(pool, batch, qo, p, false, k_ext, v_ext, s);
+  }
   std::vector<StoreUnit> units;
   const int S = kvx::kPageSize;
   for (int r = 0; r < batch->num_reqs; r++) {
@@ -1286,45 +1339,14 @@ int store_kv_rope(kvx_pool* pool, const kvx_batch* batch, const kvx_rope* rope, 
   hipStream_t s = (hipStream_t)stream;
   if (validate_mode())
     if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
-  std::vector<kvx::RopeUnit> units;
-  const int S = kvx::kPageSize;
-  for (int r = 0; r < batch->num_reqs; r++) {
-    const int64_t P = batch->prefix_lens[r], E = batch->extend_lens[r];
-    if (E == 0) continue;
-    const int64_t L = P + E;
-    for (int64_t lp = P / S; lp <= (L - 1) / S; lp++) {
-      kvx::RopeUnit u;
-      u.row_slot0 = (int32_t)(qo[(size_t)r] + lp * S - P);
-      u.page_pos = (int32_t)(batch->page_indptr[r] + lp);
-      u.slot_begin = (int32_t)(std::max<int64_t>(P, lp * S) - lp * S);
-      u.slot_end = (int32_t)(std::min<int64_t>(L, lp * S + S) - lp * S);
-      u.pos_slot0 = (int32_t)(lp * S);
-      units.push_back(u);
-    }
-  }
-  void* units_d = nullptr;
-  if (!inline_store_reqs(batch, qo, p.reqs))
-    if (int rc = pool->st_store.upload(units.data(), units.size() * sizeof(kvx::RopeUnit), s, &units_d)) return rc;
   p.q = (const uint16_t*)q;
   p.q_out = (uint16_t*)q_out;
-  p.k_ext = (const uint16_t*)k_ext;
-  p.v_ext = (const uint16_t*)v_ext;
-  p.k_pool = pool->k;
-  p.v_pool = pool->v;
-  p.page_ids = batch->page_ids;
-  p.units = (const kvx::RopeUnit*)units_d;
-  p.k_inv_scale = pool->scales_d ? pool->scales_d + 2 * pool->num_kv_heads : nullptr;
-  p.v_inv_scale = pool->scales_d ? pool->scales_d + 3 * pool->num_kv_heads : nullptr;
   p.q_norm = (const uint16_t*)rope->q_norm;
   p.k_norm = (const uint16_t*)rope->k_norm;
   p.num_q_heads = num_q_heads;
-  p.num_kv_heads = pool->num_kv_heads;
   p.rotary_dim = rd;
   p.norm_eps = rope->norm_eps;
-  hipError_t e = kvx::launch_store_kv_rope(p, (int64_t)units.size(), D, pool->kv_dtype == KVX_KV_FP8_E4M3,
-                                           rope->style == KVX_ROPE_INTERLEAVED, s);
-  if (e != hipSuccess) return hip_fail(e, "store_kv_rope kernel launch");
-  return p.reqs.n > 0 ? KVX_OK : pool->st_store.done(s);
+  return rope_store(pool, batch, qo, p, rope->style == KVX_ROPE_INTERLEAVED, k_ext, v_ext, s);
 }
 
 int extend_attention_plan(const kvx_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
@@ -1386,8 +1408,17 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
   CallBuffers buf{pool, fixed};
 
   if (is_decode_batch(batch, num_q_heads, pool->num_kv_heads))
-    return decode_attention(pool, batch, qo, q, num_q_heads, sm_scale, out, lse, s, buf);
+    return decode_attention(pool, batch, decode_rows(batch, qo), false, q, num_q_heads, sm_scale, out, lse, s, buf);
+  return tile_attention(pool, batch, qo, false, q, num_q_heads, sm_scale, out, lse, s, buf);
+}
 
+namespace {
+
+// The requests with suffix tokens (of a cross attention, with queries and keys) through tiles, or,
+// where that is a mixed batch, through both kinds of units.
+int tile_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, bool cross, const void* q,
+                   int32_t num_q_heads, float sm_scale, void* out, float* lse, hipStream_t s, CallBuffers& buf) {
+  const kvx::FixedScratch* fixed = buf.fixed;
   const int D = pool->head_dim;
   const size_t part_bytes = (size_t)kvx::kTileRows * (D + 1) * sizeof(float);
   const size_t dec_part_bytes = (size_t)kvx::kDecodeMaxGroup * (D + 1) * sizeof(float);
@@ -1397,7 +1428,7 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
   kvx::CompactPlan compact;
   bool in_args = false;
   std::vector<uint8_t> blob;  // one upload: units, then merges, then the decode units' merges
-  bool mixed = is_mixed_batch(batch, num_q_heads, pool->num_kv_heads), packed = false;
+  bool mixed = !cross && is_mixed_batch(batch, num_q_heads, pool->num_kv_heads), packed = false;
   for (;;) {
     PartLimits lim = pool_limits(mixed);
     if (fixed) {
@@ -1406,7 +1437,8 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
       if (mixed) lim = PartLimits{lim.prefill - (lim.prefill + 3) / 4, lim.decode / 4};
     }
     plan = Plan();
-    if (int rc = make_plan(batch, qo, num_q_heads, pool->num_kv_heads, D, pool->split_keys, lim, mixed, plan, packed))
+    if (int rc = make_plan(batch, qo, num_q_heads, pool->num_kv_heads, D, pool->split_keys, lim, mixed, plan, packed,
+                           cross))
       return rc;
     in_args = inline_merges(plan.merges, pool->num_kv_heads, m.plan) && compact_plan(plan, compact);
     if (in_args) break;
@@ -1443,14 +1475,16 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
   p.units = (const AttnUnit*)dev;
   p.o_part = plan.n_parts ? parts : nullptr;
   p.lse_part = plan.n_parts ? parts + (size_t)plan.n_parts * kvx::kTileRows * D : nullptr;
-  p.k_scale = pool->scales_d;
-  p.v_scale = pool->scales_d ? pool->scales_d + pool->num_kv_heads : nullptr;
+  p.k_scale = pool->k_scales();
+  p.v_scale = pool->v_scales();
   p.num_q_heads = num_q_heads;
   p.num_kv_heads = pool->num_kv_heads;
   p.group = num_q_heads / pool->num_kv_heads;
   p.tile_tok = kvx::kTileRows / p.group;
   p.scale_log2 = sm_scale * 1.4426950408889634f;
   p.mixed = plan.mixed ? 1 : 0;
+  p.page_scaled = pool->page_scaled() ? 1 : 0;
+  p.cross = cross ? 1 : 0;
   p.d_part = plan.dec_parts ? parts + (size_t)plan.n_parts * (part_bytes / sizeof(float)) : nullptr;
   p.d_lse = plan.dec_parts ? p.d_part + (size_t)plan.dec_parts * kvx::kDecodeMaxGroup * D : nullptr;
   hipError_t e = kvx::launch_extend_attention(p, (int64_t)plan.units.size(), D, pool->kv_dtype == KVX_KV_FP8_E4M3,
@@ -1470,6 +1504,7 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
   if (!plan.dec_merges.empty()) {
     kvx::DecodeMergeParams dm;
     dm.plan.n = 0;
+    dm.cross = 0;
     dm.merges = (const DecodeMerge*)((const uint8_t*)dev + plan.units.size() * sizeof(AttnUnit) +
                                      plan.merges.size() * sizeof(MergeUnit));
     dm.o_part = p.d_part;
@@ -1482,4 +1517,68 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
     if (e != hipSuccess) return hip_fail(e, "decode merge kernel launch");
   }
   return buf.done(s, !in_args);
+}
+
+// Requests of a cross attention whose rows the decode code takes, 16 at a time, each time over all
+// keys; the others go through tiles of 256 rows.
+constexpr int64_t kCrossBlocks = 1, kCrossBlocks8 = 2;
+
+int check_cross(const kvx_pool* pool, const kvx_batch* batch, std::vector<int64_t>& qo, const void* q,
+                int32_t num_q_heads, float sm_scale, const void* out, const float* lse) {
+  if (int rc = check_pool(pool)) return rc;
+  if (int rc = check_heads(num_q_heads, pool->num_kv_heads, pool->head_dim)) return rc;
+  if (!(std::isfinite(sm_scale) && sm_scale > 0.f)) return fail(KVX_EINVAL, "sm_scale must be finite and > 0");
+  if (int rc = check_batch(batch, qo, true, true)) return rc;
+  if (qo.back() == 0) return KVX_OK;
+  if (!q || !out) return fail(KVX_EINVAL, "q and out must be non-NULL");
+  if (int rc = check_align(q, "q")) return rc;
+  if (int rc = check_align(out, "out")) return rc;
+  if (lse != nullptr && ((uintptr_t)lse & 3u) != 0) return fail(KVX_EINVAL, "lse is not 4-byte aligned");
+  const size_t rows = (size_t)qo.back() * num_q_heads, bytes = rows * pool->head_dim * 2, n = rows * sizeof(float);
+  if (kvx::meet(out, bytes, q, bytes)) return fail(KVX_EINVAL, "out overlaps q");
+  if (lse != nullptr && kvx::meet(lse, n, q, bytes)) return fail(KVX_EINVAL, "lse overlaps q");
+  if (lse != nullptr && kvx::meet(lse, n, out, bytes)) return fail(KVX_EINVAL, "lse overlaps out");
+  return KVX_OK;
+}
+
+}  // namespace
+
+extern "C" int cross_attention(kvx_pool* pool, const kvx_batch* batch, const void* q, int32_t num_q_heads,
+                               float sm_scale, void* out, float* lse, kvx_stream_t stream) {
+  return kvx::guarded([&]() -> int {
+    std::vector<int64_t> qo;
+    if (int rc = check_cross(pool, batch, qo, q, num_q_heads, sm_scale, out, lse)) return rc;
+    if (qo.back() == 0) return KVX_OK;
+    hipStream_t s = (hipStream_t)stream;
+    kvx::OnDevice on;
+    if (int rc = on.enter(pool->device)) return rc;
+    if (int rc = kvx::check_stream(s, pool->device)) return rc;
+    const int32_t group = num_q_heads / pool->num_kv_heads;
+    const int64_t block = kvx::kDecodeMaxGroup / group;  // tokens whose rows the decode code takes at once
+    const int64_t most = pool->kv_dtype == KVX_KV_BF16 ? kCrossBlocks : kCrossBlocks8;
+    constexpr int64_t kEmptyTokens = 1024;  // of a request without keys, a unit
+    std::vector<StepRows> rows;
+    std::vector<int32_t> tiled(batch->extend_lens, batch->extend_lens + batch->num_reqs);
+    bool tiles = false;
+    for (int r = 0; r < batch->num_reqs; r++) {
+      const int64_t L = batch->prefix_lens[r], E = batch->extend_lens[r];
+      const int64_t each = L == 0 ? kEmptyTokens : block;
+      if (E == 0) continue;
+      if (L > 0 && (block == 0 || E > block * most)) {
+        tiles = true;
+        continue;
+      }
+      for (int64_t t = 0; t < E; t += each)
+        rows.push_back(StepRows{r, (int32_t)(qo[(size_t)r] + t), (int32_t)std::min(each, E - t), L});
+      tiled[(size_t)r] = 0;
+    }
+    CallBuffers buf{pool, nullptr};
+    if (tiles) {
+      kvx_batch sub = *batch;
+      sub.extend_lens = tiled.data();
+      if (int rc = tile_attention(pool, &sub, qo, true, q, num_q_heads, sm_scale, out, lse, s, buf)) return rc;
+    }
+    if (rows.empty()) return KVX_OK;
+    return decode_attention(pool, batch, rows, true, q, num_q_heads, sm_scale, out, lse, s, buf);
+  });
 }

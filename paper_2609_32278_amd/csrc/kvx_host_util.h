@@ -9,6 +9,7 @@
 #include <cstdint>
 #include <cstdlib>
 #include <cstring>
+#include <new>
 #include <vector>
 
 #include "kvx.h"
@@ -144,8 +145,59 @@ inline int check_align(const void* ptr, const char* name) {
   return KVX_OK;
 }
 
+// Run an entry point's body: no exception crosses the ABI, and an error of the runtime that is
+// returned is not left for the caller's next call to find.
+template <typename F>
+int guarded(F&& body) {
+  report(KVX_OK, "%s", "");
+  try {
+    const int rc = body();
+    if (rc == KVX_EHIP || rc == KVX_ENOMEM) (void)hipGetLastError();
+    return rc;
+  } catch (const std::bad_alloc&) {
+    return report(KVX_ENOMEM, "host memory for the plan of the call");
+  } catch (...) {
+    return report(KVX_EINVAL, "unexpected failure on the host");
+  }
+}
+
+// The pool's device for the length of a call.
+struct OnDevice {
+  int before = -1;
+  int enter(int device) {
+    KVX_HIP(hipGetDevice(&before));
+    if (before == device) before = -1;
+    else KVX_HIP(hipSetDevice(device));
+    return KVX_OK;
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+// A stream that a call of this device's pool can be queued on.
+inline int check_stream(hipStream_t s, int device) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  const hipError_t e = hipStreamIsCapturing(s, &st);
+  if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
+  if (st != hipStreamCaptureStatusNone)
+    return report(KVX_EUNSUPPORTED, "the stream is being captured: the plan of a call is made on the host");
+  if (s == nullptr || s == hipStreamLegacy || s == hipStreamPerThread) return KVX_OK;  // the current device's
+  hipDevice_t of = device;
+  KVX_HIP(hipStreamGetDevice(s, &of));
+  if (of != device) return report(KVX_EINVAL, "the stream is of device %d, the pool of device %d", of, device);
+  return KVX_OK;
+}
+
+// Byte ranges [a, a + n) and [b, b + m) that meet.
+inline bool meet(const void* a, size_t n, const void* b, size_t m) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + m && y < x + n;
+}
+
 // Host-side checks of a batch; fills qo offsets (request r owns rows [qo[r], qo[r+1])).
-inline int check_batch(const kvx_batch* b, std::vector<int64_t>& qo, bool need_page_ids = true) {
+// cross: the E queries of a request are not among its tokens in the pool.
+inline int check_batch(const kvx_batch* b, std::vector<int64_t>& qo, bool need_page_ids = true, bool cross = false) {
   if (b == nullptr) return report(KVX_EINVAL, "batch is NULL");
   if (b->num_reqs < 0) return report(KVX_EINVAL, "num_reqs = %d < 0", b->num_reqs);
   qo.assign((size_t)b->num_reqs + 1, 0);
@@ -158,9 +210,10 @@ inline int check_batch(const kvx_batch* b, std::vector<int64_t>& qo, bool need_p
     if (P < 0 || E < 0) return report(KVX_EINVAL, "request %d: negative length (P=%lld, E=%lld)", r, (long long)P, (long long)E);
     if (P + E > (int64_t)INT32_MAX - 1024) return report(KVX_EINVAL, "request %d: sequence too long", r);
     const int64_t have = (int64_t)b->page_indptr[r + 1] - b->page_indptr[r];
-    if (have < ceil_div(P + E, kPageSize))
+    const int64_t held = cross ? P : P + E;
+    if (have < ceil_div(held, kPageSize))
       return report(KVX_EINVAL, "request %d: %lld page ids for %lld tokens (need %lld)", r, (long long)have,
-                  (long long)(P + E), (long long)ceil_div(P + E, kPageSize));
+                  (long long)held, (long long)ceil_div(held, kPageSize));
     qo[r + 1] = qo[r] + E;
   }
   if (qo.back() > (int64_t)INT32_MAX) return report(KVX_EINVAL, "total extend length exceeds 2^31-1");
@@ -207,6 +260,43 @@ inline bool inline_store_reqs(const kvx_batch* b, const std::vector<int64_t>& qo
   }
   rq.first[rq.n] = wg;
   return rq.n > 0;
+}
+
+// The touched pages of a batch's suffixes, request by request.
+inline std::vector<RopeUnit> page_units(const kvx_batch* batch, const std::vector<int64_t>& qo) {
+  std::vector<RopeUnit> units;
+  const int64_t S = kPageSize;
+  for (int r = 0; r < batch->num_reqs; r++) {
+    const int64_t P = batch->prefix_lens[r], E = batch->extend_lens[r], L = P + E;
+    if (E == 0) continue;
+    for (int64_t lp = P / S; lp <= (L - 1) / S; lp++) {
+      RopeUnit u;
+      u.row_slot0 = (int32_t)(qo[(size_t)r] + lp * S - P);
+      u.page_pos = (int32_t)(batch->page_indptr[r] + lp);
+      u.slot_begin = (int32_t)(std::max<int64_t>(P, lp * S) - lp * S);
+      u.slot_end = (int32_t)(std::min<int64_t>(L, lp * S + S) - lp * S);
+      u.pos_slot0 = (int32_t)(lp * S);
+      units.push_back(u);
+    }
+  }
+  return units;
+}
+
+// The units of a store or load call, in its arguments or uploaded through `staging`.
+template <typename Params>
+int place_units(Staging& staging, const kvx_batch* batch, const std::vector<int64_t>& qo, hipStream_t s, Params& p,
+                int64_t& n_units) {
+  p.units = nullptr;
+  if (inline_store_reqs(batch, qo, p.reqs)) {
+    n_units = p.reqs.first[p.reqs.n];
+    return KVX_OK;
+  }
+  const std::vector<RopeUnit> units = page_units(batch, qo);
+  n_units = (int64_t)units.size();
+  void* dev = nullptr;
+  if (int rc = staging.upload(units.data(), units.size() * sizeof(RopeUnit), s, &dev)) return rc;
+  p.units = (const RopeUnit*)dev;
+  return KVX_OK;
 }
 
 }  // namespace kvx

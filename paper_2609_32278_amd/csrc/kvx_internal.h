@@ -15,6 +15,11 @@ constexpr int kTileKeys = 64;   // keys per K/V tile staged in LDS
 constexpr int kAttnThreads = 512;  // 8 waves x 32 query rows
 constexpr int kNumXcd = 8;      // L2 domains of an MI355X; workgroup i runs on XCD i % 8
 
+// Powers of two that 8-bit values share (a page's K or V of one head, a group of latent values):
+// within these, every code * 2^e is a finite, normal bf16 value.
+constexpr int kMinScaleExp = -117;
+constexpr int kMaxScaleExp = 119;
+
 // One attention workgroup: a tile of suffix tokens of one request and one KV head,
 // over keys [key_begin, key_end) of the request's logical sequence.
 struct AttnUnit {
@@ -135,6 +140,8 @@ struct AttnParams {
   // For the launcher: the plan (in host memory) for the kernel arguments, or null when the
   // units were uploaded.
   const CompactPlan* compact;
+  int32_t page_scaled;  // k_scale holds a power of two a page, head and K or V
+  int32_t cross;        // the units are of a cross attention
 };
 
 struct MergeParams {
@@ -208,8 +215,26 @@ struct RopeParams {
   int32_t lg_q;
   int32_t lg_k;
   int32_t whole_page;
+  // page-scaled pool: device [num_pages, Hkv, (K, V)], which the store writes; else null.  Such a
+  // store may have no rotation (rotary_dim 0, no Q): store_kv's
+  float* page_scale;
   double rev_freq[kRopeMaxPlanes];  // plane rate in revolutions per position: f_j / (2 pi)
   StoreReqs reqs;                   // reqs.n > 0: the units come from here instead
+};
+
+// Tokens of any pool read back as bf16 rows.
+struct LoadParams {
+  const void* k_pool;
+  const void* v_pool;
+  const float* k_scale;   // fp8 pool: [Hkv]
+  const float* v_scale;
+  const float* page_scale;  // page-scaled pool: [num_pages, Hkv, (K, V)]
+  uint16_t* k_out;        // bf16 [T, Hkv, D]
+  uint16_t* v_out;
+  const int32_t* page_ids;
+  const RopeUnit* units;
+  int32_t num_kv_heads;
+  StoreReqs reqs;
 };
 
 // Page ids of one launch of the page I/O kernel in its arguments.
@@ -223,10 +248,12 @@ struct PageIoParams {
   void* v_lin;
   int32_t num_kv_heads;
   int32_t to_pool;          // 1: write pages into the pool, 0: read them out
+  float* page_scale;        // page-scaled pool (page_ids are given): [num_pages, Hkv, (K, V)]; the buffers go
+                            // on with the pages' scales, [n][Hkv]; else null
 };
 
 // Raw page records between the pool and host memory: record i = the K block then
-// the V block of page page_ids[i], at host + slots[i] * 2 * block_bytes.
+// the V block of page page_ids[i], at host + slots[i] * record_bytes.
 struct PageMoveParams {
   const int32_t* page_ids;  // device [n]
   const int32_t* slots;     // device [n]
@@ -234,6 +261,9 @@ struct PageMoveParams {
   uint8_t* v_pool;
   uint8_t* host;            // device-accessible address of pinned host memory
   int64_t block_bytes;      // Hkv * 16 * D * elem bytes (a multiple of 1 KiB)
+  int64_t record_bytes;     // of a record in host memory
+  float* page_scale;        // page-scaled pool: [num_pages, Hkv, (K, V)], which end a record; else null
+  int32_t num_kv_heads;
   int32_t to_host;          // 1: pool -> host (spill), 0: host -> pool (reload)
 };
 
@@ -250,7 +280,7 @@ struct DecodeUnit {
   int32_t head;       // KV head
   int32_t part;       // -1: final result; else index of this chunk's partial result
   int32_t req;
-  int32_t pad;
+  int32_t ntok;       // cross attention: the queries (tokens) from qo_row on; else unused
 };
 static_assert(sizeof(DecodeUnit) == 32, "DecodeUnit is 32 bytes");
 
@@ -276,6 +306,10 @@ struct DecodeArgs {
   int32_t num_kv_heads;
   int32_t group;          // Hq / Hkv <= kDecodeMaxGroup
   float scale_log2;
+  // For the launcher: k_scale holds a power of two a page, head and K or V; the units are of a cross
+  // attention, of several tokens each.
+  int32_t page_scaled;
+  int32_t cross;
 };
 
 // Page lists of the requests that decode in a batch read with non-temporal loads, to tell
@@ -304,6 +338,7 @@ struct DecodeMergeParams {
   float* lse;
   int32_t num_q_heads;
   int32_t group;
+  int32_t cross;  // most tokens of a merge of a cross attention, whose head is head | tokens << 16; else 0
   InlineMerges<DecodeMerge> plan;  // plan.n > 0: the merges
 };
 static_assert(sizeof(DecodeMergeParams) <= 4096, "kernel arguments");
@@ -339,11 +374,21 @@ hipError_t launch_mixed_attention(const AttnParams& p, int64_t n_units, int head
 // ... and of a compact plan, from the kernel arguments
 hipError_t launch_small_attention(const AttnParams& p, int64_t n_units, int head_dim, bool fp8, bool scaled_q,
                                   hipStream_t stream);
+// ... on a page-scaled pool, and of a cross attention, whatever the plan
+hipError_t launch_page_attention(const AttnParams& p, int64_t n_units, int head_dim, bool scaled_q, hipStream_t stream);
+hipError_t launch_cross_attention(const AttnParams& p, int64_t n_units, int head_dim, bool fp8, bool scaled_q,
+                                  hipStream_t stream);
+hipError_t launch_cross_page_attention(const AttnParams& p, int64_t n_units, int head_dim, bool scaled_q,
+                                       hipStream_t stream);
 hipError_t launch_merge(const MergeParams& p, int64_t n_merges, int head_dim, hipStream_t stream);
 hipError_t launch_store_kv(const StoreParams& p, int64_t n_units, int head_dim, bool fp8,
                            hipStream_t stream);
 hipError_t launch_store_kv_rope(const RopeParams& p, int64_t n_units, int head_dim, bool fp8, bool interleaved,
                                 hipStream_t stream);
+// launch_store_kv_rope into a page-scaled pool
+hipError_t launch_store_kv_page(const RopeParams& p, int64_t n_units, int head_dim, bool interleaved,
+                                hipStream_t stream);
+hipError_t launch_load_kv(const LoadParams& p, int64_t n_units, int head_dim, int32_t kv_dtype, hipStream_t stream);
 hipError_t launch_page_move(const PageMoveParams& p, int64_t n_pages, hipStream_t stream);
 hipError_t launch_page_io(const PageIoParams& p, int64_t n_pages, int head_dim, int elem_bytes,
                           hipStream_t stream);

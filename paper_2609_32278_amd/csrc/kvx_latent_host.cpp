@@ -19,6 +19,10 @@ using kvx::ceil_div;
 using kvx::check_align;
 using kvx::check_batch;
 using kvx::check_page_ids;
+using kvx::check_stream;
+using kvx::guarded;
+using kvx::meet;
+using kvx::OnDevice;
 using kvx::hip_fail;
 using kvx::LatentExpandUnit;
 using kvx::LatentMerge;
@@ -51,51 +55,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMaxPartBytes = 2ll << 30;
 constexpr int64_t kMaxExpandBytes = 2ll << 30;
 
-// Run an entry point's body: no exception crosses the ABI, and an error of the runtime that is
-// returned is not left for the caller's next call to find.
-template <typename F>
-int guarded(F&& body) {
-  report(KVX_OK, "%s", "");
-  try {
-    const int rc = body();
-    if (rc == KVX_EHIP || rc == KVX_ENOMEM) (void)hipGetLastError();
-    return rc;
-  } catch (const std::bad_alloc&) {
-    return report(KVX_ENOMEM, "host memory for the plan of the call");
-  } catch (...) {
-    return report(KVX_EINVAL, "unexpected failure on the host");
-  }
-}
-
-// The pool's device for the length of a call.
-struct OnDevice {
-  int before = -1;
-  int enter(int device) {
-    KVX_HIP(hipGetDevice(&before));
-    if (before == device) before = -1;
-    else KVX_HIP(hipSetDevice(device));
-    return KVX_OK;
-  }
-  ~OnDevice() {
-    if (before >= 0) (void)hipSetDevice(before);
-  }
-};
-
 int check_pool(const kvx_latent_pool* pool) {
   if (pool == nullptr) return report(KVX_EINVAL, "pool is NULL");
-  return KVX_OK;
-}
-
-int check_stream(hipStream_t s, int device) {
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  const hipError_t e = hipStreamIsCapturing(s, &st);
-  if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
-  if (st != hipStreamCaptureStatusNone)
-    return report(KVX_EUNSUPPORTED, "the stream is being captured: the plan of a call is made on the host");
-  if (s == nullptr || s == hipStreamLegacy || s == hipStreamPerThread) return KVX_OK;  // the current device's
-  hipDevice_t of = device;
-  KVX_HIP(hipStreamGetDevice(s, &of));
-  if (of != device) return report(KVX_EINVAL, "the stream is of device %d, the pool of device %d", of, device);
   return KVX_OK;
 }
 
@@ -120,12 +81,6 @@ int check_heads(const kvx_batch* b, int32_t Hq) {
   return KVX_OK;
 }
 
-// Byte ranges [a, a + n) and [b, b + m) that meet.
-bool meet(const void* a, size_t n, const void* b, size_t m) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + m && y < x + n;
-}
-
 // Whether [a, a + n) meets one of `rows` rows of `width` bytes, `stride` apart, from b on.
 bool meets_rows(const void* a, size_t n, const void* b, int64_t rows, size_t width, size_t stride) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
@@ -148,43 +103,6 @@ int check_results(const void* out, size_t row, const float* lse, size_t rows, co
 
 kvx::LatentPoolView view(const kvx_latent_pool* pool, const kvx_batch* batch) {
   return {pool->base, pool->page_bytes, batch->page_ids};
-}
-
-// The touched pages of a batch's suffixes, request by request.
-std::vector<kvx::RopeUnit> page_units(const kvx_batch* batch, const std::vector<int64_t>& qo) {
-  std::vector<kvx::RopeUnit> units;
-  const int64_t S = kvx::kPageSize;
-  for (int r = 0; r < batch->num_reqs; r++) {
-    const int64_t P = batch->prefix_lens[r], E = batch->extend_lens[r], L = P + E;
-    if (E == 0) continue;
-    for (int64_t lp = P / S; lp <= (L - 1) / S; lp++) {
-      kvx::RopeUnit u;
-      u.row_slot0 = (int32_t)(qo[(size_t)r] + lp * S - P);
-      u.page_pos = (int32_t)(batch->page_indptr[r] + lp);
-      u.slot_begin = (int32_t)(std::max<int64_t>(P, lp * S) - lp * S);
-      u.slot_end = (int32_t)(std::min<int64_t>(L, lp * S + S) - lp * S);
-      u.pos_slot0 = (int32_t)(lp * S);
-      units.push_back(u);
-    }
-  }
-  return units;
-}
-
-// The units of a store or load call, in its arguments or uploaded.
-template <typename Params>
-int place_units(kvx_latent_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, hipStream_t s,
-                Params& p, int64_t& n_units) {
-  p.units = nullptr;
-  if (kvx::inline_store_reqs(batch, qo, p.reqs)) {
-    n_units = p.reqs.first[p.reqs.n];
-    return KVX_OK;
-  }
-  const std::vector<kvx::RopeUnit> units = page_units(batch, qo);
-  n_units = (int64_t)units.size();
-  void* dev = nullptr;
-  if (int rc = pool->st_rows.upload(units.data(), units.size() * sizeof(kvx::RopeUnit), s, &dev)) return rc;
-  p.units = (const kvx::RopeUnit*)dev;
-  return KVX_OK;
 }
 
 int check_stride(int64_t stride, int row, const char* name) {
@@ -251,7 +169,7 @@ int store_call(kvx_latent_pool* pool, const kvx_batch* batch, const kvx_rope* ro
   if (kvx::validate_mode())
     if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
   int64_t n_units = 0;
-  if (int rc = place_units(pool, batch, qo, s, p, n_units)) return rc;
+  if (int rc = kvx::place_units(pool->st_rows, batch, qo, s, p, n_units)) return rc;
   p.pool = view(pool, batch);
   p.kv = (const uint16_t*)kv;
   p.kv_stride = kv_stride;
@@ -882,7 +800,7 @@ int load_latent(kvx_latent_pool* pool, const kvx_batch* batch, void* out, int64_
       if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
     kvx::LatentLoadParams p{};
     int64_t n_units = 0;
-    if (int rc = place_units(pool, batch, qo, s, p, n_units)) return rc;
+    if (int rc = kvx::place_units(pool->st_rows, batch, qo, s, p, n_units)) return rc;
     p.pool = view(pool, batch);
     p.out = (uint16_t*)out;
     p.out_stride = out_stride;

@@ -8,8 +8,6 @@ namespace kvx {
 
 constexpr int kLatRope = 64;        // rope_dim
 constexpr int kLatGroup = 64;       // latent values that share a scale on an fp8 pool
-constexpr int kLatMinExp = -117;    // their powers of two: every code * 2^e is a finite, normal bf16 value
-constexpr int kLatMaxExp = 119;
 
 // Where the scale byte of (slot, group) lies among a page's scale bytes.  A wave that reads a
 // page's codes takes 8 slots x 128 codes at once, 16 codes a lane; the bytes that one lane

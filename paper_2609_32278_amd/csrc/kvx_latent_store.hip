@@ -25,12 +25,6 @@ struct Angles {
   float2 cs[kPageSize][kPlanes];  // (cos, sin) of every live slot and plane
 };
 
-__device__ __forceinline__ void unpack(uint4 raw, float (&x)[8]) {
-  const uint16_t* h = (const uint16_t*)&raw;
-#pragma unroll
-  for (int e = 0; e < 8; e++) x[e] = bf16_to_f32(h[e]);
-}
-
 // Turn pieces pr (dims 8 pr ..) and pr + 4 (dims 32 + 8 pr ..) of a 64-dim head.
 template <bool INTERLEAVED>
 __device__ __forceinline__ void turn(float (&x)[8], float (&y)[8], const float2* cs, int pr) {
@@ -53,23 +47,6 @@ __device__ __forceinline__ void turn(float (&x)[8], float (&y)[8], const float2*
       y[e] = a * c.y + b * c.x;
     }
   }
-}
-
-// The group's power of two (see kvx_latent.h) from its largest magnitude: amax = 1.f 2^(E - 127)
-// is at most 448 * 2^e = 1.75 * 2^(8 + e) for e = E - 135, or one more where 1.f > 1.75.
-__device__ __forceinline__ int group_exp(float amax) {
-  const uint32_t b = __float_as_uint(amax);
-  const int e = (int)(b >> 23) - 135 + ((b & 0x7FFFFF) > 0x600000 ? 1 : 0);
-  return e < kLatMinExp ? kLatMinExp : (e > kLatMaxExp ? kLatMaxExp : e);
-}
-
-// clamp448 lets a NaN end as a number; the cache keeps it.
-__device__ __forceinline__ float clamp_keep_nan(float x) { return x != x ? x : clamp448(x); }
-
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(clamp_keep_nan(a), clamp_keep_nan(b), 0, false);
-  r = __builtin_amdgcn_cvt_pk_fp8_f32(clamp_keep_nan(c), clamp_keep_nan(d), r, true);
-  return (uint32_t)r;
 }
 
 template <int LAT, bool FP8, bool INTERLEAVED>
@@ -120,8 +97,8 @@ __global__ __launch_bounds__(kThreads) void store_latent_kernel(LatentStoreParam
         const int i = i0 + f * kThreads, r = i >> 2, pr = i & 3;
         if (i < nrows * 4 && h0 + (r & lgm) < Hq) {
           float x[8], y[8];
-          unpack(a[f], x);
-          unpack(b[f], y);
+          unpack_bf16x8(a[f], x);
+          unpack_bf16x8(b[f], y);
           turn<INTERLEAVED>(x, y, sm.cs[r >> lg], pr);
           uint16_t* dst = qo + at_row(r) + (D - kLatRope) + pr * 8;
           store16<true>(dst, pack_bf16x8(x));
@@ -159,12 +136,12 @@ __global__ __launch_bounds__(kThreads) void store_latent_kernel(LatentStoreParam
     if (tok < ntok) raw[it] = *(const uint4*)(p.kv + (row0 + tok) * p.kv_stride + c * 8);
   }
   float w[8];
-  if (p.norm) unpack(*(const uint4*)(p.norm + c * 8), w);
+  if (p.norm) unpack_bf16x8(*(const uint4*)(p.norm + c * 8), w);
 #pragma unroll
   for (int it = 0; it < ITS; it++) {
     const int tok = (it * 4 + wave) * TPW + sub, slot = u.slot_begin + tok;
     float x[8];
-    unpack(raw[it], x);
+    unpack_bf16x8(raw[it], x);
     if (p.norm) {  // uniform; lanes of tokens past the unit's sum zeros
       float ss = 0.0f;
 #pragma unroll
@@ -181,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void store_latent_kernel(LatentStoreParam
       for (int e = 0; e < 8; e++) amax = fmaxf(amax, fabsf(x[e]));
 #pragma unroll
       for (int m = 1; m < 8; m <<= 1) amax = fmaxf(amax, __shfl_xor(amax, m, 64));
-      const int ex = group_exp(amax);
+      const int ex = scale_exp(amax);
       const float by = __uint_as_float((uint32_t)(127 - ex) << 23);
       uint2 code;
       code.x = codes4(x[0] * by, x[1] * by, x[2] * by, x[3] * by);
@@ -204,8 +181,8 @@ __global__ __launch_bounds__(kThreads) void store_latent_kernel(LatentStoreParam
     uint4 a = *(const uint4*)src, b = *(const uint4*)(src + 32);
     if (p.rotate) {
       float x[8], y[8];
-      unpack(a, x);
-      unpack(b, y);
+      unpack_bf16x8(a, x);
+      unpack_bf16x8(b, y);
       turn<INTERLEAVED>(x, y, sm.cs[tok], pr);
       a = pack_bf16x8(x);
       b = pack_bf16x8(y);

@@ -21,12 +21,11 @@
 #include <type_traits>
 
 #include "kvx_internal.h"
+#include "kvx_rope_util.h"
 #include "kvx_store_util.h"
 
 namespace kvx {
 namespace {
-
-constexpr int kStoreThreads = 256;
 
 // Write the staged V rows vs[slot][dim] of one (page, head) block as the pool's
 // [dim][slot] columns, 8 slots per thread and step (16 bytes bf16 / 8 bytes fp8);
@@ -160,129 +159,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kv_kernel(StoreParams p) 
 // where a 4 GiB copy reaches 4.8 TB/s).  The price is that each group forms the page's
 // angles again, which its first loads overlap.
 //
-// A head row of D bf16 values is D/8 16-byte chunks held by D/8 consecutive
-// lanes; the RMS sum is reduced across those lanes, and in the half layout a
-// chunk of the first half meets its plane partners in the chunk rotary_dim/16
-// lanes further on (one lane shuffle per value).
-
-constexpr int kRopeBatch = 4;  // chunks per thread in flight
 constexpr int kRopeVHeads = 4;   // V heads per workgroup
-
-template <int D, bool INTERLEAVED>
-struct RopeLane {
-  static constexpr int CPR = D / 8;
-  int cc;           // chunk of the row this lane handles (fixed for the thread)
-  int partner;      // lane holding the plane partners (half layout)
-  int jb;           // first plane of the chunk
-  bool rot;         // the chunk lies inside rotary_dim
-  float sgn;        // half layout: -1 for the plane's first dims, +1 for its second
-
-  __device__ RopeLane(int rotary_dim) {
-    cc = threadIdx.x % CPR;
-    const int lane = threadIdx.x & 63;
-    if constexpr (INTERLEAVED) {
-      rot = cc < (rotary_dim >> 3);
-      jb = 4 * cc;
-      partner = lane;
-      sgn = 0.0f;
-    } else {
-      const int r16 = rotary_dim >> 4;
-      const bool first = cc < r16;
-      rot = cc < 2 * r16;
-      jb = first ? 8 * cc : 8 * (cc - r16);
-      partner = lane + (first ? r16 : (rot ? -r16 : 0));
-      sgn = first ? -1.0f : 1.0f;
-    }
-  }
-};
-
-// x: the 8 values of this lane's chunk of one row at `slot`; in place -> rotated.
-// Every lane of the row must execute this (shuffles).
-template <int D, bool INTERLEAVED>
-__device__ __forceinline__ void rope_chunk(float (&x)[8], const RopeLane<D, INTERLEAVED>& rl,
-                                           const float2* cs_slot) {
-  if constexpr (INTERLEAVED) {
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const float2 t = rl.rot ? cs_slot[rl.jb + i] : make_float2(1.0f, 0.0f);
-      const float a = x[2 * i], b = x[2 * i + 1];
-      x[2 * i] = a * t.x - b * t.y;
-      x[2 * i + 1] = a * t.y + b * t.x;
-    }
-  } else {
-    float pe[8];
-#pragma unroll
-    for (int e = 0; e < 8; e++) pe[e] = __shfl(x[e], rl.partner, 64);
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-      const float2 t = rl.rot ? cs_slot[rl.jb + e] : make_float2(1.0f, 0.0f);
-      // first dims: a cos - b sin (b = partner); second dims: b cos + a sin (a = partner)
-      x[e] = x[e] * t.x + rl.sgn * (pe[e] * t.y);
-    }
-  }
-}
-
-// Normalise and rotate `nh` heads from h0 on (nh <= 1 << lg) of the unit's ntok tokens
-// (src: the first token's row, [token][heads][D] bf16) and hand each chunk's results
-// to out(token, head, chunk, y).  The first loads are issued before angles() -- which
-// fills cs and ends in a barrier -- so that they are in flight meanwhile.
-template <int D, bool INTERLEAVED, class Angles, class Out>
-__device__ __forceinline__ void rope_rows(const uint16_t* __restrict__ src, int ntok, int heads, int h0, int nh, int lg,
-                                          int slot_begin, const float2 (*cs)[kRopeMaxPlanes],
-                                          const uint16_t* norm_w, float eps, int rotary_dim, Angles&& angles,
-                                          Out&& out) {
-  constexpr int CPR = D / 8;
-  const RopeLane<D, INTERLEAVED> rl(rotary_dim);
-  // row index rr = token << lg | head of the group; rows past the group's heads idle
-  const int n = ntok << lg;
-  constexpr int ROWS = kStoreThreads / CPR;  // rows per step
-  const int r0 = threadIdx.x / CPR;
-  auto load = [&](int rr) {
-    const int tok = rr >> lg, hh = rr & ((1 << lg) - 1);
-    return rr < n && hh < nh ? *(const uint4*)(src + ((size_t)tok * heads + h0 + hh) * D + rl.cc * 8)
-                             : make_uint4(0, 0, 0, 0);
-  };
-  uint4 raw[kRopeBatch];
-#pragma unroll
-  for (int b = 0; b < kRopeBatch; b++) raw[b] = load(r0 + b * ROWS);
-  float w[8];
-  if (norm_w) {
-    const uint4 wr = *(const uint4*)(norm_w + rl.cc * 8);
-    const uint16_t* wh = (const uint16_t*)&wr;
-#pragma unroll
-    for (int e = 0; e < 8; e++) w[e] = bf16_to_f32(wh[e]);
-  }
-  angles();
-  for (int c0 = r0; c0 - r0 < n; c0 += kRopeBatch * ROWS) {
-    uint4 next[kRopeBatch];
-#pragma unroll
-    for (int b = 0; b < kRopeBatch; b++) next[b] = load(c0 + (kRopeBatch + b) * ROWS);
-#pragma unroll
-    for (int b = 0; b < kRopeBatch; b++) {
-      const int rr = c0 + b * ROWS;
-      if (rr - r0 >= n) break;  // uniform
-      const int tok = rr >> lg, hh = rr & ((1 << lg) - 1);
-      const uint16_t* h16 = (const uint16_t*)&raw[b];
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; e++) x[e] = bf16_to_f32(h16[e]);
-      if (norm_w) {
-        float ss = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; e++) ss = fmaf(x[e], x[e], ss);
-#pragma unroll
-        for (int m = 1; m < CPR; m <<= 1) ss += __shfl_xor(ss, m, 64);
-        const float inv = 1.0f / sqrtf(ss * (1.0f / D) + eps);
-#pragma unroll
-        for (int e = 0; e < 8; e++) x[e] = (x[e] * inv) * w[e];
-      }
-      rope_chunk<D, INTERLEAVED>(x, rl, cs[slot_begin + (rr < n ? tok : 0)]);
-      if (rr < n && hh < nh) out(tok, h0 + hh, rl.cc, x);
-    }
-#pragma unroll
-    for (int b = 0; b < kRopeBatch; b++) raw[b] = next[b];
-  }
-}
 
 // Grid: x = the unit (a touched page), y = a group of heads: first the groups of
 // 1 << p.lg_q Q heads, then those of 1 << p.lg_k K heads, then those of HB V heads.  With
@@ -310,15 +187,7 @@ __global__ __launch_bounds__(kStoreThreads) void store_kv_rope_kernel(RopeParams
   auto angles = [&]() {
     if (have_angles) return;  // uniform
     have_angles = true;
-    const int planes = p.rotary_dim / 2;
-    for (int e = threadIdx.x; e < ntok * planes; e += kStoreThreads) {
-      const int s = u.slot_begin + e / planes, j = e % planes;
-      double rev = (double)(u.pos_slot0 + s) * p.rev_freq[j];  // exact position times the rate
-      rev -= rint(rev);                                          // [-1/2, 1/2] turn, exact
-      float sn, cn;
-      sincospif(2.0f * (float)rev, &sn, &cn);
-      sm.cs[s][j] = make_float2(cn, sn);
-    }
+    fill_angles(sm.cs, u, p.rotary_dim, p.rev_freq);
     __syncthreads();
   };
 
@@ -382,16 +251,25 @@ __global__ __launch_bounds__(kStoreThreads) void store_kv_rope_kernel(RopeParams
 }
 
 // Spill / reload of whole pages between the pool and pinned host memory.  One
-// workgroup per (page, K|V block): the block is contiguous on both sides, so
+// workgroup per (page, K|V block), and one for a page's scales where it has some: the block is contiguous on both sides, so
 // every lane moves 16-byte pieces, four in flight before any store (host memory
 // is reached over the host link: latency is long, concurrency hides it).
 __global__ __launch_bounds__(256) void page_move_kernel(PageMoveParams p) {
   constexpr int kUnroll = 4;
   const int i = blockIdx.x;
-  const int kv = blockIdx.y;  // 0: K block, 1: V block
+  const int kv = blockIdx.y;  // 0: K block, 1: V block, 2: scales
   const int64_t page = p.page_ids[i];
+  uint8_t* host = p.host + (int64_t)p.slots[i] * p.record_bytes + kv * p.block_bytes;
+  if (kv == 2) {
+    const int n = 2 * p.num_kv_heads;
+    float* scale = p.page_scale + page * n;
+    for (int h = threadIdx.x; h < n; h += 256) {
+      if (p.to_host) ((float*)host)[h] = scale[h];
+      else scale[h] = ((const float*)host)[h];
+    }
+    return;
+  }
   uint8_t* dev = (kv == 0 ? p.k_pool : p.v_pool) + page * p.block_bytes;
-  uint8_t* host = p.host + ((int64_t)p.slots[i] * 2 + kv) * p.block_bytes;
   const uint8_t* src = p.to_host ? dev : host;
   uint8_t* dst = p.to_host ? host : dev;
   const int64_t pieces = p.block_bytes / 16;
@@ -493,6 +371,21 @@ __global__ __launch_bounds__(256) void page_io_kernel(PageIoParams p, int32_t n_
   }
 }
 
+// The scales of a page-scaled pool's pages, to or from [n][Hkv] arrays.
+__global__ __launch_bounds__(256) void page_scales_kernel(PageIoParams p, int64_t n, float* k_lin, float* v_lin) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int H = p.num_kv_heads;
+  if (i >= n * H) return;
+  float* scale = p.page_scale + 2 * ((int64_t)p.page_ids[i / H] * H + i % H);
+  if (p.to_pool) {
+    scale[0] = k_lin[i];
+    scale[1] = v_lin[i];
+  } else {
+    k_lin[i] = scale[0];
+    v_lin[i] = scale[1];
+  }
+}
+
 }  // namespace
 
 hipError_t launch_store_kv(const StoreParams& p, int64_t n_units, int head_dim, bool fp8,
@@ -543,6 +436,7 @@ static int64_t rope_groups(RopeParams& p, int64_t n_units) {
 hipError_t launch_store_kv_rope(const RopeParams& params, int64_t n_units, int head_dim, bool fp8, bool interleaved,
                                 hipStream_t stream) {
   if (n_units <= 0) return hipSuccess;
+  if (params.page_scale != nullptr) return launch_store_kv_page(params, n_units, head_dim, interleaved, stream);
   RopeParams p = params;
   const int64_t groups = rope_groups(p, n_units);
   dim3 grid((unsigned)n_units, (unsigned)groups), block(kStoreThreads);
@@ -560,7 +454,7 @@ hipError_t launch_store_kv_rope(const RopeParams& params, int64_t n_units, int h
 
 hipError_t launch_page_move(const PageMoveParams& p, int64_t n_pages, hipStream_t stream) {
   if (n_pages <= 0) return hipSuccess;
-  hipLaunchKernelGGL(page_move_kernel, dim3((unsigned)n_pages, 2), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL(page_move_kernel, dim3((unsigned)n_pages, p.page_scale != nullptr ? 3 : 2), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -598,6 +492,11 @@ hipError_t launch_page_io(const PageIoParams& p, int64_t n_pages, int head_dim, 
   } else {
     if (elem_bytes == 2) launch_page_io_dir<64, 2>(p, n_pages, stream);
     else launch_page_io_dir<64, 1>(p, n_pages, stream);
+  }
+  if (p.page_scale != nullptr) {
+    const int64_t entries = n_pages * p.num_kv_heads, codes = entries * kPageSize * head_dim;
+    hipLaunchKernelGGL(page_scales_kernel, dim3((unsigned)((entries + 255) / 256)), dim3(256), 0, stream, p, n_pages,
+                       (float*)((uint8_t*)p.k_lin + codes), (float*)((uint8_t*)p.v_lin + codes));
   }
   return hipGetLastError();
 }

@@ -32,6 +32,24 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return (uint32_t)r;
 }
 
+// The power of two of values that share one, from their largest magnitude: the smallest e with
+// amax <= 448 * 2^e, within [kMinScaleExp, kMaxScaleExp].  amax = 1.f 2^(E - 127) is at most
+// 448 * 2^e = 1.75 * 2^(8 + e) for e = E - 135, or one more where 1.f > 1.75.
+__device__ __forceinline__ int scale_exp(float amax) {
+  const uint32_t b = __float_as_uint(amax);
+  const int e = (int)(b >> 23) - 135 + ((b & 0x7FFFFF) > 0x600000 ? 1 : 0);
+  return e < kMinScaleExp ? kMinScaleExp : (e > kMaxScaleExp ? kMaxScaleExp : e);
+}
+
+// clamp448 lets a NaN end as a number; the cache keeps it.
+__device__ __forceinline__ float clamp_keep_nan(float x) { return x != x ? x : clamp448(x); }
+
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(clamp_keep_nan(a), clamp_keep_nan(b), 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(clamp_keep_nan(c), clamp_keep_nan(d), r, true);
+  return (uint32_t)r;
+}
+
 __device__ __forceinline__ uint4 pack_bf16x8(const float (&y)[8]) {
   uint4 r;
   uint32_t* w = (uint32_t*)&r;
@@ -41,6 +59,12 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&y)[8]) {
     w[i] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | ((uint32_t)__builtin_bit_cast(uint16_t, hi) << 16);
   }
   return r;
+}
+
+__device__ __forceinline__ void unpack_bf16x8(uint4 raw, float (&x)[8]) {
+  const uint16_t* h = (const uint16_t*)&raw;
+#pragma unroll
+  for (int e = 0; e < 8; e++) x[e] = bf16_to_f32(h[e]);
 }
 
 // The unit of workgroup b of a small batch (see StoreReqs); uniform.

@@ -19,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libkvx.so")
 
 KVX_OK, KVX_EINVAL, KVX_ENOMEM, KVX_ERANGE, KVX_EUNSUPPORTED, KVX_EHIP = range(6)
-KVX_KV_BF16, KVX_KV_FP8_E4M3 = 0, 1
+KVX_KV_BF16, KVX_KV_FP8_E4M3, KVX_KV_FP8_PAGE = 0, 1, 2
 STATUS_NAMES = {0: "KVX_OK", 1: "KVX_EINVAL", 2: "KVX_ENOMEM", 3: "KVX_ERANGE",
                 4: "KVX_EUNSUPPORTED", 5: "KVX_EHIP"}
 
@@ -31,7 +31,7 @@ NOALLOC_PLAN_BYTES, NOALLOC_PARTS_BYTES = 8 << 20, 56 << 20  # KVX_NOALLOC_* in 
 
 # Every symbol the headers in include/ declare.
 EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_pool_layout", "kv_pool_write_pages",
-           "kv_pool_read_pages", "kv_pool_record_bytes", "kv_pool_spill", "kv_pool_reload", "store_kv", "store_kv_rope", "extend_attention", "extend_attention_noalloc", "extend_attention_plan",
+           "kv_pool_read_pages", "kv_pool_record_bytes", "kv_pool_spill", "kv_pool_reload", "store_kv", "store_kv_rope", "load_kv", "cross_attention", "extend_attention", "extend_attention_noalloc", "extend_attention_plan",
            "kv_pool_set_split_keys", "kv_pool_set_scaled_q", "kvx_last_error",
            "kvx_cache_create", "kvx_cache_create_tiered", "kvx_cache_set_recency_tiers", "kvx_cache_destroy", "kvx_cache_begin_turn",
            "kvx_cache_begin_turn_tiered", "kvx_cache_end_turn", "kvx_cache_complete", "kvx_cache_agent",
@@ -136,7 +136,9 @@ def lib():
             "kv_pool_reload": [P, P, P, i64, P, i64, P],
             "store_kv": [P, ctypes.POINTER(kvx_batch), P, P, P],
             "store_kv_rope": [P, ctypes.POINTER(kvx_batch), ctypes.POINTER(kvx_rope), P, i32, P, P, P, P],
+            "load_kv": [P, ctypes.POINTER(kvx_batch), P, P, P],
             "extend_attention": [P, ctypes.POINTER(kvx_batch), P, i32, f32, P, P, P],
+            "cross_attention": [P, ctypes.POINTER(kvx_batch), P, i32, f32, P, P, P],
             "extend_attention_noalloc": [P, ctypes.POINTER(kvx_batch), P, i32, f32, P, P, P],
             "extend_attention_plan": [ctypes.POINTER(kvx_batch), i32, i32, i32, i32, P, i64, ctypes.POINTER(i64)],
             "kv_pool_set_split_keys": [P, i32],
@@ -283,9 +285,11 @@ def _geometry(pool) -> tuple:
 
 
 def _page_buffers(pool, n, k, v) -> None:
-    hkv, d, eb = _geometry(pool)
-    _need(k, n * hkv * 16 * d * eb, "K buffer")
-    _need(v, n * hkv * 16 * d * eb, "V buffer")
+    lay = kv_pool_layout(pool)
+    scales = 4 if lay["kv_dtype"] == KVX_KV_FP8_PAGE else 0  # behind the codes
+    nbytes = n * lay["num_kv_heads"] * (16 * lay["head_dim"] * lay["elem_bytes"] + scales)
+    _need(k, nbytes, "K buffer")
+    _need(v, nbytes, "V buffer")
 
 
 def kv_pool_write_pages(pool, page_ids, k_src, v_src, stream=None) -> None:
@@ -373,6 +377,28 @@ def store_kv_rope(pool, batch: Batch, k_ext, v_ext, *, theta: float = 10000.0, r
                  _dptr(q_norm), _dptr(k_norm), float(norm_eps))
     _check(lib().store_kv_rope(pool, ctypes.byref(batch.c), ctypes.byref(r), _dptr(q), int(num_q_heads),
                                _dptr(q_out), _dptr(k_ext), _dptr(v_ext), _stream(stream)), "store_kv_rope")
+
+
+def load_kv(pool, batch: Batch, k_out, v_out, stream=None) -> None:
+    """Tokens [P, P + E) of every request as bf16 rows: k_out, v_out [T, num_kv_heads, head_dim]."""
+    hkv, d, _ = _geometry(pool)
+    for name, buf in (("k_out", k_out), ("v_out", v_out)):
+        _elems(buf, 2, name)
+        _need(buf, 2 * batch.total_extend * hkv * d, name)
+    _check(lib().load_kv(pool, ctypes.byref(batch.c), _dptr(k_out), _dptr(v_out), _stream(stream, k_out, v_out)),
+           "load_kv")
+
+
+def cross_attention(pool, batch: Batch, q, num_q_heads: int, sm_scale: float, out, lse=None, stream=None) -> None:
+    """Attention of a request's extend_lens[r] queries to all of the prefix_lens[r] tokens it has in
+    the pool, without a causal mask.  q, out: [T, num_q_heads, head_dim]; lse: [T, num_q_heads]."""
+    _, d, _ = _geometry(pool)
+    rows = batch.total_extend * int(num_q_heads)
+    for name, buf, size, width in (("q", q, 2, d), ("out", out, 2, d), ("lse", lse, 4, 1)):
+        _elems(buf, size, name)
+        _need(buf, size * rows * width, name)
+    _check(lib().cross_attention(pool, ctypes.byref(batch.c), _dptr(q), int(num_q_heads), float(sm_scale), _dptr(out),
+                                 _dptr(lse), _stream(stream, q, out)), "cross_attention")
 
 
 def extend_attention(pool, batch: Batch, q, num_q_heads: int, sm_scale: float, out, lse=None, stream=None) -> None:
