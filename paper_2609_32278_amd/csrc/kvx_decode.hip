@@ -32,7 +32,6 @@ using decode::pack2;
 constexpr int kWaves = kDecodeThreads / 64;
 
 // The work item of this workgroup (scalar loads: everything derived stays uniform).
-template <bool CROSS>
 __device__ __forceinline__ DecodeUnit unit_of(const DecodeParams& p) {
   using decode::const_i32_ptr;
   const_i32_ptr w = (const_i32_ptr)(p.units + blockIdx.x);
@@ -50,7 +49,6 @@ __device__ __forceinline__ DecodeUnit unit_of(const DecodeParams& p) {
   u.key_end = w[3];
   u.head = w[4] + h;
   u.part = w[5] < 0 ? -1 : w[5] + h * w[6];
-  if constexpr (CROSS) u.ntok = w[7];
   return u;
 }
 
@@ -80,27 +78,14 @@ __device__ __forceinline__ bool chunk_is_shared(const DecodeParams& p, const Dec
 // 128 agents on one 16k prefix 718 / 928 / 728, on 16 of them 760 / 1075 / 751, on one of 4k
 // with 4k private tokens each 564 / 554 / 523; 128 on one of 64k, fp8 pool, 64/8/128 heads,
 // 1176 / 1997 / 1188.
-// CROSS: the units of a cross attention, of the queries of several tokens each (at most 16 rows).
-// One without keys has nothing to attend to: its rows, any number of them, become zeros.
-template <int D, bool FP8, bool NT, bool PAGE = false, bool CROSS = false>
+template <int D, bool FP8, bool NT>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(DecodeParams p) {
   __shared__ float o[kWaves * kRows * D], m[kWaves * kRows], l[kWaves * kRows];
   const decode::CombineShared<D, kWaves> sm{o, m, l};
-  const DecodeUnit u = unit_of<CROSS>(p);
-  if constexpr (CROSS) {
-    if (u.key_end == 0) {  // uniform
-      for (int64_t i = threadIdx.x; i < (int64_t)u.ntok * p.a.group * (D / 8); i += kDecodeThreads) {
-        const int row = (int)(i / (D / 8)), c = (int)(i % (D / 8));
-        const size_t orow = decode::query_row<true>(p.a, u, row);
-        *(uint4*)(p.a.out + orow * D + 8 * c) = make_uint4(0, 0, 0, 0);
-        if (p.a.lse != nullptr && c == 0) p.a.lse[orow] = -INFINITY;
-      }
-      return;
-    }
-  }
+  const DecodeUnit u = unit_of(p);
   auto nt = [&]() { return NT && !chunk_is_shared(p, u); };
-  if constexpr (FP8) decode::decode_unit_fp8<D, kWaves, false, PAGE, CROSS>(p.a, u, sm, nt);
-  else decode::decode_unit<D, kWaves, false, CROSS>(p.a, u, sm, nt);
+  if constexpr (FP8) decode::decode_unit_fp8<D, kWaves, false>(p.a, u, sm, nt);
+  else decode::decode_unit<D, kWaves, false>(p.a, u, sm, nt);
 }
 
 // Combine the parts of a split decode key range: o = sum_p e^{lse_p - M} o_p / sum_p e^{lse_p - M}.
@@ -109,9 +94,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(DecodeParams 
 // every such part each, so that the parts' loads are in flight together; the groups
 // meet in LDS.  One workgroup per merge with a serial loop over the parts took 43 us for
 // 192 merges of 3-22 parts (8 rows of 128), this takes 4.3 us.
-// CROSS: a merge of several tokens' rows (row = token * group + head), the grid as deep as the
-// most of them.
-template <int D, bool CROSS = false>
+template <int D>
 __global__ __launch_bounds__(256) void decode_merge_kernel(DecodeMergeParams p) {
   constexpr int C4 = D / 4;        // lanes per row
   constexpr int PG = 256 / C4;     // part groups
@@ -128,10 +111,6 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(DecodeMergeParams p) 
     mu = p.merges[blockIdx.x];
   }
   const int row = blockIdx.y;
-  if constexpr (CROSS) {
-    if (row >= (mu.head >> 16) * p.group) return;
-    mu.head &= 0xFFFF;
-  }
   const int c = threadIdx.x % C4, pg = threadIdx.x / C4;
   const float* lse = p.lse_part + (size_t)mu.part0 * kRows + row;
   const float* o = p.o_part + ((size_t)mu.part0 * kRows + row) * D + 4 * c;
@@ -179,51 +158,38 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(DecodeMergeParams p) 
     acc += e * sm_o[i][c];
   }
   const float inv = wsum > 0.f ? 1.0f / wsum : 0.f;
-  const size_t orow = CROSS ? (size_t)(mu.qo_row + row / p.group) * p.num_q_heads + mu.head * p.group + row % p.group
-                            : (size_t)mu.qo_row * p.num_q_heads + mu.head * p.group + row;
+  const size_t orow = (size_t)mu.qo_row * p.num_q_heads + mu.head * p.group + row;
   *(uint2*)(p.out + orow * D + 4 * c) = make_uint2(pack2(acc[0] * inv, acc[1] * inv), pack2(acc[2] * inv, acc[3] * inv));
   if (p.lse != nullptr && c == 0) p.lse[orow] = M + __logf(wsum);
 }
 
 }  // namespace
 
-template <int D, bool FP8, bool PAGE, bool CROSS>
-static void launch_decode_nt(const DecodeParams& p, int64_t n_units, hipStream_t stream) {
+template <int D, bool FP8>
+static void launch_decode_for(const DecodeParams& p, int64_t n_units, hipStream_t stream) {
   const dim3 grid((unsigned)n_units), block(kDecodeThreads);
-  if (p.lists.n > 0) hipLaunchKernelGGL((decode_kernel<D, FP8, true, PAGE, CROSS>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((decode_kernel<D, FP8, false, PAGE, CROSS>), grid, block, 0, stream, p);
-}
-
-template <int D, bool FP8, bool PAGE>
-static void launch_decode_pool(const DecodeParams& p, int64_t n_units, hipStream_t stream) {
-  if (p.a.cross) launch_decode_nt<D, FP8, PAGE, true>(p, n_units, stream);
-  else launch_decode_nt<D, FP8, PAGE, false>(p, n_units, stream);
-}
-
-template <int D>
-static void launch_decode_for(const DecodeParams& p, int64_t n_units, bool fp8, hipStream_t stream) {
-  if (p.a.page_scaled) launch_decode_pool<D, true, true>(p, n_units, stream);
-  else if (fp8) launch_decode_pool<D, true, false>(p, n_units, stream);
-  else launch_decode_pool<D, false, false>(p, n_units, stream);
+  if (p.lists.n > 0) hipLaunchKernelGGL((decode_kernel<D, FP8, true>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((decode_kernel<D, FP8, false>), grid, block, 0, stream, p);
 }
 
 hipError_t launch_decode(const DecodeParams& p, int64_t n_units, int head_dim, bool fp8, hipStream_t stream) {
+  if (p.rows != nullptr) return launch_rows(*p.rows, head_dim, stream);
   if (n_units <= 0) return hipSuccess;
-  if (head_dim == 128) launch_decode_for<128>(p, n_units, fp8, stream);
-  else launch_decode_for<64>(p, n_units, fp8, stream);
+  if (head_dim == 128) {
+    if (fp8) launch_decode_for<128, true>(p, n_units, stream);
+    else launch_decode_for<128, false>(p, n_units, stream);
+  } else {
+    if (fp8) launch_decode_for<64, true>(p, n_units, stream);
+    else launch_decode_for<64, false>(p, n_units, stream);
+  }
   return hipGetLastError();
 }
 
 hipError_t launch_decode_merge(const DecodeMergeParams& p, int64_t n_merges, int head_dim, hipStream_t stream) {
   if (n_merges <= 0) return hipSuccess;
-  const dim3 grid((unsigned)n_merges, (unsigned)(p.cross > 0 ? p.cross * p.group : p.group)), block(256);
-  if (head_dim == 128) {
-    if (p.cross > 0) hipLaunchKernelGGL((decode_merge_kernel<128, true>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((decode_merge_kernel<128>), grid, block, 0, stream, p);
-  } else {
-    if (p.cross > 0) hipLaunchKernelGGL((decode_merge_kernel<64, true>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((decode_merge_kernel<64>), grid, block, 0, stream, p);
-  }
+  const dim3 grid((unsigned)n_merges, (unsigned)p.group), block(256);
+  if (head_dim == 128) hipLaunchKernelGGL(decode_merge_kernel<128>, grid, block, 0, stream, p);
+  else hipLaunchKernelGGL(decode_merge_kernel<64>, grid, block, 0, stream, p);
   return hipGetLastError();
 }
 

@@ -58,13 +58,6 @@ __device__ __forceinline__ uint4 fp8x8_bf16(uint2 c, float by = 1.0f) {
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, by, true)));
 }
 
-// Row n of a unit's queries among all of them (see combine_waves).
-template <bool CROSS>
-__device__ __forceinline__ size_t query_row(const DecodeArgs& p, const DecodeUnit& u, int n) {
-  if constexpr (CROSS) return (size_t)(u.qo_row + n / p.group) * p.num_q_heads + u.head * p.group + n % p.group;
-  else return (size_t)u.qo_row * p.num_q_heads + u.head * p.group + n;
-}
-
 // Shared memory of a workgroup's combine: every wave's O [NW][kRows][D], row maxima and
 // sums [NW][kRows] each.
 template <int D, int NW>
@@ -80,13 +73,12 @@ struct CombineShared {
 // NaN (a NaN or an infinite score) is written as zeros, and as NaN with NANS, which is
 // what a prefill tile gives: one-token requests beside longer ones keep that.  They also
 // get a tile's `none` where no score is above -inf: 0, on an fp8 pool NaN.
-// CROSS: the unit's rows are u.ntok tokens of G heads each (row = token * G + head).
-template <int D, int NW, bool NANS, bool CROSS = false>
+template <int D, int NW, bool NANS>
 __device__ __forceinline__ void combine_waves(const DecodeArgs& p, const DecodeUnit& u, CombineShared<D, NW> sm,
                                               const f32x4 (&o)[D / 16], float m_run, float l_run, float vscale,
                                               float none) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n = lane & 15, g = lane >> 4, G = p.group, rows = CROSS ? u.ntok * G : G;
+  const int n = lane & 15, g = lane >> 4, G = p.group;
   const float l_row = group_sum(l_run);
   if (g == 0) {
     sm.m[wave * kRows + n] = m_run;
@@ -97,7 +89,7 @@ __device__ __forceinline__ void combine_waves(const DecodeArgs& p, const DecodeU
 #pragma unroll
     for (int i = 0; i < 4; i++) sm.o[(wave * kRows + n) * D + 16 * b + 4 * g + i] = o[b][i];
   __syncthreads();
-  for (int idx = threadIdx.x; idx < rows * D; idx += 64 * NW) {
+  for (int idx = threadIdx.x; idx < G * D; idx += 64 * NW) {
     const int row = idx / D, d = idx - row * D;
     float M = -INFINITY;
 #pragma unroll
@@ -114,8 +106,7 @@ __device__ __forceinline__ void combine_waves(const DecodeArgs& p, const DecodeU
     const float val = wsum > 0.f ? acc * vscale / wsum : !NANS ? 0.f : wsum == 0.f ? none : acc * 0.f;
     const float lse_v = wsum > 0.f ? (M + __log2f(wsum)) * kLn2 : -INFINITY;
     if (u.part < 0) {
-      const size_t orow = CROSS ? (size_t)(u.qo_row + row / G) * p.num_q_heads + u.head * G + row % G
-                                : (size_t)u.qo_row * p.num_q_heads + u.head * G + row;
+      const size_t orow = (size_t)u.qo_row * p.num_q_heads + u.head * G + row;
       p.out[orow * D + d] = __builtin_bit_cast(uint16_t, (__bf16)val);
       if (p.lse != nullptr && d == 0) p.lse[orow] = lse_v;
     } else {
@@ -140,7 +131,7 @@ struct PlainLoads {
 
 // One unit on NW waves; wave w takes page pairs w, w + NW, ...  nt: asked once the first
 // (plain) loads are on their way, whether to read the further pages non-temporally; uniform.
-template <int D, int NW, bool NANS, bool CROSS = false, class Nt>
+template <int D, int NW, bool NANS, class Nt>
 __device__ __forceinline__ void decode_unit(const DecodeArgs& p, const DecodeUnit& u, CombineShared<D, NW> sm, Nt&& nt) {
   constexpr int QS = D / 32;   // QK reduction steps
   constexpr int DB = D / 16;   // PV output blocks
@@ -154,8 +145,8 @@ __device__ __forceinline__ void decode_unit(const DecodeArgs& p, const DecodeUni
   // Q^T B-operands: dims 32 s + 8 g .. +8 of query row n (zero past the group)
   bf16x8 qf[QS];
   {
-    const bool valid = n < (CROSS ? u.ntok * G : G);
-    const uint4* src = (const uint4*)(p.q + query_row<CROSS>(p, u, valid ? n : 0) * D + 8 * g);
+    const bool valid = n < G;
+    const uint4* src = (const uint4*)(p.q + ((size_t)u.qo_row * p.num_q_heads + u.head * G + (valid ? n : 0)) * D + 8 * g);
 #pragma unroll
     for (int s = 0; s < QS; s++) qf[s] = __builtin_bit_cast(bf16x8, valid ? src[4 * s] : make_uint4(0, 0, 0, 0));
   }
@@ -289,7 +280,7 @@ __device__ __forceinline__ void decode_unit(const DecodeArgs& p, const DecodeUni
   else
     for (int j = wave; j < n_pairs; j += NW) compute(j, j + NW, r, std::false_type{});
 
-  combine_waves<D, NW, NANS, CROSS>(p, u, sm, o, m_run, l_run, 1.0f, 0.f);
+  combine_waves<D, NW, NANS>(p, u, sm, o, m_run, l_run, 1.0f, 0.f);
 }
 
 // ---------------------------------------------------------------- fp8 pool
@@ -317,7 +308,7 @@ struct QuadRegs {
 
 // PAGE: a page-scaled pool, whose powers of two the conversions take (k_scale: all of them, K
 // and V of every page and head side by side).
-template <int D, int NW, bool NANS, bool PAGE = false, bool CROSS = false, class Nt>
+template <int D, int NW, bool NANS, bool PAGE = false, class Nt>
 __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const DecodeUnit& u, CombineShared<D, NW> sm,
                                                 Nt&& nt) {
   constexpr int KS = D / 64;  // K loads per MFMA row block
@@ -331,8 +322,9 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
   // Q^T B-operands: k-step (i, h) takes dims 64 i + 16 g + 8 h .. +8 of query row n
   bf16x8 qf[KS][2];
   {
-    const bool valid = n < (CROSS ? u.ntok * G : G);
-    const uint4* src = (const uint4*)(p.q + query_row<CROSS>(p, u, valid ? n : 0) * D + 16 * g);
+    const bool valid = n < G;
+    const uint4* src =
+        (const uint4*)(p.q + ((size_t)u.qo_row * p.num_q_heads + u.head * G + (valid ? n : 0)) * D + 16 * g);
 #pragma unroll
     for (int i = 0; i < KS; i++)
 #pragma unroll
@@ -480,8 +472,8 @@ __device__ __forceinline__ void decode_unit_fp8(const DecodeArgs& p, const Decod
   else
     for (; j < n_full; j += NW) compute(j, j + NW, r, std::false_type{}, std::false_type{});
   if (j < n_quads) compute(j, j + NW, r, std::true_type{}, std::false_type{});
-  combine_waves<D, NW, NANS, CROSS>(p, u, sm, o, m_run, l_run, PAGE ? 1.0f : p.v_scale[u.head],
-                                    PAGE ? 0.f : __builtin_nanf(""));
+  combine_waves<D, NW, NANS>(p, u, sm, o, m_run, l_run, PAGE ? 1.0f : p.v_scale[u.head],
+                             PAGE ? 0.f : __builtin_nanf(""));
 }
 
 

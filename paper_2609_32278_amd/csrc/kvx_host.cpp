@@ -632,30 +632,17 @@ bool is_decode_batch(const kvx_batch* b, int32_t Hq, int32_t Hkv) {
   return any;
 }
 
-// Rows that the decode code takes at once: the query heads of one token (ntok 0), or of the
-// ntok tokens of a cross attention, over keys [0, keys) of request r.
-struct StepRows {
-  int32_t r, qo_row, ntok;
-  int64_t keys;
-};
-
-std::vector<StepRows> decode_rows(const kvx_batch* b, const std::vector<int64_t>& qo) {
-  std::vector<StepRows> rows;
-  for (int r = 0; r < b->num_reqs; r++)
-    if (b->extend_lens[r] == 1) rows.push_back(StepRows{r, (int32_t)qo[(size_t)r], 0, (int64_t)b->prefix_lens[r] + 1});
-  return rows;
-}
-
-// Work plan of a decode step: the key range of each rows and KV head is cut into
+// Work plan of a decode step: each (request, KV head) key range [0, P] is cut into
 // chunks of a common length, a multiple of 64 keys chosen so that the batch yields
 // about 2048 chunks (8 per CU, of which two to four run at a time), at
 // least 512 keys each; a range of more than one chunk becomes parts merged by
 // log-sum-exp.  Chunks are dispatched longest first.
-int make_step_plan(const kvx_batch* b, const std::vector<StepRows>& rows, int32_t Hkv, int32_t split_keys,
-                   int64_t max_parts, DecodePlan& plan) {
+int make_decode_plan(const kvx_batch* b, const std::vector<int64_t>& qo, int32_t Hkv, int32_t split_keys,
+                     int64_t max_parts, DecodePlan& plan) {
   const int64_t A = kvx::kDecodeChunkAlign;
   int64_t total = 0;
-  for (const StepRows& w : rows) total += (int64_t)Hkv * w.keys;
+  for (int r = 0; r < b->num_reqs; r++)
+    if (b->extend_lens[r] == 1) total += (int64_t)Hkv * ((int64_t)b->prefix_lens[r] + 1);
   int64_t chunk;
   if (split_keys > 0) {
     chunk = split_keys;
@@ -665,33 +652,35 @@ int make_step_plan(const kvx_batch* b, const std::vector<StepRows>& rows, int32_
   }
   for (;;) {  // bound the partial results like the prefill planner does
     int64_t parts = 0;
-    for (const StepRows& w : rows) {
-      const int64_t n = (w.keys + chunk - 1) / chunk;
+    for (int r = 0; r < b->num_reqs; r++) {
+      if (b->extend_lens[r] != 1) continue;
+      const int64_t n = ((int64_t)b->prefix_lens[r] + 1 + chunk - 1) / chunk;
       if (n > 1) parts += n * Hkv;
     }
     if (parts <= max_parts) break;
     chunk *= 2;
   }
-  for (const StepRows& w : rows) {
-    const int64_t nc = std::max<int64_t>(1, (w.keys + chunk - 1) / chunk);
+  for (int r = 0; r < b->num_reqs; r++) {
+    if (b->extend_lens[r] != 1) continue;
+    const int64_t L = (int64_t)b->prefix_lens[r] + 1;
+    const int64_t nc = (L + chunk - 1) / chunk;
     const int64_t part0 = plan.n_parts;
     for (int64_t c = 0; c < nc; c++) {
       for (int32_t h = 0; h < Hkv; h++) {  // heads side by side (see InlinePlan)
         DecodeUnit u{};
-        u.qo_row = w.qo_row;
-        u.page_base = b->page_indptr[w.r];
+        u.qo_row = (int32_t)qo[(size_t)r];
+        u.page_base = b->page_indptr[r];
         u.key_begin = (int32_t)(c * chunk);
-        u.key_end = (int32_t)std::min<int64_t>(w.keys, (c + 1) * chunk);
+        u.key_end = (int32_t)std::min<int64_t>(L, (c + 1) * chunk);
         u.head = h;
         u.part = nc > 1 ? (int32_t)(part0 + h * nc + c) : -1;
-        u.req = w.r;
-        u.ntok = w.ntok;
+        u.req = r;
         plan.units.push_back(u);
       }
     }
     if (nc > 1) {
       for (int32_t h = 0; h < Hkv; h++)
-        plan.merges.push_back(DecodeMerge{w.qo_row, h | w.ntok << 16, (int32_t)(part0 + h * nc), (int32_t)nc});
+        plan.merges.push_back(DecodeMerge{(int32_t)qo[(size_t)r], h, (int32_t)(part0 + h * nc), (int32_t)nc});
       plan.n_parts += nc * Hkv;
     }
   }
@@ -704,11 +693,6 @@ int make_step_plan(const kvx_batch* b, const std::vector<StepRows>& rows, int32_
     plan.items.push_back(it);
   }
   return KVX_OK;
-}
-
-int make_decode_plan(const kvx_batch* b, const std::vector<int64_t>& qo, int32_t Hkv, int32_t split_keys,
-                     int64_t max_parts, DecodePlan& plan) {
-  return make_step_plan(b, decode_rows(b, qo), Hkv, split_keys, max_parts, plan);
 }
 
 int check_heads(int32_t Hq, int32_t Hkv, int32_t D) {
@@ -853,15 +837,13 @@ std::vector<uint8_t> plan_blob(const std::vector<U>& units, const std::vector<M>
 // every page list would cost each unit more than these loads give.
 constexpr int64_t kStreamBytes = 256ll << 20;
 
-// The rows of a decode step, or of a cross attention.
-int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<StepRows>& rows, bool cross,
-                     const void* q, int32_t num_q_heads, float sm_scale, void* out, float* lse, hipStream_t s,
-                     CallBuffers& buf) {
+int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, const void* q,
+                     int32_t num_q_heads, float sm_scale, void* out, float* lse, hipStream_t s, CallBuffers& buf) {
   const int D = pool->head_dim;
   constexpr int R = kvx::kDecodeMaxGroup;
   DecodePlan plan;
-  if (int rc = make_step_plan(batch, rows, pool->num_kv_heads, pool->split_keys,
-                              buf.max_parts((size_t)R * (D + 1) * sizeof(float)), plan))
+  if (int rc = make_decode_plan(batch, qo, pool->num_kv_heads, pool->split_keys,
+                                buf.max_parts((size_t)R * (D + 1) * sizeof(float)), plan))
     return rc;
   kvx::DecodeParams dp;
   kvx::DecodeMergeParams m;
@@ -873,14 +855,12 @@ int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<S
   }
   int64_t kv_bytes = 0;  // K and V, page lists that share pages counted each
   std::vector<int32_t> lists;
-  bool again = false;  // a request's keys are read for several rows
-  for (const StepRows& w : rows) {
-    if (w.keys == 0) continue;
-    kv_bytes += 2 * w.keys * pool->num_kv_heads * D * pool->elem_bytes;
-    again |= !lists.empty() && lists.back() == batch->page_indptr[w.r];
-    lists.push_back(batch->page_indptr[w.r]);
+  for (int r = 0; r < batch->num_reqs; r++) {
+    if (batch->extend_lens[r] != 1) continue;
+    kv_bytes += 2 * ((int64_t)batch->prefix_lens[r] + 1) * pool->num_kv_heads * D * pool->elem_bytes;
+    lists.push_back(batch->page_indptr[r]);
   }
-  const bool streams = kv_bytes > kStreamBytes && lists.size() <= (size_t)kvx::kShareReqs && !again;
+  const bool streams = kv_bytes > kStreamBytes && lists.size() <= (size_t)kvx::kShareReqs;
   dp.lists.base = nullptr;
   dp.lists.n = streams ? (int32_t)lists.size() : 0;
   const size_t lists_at = blob.size();
@@ -923,8 +903,6 @@ int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<S
   p.num_kv_heads = pool->num_kv_heads;
   p.group = num_q_heads / pool->num_kv_heads;
   p.scale_log2 = sm_scale * 1.4426950408889634f;
-  p.page_scaled = pool->page_scaled() ? 1 : 0;
-  p.cross = cross ? 1 : 0;
   if (!in_args && dp.lists.n > 0) dp.lists.base = (const int32_t*)((const uint8_t*)dev + lists_at);
   hipError_t e = kvx::launch_decode(dp, (int64_t)plan.units.size(), D, pool->kv_dtype == KVX_KV_FP8_E4M3, s);
   if (e != hipSuccess) return hip_fail(e, "decode kernel launch");
@@ -936,12 +914,172 @@ int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<S
     m.lse = lse;
     m.num_q_heads = num_q_heads;
     m.group = p.group;
-    m.cross = 0;
-    if (cross)
-      for (const DecodeMerge& x : plan.merges) m.cross = std::max(m.cross, x.head >> 16);
     e = kvx::launch_decode_merge(m, (int64_t)plan.merges.size(), D, s);
     if (e != hipSuccess) return hip_fail(e, "decode merge kernel launch");
   }
+  return buf.done(s, !in_args);
+}
+
+// ---- few query rows over all keys of their request (kvx_rows.hip)
+using kvx::RowsEntry;
+
+struct RowsRequest {
+  int32_t qo_row, ntok, page_base;
+  int64_t keys;
+};
+
+// Requests with more rows than two entries go through tiles.
+constexpr int64_t kRowsOfRequest = 2 * kvx::kRowsMax;
+
+bool has_few_rows(int64_t tokens, int32_t group) { return group <= kvx::kRowsMax && tokens * group <= kRowsOfRequest; }
+
+// A request's tokens as entries, of nearly equal size.  They run next to each other on one XCD, where
+// the second finds the keys that the first read in the L2.
+void add_rows(std::vector<RowsRequest>& reqs, int32_t qo_row, int32_t tokens, int32_t page_base, int64_t keys,
+              int32_t group, bool causal) {
+  const int32_t most = kvx::kRowsMax / group, n = (tokens + most - 1) / most, each = (tokens + n - 1) / n;
+  for (int32_t t = 0; t < tokens; t += each) {
+    const int32_t ntok = std::min(each, tokens - t);
+    reqs.push_back(RowsRequest{qo_row + t, ntok, page_base, causal ? keys - (tokens - t - ntok) : keys});
+  }
+}
+
+// Entries and code words of a plan: every entry's ranges are of equal length, units go longest first.
+//
+// The length, in keys of all KV heads over the 512 workgroups that run at a time: a batch that
+// gives each of them at most 1024 is cut to one unit each (at least 384 keys), a larger one into
+// four rounds, or two where a workgroup takes two blocks of rows (whose ranges cost twice as
+// much to merge).  Unless whole ranges are estimated to be done sooner, without the merge's
+// launch (400 keys); a unit's start costs 150.  us a call at lengths of 256 / 512 / 1024 / 2048 /
+// 4096 / whole: 4 agents of 1k to 8k, 32/8/128 heads, 18.6 / 17.5 / 17.7 / 21.9 / 31 / 37 (384:
+// 17.0); 24 on 16k to 131k, 64/8/128, 616 / 607 / 587 / 499 / 462 / - (8192: 479); 48 single queries
+// of 16/16/64 heads on 200 to 1500 30.9 / 29.9 / 30.4 / - / - / 25.1; 33 times 1 to 5 queries of
+// 64/8/128 heads on 2k to 20k 200 / 146 / 132 / 121 / 121 / 119.
+struct RowsPlan {
+  std::vector<uint32_t> words;
+  int64_t n_codes = 0, n_parts = 0;
+};
+
+RowsPlan make_rows_plan(const std::vector<RowsRequest>& reqs, int32_t Hkv, int32_t blocks, int32_t split_keys,
+                        int64_t max_parts, bool small) {
+  const int64_t A = kvx::kDecodeChunkAlign, kMaxRanges = 1 << kvx::kRowsRangeBits;
+  int64_t total = 0, longest = 0;
+  for (const RowsRequest& q : reqs) {
+    total += Hkv * q.keys;
+    longest = std::max(longest, q.keys);
+  }
+  constexpr int64_t kSlots = 512, kStart = 150, kMerge = 400;
+  int64_t len = split_keys;
+  if (split_keys == 0) {
+    const int64_t share = ceil_div(total, kSlots);
+    len = share <= 1024 ? std::max<int64_t>(384, share) : std::max<int64_t>(1024, share * blocks / 4);
+    auto done_by = [&](int64_t units, int64_t most) {
+      return std::max(most + kStart, (total + units * kStart) / kSlots + most / 2);
+    };
+    int64_t units = 0;
+    for (const RowsRequest& q : reqs) units += Hkv * ceil_div(std::max<int64_t>(1, q.keys), len);
+    if (done_by((int64_t)reqs.size() * Hkv, longest) <= done_by(units, std::min(len, longest)) + kMerge)
+      len = std::max(len, longest);
+  }
+  auto ranges_of = [&](int64_t keys) -> int64_t {
+    if (split_keys > 0) return std::max<int64_t>(1, ceil_div(keys, len));
+    return std::max<int64_t>(1, ceil_div(keys, len));
+  };
+  auto len_of = [&](int64_t keys) {
+    return split_keys > 0 ? len : std::max(A, ceil_div(ceil_div(keys, ranges_of(keys)), A) * A);
+  };
+  for (;;) {  // the parts bounded, and a small batch's plan in the kernel arguments, if twice the length makes it fit
+    int64_t parts = 0, most = 0, codes = 0;
+    for (const RowsRequest& q : reqs) {
+      const int64_t n = ceil_div(std::max<int64_t>(1, q.keys), len_of(q.keys));
+      if (n > 1) parts += n * Hkv;
+      most = std::max(most, n);
+      codes += n;
+    }
+    const int64_t fit = kvx::kRowsWords - (int64_t)reqs.size() * kvx::kRowsEntryWords;
+    const bool tighten = small && split_keys == 0 && codes > fit && (int64_t)reqs.size() <= fit;
+    if (parts <= max_parts && most <= kMaxRanges && !tighten) break;
+    len = ceil_div(len * 5 / 4, A) * A;
+  }
+  RowsPlan plan;
+  std::vector<std::pair<int64_t, uint32_t>> codes;  // length, code
+  for (size_t i = 0; i < reqs.size(); i++) {
+    const RowsRequest& q = reqs[i];
+    const int64_t l = len_of(q.keys), n = ceil_div(std::max<int64_t>(1, q.keys), l);
+    RowsEntry e{q.qo_row, q.ntok, q.page_base, (int32_t)q.keys, n > 1 ? (int32_t)plan.n_parts : -1,
+                (int32_t)std::min<int64_t>(l, INT32_MAX / A * A)};
+    plan.words.resize(plan.words.size() + kvx::kRowsEntryWords);
+    std::memcpy(plan.words.data() + plan.words.size() - kvx::kRowsEntryWords, &e, sizeof e);
+    for (int64_t c = 0; c < n; c++)
+      codes.push_back({std::min(l, q.keys - c * l), (uint32_t)i << kvx::kRowsRangeBits | (uint32_t)c});
+    if (n > 1) plan.n_parts += n * Hkv;
+  }
+  std::stable_sort(codes.begin(), codes.end(), [](const auto& x, const auto& y) { return x.first > y.first; });
+  for (const auto& c : codes) plan.words.push_back(c.second);
+  plan.n_codes = (int64_t)codes.size();
+  return plan;
+}
+
+// causal: an entry's tokens are the last ones of its keys (extend_attention's suffixes).
+int rows_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<RowsRequest>& reqs, bool causal,
+                   const void* q, int32_t num_q_heads, float sm_scale, void* out, float* lse, hipStream_t s,
+                   CallBuffers& buf) {
+  const int D = pool->head_dim, Hkv = pool->num_kv_heads;
+  kvx::RowsParams p{};
+  p.group = num_q_heads / Hkv;
+  int64_t rows = 1, kv_bytes = 0;
+  for (const RowsRequest& x : reqs) {
+    if (x.keys > 0) rows = std::max<int64_t>(rows, (int64_t)x.ntok * p.group);
+    kv_bytes += 2 * x.keys * Hkv * D * pool->elem_bytes;
+  }
+  p.rows = (int32_t)rows;
+  p.blocks = rows <= 16 ? 1 : 2;
+  const size_t part_floats = (size_t)16 * p.blocks * (D + 1);
+  const RowsPlan plan =
+      make_rows_plan(reqs, Hkv, p.blocks, pool->split_keys, buf.max_parts(part_floats * sizeof(float)), kv_bytes <= kStreamBytes);
+  const bool in_args = plan.words.size() <= (size_t)kvx::kRowsWords;
+  std::vector<uint8_t> blob;
+  if (in_args) {
+    std::copy(plan.words.begin(), plan.words.end(), p.in_args);
+  } else {
+    blob.resize(plan.words.size() * sizeof(uint32_t));
+    std::memcpy(blob.data(), plan.words.data(), blob.size());
+  }
+  if (int rc = buf.check_plan(blob.size())) return rc;
+  if (int rc = use_device(pool)) return rc;
+  if (validate_mode())
+    if (int rc = check_page_ids(pool->num_pages, batch, s)) return rc;
+  if (int rc = buf.bind()) return rc;
+  float* parts = nullptr;
+  if (plan.n_parts > 0)
+    if (int rc = buf.parts((size_t)plan.n_parts * part_floats * sizeof(float), s, &parts)) return rc;
+  void* dev = nullptr;
+  if (!in_args)
+    if (int rc = buf.upload(blob, s, &dev)) return rc;
+  p.q = (const uint16_t*)q;
+  p.out = (uint16_t*)out;
+  p.lse = lse;
+  p.k_pool = pool->k;
+  p.v_pool = pool->v;
+  p.page_ids = batch->page_ids;
+  p.o_part = parts;
+  p.lse_part = parts ? parts + (size_t)plan.n_parts * 16 * p.blocks * D : nullptr;
+  p.k_scale = pool->k_scales();
+  p.v_scale = pool->v_scales();
+  p.words = (const uint32_t*)dev;
+  p.n_entries = (int32_t)reqs.size();
+  p.n_codes = (int32_t)plan.n_codes;
+  p.num_q_heads = num_q_heads;
+  p.num_kv_heads = Hkv;
+  p.causal = causal ? 1 : 0;
+  p.any_parts = plan.n_parts > 0 ? 1 : 0;
+  p.streams = kv_bytes > kStreamBytes && reqs.size() <= (size_t)kvx::kShareReqs ? 1 : 0;
+  p.kv_dtype = pool->kv_dtype;
+  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  kvx::DecodeParams dp;
+  dp.rows = &p;
+  const hipError_t e = kvx::launch_decode(dp, p.n_codes, D, pool->kv_dtype == KVX_KV_FP8_E4M3, s);
+  if (e != hipSuccess) return hip_fail(e, "rows kernel launch");
   return buf.done(s, !in_args);
 }
 
@@ -1407,8 +1545,18 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
   hipStream_t s = (hipStream_t)stream;
   CallBuffers buf{pool, fixed};
 
+  const int32_t group = num_q_heads / pool->num_kv_heads;
+  bool few = pool->page_scaled();
+  for (int r = 0; few && r < batch->num_reqs; r++) few = has_few_rows(batch->extend_lens[r], group);
+  if (few) {
+    std::vector<RowsRequest> reqs;
+    for (int r = 0; r < batch->num_reqs; r++)
+      if (const int32_t E = batch->extend_lens[r])
+        add_rows(reqs, (int32_t)qo[(size_t)r], E, batch->page_indptr[r], (int64_t)batch->prefix_lens[r] + E, group, true);
+    return rows_attention(pool, batch, reqs, true, q, num_q_heads, sm_scale, out, lse, s, buf);
+  }
   if (is_decode_batch(batch, num_q_heads, pool->num_kv_heads))
-    return decode_attention(pool, batch, decode_rows(batch, qo), false, q, num_q_heads, sm_scale, out, lse, s, buf);
+    return decode_attention(pool, batch, qo, q, num_q_heads, sm_scale, out, lse, s, buf);
   return tile_attention(pool, batch, qo, false, q, num_q_heads, sm_scale, out, lse, s, buf);
 }
 
@@ -1504,7 +1652,6 @@ int tile_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int
   if (!plan.dec_merges.empty()) {
     kvx::DecodeMergeParams dm;
     dm.plan.n = 0;
-    dm.cross = 0;
     dm.merges = (const DecodeMerge*)((const uint8_t*)dev + plan.units.size() * sizeof(AttnUnit) +
                                      plan.merges.size() * sizeof(MergeUnit));
     dm.o_part = p.d_part;
@@ -1518,10 +1665,6 @@ int tile_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int
   }
   return buf.done(s, !in_args);
 }
-
-// Requests of a cross attention whose rows the decode code takes, 16 at a time, each time over all
-// keys; the others go through tiles of 256 rows.
-constexpr int64_t kCrossBlocks = 1, kCrossBlocks8 = 2;
 
 int check_cross(const kvx_pool* pool, const kvx_batch* batch, std::vector<int64_t>& qo, const void* q,
                 int32_t num_q_heads, float sm_scale, const void* out, const float* lse) {
@@ -1554,22 +1697,21 @@ extern "C" int cross_attention(kvx_pool* pool, const kvx_batch* batch, const voi
     if (int rc = on.enter(pool->device)) return rc;
     if (int rc = kvx::check_stream(s, pool->device)) return rc;
     const int32_t group = num_q_heads / pool->num_kv_heads;
-    const int64_t block = kvx::kDecodeMaxGroup / group;  // tokens whose rows the decode code takes at once
-    const int64_t most = pool->kv_dtype == KVX_KV_BF16 ? kCrossBlocks : kCrossBlocks8;
-    constexpr int64_t kEmptyTokens = 1024;  // of a request without keys, a unit
-    std::vector<StepRows> rows;
+    constexpr int32_t kEmptyTokens = 1024;  // of a request without keys, an entry
+    std::vector<RowsRequest> few;
     std::vector<int32_t> tiled(batch->extend_lens, batch->extend_lens + batch->num_reqs);
     bool tiles = false;
     for (int r = 0; r < batch->num_reqs; r++) {
-      const int64_t L = batch->prefix_lens[r], E = batch->extend_lens[r];
-      const int64_t each = L == 0 ? kEmptyTokens : block;
+      const int32_t L = batch->prefix_lens[r], E = batch->extend_lens[r], row = (int32_t)qo[(size_t)r];
       if (E == 0) continue;
-      if (L > 0 && (block == 0 || E > block * most)) {
+      if (L > 0 && !has_few_rows(E, group)) {
         tiles = true;
         continue;
       }
-      for (int64_t t = 0; t < E; t += each)
-        rows.push_back(StepRows{r, (int32_t)(qo[(size_t)r] + t), (int32_t)std::min(each, E - t), L});
+      if (L > 0) add_rows(few, row, E, batch->page_indptr[r], L, group, false);
+      else
+        for (int32_t t = 0; t < E; t += kEmptyTokens)
+          few.push_back(RowsRequest{row + t, std::min(kEmptyTokens, E - t), batch->page_indptr[r], 0});
       tiled[(size_t)r] = 0;
     }
     CallBuffers buf{pool, nullptr};
@@ -1578,7 +1720,7 @@ extern "C" int cross_attention(kvx_pool* pool, const kvx_batch* batch, const voi
       sub.extend_lens = tiled.data();
       if (int rc = tile_attention(pool, &sub, qo, true, q, num_q_heads, sm_scale, out, lse, s, buf)) return rc;
     }
-    if (rows.empty()) return KVX_OK;
-    return decode_attention(pool, batch, rows, true, q, num_q_heads, sm_scale, out, lse, s, buf);
+    if (few.empty()) return KVX_OK;
+    return rows_attention(pool, batch, few, false, q, num_q_heads, sm_scale, out, lse, s, buf);
   });
 }

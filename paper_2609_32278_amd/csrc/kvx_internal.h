@@ -280,7 +280,7 @@ struct DecodeUnit {
   int32_t head;       // KV head
   int32_t part;       // -1: final result; else index of this chunk's partial result
   int32_t req;
-  int32_t ntok;       // cross attention: the queries (tokens) from qo_row on; else unused
+  int32_t pad;
 };
 static_assert(sizeof(DecodeUnit) == 32, "DecodeUnit is 32 bytes");
 
@@ -306,10 +306,6 @@ struct DecodeArgs {
   int32_t num_kv_heads;
   int32_t group;          // Hq / Hkv <= kDecodeMaxGroup
   float scale_log2;
-  // For the launcher: k_scale holds a power of two a page, head and K or V; the units are of a cross
-  // attention, of several tokens each.
-  int32_t page_scaled;
-  int32_t cross;
 };
 
 // Page lists of the requests that decode in a batch read with non-temporal loads, to tell
@@ -322,8 +318,10 @@ struct DecodeLists {
   int32_t in_args[kInlineUnits + 1];
 };
 
+struct RowsParams;
 struct DecodeParams {
   DecodeArgs a;
+  const RowsParams* rows = nullptr;  // for the launcher: this instead (host memory)
   const DecodeUnit* units;
   DecodeLists lists;
   InlinePlan<DecodeUnit> plan;  // plan.n > 0: the units (and lists.in_args the lists)
@@ -338,10 +336,54 @@ struct DecodeMergeParams {
   float* lse;
   int32_t num_q_heads;
   int32_t group;
-  int32_t cross;  // most tokens of a merge of a cross attention, whose head is head | tokens << 16; else 0
   InlineMerges<DecodeMerge> plan;  // plan.n > 0: the merges
 };
 static_assert(sizeof(DecodeMergeParams) <= 4096, "kernel arguments");
+
+// ---- few query rows of a request over all its keys: decode steps on a page-scaled pool, drafted
+// tokens and cross attention (kvx_rows.hip)
+constexpr int kRowsMax = 32;  // rows (token x query heads of one KV head) of an entry
+struct RowsEntry {
+  int32_t qo_row;     // first row of q (a token's heads are rows of one KV head after the other)
+  int32_t ntok;       // tokens; of one without keys any number
+  int32_t page_base;  // offset of the request's page list in page_ids
+  int32_t keys;       // keys [0, keys) of the request; 0: the rows become zeros
+  int32_t part0;      // partial results of (KV head 0, range 0), head h `parts` further on; -1: a single range
+  int32_t len;        // keys of a range, a multiple of kDecodeChunkAlign
+};
+constexpr int kRowsEntryWords = sizeof(RowsEntry) / 4;
+static_assert(kRowsEntryWords == 6, "six words per entry");
+// A unit is (entry, range, KV head): code word `entry << 12 | range` for all KV heads of it.
+constexpr int kRowsRangeBits = 12;
+constexpr int kRowsWords = 940;  // entries, then code words
+struct RowsParams {
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  const void* k_pool;
+  const void* v_pool;
+  const int32_t* page_ids;
+  float* o_part;            // fp32 [parts][rows of a part][D]
+  float* lse_part;          // fp32 [parts][rows of a part]
+  const float* k_scale;     // fp8 pool: [Hkv]; page-scaled pool: [num_pages, Hkv, (K, V)]
+  const float* v_scale;
+  const uint32_t* words;    // device: the entries and codes, or null: in_args
+  int32_t n_entries;
+  int32_t n_codes;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t group;
+  int32_t causal;           // the last token of an entry sees all its keys, the one before it one less, ...
+  int32_t blocks;           // 16-row blocks of the entry with the most rows: 1 or 2
+  int32_t rows;             // rows of that entry
+  int32_t any_parts;        // some entry has several ranges
+  int32_t streams;          // pages that one request alone holds are read with non-temporal loads
+  int32_t kv_dtype;
+  float scale_log2;
+  uint32_t in_args[kRowsWords];
+};
+static_assert(sizeof(RowsParams) <= 4096, "kernel arguments");
+hipError_t launch_rows(const RowsParams& p, int head_dim, hipStream_t stream);
 
 hipError_t launch_decode(const DecodeParams& p, int64_t n_units, int head_dim, bool fp8, hipStream_t stream);
 hipError_t launch_decode_merge(const DecodeMergeParams& p, int64_t n_merges, int head_dim, hipStream_t stream);

@@ -112,49 +112,42 @@ hipError_t launch_merge(const MergeParams& p, int64_t n, int, hipStream_t) {
   }
   return hipSuccess;
 }
-hipError_t launch_decode(const DecodeParams& p, int64_t n, int, bool, hipStream_t) {
+hipError_t launch_decode(const DecodeParams& dp, int64_t, int, bool, hipStream_t) {
   g_launches++;
   g_on = fake::current;
-  CHECK(p.a.cross == 1);
-  for (int64_t i = 0; i < n; i++) {
-    DecodeUnit u;
-    if (p.plan.n > 0) {
-      const int h = (int)(i % p.plan.heads);
-      u = p.plan.unit[i / p.plan.heads];
-      u.part = u.part < 0 ? -1 : u.part + h * u.req;
-      u.head += h;
-    } else {
-      u = p.units[i];
-    }
-    CHECK(u.ntok >= 1 && u.head < p.a.num_kv_heads);
-    if (u.key_end > 0) CHECK(u.ntok * p.a.group <= kDecodeMaxGroup && u.key_begin % kDecodeChunkAlign == 0);
-    for (int t = 0; t < u.ntok; t++) {
-      if (u.key_end == 0) g_empty[{u.qo_row + t, u.head}]++;
-      else g_stepped[{u.qo_row + t, u.head}].push_back(Range{u.page_base, u.key_begin, u.key_end, u.part});
-    }
+  CHECK(dp.rows != nullptr);
+  const RowsParams& p = *dp.rows;
+  CHECK(p.causal == 0 && (p.blocks == 1 || p.blocks == 2));
+  const uint32_t* w = p.words ? p.words : p.in_args;
+  if (!p.words) CHECK(p.n_entries * kRowsEntryWords + p.n_codes <= kRowsWords);
+  bool parts = false;
+  for (int32_t i = 0; i < p.n_codes; i++) {
+    const uint32_t code = w[kRowsEntryWords * p.n_entries + i];
+    CHECK((int32_t)(code >> kRowsRangeBits) < p.n_entries);
+    RowsEntry e;
+    std::memcpy(&e, w + kRowsEntryWords * (code >> kRowsRangeBits), sizeof e);
+    const int32_t range = (int32_t)(code & ((1u << kRowsRangeBits) - 1));
+    CHECK(e.ntok >= 1 && e.len > 0 && e.len % kDecodeChunkAlign == 0);
+    const int32_t n = e.keys > 0 ? (e.keys - 1) / e.len + 1 : 1;
+    CHECK(range < n && (e.part0 >= 0) == (n > 1));
+    if (e.keys > 0) CHECK(e.ntok * p.group <= 16 * p.blocks);
+    parts |= n > 1;
+    for (int32_t h = 0; h < p.num_kv_heads; h++)
+      for (int t = 0; t < e.ntok; t++) {
+        const std::pair<int64_t, int32_t> at{e.qo_row + t, h};
+        if (e.keys == 0) {
+          g_empty[at]++;
+          continue;
+        }
+        const int64_t begin = (int64_t)range * e.len, end = std::min<int64_t>(e.keys, begin + e.len);
+        g_stepped[at].push_back(Range{e.page_base, (int32_t)begin, (int32_t)end, n > 1 ? e.part0 + h * n + range : -1});
+        if (n > 1) g_step_merge[at] = {e.part0 + h * n, n};
+      }
   }
+  CHECK(parts == (p.any_parts != 0));
   return hipSuccess;
 }
-hipError_t launch_decode_merge(const DecodeMergeParams& p, int64_t n, int, hipStream_t) {
-  for (int64_t i = 0; i < n; i++) {
-    DecodeMerge m;
-    if (p.plan.n > 0) {
-      const int h = (int)(i % p.plan.heads);
-      m = p.plan.merge[i / p.plan.heads];
-      m.head += h;
-      m.part0 += h * m.nparts;
-    } else {
-      m = p.merges[i];
-    }
-    const int ntok = m.head >> 16;
-    CHECK(ntok >= 1 && ntok <= p.cross);
-    for (int t = 0; t < ntok; t++) {
-      CHECK(!g_step_merge.count({m.qo_row + t, m.head & 0xFFFF}));
-      g_step_merge[{m.qo_row + t, m.head & 0xFFFF}] = {m.part0, m.nparts};
-    }
-  }
-  return hipSuccess;
-}
+hipError_t launch_decode_merge(const DecodeMergeParams&, int64_t, int, hipStream_t) { std::exit(4); }
 hipError_t launch_store_kv(const StoreParams&, int64_t, int, bool, hipStream_t) { std::exit(4); }
 hipError_t launch_store_kv_rope(const RopeParams&, int64_t, int, bool, bool, hipStream_t) { std::exit(4); }
 hipError_t launch_page_move(const PageMoveParams&, int64_t, hipStream_t) { std::exit(4); }
