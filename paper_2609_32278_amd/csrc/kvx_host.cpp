@@ -928,10 +928,18 @@ struct RowsRequest {
   int64_t keys;
 };
 
-// Requests with more rows than two entries go through tiles.
-constexpr int64_t kRowsOfRequest = 2 * kvx::kRowsMax;
+// Entries of 32 rows that cost as much as a tile of 256 over the same keys.  us a call, entries /
+// tiles, requests of one size: 24 x 12/12/64 heads on 1200 keys, bf16 pool: 96 rows 38 / 51, 128 rows 44 / 53,
+// on 8000 keys 300 / 267; 8/8/128 heads, bf16: 64 rows 39 / 39, 96 rows 52 / 40; 8-bit pools, 128
+// rows: 12/12/64 heads 32 / 54, 8/8/128 38 / 45 (8000 keys 176 / 265, 214 / 258), 192 rows 8/8/128
+// 67 / 48.  Both kinds in one batch take two launches, which loses against either: 24 requests of
+// 3 to 224 rows of 12/12/64 heads on 700 to 1800 keys 53 / 40, both 61.
+int64_t entries_per_tile(const kvx_pool* pool) {
+  if (pool->kv_dtype != KVX_KV_BF16) return 4;
+  return pool->head_dim == 64 ? 3 : 2;
+}
 
-bool has_few_rows(int64_t tokens, int32_t group) { return group <= kvx::kRowsMax && tokens * group <= kRowsOfRequest; }
+int64_t entries_of(int64_t tokens, int32_t group) { return ceil_div(tokens, kvx::kRowsMax / group); }
 
 // A request's tokens as entries, of nearly equal size.  They run next to each other on one XCD, where
 // the second finds the keys that the first read in the L2.
@@ -949,37 +957,36 @@ void add_rows(std::vector<RowsRequest>& reqs, int32_t qo_row, int32_t tokens, in
 // The length, in keys of all KV heads over the 512 workgroups that run at a time: a batch that
 // gives each of them at most 1024 is cut to one unit each (at least 384 keys), a larger one into
 // four rounds, or two where a workgroup takes two blocks of rows (whose ranges cost twice as
-// much to merge).  Unless whole ranges are estimated to be done sooner, without the merge's
-// launch (400 keys); a unit's start costs 150.  us a call at lengths of 256 / 512 / 1024 / 2048 /
-// 4096 / whole: 4 agents of 1k to 8k, 32/8/128 heads, 18.6 / 17.5 / 17.7 / 21.9 / 31 / 37 (384:
-// 17.0); 24 on 16k to 131k, 64/8/128, 616 / 607 / 587 / 499 / 462 / - (8192: 479); 48 single queries
-// of 16/16/64 heads on 200 to 1500 30.9 / 29.9 / 30.4 / - / - / 25.1; 33 times 1 to 5 queries of
-// 64/8/128 heads on 2k to 20k 200 / 146 / 132 / 121 / 121 / 119.
+// much to merge).  Unless whole ranges are estimated to be done sooner: a merge costs 10 us, a lone
+// workgroup takes 200 keys a us (120 of a bf16 pool), all of them together read 5.6 TB/s, and half
+// of the longest unit is left over at the end.  us a call at lengths of 256 / 512 / 1024 / 2048 / 4096 /
+// whole: 4 agents of 1k to 8k, 32/8/128 heads, 18.6 / 17.5 / 17.7 / 21.9 / 31 / 37; 24 on 16k to 131k,
+// 64/8/128, 616 / 607 / 587 / 499 / 462 / - (8192: 479); 48 single queries of 16/16/64 heads on 200
+// to 1500, bf16, 30.9 / 29.9 / 30.4 / - / - / 25.1; 33 times 1 to 5 queries of 64/8/128 heads on 2k
+// to 20k 200 / 146 / 132 / 121 / 121 / 119; 24 on 1200, 8/8/128, 24 / 24 / 22 / - / - / 18.4; 40 on
+// 5000 128 / 84 / 84 / 83 / 90 / 96.
 struct RowsPlan {
   std::vector<uint32_t> words;
   int64_t n_codes = 0, n_parts = 0;
 };
 
-RowsPlan make_rows_plan(const std::vector<RowsRequest>& reqs, int32_t Hkv, int32_t blocks, int32_t split_keys,
-                        int64_t max_parts, bool small) {
+RowsPlan make_rows_plan(const std::vector<RowsRequest>& reqs, int32_t Hkv, int32_t blocks, int32_t key_bytes,
+                        bool bf16, int32_t split_keys, int64_t max_parts) {
   const int64_t A = kvx::kDecodeChunkAlign, kMaxRanges = 1 << kvx::kRowsRangeBits;
   int64_t total = 0, longest = 0;
   for (const RowsRequest& q : reqs) {
     total += Hkv * q.keys;
     longest = std::max(longest, q.keys);
   }
-  constexpr int64_t kSlots = 512, kStart = 150, kMerge = 400;
+  constexpr int64_t kSlots = 512;
+  constexpr double kMerge = 10.0, kBytesPerUs = 5.6e6;
+  const double read = (double)total * key_bytes / kBytesPerUs, rate = bf16 ? 120.0 : 200.0;
   int64_t len = split_keys;
   if (split_keys == 0) {
     const int64_t share = ceil_div(total, kSlots);
     len = share <= 1024 ? std::max<int64_t>(384, share) : std::max<int64_t>(1024, share * blocks / 4);
-    auto done_by = [&](int64_t units, int64_t most) {
-      return std::max(most + kStart, (total + units * kStart) / kSlots + most / 2);
-    };
-    int64_t units = 0;
-    for (const RowsRequest& q : reqs) units += Hkv * ceil_div(std::max<int64_t>(1, q.keys), len);
-    if (done_by((int64_t)reqs.size() * Hkv, longest) <= done_by(units, std::min(len, longest)) + kMerge)
-      len = std::max(len, longest);
+    auto done_by = [&](int64_t most) { return std::max((double)most / rate, read + 0.5 * (double)most / rate); };
+    if (len < longest && done_by(longest) < 0.9 * (done_by(len) + kMerge)) len = longest;
   }
   auto ranges_of = [&](int64_t keys) -> int64_t {
     if (split_keys > 0) return std::max<int64_t>(1, ceil_div(keys, len));
@@ -997,7 +1004,7 @@ RowsPlan make_rows_plan(const std::vector<RowsRequest>& reqs, int32_t Hkv, int32
       codes += n;
     }
     const int64_t fit = kvx::kRowsWords - (int64_t)reqs.size() * kvx::kRowsEntryWords;
-    const bool tighten = small && split_keys == 0 && codes > fit && (int64_t)reqs.size() <= fit;
+    const bool tighten = (int64_t)(read * kBytesPerUs) <= kStreamBytes && split_keys == 0 && codes > fit && (int64_t)reqs.size() <= fit;
     if (parts <= max_parts && most <= kMaxRanges && !tighten) break;
     len = ceil_div(len * 5 / 4, A) * A;
   }
@@ -1027,16 +1034,18 @@ int rows_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<Row
   const int D = pool->head_dim, Hkv = pool->num_kv_heads;
   kvx::RowsParams p{};
   p.group = num_q_heads / Hkv;
+  const int32_t key_bytes = 2 * D * pool->elem_bytes;  // of one KV head
   int64_t rows = 1, kv_bytes = 0;
   for (const RowsRequest& x : reqs) {
     if (x.keys > 0) rows = std::max<int64_t>(rows, (int64_t)x.ntok * p.group);
-    kv_bytes += 2 * x.keys * Hkv * D * pool->elem_bytes;
+    kv_bytes += x.keys * Hkv * key_bytes;
   }
   p.rows = (int32_t)rows;
   p.blocks = rows <= 16 ? 1 : 2;
   const size_t part_floats = (size_t)16 * p.blocks * (D + 1);
   const RowsPlan plan =
-      make_rows_plan(reqs, Hkv, p.blocks, pool->split_keys, buf.max_parts(part_floats * sizeof(float)), kv_bytes <= kStreamBytes);
+      make_rows_plan(reqs, Hkv, p.blocks, key_bytes, pool->kv_dtype == KVX_KV_BF16, pool->split_keys,
+                     buf.max_parts(part_floats * sizeof(float)));
   const bool in_args = plan.words.size() <= (size_t)kvx::kRowsWords;
   std::vector<uint8_t> blob;
   if (in_args) {
@@ -1546,8 +1555,9 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
   CallBuffers buf{pool, fixed};
 
   const int32_t group = num_q_heads / pool->num_kv_heads;
-  bool few = pool->page_scaled();
-  for (int r = 0; few && r < batch->num_reqs; r++) few = has_few_rows(batch->extend_lens[r], group);
+  bool few = pool->page_scaled() && group <= kvx::kRowsMax;
+  for (int r = 0; few && r < batch->num_reqs; r++)
+    few = entries_of(batch->extend_lens[r], group) <= entries_per_tile(pool);
   if (few) {
     std::vector<RowsRequest> reqs;
     for (int r = 0; r < batch->num_reqs; r++)
@@ -1698,13 +1708,20 @@ extern "C" int cross_attention(kvx_pool* pool, const kvx_batch* batch, const voi
     if (int rc = kvx::check_stream(s, pool->device)) return rc;
     const int32_t group = num_q_heads / pool->num_kv_heads;
     constexpr int32_t kEmptyTokens = 1024;  // of a request without keys, an entry
+    // either kind of launch for all requests with keys, whichever is estimated to be faster
+    double as_rows = 0.0, as_tiles = 0.0;
+    for (int r = 0; group <= kvx::kRowsMax && r < batch->num_reqs; r++) {
+      as_rows += (double)entries_of(batch->extend_lens[r], group) * batch->prefix_lens[r];
+      as_tiles += (double)ceil_div(batch->extend_lens[r], kvx::kTileRows / group) * batch->prefix_lens[r];
+    }
+    const bool rows = group <= kvx::kRowsMax && as_rows <= (double)entries_per_tile(pool) * as_tiles;
     std::vector<RowsRequest> few;
     std::vector<int32_t> tiled(batch->extend_lens, batch->extend_lens + batch->num_reqs);
     bool tiles = false;
     for (int r = 0; r < batch->num_reqs; r++) {
       const int32_t L = batch->prefix_lens[r], E = batch->extend_lens[r], row = (int32_t)qo[(size_t)r];
       if (E == 0) continue;
-      if (L > 0 && !has_few_rows(E, group)) {
+      if (L > 0 && !rows) {
         tiles = true;
         continue;
       }
