@@ -1046,6 +1046,9 @@ int rows_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<Row
   const RowsPlan plan =
       make_rows_plan(reqs, Hkv, p.blocks, key_bytes, pool->kv_dtype == KVX_KV_BF16, pool->split_keys,
                      buf.max_parts(part_floats * sizeof(float)));
+  if (int rc = kvx::check_grid(plan.n_codes * Hkv)) return rc;
+  if (reqs.size() >= (size_t)1 << (32 - kvx::kRowsRangeBits))
+    return fail(KVX_EUNSUPPORTED, "more than %d requests of a few rows in one call", (1 << (32 - kvx::kRowsRangeBits)) - 1);
   const bool in_args = plan.words.size() <= (size_t)kvx::kRowsWords;
   std::vector<uint8_t> blob;
   if (in_args) {
@@ -1376,6 +1379,8 @@ int kv_pool_reload(kvx_pool* pool, const int32_t* page_ids, const int32_t* slots
 static int rope_store(kvx_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, kvx::RopeParams& p,
                       bool interleaved, const void* k_ext, const void* v_ext, hipStream_t s) {
   int64_t n_units = 0;
+  if (pool->page_scaled())
+    if (int rc = kvx::check_grid(kvx::touched_pages(batch))) return rc;
   if (int rc = kvx::place_units(pool->st_store, batch, qo, s, p, n_units)) return rc;
   p.k_ext = (const uint16_t*)k_ext;
   p.v_ext = (const uint16_t*)v_ext;

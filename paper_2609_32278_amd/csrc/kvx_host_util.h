@@ -262,6 +262,15 @@ inline bool inline_store_reqs(const kvx_batch* b, const std::vector<int64_t>& qo
   return rq.n > 0;
 }
 
+inline int64_t touched_pages(const kvx_batch* batch) {
+  int64_t n = 0;
+  for (int r = 0; r < batch->num_reqs; r++) {
+    const int64_t P = batch->prefix_lens[r], E = batch->extend_lens[r];
+    if (E > 0) n += (P + E - 1) / kPageSize - P / kPageSize + 1;
+  }
+  return n;
+}
+
 // The touched pages of a batch's suffixes, request by request.
 inline std::vector<RopeUnit> page_units(const kvx_batch* batch, const std::vector<int64_t>& qo) {
   std::vector<RopeUnit> units;
@@ -280,6 +289,14 @@ inline std::vector<RopeUnit> page_units(const kvx_batch* batch, const std::vecto
     }
   }
   return units;
+}
+
+// A grid's x dimension, in workgroups of 256: the launch has less than 2^32 threads.
+constexpr int64_t kMaxGrid = (1 << 24) - 1;
+inline int check_grid(int64_t groups) {
+  if (groups > kMaxGrid)
+    return report(KVX_EUNSUPPORTED, "%lld workgroups in one launch (at most %lld)", (long long)groups, (long long)kMaxGrid);
+  return KVX_OK;
 }
 
 // The units of a store or load call, in its arguments or uploaded through `staging`.

@@ -26,6 +26,7 @@ extern "C" int load_kv(const kvx_pool* pool, const kvx_batch* batch, void* k_out
     kvx::LoadParams p{};
     kvx::Staging& units = const_cast<kvx_pool*>(pool)->st_load;
     int64_t n_units = 0;
+    if (int rc = kvx::check_grid(kvx::touched_pages(batch))) return rc;
     if (int rc = kvx::place_units(units, batch, qo, s, p, n_units)) return rc;
     p.k_pool = pool->k;
     p.v_pool = pool->v;

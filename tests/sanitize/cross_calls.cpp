@@ -68,7 +68,8 @@ struct Range {
 static std::map<std::pair<int64_t, int32_t>, std::vector<Range>> g_tiled, g_stepped;
 static std::map<std::pair<int64_t, int32_t>, std::pair<int32_t, int32_t>> g_tile_merge, g_step_merge;  // part0, parts
 static std::map<std::pair<int64_t, int32_t>, int> g_empty;
-static int g_launches = 0, g_on = -1, g_loads = 0;
+static std::map<int64_t, int32_t> g_sees;  // keys that a token of a draft sees
+static int g_launches = 0, g_on = -1, g_loads = 0, g_causal = 0;
 
 static void forget() {
   g_tiled.clear();
@@ -76,6 +77,7 @@ static void forget() {
   g_tile_merge.clear();
   g_step_merge.clear();
   g_empty.clear();
+  g_sees.clear();
   g_launches = g_loads = 0;
 }
 
@@ -117,7 +119,7 @@ hipError_t launch_decode(const DecodeParams& dp, int64_t, int, bool, hipStream_t
   g_on = fake::current;
   CHECK(dp.rows != nullptr);
   const RowsParams& p = *dp.rows;
-  CHECK(p.causal == 0 && (p.blocks == 1 || p.blocks == 2));
+  CHECK(p.causal == g_causal && (p.blocks == 1 || p.blocks == 2));
   const uint32_t* w = p.words ? p.words : p.in_args;
   if (!p.words) CHECK(p.n_entries * kRowsEntryWords + p.n_codes <= kRowsWords);
   bool parts = false;
@@ -135,6 +137,7 @@ hipError_t launch_decode(const DecodeParams& dp, int64_t, int, bool, hipStream_t
     for (int32_t h = 0; h < p.num_kv_heads; h++)
       for (int t = 0; t < e.ntok; t++) {
         const std::pair<int64_t, int32_t> at{e.qo_row + t, h};
+        if (p.causal) g_sees[e.qo_row + t] = e.keys - (e.ntok - 1 - t);
         if (e.keys == 0) {
           g_empty[at]++;
           continue;
@@ -269,6 +272,67 @@ void coverage() {
   release(p);
 }
 
+// extend_attention of few tokens a request on a page-scaled pool: the same launches, each token
+// seeing one key more than the one before it.
+void drafts() {
+  std::mt19937 rng(11);
+  for (int trial = 0; trial < 300; trial++) {
+    const int32_t groups[] = {1, 2, 3, 5, 8, 16, 20, 32};
+    const int32_t hkv = 1 + (int32_t)(rng() % 8), g = groups[rng() % 8];
+    std::vector<int32_t> P, E, total;
+    for (int r = 0, n = 1 + (int)(rng() % (trial % 10 == 0 ? 250 : 10)); r < n; r++) {
+      P.push_back((int32_t)(rng() % 3000));
+      E.push_back((int32_t)(rng() % (4 * (32 / g) + 1)));
+      total.push_back(P.back() + E.back());
+    }
+    TestBatch t(total, E);  // pages for prefix and suffix
+    t.b.prefix_lens = P.data();
+    kvx_pool p = pool_of(hkv, rng() % 2 ? 64 : 128, KVX_KV_FP8_PAGE);
+    if (trial % 4 == 0) p.split_keys = 64 * (1 + (int32_t)(rng() % 8));
+    forget();
+    g_causal = 1;
+    CHECK(extend_attention(&p, &t.b, far_away(1), hkv * g, 0.125f, far_away(2), nullptr, nullptr) == KVX_OK);
+    g_causal = 0;
+    CHECK(g_tiled.empty() && g_launches == (t.total() > 0 ? 1 : 0));
+    int64_t row = 0;
+    for (size_t r = 0; r < P.size(); r++)
+      for (int32_t e = 0; e < E[r]; e++, row++) {
+        CHECK(g_sees[row] == P[r] + e + 1);
+        for (int32_t h = 0; h < hkv; h++) {
+          std::vector<Range> ranges = g_stepped[{row, h}];
+          std::sort(ranges.begin(), ranges.end(), [](const Range& x, const Range& y) { return x.begin < y.begin; });
+          int32_t upto = 0;
+          for (const Range& x : ranges) {
+            CHECK(x.begin == upto && x.page_base == t.indptr[r]);
+            upto = x.end;
+          }
+          CHECK(upto >= P[r] + e + 1 && upto <= P[r] + E[r]);
+        }
+      }
+    CHECK((int64_t)g_sees.size() == t.total());
+    release(p);
+  }
+}
+
+// Launches that a grid cannot hold are refused before any work.
+void limits() {
+  kvx_pool p = pool_of(32, 64, KVX_KV_BF16);
+  const TestBatch many(std::vector<int32_t>(600000, 1), std::vector<int32_t>(600000, 1));
+  CHECK(cross(p, many, 32) == KVX_EUNSUPPORTED && g_launches == 0);
+  release(p);
+  p = pool_of(1, 64, KVX_KV_BF16);
+  const TestBatch more(std::vector<int32_t>(1 << 20, 1), std::vector<int32_t>(1 << 20, 1));
+  CHECK(cross(p, more, 1) == KVX_EUNSUPPORTED && g_launches == 0);
+  TestBatch longest({300000000}, {300000000});
+  std::vector<int32_t> zero{0};
+  longest.b.prefix_lens = zero.data();
+  CHECK(load_kv(&p, &longest.b, far_away(1), far_away(2), nullptr) == KVX_EUNSUPPORTED && g_loads == 0);
+  release(p);
+  p = pool_of(1, 64, KVX_KV_FP8_PAGE);
+  CHECK(store_kv(&p, &longest.b, far_away(1), far_away(2), nullptr) == KVX_EUNSUPPORTED);
+  release(p);
+}
+
 void refusals() {
   kvx_pool p = pool_of(2, 64, KVX_KV_BF16);
   const TestBatch t({40, 0, 7}, {3, 2, 1});
@@ -383,6 +447,8 @@ int main(int argc, char** argv) {
   const std::string what = argc > 1 ? argv[1] : "";
   (void)g_mem;
   if (what == "coverage") coverage();
+  else if (what == "drafts") drafts();
+  else if (what == "limits") limits();
   else if (what == "refusals") refusals();
   else if (what == "streams") streams();
   else if (what == "pools") pools();

@@ -68,6 +68,34 @@ def test_cross(setup, L, E, hkv, group, d, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("dtype", POOLS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group,tokens", [(1, 64), (1, 65), (1, 96), (1, 128), (1, 129), (3, 33), (8, 16), (8, 17), (32, 4), (33, 3)])
+def test_as_entries_and_as_tiles(setup, dtype, d, group, tokens):  # noqa: F811
+    """Around the numbers of rows where a batch changes from entries of 32 rows to tiles."""
+    s = setup([333, 70], [tokens, 1], 2, d, dtype, cross=True)
+    run(s, s.fill(lens=s.P), group, 0.1)
+
+
+@pytest.mark.parametrize("dtype", POOLS)
+@pytest.mark.parametrize("e", [1, 3, 200])
+@pytest.mark.parametrize("split", [0, 64])
+def test_a_nan_query_stays_in_its_row(setup, dtype, e, split):  # noqa: F811
+    s = setup([300, 90], [e, e], 2, 64, dtype, cross=True)
+    s.fill(lens=s.P)
+    kvx.kv_pool_set_split_keys(s.pool, split)
+    q = s.normal(s.T, 8, 64)
+    bad = q.clone()
+    bad[e - 1, 3, 5] = float("nan")
+    out, good = torch.empty_like(q), torch.empty_like(q)
+    kvx.cross_attention(s.pool, s.batch, bad, 8, 0.125, out)
+    kvx.cross_attention(s.pool, s.batch, q, 8, 0.125, good)
+    rest = torch.ones(s.T, 8, dtype=torch.bool, device=DEV)
+    rest[e - 1, 3] = False
+    assert torch.isnan(out[e - 1, 3]).all() and torch.isfinite(good).all()
+    assert torch.equal(out[rest], good[rest])
+
+
+@pytest.mark.parametrize("dtype", POOLS)
 @pytest.mark.parametrize("e", [1, 3, 20])
 def test_many_requests(setup, dtype, e):  # noqa: F811
     """More requests than the kernel arguments hold, some without states, some without queries."""

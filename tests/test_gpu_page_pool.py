@@ -401,6 +401,130 @@ def test_decode(setup, d, n, hkv, group):
     check_extend(s, held, q, 0.09, out, lse)
 
 
+DRAFTS = [
+    # P, E, hkv, group: at most 128 rows a request
+    ([0, 5, 300], [2, 3, 1], 2, 1),
+    ([1000, 63, 64, 0], [5, 33, 2, 40], 1, 3),
+    ([40, 700], [16, 7], 3, 8),
+    ([511, 512, 513], [4, 0, 3], 2, 16),
+    ([90, 1300], [6, 1], 1, 20),
+    ([200], [4], 2, 32),
+    ([17, 400], [128, 100], 2, 1),
+    ([(31 * i) % 500 for i in range(200)], [1 + i % 6 for i in range(200)], 1, 4),  # more than the arguments hold
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("P,E,hkv,group", DRAFTS)
+def test_drafts(setup, P, E, hkv, group, d):
+    """A few tokens a request, each seeing one key more than the one before it."""
+    s = setup(P, E, hkv, d)
+    held = s.fill()
+    q = s.normal(s.T, hkv * group, d)
+    for split in (0, 64, 320):
+        kvx.kv_pool_set_split_keys(s.pool, split)
+        out, lse = attend(s, q, hkv * group, 0.09)
+        check_extend(s, held, q, 0.09, out, lse)
+    out, lse = attend(s, q, hkv * group, 0.09, kvx.extend_attention_noalloc)
+    check_extend(s, held, q, 0.09, out, lse)
+
+
+@pytest.mark.parametrize("e", [1, 3, 200])
+@pytest.mark.parametrize("split", [0, 64])
+def test_a_nan_query_stays_in_its_row(setup, e, split):
+    P, E = [300, 90], [e, e]
+    s = setup(P, E, 2, 128)
+    held = s.fill()
+    kvx.kv_pool_set_split_keys(s.pool, split)
+    q = s.normal(s.T, 8, 128)
+    bad = q.clone()
+    bad[e - 1, 3, 5] = float("nan")
+    out, _ = attend(s, bad, 8, 0.09)
+    assert torch.isnan(out[e - 1, 3]).all()
+    rest = torch.ones(s.T, 8, dtype=torch.bool, device=DEV)
+    rest[e - 1, 3] = False
+    assert torch.isfinite(out[rest]).all()
+    good, _ = attend(s, q, 8, 0.09)
+    assert torch.equal(out[rest], good[rest])
+    check_extend(s, held, q, 0.09, good)
+
+
+def gpu_attend(q, k, v, scale):
+    """One query [Hq, d] over k, v [n, Hkv, d] in float64 on the GPU: output and its bound (page_ref.attend)."""
+    Hq, d = q.shape
+    g = Hq // k.shape[1]
+    k, v = k.double().transpose(0, 1), v.double().transpose(0, 1)
+    qh = q.double().view(-1, g, d)
+    w = torch.softmax(torch.matmul(qh, k.transpose(1, 2).contiguous()) * scale, -1)
+    mag = torch.matmul(qh.abs(), k.abs().transpose(1, 2).contiguous()).amax(-1, keepdim=True) * scale
+    o, size = torch.matmul(w, v), torch.matmul(w, v.abs())
+    err = torch.expm1(2 * (d + 4) * ref.F32 * mag) + ref.HALF_BF16 + (16 + k.shape[1] / 64) * ref.F32
+    tol = err * (size + o.abs()) + ref.HALF_BF16 * o.abs() * (1 + err) + 1e-38
+    return o.reshape(Hq, d).cpu().numpy(), tol.reshape(Hq, d).cpu().numpy()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_decode_that_streams(setup, shared):
+    """More K and V than the Infinity Cache holds: pages of one request alone are loaded
+    past the caches, those of a prefix that several hold are not."""
+    P, n = [50000, 61003, 40017], 3
+    s = setup(P, [1] * n, 8, 128, poison=False)
+    if shared:
+        pages = s.host_pages.copy()
+        for r in (1, 2):
+            pages[s.indptr[r]:s.indptr[r] + 2000] = pages[:2000]
+        s.host_pages, s.pages = pages, torch.from_numpy(pages).to(DEV)
+    s.batch = kvx.Batch(P, [1] * n, s.indptr, s.pages)
+    lens = [p + 1 for p in P]
+    whole = kvx.Batch([0] * n, lens, s.indptr, s.pages)
+    kvx.store_kv(s.pool, whole, s.normal(sum(lens), 8, 128), s.normal(sum(lens), 8, 128))
+    q = s.normal(n, 64, 128)
+    out = torch.empty_like(q)
+    kvx.extend_attention(s.pool, s.batch, q, 64, 0.09, out)
+    for r in range(n):
+        k, v = (torch.empty(lens[r], 8, 128, dtype=BF16, device=DEV) for _ in range(2))
+        one = kvx.Batch([0], [lens[r]], [0, len(s.pages_of(r))], torch.from_numpy(s.pages_of(r).copy()).to(DEV))
+        kvx.load_kv(s.pool, one, k, v)
+        o, tol = gpu_attend(q[r], k, v, 0.09)
+        ref.check(ref.f64(out[r]), o, tol, f"request {r}")
+
+
+def test_pages_past_2_gib(setup):
+    """Codes and scales of pages whose offsets pass 2^31 bytes, written, read and attended."""
+    pages, hkv, d = (1 << 21) + 100, 1, 64
+    pool = kvx.kv_pool_create(pages, 16, hkv, d, PAGE)
+    try:
+        s = setup([130, 20], [50, 1], hkv, d)  # its page table, moved to the end of the large pool
+        s.host_pages = (pages - 1 - s.host_pages).astype(np.int32)
+        s.pages = torch.from_numpy(s.host_pages).to(DEV)
+        k, v = s.normal(201, hkv, d), s.normal(201, hkv, d)
+        whole = kvx.Batch([0, 0], [180, 21], s.indptr, s.pages)
+        kvx.store_kv(pool, whole, k, v)
+        small = ref.PagePool(s.num_pages, hkv, d)
+        small.store(lambda r: pages - 1 - s.host_pages[s.indptr[r]:s.indptr[r + 1]], [0, 0], [180, 21], ref.f64(k), ref.f64(v))
+        held = [small.rows(pages - 1 - s.host_pages[s.indptr[r]:s.indptr[r + 1]], 0, n) for r, n in enumerate((180, 21))]
+        ko, vo = (torch.empty(201, hkv, d, dtype=BF16, device=DEV) for _ in range(2))
+        kvx.load_kv(pool, whole, ko, vo)
+        for i, got in enumerate((ko, vo)):
+            assert (ref.f64(got) == np.concatenate([h[i] for h in held])).all()
+        q = s.normal(51, 4, d)
+        out = torch.empty_like(q)
+        b = kvx.Batch([130, 20], [50, 1], s.indptr, s.pages)
+        kvx.extend_attention(pool, b, q, 4, 0.125, out)
+        check_extend(s, held, q, 0.125, out)
+        kvx.kv_pool_set_split_keys(pool, 64)
+        kvx.extend_attention(pool, b, q, 4, 0.125, out)
+        check_extend(s, held, q, 0.125, out)
+        # the same through the few-rows kernel
+        kvx.cross_attention(pool, kvx.Batch([180, 21], [1, 1], s.indptr, s.pages), q[:2].contiguous(), 4, 0.125, out[:2])
+        for r in range(2):
+            o, _, to, _ = ref.attend(ref.f64(q[r:r + 1]), *held[r], 0.125)
+            ref.check(ref.f64(out[r:r + 1]), o, to, f"request {r}")
+    finally:
+        torch.cuda.synchronize()
+        kvx.kv_pool_destroy(pool)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_mixed_batch(setup, d):
     """One-token suffixes beside longer ones, enough of them that the decode code takes them."""
