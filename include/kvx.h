@@ -271,7 +271,9 @@ int store_kv_rope(kvx_pool *pool, const kvx_batch *batch, const kvx_rope *rope, 
  * query heads share a KV head -- runs a dedicated decode kernel (key chunks of
  * each request and KV head streamed from HBM); the result is the same operation.
  * In a batch that mixes one-token suffixes with longer ones, the one-token suffixes
- * may take the same code next to the prefill tiles.
+ * may take the same code next to the prefill tiles.  On a page-scaled pool a batch whose
+ * requests have few rows each (whole tokens, times the query heads that share a KV head, in at most
+ * four groups of up to 32 rows) runs such a kernel of its own: decode steps and drafted tokens.
  * Uses a library-owned device workspace (grown with hipMallocAsync when a batch
  * needs more than any earlier one; at most 2 GiB of partial results).  Errors: EINVAL, EUNSUPPORTED, ERANGE (validation
  * mode), ENOMEM, EHIP.  R = 0 or T = 0: no-op.
@@ -318,7 +320,9 @@ int extend_attention_noalloc(kvx_pool *pool, const kvx_batch *batch, const void 
  *           queries E_r; its pages are ceil(L_r / 16) (more may be listed)
  *   q, num_q_heads, sm_scale, out, lse   as for extend_attention, T = sum E_r
  * A request without tokens (L_r = 0) gives zeros, and an lse of -inf.
- * The queries' number has no part in how a row is computed beyond the order of its sums.
+ * Products take bf16 operands (the softmax weights are rounded to bf16) and accumulate in
+ * float32.  Rows of the pool that it reads are finite: one that is not may reach every query of its
+ * request.  Slots past a request's L_r tokens reach none, whatever they hold.
  * All pool types; kv_pool_set_split_keys and kv_pool_set_scaled_q (for the requests with more
  * queries than a few) hold here too.  out and lse overlap neither q nor each other (EINVAL).
  * Runs on the pool's device and leaves the caller's current device as it was; a stream of
@@ -352,7 +356,8 @@ typedef struct {
  * within each XCD longest first or, in large unsplit batches, request by request;
  * for a decode step, key chunks of every (request, KV head), longest first
  * (tok_count 1); in a batch that mixes both, the one-token suffixes may be such
- * chunks, whose parts are numbered after the tiles'.  Writes at most `cap` items to
+ * chunks, whose parts are numbered after the tiles'.  (A page-scaled pool's batches of few
+ * rows are planned otherwise, see extend_attention.)  Writes at most `cap` items to
  * `items` (may be NULL) and the total count to *count.
  *   num_kv_heads, num_q_heads, head_dim as for extend_attention.
  *   split_keys   as set by kv_pool_set_split_keys (0 = automatic).
@@ -366,8 +371,8 @@ int extend_attention_plan(const kvx_batch *batch, int32_t num_q_heads, int32_t n
  * Key-range split length of extend_attention on this pool (tokens, a multiple
  * of 64, or 0 = automatic, the default).  A non-zero value splits every key
  * range longer than it (a decode step, and the one-token suffixes of a mixed batch: chunks
- * of that many keys; more where the parts would be too many); used to
- * exercise the split path.  A setting of the pool: takes effect for calls queued
+ * of that many keys, and those of a batch of few rows on a page-scaled pool; more where the
+ * parts would be too many); used to exercise the split path.  A setting of the pool: takes effect for calls queued
  * after it, from the pool's one host thread.  Errors: EINVAL.
  */
 int kv_pool_set_split_keys(kvx_pool *pool, int32_t keys);

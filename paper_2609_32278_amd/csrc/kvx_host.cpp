@@ -897,8 +897,8 @@ int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<i
   dp.units = (const DecodeUnit*)dev;
   p.o_part = plan.n_parts ? parts : nullptr;
   p.lse_part = plan.n_parts ? parts + (size_t)plan.n_parts * R * D : nullptr;
-  p.k_scale = pool->k_scales();
-  p.v_scale = pool->v_scales();
+  p.k_scale = pool->scales_d;
+  p.v_scale = pool->scales_d ? pool->scales_d + pool->num_kv_heads : nullptr;
   p.num_q_heads = num_q_heads;
   p.num_kv_heads = pool->num_kv_heads;
   p.group = num_q_heads / pool->num_kv_heads;
@@ -941,8 +941,8 @@ int64_t entries_per_tile(const kvx_pool* pool) {
 
 int64_t entries_of(int64_t tokens, int32_t group) { return ceil_div(tokens, kvx::kRowsMax / group); }
 
-// A request's tokens as entries, of nearly equal size.  They run next to each other on one XCD, where
-// the second finds the keys that the first read in the L2.
+// A request's tokens as entries, of nearly equal size.  They run at about the same time, with KV heads
+// a multiple of 8 on one XCD, where the second finds in the L2 the keys that the first read.
 void add_rows(std::vector<RowsRequest>& reqs, int32_t qo_row, int32_t tokens, int32_t page_base, int64_t keys,
               int32_t group, bool causal) {
   const int32_t most = kvx::kRowsMax / group, n = (tokens + most - 1) / most, each = (tokens + n - 1) / n;
@@ -988,14 +988,11 @@ RowsPlan make_rows_plan(const std::vector<RowsRequest>& reqs, int32_t Hkv, int32
     auto done_by = [&](int64_t most) { return std::max((double)most / rate, read + 0.5 * (double)most / rate); };
     if (len < longest && done_by(longest) < 0.9 * (done_by(len) + kMerge)) len = longest;
   }
-  auto ranges_of = [&](int64_t keys) -> int64_t {
-    if (split_keys > 0) return std::max<int64_t>(1, ceil_div(keys, len));
-    return std::max<int64_t>(1, ceil_div(keys, len));
+  auto len_of = [&](int64_t keys) {  // of an entry's ranges, all alike unless forced
+    if (split_keys > 0) return len;
+    return std::max(A, ceil_div(ceil_div(keys, std::max<int64_t>(1, ceil_div(keys, len))), A) * A);
   };
-  auto len_of = [&](int64_t keys) {
-    return split_keys > 0 ? len : std::max(A, ceil_div(ceil_div(keys, ranges_of(keys)), A) * A);
-  };
-  for (;;) {  // the parts bounded, and a small batch's plan in the kernel arguments, if twice the length makes it fit
+  for (;;) {  // longer ranges: to bound the parts, and to keep a small batch's plan in the kernel arguments
     int64_t parts = 0, most = 0, codes = 0;
     for (const RowsRequest& q : reqs) {
       const int64_t n = ceil_div(std::max<int64_t>(1, q.keys), len_of(q.keys));
@@ -1004,7 +1001,8 @@ RowsPlan make_rows_plan(const std::vector<RowsRequest>& reqs, int32_t Hkv, int32
       codes += n;
     }
     const int64_t fit = kvx::kRowsWords - (int64_t)reqs.size() * kvx::kRowsEntryWords;
-    const bool tighten = (int64_t)(read * kBytesPerUs) <= kStreamBytes && split_keys == 0 && codes > fit && (int64_t)reqs.size() <= fit;
+    const bool tighten =
+        split_keys == 0 && total * key_bytes <= kStreamBytes && codes > fit && (int64_t)reqs.size() <= fit;
     if (parts <= max_parts && most <= kMaxRanges && !tighten) break;
     len = ceil_div(len * 5 / 4, A) * A;
   }
