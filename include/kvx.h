@@ -152,8 +152,9 @@ int kv_pool_read_pages(const kvx_pool *pool, const int32_t *page_ids, int64_t n,
  * (the paper's stated future work, Section 6: keep evicted KV in a slower tier
  * and bring it back).  A spill record holds one page exactly as the pool holds
  * it -- its K block then its V block, kv_pool_record_bytes() bytes, raw (bf16 or
- * fp8 codes; the scales of heads stay with the pool, those of a page are in its record) -- so spill + reload is a bit-exact
- * round trip into any page of a pool of the same shape and dtype.
+ * fp8 codes; the scales of heads stay with the pool, those of a page are in its
+ * record) -- so spill + reload is a bit-exact round trip into any page of a pool
+ * of the same shape and dtype.
  *   kv_pool_spill:  record slots[i] of host := page page_ids[i]
  *   kv_pool_reload: page page_ids[i] := record slots[i] of host
  * page_ids, slots: host [n]; page ids in [0, num_pages), slots in [0, host_slots);

@@ -27,7 +27,8 @@ HIP_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall",
 # The scheduler's own count of live registers, for the prefill kernels of 8-bit pools in their
 # exact form: at 244 to 256 VGPRs the generic one overcounts three of their four unrolled
 # iterations and lines the products up without anything beside them (1064 against 1156 TFLOP/s).
-EXTRA_FLAGS = {name: ["-mllvm", "-amdgpu-use-amdgpu-trackers=1"] for name in ("kvx_page_attn.hip", "kvx_cross.hip", "kvx_cross_page.hip")}
+EXTRA_FLAGS = {name: ["-mllvm", "-amdgpu-use-amdgpu-trackers=1"]
+               for name in ("kvx_page_attn.hip", "kvx_cross.hip", "kvx_cross_page.hip")}
 
 
 def hipcc() -> str:

