@@ -84,7 +84,8 @@ enum kvx_kv_dtype {
  * again (only values below 2^-6 * 2^e can change).  Each new value is stored as
  * e4m3(clamp(x * 2^-e, -448, 448)), rounded to nearest even, NaN as NaN (it counts for no
  * maximum).  The slots of a written page past the batch's last token of the request become
- * zero.  Every stored value is a bf16 number: the attention and load_kv read it exactly. */
+ * zero, so a page that a batch writes is listed by no other request that writes it.  Every stored
+ * value is a bf16 number: the attention and load_kv read it exactly. */
 
 /* ------------------------------------------------------------------ the pool */
 
