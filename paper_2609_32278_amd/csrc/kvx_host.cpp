@@ -1395,8 +1395,7 @@ static int rope_store(kvx_pool* pool, const kvx_batch* batch, const std::vector<
   return p.units ? pool->st_store.done(s) : KVX_OK;
 }
 
-int store_kv(kvx_pool* pool, const kvx_batch* batch, const void* k_ext, const void* v_ext, kvx_stream_t stream) {
-  g_last_error.clear();
+static int store_call(kvx_pool* pool, const kvx_batch* batch, const void* k_ext, const void* v_ext, kvx_stream_t stream) {
   if (int rc = check_pool(pool)) return rc;
   std::vector<int64_t> qo;
   if (int rc = check_batch(batch, qo)) return rc;
@@ -1445,9 +1444,13 @@ int store_kv(kvx_pool* pool, const kvx_batch* batch, const void* k_ext, const vo
   return p.reqs.n > 0 ? KVX_OK : pool->st_store.done(s);
 }
 
-int store_kv_rope(kvx_pool* pool, const kvx_batch* batch, const kvx_rope* rope, const void* q, int32_t num_q_heads,
-                  void* q_out, const void* k_ext, const void* v_ext, kvx_stream_t stream) {
-  g_last_error.clear();
+int store_kv(kvx_pool* pool, const kvx_batch* batch, const void* k_ext, const void* v_ext, kvx_stream_t stream) {
+  return kvx::guarded([&]() { return store_call(pool, batch, k_ext, v_ext, stream); });
+}
+
+static int store_rope_call(kvx_pool* pool, const kvx_batch* batch, const kvx_rope* rope, const void* q,
+                           int32_t num_q_heads, void* q_out, const void* k_ext, const void* v_ext,
+                           kvx_stream_t stream) {
   if (int rc = check_pool(pool)) return rc;
   std::vector<int64_t> qo;
   if (int rc = check_batch(batch, qo)) return rc;
@@ -1499,6 +1502,13 @@ int store_kv_rope(kvx_pool* pool, const kvx_batch* batch, const kvx_rope* rope, 
   return rope_store(pool, batch, qo, p, rope->style == KVX_ROPE_INTERLEAVED, k_ext, v_ext, s);
 }
 
+int store_kv_rope(kvx_pool* pool, const kvx_batch* batch, const kvx_rope* rope, const void* q, int32_t num_q_heads,
+                  void* q_out, const void* k_ext, const void* v_ext, kvx_stream_t stream) {
+  return kvx::guarded([&]() {
+    return store_rope_call(pool, batch, rope, q, num_q_heads, q_out, k_ext, v_ext, stream);
+  });
+}
+
 int extend_attention_plan(const kvx_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                           int32_t split_keys, kvx_work_item* items, int64_t cap, int64_t* count) {
   g_last_error.clear();
@@ -1541,9 +1551,8 @@ int extend_attention(kvx_pool* pool, const kvx_batch* batch, const void* q, int3
 
 }  // extern "C"
 
-int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, int32_t num_q_heads, float sm_scale,
-                        void* out, float* lse, kvx_stream_t stream, const FixedScratch* fixed) {
-  g_last_error.clear();
+static int attend(kvx_pool* pool, const kvx_batch* batch, const void* q, int32_t num_q_heads, float sm_scale, void* out,
+                  float* lse, kvx_stream_t stream, const kvx::FixedScratch* fixed) {
   if (int rc = check_pool(pool)) return rc;
   if (int rc = check_heads(num_q_heads, pool->num_kv_heads, pool->head_dim)) return rc;
   if (!(std::isfinite(sm_scale) && sm_scale > 0.f)) return fail(KVX_EINVAL, "sm_scale must be finite and > 0");
@@ -1571,6 +1580,11 @@ int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, i
   if (is_decode_batch(batch, num_q_heads, pool->num_kv_heads))
     return decode_attention(pool, batch, qo, q, num_q_heads, sm_scale, out, lse, s, buf);
   return tile_attention(pool, batch, qo, false, q, num_q_heads, sm_scale, out, lse, s, buf);
+}
+
+int kvx::attention_call(kvx_pool* pool, const kvx_batch* batch, const void* q, int32_t num_q_heads, float sm_scale,
+                        void* out, float* lse, kvx_stream_t stream, const FixedScratch* fixed) {
+  return guarded([&]() { return attend(pool, batch, q, num_q_heads, sm_scale, out, lse, stream, fixed); });
 }
 
 namespace {

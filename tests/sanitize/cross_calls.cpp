@@ -8,8 +8,20 @@
 #include "kvx_load.cpp"
 
 #include <map>
+#include <new>
 #include <random>
 #include <tuple>
+
+// Host allocations until one fails; < 0: none does.
+static int g_allocs = -1;
+void* operator new(size_t n) {
+  if (g_allocs >= 0 && g_allocs-- == 0) throw std::bad_alloc();
+  if (void* p = std::malloc(n)) return p;
+  throw std::bad_alloc();
+}
+void* operator new(size_t n, const std::nothrow_t&) noexcept { return std::malloc(n); }
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, size_t) noexcept { std::free(p); }
 
 struct ihipStream_t {
   int device;
@@ -152,7 +164,7 @@ hipError_t launch_decode(const DecodeParams& dp, int64_t, int, bool, hipStream_t
 }
 hipError_t launch_decode_merge(const DecodeMergeParams&, int64_t, int, hipStream_t) { std::exit(4); }
 hipError_t launch_store_kv(const StoreParams&, int64_t, int, bool, hipStream_t) { std::exit(4); }
-hipError_t launch_store_kv_rope(const RopeParams&, int64_t, int, bool, bool, hipStream_t) { std::exit(4); }
+hipError_t launch_store_kv_rope(const RopeParams&, int64_t, int, bool, bool, hipStream_t) { return hipSuccess; }
 hipError_t launch_page_move(const PageMoveParams&, int64_t, hipStream_t) { std::exit(4); }
 hipError_t launch_page_io(const PageIoParams&, int64_t, int, int, hipStream_t) { std::exit(4); }
 hipError_t launch_load_kv(const LoadParams&, int64_t, int, int32_t, hipStream_t) {
@@ -421,6 +433,43 @@ void streams() {
   release(p);
 }
 
+// Whichever host allocation of a call fails, the call says so and leaves the pool as it was.
+void memory() {
+  std::vector<int32_t> P, E;
+  for (int i = 0; i < 300; i++) {
+    P.push_back(1 + 97 * i);
+    E.push_back(1 + i % 3);
+  }
+  const TestBatch large(P, E, 1), small({700, 900}, {1, 2}, 1), tiles({700, 900}, {400, 3}, 25);
+  kvx_rope rope{10000.0, nullptr, 64, KVX_ROPE_HALF, nullptr, nullptr, 1e-6f};
+  kvx_pool p = pool_of(2, 64, KVX_KV_FP8_PAGE);
+  for (const TestBatch* t : {&large, &small, &tiles})
+    for (int what = 0; what < 5; what++) {
+      if (what == 0 && t == &tiles) continue;  // the stand-in's tiles are cross attention's
+      g_causal = what == 0;
+      auto call = [&]() {
+        if (what == 0) return extend_attention(&p, &t->b, far_away(1), 6, 0.1f, far_away(2), nullptr, nullptr);
+        if (what == 1) return cross_attention(&p, &t->b, far_away(1), 6, 0.1f, far_away(2), nullptr, nullptr);
+        if (what == 2) return store_kv(&p, &t->b, far_away(1), far_away(2), nullptr);
+        if (what == 3) return store_kv_rope(&p, &t->b, &rope, nullptr, 0, nullptr, far_away(1), far_away(2), nullptr);
+        return load_kv(&p, &t->b, far_away(1), far_away(2), nullptr);
+      };
+      int failed = 0, rc = KVX_ENOMEM;
+      for (; rc == KVX_ENOMEM && failed < 10000; failed++) {
+        forget();
+        g_allocs = failed;
+        rc = call();
+        const bool whole = g_allocs >= 0;
+        g_allocs = -1;
+        CHECK(rc == (whole ? KVX_OK : KVX_ENOMEM));
+      }
+      CHECK(rc == KVX_OK && failed > 1);
+    }
+  g_causal = 0;
+  p.st_store.release();
+  release(p);
+}
+
 // A pool's own refusals, and what a page-scaled pool adds to its buffers.
 void pools() {
   kvx_pool* p = nullptr;
@@ -452,6 +501,7 @@ int main(int argc, char** argv) {
   else if (what == "refusals") refusals();
   else if (what == "streams") streams();
   else if (what == "pools") pools();
+  else if (what == "memory") memory();
   else return 2;
   std::printf("%s passed\n", what.c_str());
   return 0;

@@ -33,7 +33,7 @@ def driver(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("check", ["coverage", "drafts", "limits", "refusals", "streams", "pools"])
+@pytest.mark.parametrize("check", ["coverage", "drafts", "limits", "refusals", "streams", "pools", "memory"])
 def test_host_calls(driver, check, tmp_path):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
     run = subprocess.run([driver, check], capture_output=True, text=True, env=env, timeout=300, cwd=tmp_path)
