@@ -754,13 +754,6 @@ struct CallBuffers {
     }
     return pool->st_attn.upload(blob.data(), blob.size(), s, out);
   }
-  // staged: the call's kernels read the staging buffer
-  int done(hipStream_t s, bool staged) {
-    if (fixed) return KVX_OK;
-    if (staged)
-      if (int rc = pool->st_attn.done(s)) return rc;
-    return pool->parts.done(s);
-  }
 };
 
 // The units of a decode plan in kernel arguments, if they fit (see InlinePlan).
@@ -917,7 +910,7 @@ int decode_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<i
     e = kvx::launch_decode_merge(m, (int64_t)plan.merges.size(), D, s);
     if (e != hipSuccess) return hip_fail(e, "decode merge kernel launch");
   }
-  return buf.done(s, !in_args);
+  return KVX_OK;
 }
 
 // ---- few query rows over all keys of their request (kvx_rows.hip)
@@ -957,14 +950,17 @@ void add_rows(std::vector<RowsRequest>& reqs, int32_t qo_row, int32_t tokens, in
 // The length, in keys of all KV heads over the 512 workgroups that run at a time: a batch that
 // gives each of them at most 1024 is cut to one unit each (at least 384 keys), a larger one into
 // four rounds, or two where a workgroup takes two blocks of rows (whose ranges cost twice as
-// much to merge).  Unless whole ranges are estimated to be done sooner: a merge costs 10 us, a lone
+// much to merge).  Unless whole ranges are estimated to be done sooner: a merge costs 6 us, a lone
 // workgroup takes 200 keys a us (120 of a bf16 pool), all of them together read 5.6 TB/s, and half
 // of the longest unit is left over at the end.  us a call at lengths of 256 / 512 / 1024 / 2048 / 4096 /
-// whole: 4 agents of 1k to 8k, 32/8/128 heads, 18.6 / 17.5 / 17.7 / 21.9 / 31 / 37; 24 on 16k to 131k,
-// 64/8/128, 616 / 607 / 587 / 499 / 462 / - (8192: 479); 48 single queries of 16/16/64 heads on 200
-// to 1500, bf16, 30.9 / 29.9 / 30.4 / - / - / 25.1; 33 times 1 to 5 queries of 64/8/128 heads on 2k
-// to 20k 200 / 146 / 132 / 121 / 121 / 119; 24 on 1200, 8/8/128, 24 / 24 / 22 / - / - / 18.4; 40 on
-// 5000 128 / 84 / 84 / 83 / 90 / 96.
+// whole: 4 agents of 1k to 8k, 32/8/128 heads, 12.2 / 11.6 / 13.0 / 17.9 / 27 / 33; 24 on 16k to 131k,
+// 64/8/128, 613 / 604 / 581 / 497 / 458 / 978 (8192: 473); 48 single queries of 16/16/64 heads on 200
+// to 1500, bf16, 24.4 / 24.7 / 24.8 / - / - / 22.0; 33 times 1 to 5 queries of 64/8/128 heads on 2k
+// to 20k 191 / 139 / 124 / 113 / 113 / 169; 24 on 1200, 8/8/128, 17.2 / 17.8 / 16.3 / - / - / 13.2; 40 on
+// 5000 111 / 75 / 75 / 75 / 83 / 91; 23 times 5 queries of 16/2/128 heads on 17 to 1146, bf16,
+// 13.6 / 15.8 / 20.7 / - / - / 18.3; 10 times 27 of 28/14/128 on 376 to 2651, fp8, 33 / 28 / 23 / 26.5 / - / 26.2.
+// Merges estimated at 10 us leave the last but one and 10 times 9 of 5/5/128 on 1193 to 1920 whole (18.7
+// and 14.3, now 14.7 and 10.7); at 5 us the 48 single queries are cut too.
 struct RowsPlan {
   std::vector<uint32_t> words;
   int64_t n_codes = 0, n_parts = 0;
@@ -979,7 +975,7 @@ RowsPlan make_rows_plan(const std::vector<RowsRequest>& reqs, int32_t Hkv, int32
     longest = std::max(longest, q.keys);
   }
   constexpr int64_t kSlots = 512;
-  constexpr double kMerge = 10.0, kBytesPerUs = 5.6e6;
+  constexpr double kMerge = 6.0, kBytesPerUs = 5.6e6;
   const double read = (double)total * key_bytes / kBytesPerUs, rate = bf16 ? 120.0 : 200.0;
   int64_t len = split_keys;
   if (split_keys == 0) {
@@ -1090,7 +1086,7 @@ int rows_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<Row
   dp.rows = &p;
   const hipError_t e = kvx::launch_decode(dp, p.n_codes, D, pool->kv_dtype == KVX_KV_FP8_E4M3, s);
   if (e != hipSuccess) return hip_fail(e, "rows kernel launch");
-  return buf.done(s, !in_args);
+  return KVX_OK;
 }
 
 int tile_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int64_t>& qo, bool cross, const void* q,
@@ -1275,7 +1271,7 @@ static int page_io(kvx_pool* pool, const int32_t* page_ids, int64_t n, void* k_l
   p.page_scale = pool->page_scales;
   hipError_t e = kvx::launch_page_io(p, n, pool->head_dim, pool->elem_bytes, s);
   if (e != hipSuccess) return hip_fail(e, "page io kernel launch");
-  return in_args ? KVX_OK : pool->st_io.done(s);
+  return KVX_OK;
 }
 
 int kv_pool_write_pages(kvx_pool* pool, const int32_t* page_ids, int64_t n, const void* k_src, const void* v_src,
@@ -1357,7 +1353,7 @@ static int page_move(kvx_pool* pool, const int32_t* page_ids, const int32_t* slo
   p.to_host = to_host;
   hipError_t e = kvx::launch_page_move(p, n, s);
   if (e != hipSuccess) return hip_fail(e, "page move kernel launch");
-  return pool->st_move.done(s);
+  return KVX_OK;
 }
 
 int kv_pool_spill(const kvx_pool* pool, const int32_t* page_ids, const int32_t* slots, int64_t n, void* host,
@@ -1392,7 +1388,7 @@ static int rope_store(kvx_pool* pool, const kvx_batch* batch, const std::vector<
   const hipError_t e =
       kvx::launch_store_kv_rope(p, n_units, pool->head_dim, pool->kv_dtype == KVX_KV_FP8_E4M3, interleaved, s);
   if (e != hipSuccess) return hip_fail(e, p.rotary_dim > 0 ? "store_kv_rope kernel launch" : "store_kv kernel launch");
-  return p.units ? pool->st_store.done(s) : KVX_OK;
+  return KVX_OK;
 }
 
 static int store_call(kvx_pool* pool, const kvx_batch* batch, const void* k_ext, const void* v_ext, kvx_stream_t stream) {
@@ -1441,7 +1437,7 @@ static int store_call(kvx_pool* pool, const kvx_batch* batch, const void* k_ext,
   p.num_kv_heads = pool->num_kv_heads;
   hipError_t e = kvx::launch_store_kv(p, (int64_t)units.size(), pool->head_dim, pool->kv_dtype == KVX_KV_FP8_E4M3, s);
   if (e != hipSuccess) return hip_fail(e, "store_kv kernel launch");
-  return p.reqs.n > 0 ? KVX_OK : pool->st_store.done(s);
+  return KVX_OK;
 }
 
 int store_kv(kvx_pool* pool, const kvx_batch* batch, const void* k_ext, const void* v_ext, kvx_stream_t stream) {
@@ -1690,7 +1686,7 @@ int tile_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int
     e = kvx::launch_decode_merge(dm, (int64_t)plan.dec_merges.size(), D, s);
     if (e != hipSuccess) return hip_fail(e, "decode merge kernel launch");
   }
-  return buf.done(s, !in_args);
+  return KVX_OK;
 }
 
 int check_cross(const kvx_pool* pool, const kvx_batch* batch, std::vector<int64_t>& qo, const void* q,

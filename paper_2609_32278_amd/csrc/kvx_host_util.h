@@ -34,16 +34,16 @@ inline bool validate_mode() {
 
 // Pinned host buffer + device buffer + events: a reusable upload channel.  The
 // host side is rewritten only after the previous copy out of it has completed.
-// The device buffer grows with the stream-ordered allocator: the old buffer is
-// freed in stream order behind `used` (recorded after the last kernels that read
-// it), so growing never waits on the host for the device.
+// The device buffer grows with the stream-ordered allocator, so growing never waits on the
+// host for the device.  The old buffer is freed on the stream of the call that needs a larger one,
+// which is behind the kernels that read it: a pool's calls are ordered by contract.  (An event after
+// every call's kernels to wait for there instead takes 3 us of a small call.)
 struct Staging {
   void* host = nullptr;
   size_t host_cap = 0;
   void* dev = nullptr;
   size_t dev_cap = 0;
-  hipEvent_t ev = nullptr;    // after the last copy out of `host`
-  hipEvent_t used = nullptr;  // after the last kernels that read `dev`
+  hipEvent_t ev = nullptr;  // after the last copy out of `host`
   bool pending = false;
 
   // Only after the device has gone idle (pool destruction).
@@ -52,7 +52,6 @@ struct Staging {
       (void)hipEventSynchronize(ev);
       (void)hipEventDestroy(ev);
     }
-    if (used) (void)hipEventDestroy(used);
     if (host) (void)hipHostFree(host);
     if (dev) (void)hipFreeAsync(dev, nullptr);
     *this = Staging();
@@ -60,10 +59,8 @@ struct Staging {
 
   // Copy `bytes` from `src` to device memory ordered on `stream`; *out receives the
   // device address (valid until the next upload on this channel is ordered after it).
-  // The caller records done() on the stream after the kernels that read it.
   int upload(const void* src, size_t bytes, hipStream_t stream, void** out) {
     if (!ev) KVX_HIP(hipEventCreateWithFlags(&ev, hipEventDisableTiming));
-    if (!used) KVX_HIP(hipEventCreateWithFlags(&used, hipEventDisableTiming));
     if (pending) {
       KVX_HIP(hipEventSynchronize(ev));
       pending = false;
@@ -77,11 +74,7 @@ struct Staging {
       host_cap = cap;
     }
     if (bytes > dev_cap) {
-      if (dev) {
-        // earlier kernels (on any stream) that read the old buffer precede `used`
-        KVX_HIP(hipStreamWaitEvent(stream, used, 0));
-        KVX_HIP(hipFreeAsync(dev, stream));
-      }
+      if (dev) KVX_HIP(hipFreeAsync(dev, stream));
       dev = nullptr;
       dev_cap = 0;
       size_t cap = std::max<size_t>(bytes + bytes / 2, 4096);
@@ -95,23 +88,15 @@ struct Staging {
     *out = dev;
     return KVX_OK;
   }
-
-  int done(hipStream_t stream) {
-    KVX_HIP(hipEventRecord(used, stream));
-    return KVX_OK;
-  }
 };
 
 // Device scratch that only grows, with the same stream-ordered replacement.
 struct Workspace {
   void* ptr = nullptr;
   size_t cap = 0;
-  hipEvent_t used = nullptr;  // after the last kernels that used `ptr`
   int ensure(size_t bytes, hipStream_t stream) {
-    if (!used) KVX_HIP(hipEventCreateWithFlags(&used, hipEventDisableTiming));
     if (bytes <= cap) return KVX_OK;
     if (ptr) {
-      KVX_HIP(hipStreamWaitEvent(stream, used, 0));
       KVX_HIP(hipFreeAsync(ptr, stream));
       ptr = nullptr;
       cap = 0;
@@ -122,17 +107,11 @@ struct Workspace {
     cap = c;
     return KVX_OK;
   }
-  int done(hipStream_t stream) {
-    if (used) KVX_HIP(hipEventRecord(used, stream));
-    return KVX_OK;
-  }
   // Only after the device has gone idle (pool destruction).
   void release() {
     if (ptr) (void)hipFreeAsync(ptr, nullptr);
-    if (used) (void)hipEventDestroy(used);
     ptr = nullptr;
     cap = 0;
-    used = nullptr;
   }
 };
 

@@ -180,7 +180,7 @@ int store_call(kvx_latent_pool* pool, const kvx_batch* batch, const kvx_rope* ro
   const hipError_t e =
       kvx::launch_store_latent(p, n_units, pool->latent_dim, pool->dtype == KVX_LATENT_FP8, interleaved, s);
   if (e != hipSuccess) return hip_fail(e, "store_latent kernel launch");
-  return p.units ? pool->st_rows.done(s) : KVX_OK;
+  return KVX_OK;
 }
 
 // ------------------------------------------------------------------ plans
@@ -681,7 +681,7 @@ int launch_absorbed(kvx_latent_pool* pool, const kvx_batch* batch, const Absorbe
     e = kvx::launch_latent_merge(m, (int64_t)plan.merges.size(), small, rows, pool->latent_dim, plan.row_blocks, s);
     if (e != hipSuccess) return hip_fail(e, "latent merge kernel launch");
   }
-  return plan.n_parts > 0 ? pool->parts.done(s) : KVX_OK;
+  return KVX_OK;
 }
 
 }  // namespace
@@ -806,7 +806,7 @@ int load_latent(kvx_latent_pool* pool, const kvx_batch* batch, void* out, int64_
     p.out_stride = out_stride;
     const hipError_t e = kvx::launch_load_latent(p, n_units, pool->latent_dim, pool->dtype == KVX_LATENT_FP8, s);
     if (e != hipSuccess) return hip_fail(e, "load_latent kernel launch");
-    return p.units ? pool->st_rows.done(s) : KVX_OK;
+    return KVX_OK;
   });
 }
 
@@ -847,7 +847,7 @@ int latent_attention(kvx_latent_pool* pool, const kvx_batch* batch, const void* 
     if (int rc = launch_absorbed(pool, batch, plan, (const uint8_t*)dev, units_at, merges_at, q, num_q_heads, sm_scale,
                                  out, lse, s))
       return rc;
-    return plan.in_args ? KVX_OK : pool->st_plan.done(s);
+    return KVX_OK;
   });
 }
 
@@ -981,7 +981,6 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
       p.lse_out = lse;
       e = kvx::launch_latent_output(p, (int64_t)rows.size(), lat, D, s);
       if (e != hipSuccess) return hip_fail(e, "latent output product launch");
-      if (int rc = pool->absorbed.done(s)) return rc;
     }
     if (!expanded.empty()) {
       const size_t r_bytes = (size_t)x_rows * kvx::kLatRope * 2;
@@ -1036,11 +1035,8 @@ int latent_extend_attention(kvx_latent_pool* pool, const kvx_batch* batch, const
           if (e != hipSuccess) return hip_fail(e, "expanded merge launch");
         }
       }
-      if (int rc = pool->expanded.done(s)) return rc;
-      if (n_parts > 0)
-        if (int rc = pool->parts.done(s)) return rc;
     }
-    return blob.bytes.empty() ? KVX_OK : pool->st_plan.done(s);
+    return KVX_OK;
   });
 }
 

@@ -39,6 +39,6 @@ extern "C" int load_kv(const kvx_pool* pool, const kvx_batch* batch, void* k_out
     p.num_kv_heads = pool->num_kv_heads;
     const hipError_t e = kvx::launch_load_kv(p, n_units, pool->head_dim, pool->kv_dtype, s);
     if (e != hipSuccess) return kvx::hip_fail(e, "load_kv kernel launch");
-    return p.units ? units.done(s) : KVX_OK;
+    return KVX_OK;
   });
 }
