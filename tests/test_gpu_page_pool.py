@@ -269,10 +269,11 @@ def test_load_from_the_other_pools(setup, dtype, hkv, d):
 
 
 def test_raw_pages_and_spill_carry_the_scales(setup):
-    s = setup([0, 0], [50, 100], 3, 64)
+    heads, block = 5, 5 * 16 * 64  # block: the codes of a page, of K or V
+    s = setup([0, 0], [50, 100], heads, 64)
     s.fill()
-    n, m = s.num_pages, s.num_pages * 3 * 16 * 64
-    bufs = [torch.empty(m + 4 * n * 3, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    n, m = s.num_pages, s.num_pages * block
+    bufs = [torch.empty(m + 4 * n * heads, dtype=torch.uint8, device=DEV) for _ in range(2)]
     kvx.kv_pool_read_pages(s.pool, np.arange(n), *bufs)
     rec = kvx.kv_pool_record_bytes(s.pool)
     host = torch.empty(n * rec, dtype=torch.uint8, pin_memory=True)
@@ -280,11 +281,11 @@ def test_raw_pages_and_spill_carry_the_scales(setup):
     torch.cuda.synchronize()
     # a record: the K block, the V block as the pool holds it, (K, V) scales of each head
     for page in (0, n - 1):
-        r = host[(n - 1 - page) * rec:][:2 * 3 * 1024 + 24]
-        assert torch.equal(r[:3072], bufs[0][page * 3072:(page + 1) * 3072].cpu())
-        sc = r[6144:].view(torch.float32).view(3, 2)
+        r = host[(n - 1 - page) * rec:][:2 * block + 8 * heads]
+        assert torch.equal(r[:block], bufs[0][page * block:(page + 1) * block].cpu())
+        sc = r[2 * block:].view(torch.float32).view(heads, 2)
         for i in range(2):
-            assert torch.equal(sc[:, i], bufs[i][m:].view(torch.float32).view(n, 3)[page].cpu())
+            assert torch.equal(sc[:, i], bufs[i][m:].view(torch.float32).view(n, heads)[page].cpu())
     before = s.raw()
     s.poison()
     kvx.kv_pool_reload(s.pool, np.arange(n), np.arange(n)[::-1].copy(), host, n)
