@@ -276,6 +276,10 @@ int store_kv_rope(kvx_pool *pool, const kvx_batch *batch, const kvx_rope *rope, 
  * may take the same code next to the prefill tiles.  On a page-scaled pool a batch whose
  * requests have few rows each (whole tokens, times the query heads that share a KV head, in at most
  * four groups of up to 32 rows) runs such a kernel of its own: decode steps and drafted tokens.
+ * A K or V that is not finite reaches the rows that see its token.  Where rows run as prefill
+ * tiles (KVX_TILE_ROWS), such a V of a suffix token may reach the rows of its tile before it too (their
+ * weight of zero times it is NaN); decode steps and the batches of few rows on a page-scaled
+ * pool keep it to the rows that see it.
  * Uses a library-owned device workspace (grown with hipMallocAsync when a batch
  * needs more than any earlier one; at most 2 GiB of partial results).  Errors: EINVAL, EUNSUPPORTED, ERANGE (validation
  * mode), ENOMEM, EHIP.  R = 0 or T = 0: no-op.

@@ -352,6 +352,51 @@ struct Step8 {
   float kby, vby;  // page-scaled pool: the powers of two of the lane's K page and V page
 };
 
+// 0x80 in every byte of w that is a NaN code
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+
+// NaN codes of c as zeros; nans: where there were any.
+__device__ __forceinline__ uint4 without_nans(uint4 c, uint32_t& nans) {
+  uint32_t* w = (uint32_t*)&c;
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    const uint32_t is = nan_codes(w[e]);
+    nans |= is;
+    w[e] &= ~((is >> 7) * 0xFFu);
+  }
+  return c;
+}
+
+// Rows that see a NaN value get NaN in its dim: where the product of "is NaN" (dims x keys) and "is
+// seen" (keys x rows), ones and zeros, is not 0.  v: the lane's codes of the first 16 dims, key0:
+// their first slot's key.  Read again, one block after the other: kept for this, or cleaned ahead of
+// the products, the codes cost registers (256 for 235 in two blocks of rows, D = 128, or spills).
+template <int D, int NB>
+__device__ __forceinline__ void nan_to_rows(const char* v, int key0, const int (&limit)[NB], State<D, NB>& st) {
+#pragma unroll
+  for (int b = 0; b < NB; b++) {
+    uint32_t w[8];  // slots 2 e, 2 e + 1: bf16 ones
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+      w[e] = (key0 + 2 * e < limit[b] ? 0x3F80u : 0u) | (key0 + 2 * e + 1 < limit[b] ? 0x3F800000u : 0u);
+#pragma unroll
+    for (int d = 0; d < D / 16; d++) {
+      auto ones = [](uint32_t c) { return (nan_codes(c) >> 7) * 0x38u; };  // e4m3 1.0
+      const uint4 c = load16<false>(v + 256 * d);
+      f32x4 n = {0.f, 0.f, 0.f, 0.f};
+      n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          __builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(ones(c.x), ones(c.y)))),
+          __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3])), n, 0, 0, 0);
+      n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          __builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(ones(c.z), ones(c.w)))),
+          __builtin_bit_cast(bf16x8, make_uint4(w[4], w[5], w[6], w[7])), n, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 4; e++) st.o[b][d][e] = n[e] > 0.f ? __builtin_nanf("") : st.o[b][d][e];
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
 template <int D, int NB, bool PAGE, class Nt>
 __device__ __forceinline__ void rows_unit8(const RowsParams& p, const RowsUnit& u, Combine sm, Nt&& nt, int part_rows) {
   using S = Step8<D>;
@@ -407,6 +452,13 @@ __device__ __forceinline__ void rows_unit8(const RowsParams& p, const RowsUnit& 
     for (int b = 0; b < DB; b++) r.v[b] = load16<decltype(nt_flag)::value>(src + 256 * b);
   };
   const float scale = PAGE ? p.scale_log2 : p.scale_log2 * p.k_scale[u.head];
+  const int all_see = p.causal ? u.keys - (u.ntok - 1) : u.keys;  // keys [0, all_see) are visible to every row
+  // some row does not see all of a step's keys: the weight of such a key is 0 there, but 0 * NaN is not
+  auto hides = [&](int step) {
+    const int end = u.key_begin + KEYS * (step + 1);
+    return PAGE && (end < u.key_end ? end : u.key_end) > all_see;
+  };
+  uint32_t nans = 0;  // codes of such steps that are NaN: zeros in the products, told to the rows at the end
   State<D, NB> st;
   st.clear();
   auto compute = [&](int step, S& r, auto tail_flag, auto nt_flag) {
@@ -459,6 +511,7 @@ __device__ __forceinline__ void rows_unit8(const RowsParams& p, const RowsUnit& 
     for (int d = 0; d < DB; d++) {
       uint4 c = r.v[d];
       if constexpr (TAIL) c = make_uint4(c.x & mask[0], c.y & mask[1], c.z & mask[2], c.w & mask[3]);
+      if (TAIL && PAGE && hides(step)) c = without_nans(c, nans);  // uniform
       const bf16x8 lo = __builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.x, c.y), vby));
       const bf16x8 hi = __builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.z, c.w), vby));
 #pragma unroll
@@ -477,7 +530,6 @@ __device__ __forceinline__ void rows_unit8(const RowsParams& p, const RowsUnit& 
     load_k(w, r, std::false_type{});
     load_v(w, r, std::false_type{});
   }
-  const int all_see = p.causal ? u.keys - (u.ntok - 1) : u.keys;  // keys [0, all_see) are visible to every row
   const int whole = ((all_see < u.key_end ? all_see : u.key_end) - u.key_begin);
   const int n_full = whole > 0 ? whole / KEYS : 0;
   int j = wave;
@@ -485,7 +537,19 @@ __device__ __forceinline__ void rows_unit8(const RowsParams& p, const RowsUnit& 
     for (; j < n_full; j += kWaves) compute(j, r, std::false_type{}, std::true_type{});
   else
     for (; j < n_full; j += kWaves) compute(j, r, std::false_type{}, std::false_type{});
+  const int first_tail = j;
   for (; j < n_steps; j += kWaves) compute(j, r, std::true_type{}, std::false_type{});
+  if constexpr (PAGE) {
+    if (__any(nans != 0))
+      for (j = first_tail; j < n_steps; j += kWaves)
+        if (hides(j)) {
+          const char* v = vbase + (uint64_t)pick(ids_of(j), g & 1, g & 2) * page_bytes;
+          int seen[NB];
+#pragma unroll
+          for (int b = 0; b < NB; b++) seen[b] = limit[b] < u.key_end ? limit[b] : u.key_end;
+          nan_to_rows<D, NB>(v, u.key_begin + KEYS * j + 16 * g, seen, st);
+        }
+  }
   finish<D, NB>(p, u, sm, st, PAGE ? 1.0f : p.v_scale[u.head], part_rows);
 }
 

@@ -450,6 +450,36 @@ def test_a_nan_query_stays_in_its_row(setup, e, split):
     check_extend(s, held, q, 0.09, good)
 
 
+@pytest.mark.parametrize("split", [0, 64])
+@pytest.mark.parametrize("group,d,e", [(1, 64, 2), (4, 128, 5), (2, 64, 16), (3, 128, 21), (1, 128, 40), (16, 64, 4)])
+def test_a_nan_token_of_a_draft_reaches_no_token_before_it(setup, group, d, e, split):
+    """NaN in V of a drafted token, of one from before, and in a drafted K: only the rows that see
+    the token have it, V's in its dims alone; all else is what it is with zeros in its place."""
+    P, E, hkv = [300, 90, 0], [e, e, e], 2
+    n = [p + e for p in P]
+    tokens = [(0, 300 + e - 1), (0, 300 + e // 2), (1, 90 + e - 1), (1, 70), (2, 1)]  # (request, token)
+    for of_k in (False, True):
+        outs = []
+        for bad in (0.0, float("nan")):
+            s = setup(P, E, hkv, d)
+            kv = [s.normal(sum(n), hkv, d), s.normal(sum(n), hkv, d)]
+            for i, (r, t) in enumerate(tokens[:3] if of_k else tokens):
+                kv[0 if of_k else 1][sum(n[:r]) + t, i % hkv, 7 * i:7 * i + 3] = bad
+            s.fill(seed_rows=kv)
+            kvx.kv_pool_set_split_keys(s.pool, split)
+            outs.append(attend(s, s.normal(s.T, hkv * group, d), hkv * group, 0.09))
+        want = torch.zeros(s.T, hkv * group, d, dtype=torch.bool, device=DEV)
+        for i, (r, t) in enumerate(tokens[:3] if of_k else tokens):
+            h, first = i % hkv, sum(E[:r]) + max(0, t - P[r])
+            dims = slice(None) if of_k else slice(7 * i, 7 * i + 3)
+            want[first:sum(E[:r + 1]), h * group:(h + 1) * group, dims] = True
+        (good, good_lse), (out, lse) = outs
+        assert torch.equal(torch.isnan(out), want)
+        assert torch.equal(out[~want], good[~want])
+        seen = want.any(-1) if of_k else torch.zeros_like(want[..., 0])
+        assert torch.isnan(lse[seen]).all() and torch.equal(lse[~seen], good_lse[~seen])
+
+
 def gpu_attend(q, k, v, scale):
     """One query [Hq, d] over k, v [n, Hkv, d] in float64 on the GPU: output and its bound (page_ref.attend)."""
     Hq, d = q.shape
