@@ -12,6 +12,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <functional>
+#include <memory>
 #include <numeric>
 #include <queue>
 #include <string>
@@ -38,27 +39,31 @@ using kvx::StoreUnit;
 
 namespace {
 
-thread_local std::string g_last_error;
+// In place: an error is reported where host memory is short, too.
+thread_local char g_last_error[512];
 
-int fail(int code, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  g_last_error = buf;
+int set_error(int code, const char* fmt, va_list ap) noexcept {
+  vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
   return code;
 }
+
+int fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  set_error(code, fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+void clear_error() { g_last_error[0] = 0; }
 
 }  // namespace
 
 int kvx::report(int code, const char* fmt, ...) {
-  char buf[512];
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
+  set_error(code, fmt, ap);
   va_end(ap);
-  g_last_error = buf;
   return code;
 }
 
@@ -1096,10 +1101,10 @@ int tile_attention(kvx_pool* pool, const kvx_batch* batch, const std::vector<int
 
 extern "C" {
 
-const char* kvx_last_error(void) { return g_last_error.c_str(); }
+const char* kvx_last_error(void) { return g_last_error; }
 
 int kv_pool_set_split_keys(kvx_pool* pool, int32_t keys) {
-  g_last_error.clear();
+  clear_error();
   if (int rc = check_pool(pool)) return rc;
   if (keys < 0 || keys % kvx::kTileKeys != 0)
     return fail(KVX_EINVAL, "split keys %d: must be 0 or a positive multiple of %d", keys, kvx::kTileKeys);
@@ -1108,16 +1113,24 @@ int kv_pool_set_split_keys(kvx_pool* pool, int32_t keys) {
 }
 
 int kv_pool_set_scaled_q(kvx_pool* pool, int32_t enable) {
-  g_last_error.clear();
+  clear_error();
   if (int rc = check_pool(pool)) return rc;
   if (enable != 0 && enable != 1) return fail(KVX_EINVAL, "scaled_q %d: must be 0 or 1", enable);
   pool->scaled_q = enable;
   return KVX_OK;
 }
 
-int kv_pool_create(int64_t num_pages, int32_t page_size, int32_t num_kv_heads, int32_t head_dim,
-                   int32_t kv_dtype, const float* k_scale, const float* v_scale, kvx_pool** out) {
-  g_last_error.clear();
+// A pool's memory and its handle; the device is idle.
+static void free_pool(kvx_pool* pool) {
+  if (pool->k) (void)hipFree(pool->k);
+  if (pool->v) (void)hipFree(pool->v);
+  if (pool->scales_d) (void)hipFree(pool->scales_d);
+  if (pool->page_scales) (void)hipFree(pool->page_scales);
+  delete pool;
+}
+
+static int create_pool(int64_t num_pages, int32_t page_size, int32_t num_kv_heads, int32_t head_dim,
+                       int32_t kv_dtype, const float* k_scale, const float* v_scale, kvx_pool** out) {
   if (out == nullptr) return fail(KVX_EINVAL, "out is NULL");
   *out = nullptr;
   if (num_pages <= 0) return fail(KVX_EINVAL, "num_pages = %lld must be > 0", (long long)num_pages);
@@ -1140,30 +1153,25 @@ int kv_pool_create(int64_t num_pages, int32_t page_size, int32_t num_kv_heads, i
   const size_t bytes = (size_t)num_pages * num_kv_heads * page_size * head_dim * eb;
   if (bytes / (size_t)num_pages / (size_t)eb != (size_t)num_kv_heads * page_size * head_dim)
     return fail(KVX_EINVAL, "pool size overflows");
-  kvx_pool* p = new kvx_pool();
+  struct Unmade {
+    void operator()(kvx_pool* p) const { free_pool(p); }
+  };
+  std::unique_ptr<kvx_pool, Unmade> p(new kvx_pool());
   p->num_pages = num_pages;
   p->page_size = page_size;
   p->num_kv_heads = num_kv_heads;
   p->head_dim = head_dim;
   p->kv_dtype = kv_dtype;
   p->elem_bytes = eb;
-  auto cleanup = [&](int rc) {
-    if (p->k) (void)hipFree(p->k);
-    if (p->v) (void)hipFree(p->v);
-    if (p->scales_d) (void)hipFree(p->scales_d);
-    if (p->page_scales) (void)hipFree(p->page_scales);
-    delete p;
-    return rc;
-  };
   hipError_t e = hipGetDevice(&p->device);
-  if (e != hipSuccess) return cleanup(hip_fail(e, "hipGetDevice"));
+  if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
   e = hipMalloc(&p->k, bytes);
-  if (e != hipSuccess) return cleanup(hip_fail(e, "hipMalloc(K pool)"));
+  if (e != hipSuccess) return hip_fail(e, "hipMalloc(K pool)");
   e = hipMalloc(&p->v, bytes);
-  if (e != hipSuccess) return cleanup(hip_fail(e, "hipMalloc(V pool)"));
+  if (e != hipSuccess) return hip_fail(e, "hipMalloc(V pool)");
   e = hipMemset(p->k, 0, bytes);
   if (e == hipSuccess) e = hipMemset(p->v, 0, bytes);
-  if (e != hipSuccess) return cleanup(hip_fail(e, "hipMemset(pool)"));
+  if (e != hipSuccess) return hip_fail(e, "hipMemset(pool)");
   if (kv_dtype == KVX_KV_FP8_E4M3) {
     std::vector<float> s((size_t)4 * num_kv_heads);
     for (int h = 0; h < num_kv_heads; h++) {
@@ -1174,25 +1182,32 @@ int kv_pool_create(int64_t num_pages, int32_t page_size, int32_t num_kv_heads, i
     }
     e = hipMalloc(&p->scales_d, s.size() * sizeof(float));
     if (e == hipSuccess) e = hipMemcpy(p->scales_d, s.data(), s.size() * sizeof(float), hipMemcpyHostToDevice);
-    if (e != hipSuccess) return cleanup(hip_fail(e, "fp8 scales"));
+    if (e != hipSuccess) return hip_fail(e, "fp8 scales");
   }
   if (kv_dtype == KVX_KV_FP8_PAGE) {
     const size_t scale_bytes = (size_t)num_pages * num_kv_heads * 2 * sizeof(float);
     void* ptr = nullptr;
     e = hipMalloc(&ptr, scale_bytes);
-    if (e != hipSuccess) return cleanup(hip_fail(e, "hipMalloc(page scales)"));
+    if (e != hipSuccess) return hip_fail(e, "hipMalloc(page scales)");
     p->page_scales = (float*)ptr;
     e = hipMemset(ptr, 0, scale_bytes);
-    if (e != hipSuccess) return cleanup(hip_fail(e, "hipMemset(page scales)"));
+    if (e != hipSuccess) return hip_fail(e, "hipMemset(page scales)");
   }
   e = hipDeviceSynchronize();
-  if (e != hipSuccess) return cleanup(hip_fail(e, "hipDeviceSynchronize"));
-  *out = p;
+  if (e != hipSuccess) return hip_fail(e, "hipDeviceSynchronize");
+  *out = p.release();
   return KVX_OK;
 }
 
+int kv_pool_create(int64_t num_pages, int32_t page_size, int32_t num_kv_heads, int32_t head_dim,
+                   int32_t kv_dtype, const float* k_scale, const float* v_scale, kvx_pool** out) {
+  return kvx::guarded([&]() {
+    return create_pool(num_pages, page_size, num_kv_heads, head_dim, kv_dtype, k_scale, v_scale, out);
+  });
+}
+
 int kv_pool_destroy(kvx_pool* pool) {
-  g_last_error.clear();
+  clear_error();
   if (pool == nullptr) return KVX_OK;
   (void)use_device(pool);
   hipError_t e = hipDeviceSynchronize();
@@ -1202,17 +1217,13 @@ int kv_pool_destroy(kvx_pool* pool) {
   pool->st_io.release();
   pool->st_move.release();
   pool->parts.release();
-  if (pool->k) (void)hipFree(pool->k);
-  if (pool->v) (void)hipFree(pool->v);
-  if (pool->scales_d) (void)hipFree(pool->scales_d);
-  if (pool->page_scales) (void)hipFree(pool->page_scales);
-  delete pool;
+  free_pool(pool);
   if (e != hipSuccess) return hip_fail(e, "hipDeviceSynchronize");
   return KVX_OK;
 }
 
 int kv_pool_layout(const kvx_pool* pool, kvx_pool_layout* out) {
-  g_last_error.clear();
+  clear_error();
   if (int rc = check_pool(pool)) return rc;
   if (out == nullptr) return fail(KVX_EINVAL, "out is NULL");
   const int64_t S = pool->page_size, D = pool->head_dim, H = pool->num_kv_heads;
@@ -1276,13 +1287,13 @@ static int page_io(kvx_pool* pool, const int32_t* page_ids, int64_t n, void* k_l
 
 int kv_pool_write_pages(kvx_pool* pool, const int32_t* page_ids, int64_t n, const void* k_src, const void* v_src,
                         kvx_stream_t stream) {
-  g_last_error.clear();
+  clear_error();
   return page_io(pool, page_ids, n, const_cast<void*>(k_src), const_cast<void*>(v_src), 1, stream);
 }
 
 int kv_pool_read_pages(const kvx_pool* pool, const int32_t* page_ids, int64_t n, void* k_dst, void* v_dst,
                        kvx_stream_t stream) {
-  g_last_error.clear();
+  clear_error();
   return page_io(const_cast<kvx_pool*>(pool), page_ids, n, k_dst, v_dst, 0, stream);
 }
 
@@ -1297,7 +1308,7 @@ static int64_t record_bytes(const kvx_pool* pool) {
 }
 
 int kv_pool_record_bytes(const kvx_pool* pool, int64_t* bytes) {
-  g_last_error.clear();
+  clear_error();
   if (int rc = check_pool(pool)) return rc;
   if (bytes == nullptr) return fail(KVX_EINVAL, "bytes is NULL");
   *bytes = record_bytes(pool);
@@ -1358,14 +1369,13 @@ static int page_move(kvx_pool* pool, const int32_t* page_ids, const int32_t* slo
 
 int kv_pool_spill(const kvx_pool* pool, const int32_t* page_ids, const int32_t* slots, int64_t n, void* host,
                   int64_t host_slots, kvx_stream_t stream) {
-  g_last_error.clear();
-  return page_move(const_cast<kvx_pool*>(pool), page_ids, slots, n, host, host_slots, 1, stream);
+  return kvx::guarded(
+      [&]() { return page_move(const_cast<kvx_pool*>(pool), page_ids, slots, n, host, host_slots, 1, stream); });
 }
 
 int kv_pool_reload(kvx_pool* pool, const int32_t* page_ids, const int32_t* slots, int64_t n, const void* host,
                    int64_t host_slots, kvx_stream_t stream) {
-  g_last_error.clear();
-  return page_move(pool, page_ids, slots, n, host, host_slots, 0, stream);
+  return kvx::guarded([&]() { return page_move(pool, page_ids, slots, n, host, host_slots, 0, stream); });
 }
 
 // The launch of store_kv_rope, and of store_kv into a page-scaled pool: the call's arguments
@@ -1505,9 +1515,8 @@ int store_kv_rope(kvx_pool* pool, const kvx_batch* batch, const kvx_rope* rope, 
   });
 }
 
-int extend_attention_plan(const kvx_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
-                          int32_t split_keys, kvx_work_item* items, int64_t cap, int64_t* count) {
-  g_last_error.clear();
+static int list_items(const kvx_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                      int32_t split_keys, kvx_work_item* items, int64_t cap, int64_t* count) {
   if (count == nullptr) return fail(KVX_EINVAL, "count is NULL");
   *count = 0;
   if (int rc = check_heads(num_q_heads, num_kv_heads, head_dim)) return rc;
@@ -1538,6 +1547,12 @@ int extend_attention_plan(const kvx_batch* batch, int32_t num_q_heads, int32_t n
     for (int64_t i = 0; i < m; i++) items[i] = out_items[(size_t)i];
   }
   return KVX_OK;
+}
+
+int extend_attention_plan(const kvx_batch* batch, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                          int32_t split_keys, kvx_work_item* items, int64_t cap, int64_t* count) {
+  return kvx::guarded(
+      [&]() { return list_items(batch, num_q_heads, num_kv_heads, head_dim, split_keys, items, cap, count); });
 }
 
 int extend_attention(kvx_pool* pool, const kvx_batch* batch, const void* q, int32_t num_q_heads, float sm_scale,
