@@ -355,16 +355,10 @@ struct Step8 {
 // 0x80 in every byte of w that is a NaN code
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
-// NaN codes of c as zeros; nans: where there were any.
-__device__ __forceinline__ uint4 without_nans(uint4 c, uint32_t& nans) {
-  uint32_t* w = (uint32_t*)&c;
-#pragma unroll
-  for (int e = 0; e < 4; e++) {
-    const uint32_t is = nan_codes(w[e]);
-    nans |= is;
-    w[e] &= ~((is >> 7) * 0xFFu);
-  }
-  return c;
+// NaN codes of c as zeros
+__device__ __forceinline__ uint4 without_nans(uint4 c) {
+  auto clean = [](uint32_t w) { return w & ~((nan_codes(w) >> 7) * 0xFFu); };
+  return make_uint4(clean(c.x), clean(c.y), clean(c.z), clean(c.w));
 }
 
 // Rows that see a NaN value get NaN in its dim: where the product of "is NaN" (dims x keys) and "is
@@ -453,14 +447,16 @@ __device__ __forceinline__ void rows_unit8(const RowsParams& p, const RowsUnit& 
   };
   const float scale = PAGE ? p.scale_log2 : p.scale_log2 * p.k_scale[u.head];
   const int all_see = p.causal ? u.keys - (u.ntok - 1) : u.keys;  // keys [0, all_see) are visible to every row
-  // some row does not see all of a step's keys: the weight of such a key is 0 there, but 0 * NaN is not
+  // Some row does not see all of a step's keys: the weight of such a key is 0 there, but 0 * NaN is not.
+  // Where NaN came out of a unit with such steps, it is computed again without their NaN codes, and the
+  // rows that see these are told.  (Looking at the codes of each such step instead takes 0.5 us of a
+  // call on few keys; the look at the sums 0.1 to 0.3.)
   auto hides = [&](int step) {
     const int end = u.key_begin + KEYS * (step + 1);
     return PAGE && (end < u.key_end ? end : u.key_end) > all_see;
   };
-  uint32_t nans = 0;  // codes of such steps that are NaN: zeros in the products, told to the rows at the end
+  bool again = false;
   State<D, NB> st;
-  st.clear();
   auto compute = [&](int step, S& r, auto tail_flag, auto nt_flag) {
     constexpr bool TAIL = decltype(tail_flag)::value;
     const int next = step + kWaves;
@@ -511,7 +507,7 @@ __device__ __forceinline__ void rows_unit8(const RowsParams& p, const RowsUnit& 
     for (int d = 0; d < DB; d++) {
       uint4 c = r.v[d];
       if constexpr (TAIL) c = make_uint4(c.x & mask[0], c.y & mask[1], c.z & mask[2], c.w & mask[3]);
-      if (TAIL && PAGE && hides(step)) c = without_nans(c, nans);  // uniform
+      if (TAIL && PAGE && __builtin_expect(again, 0) && hides(step)) c = without_nans(c);  // uniform
       const bf16x8 lo = __builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.x, c.y), vby));
       const bf16x8 hi = __builtin_bit_cast(bf16x8, fp8x8_bf16(make_uint2(c.z, c.w), vby));
 #pragma unroll
@@ -524,31 +520,45 @@ __device__ __forceinline__ void rows_unit8(const RowsParams& p, const RowsUnit& 
     }
     if (more) load_v(nx, r, nt_flag);
   };
-  S r;
-  if (wave < n_steps) {
-    const ids_t w = ids_of(wave);
-    load_k(w, r, std::false_type{});
-    load_v(w, r, std::false_type{});
-  }
   const int whole = ((all_see < u.key_end ? all_see : u.key_end) - u.key_begin);
   const int n_full = whole > 0 ? whole / KEYS : 0;
-  int j = wave;
-  if (nt())
-    for (; j < n_full; j += kWaves) compute(j, r, std::false_type{}, std::true_type{});
-  else
-    for (; j < n_full; j += kWaves) compute(j, r, std::false_type{}, std::false_type{});
-  const int first_tail = j;
-  for (; j < n_steps; j += kWaves) compute(j, r, std::true_type{}, std::false_type{});
-  if constexpr (PAGE) {
-    if (__any(nans != 0))
-      for (j = first_tail; j < n_steps; j += kWaves)
-        if (hides(j)) {
-          const char* v = vbase + (uint64_t)pick(ids_of(j), g & 1, g & 2) * page_bytes;
-          int seen[NB];
+  for (;;) {
+    st.clear();
+    S r;
+    if (wave < n_steps) {
+      const ids_t w = ids_of(wave);
+      load_k(w, r, std::false_type{});
+      load_v(w, r, std::false_type{});
+    }
+    int j = wave;
+    if (nt())
+      for (; j < n_full; j += kWaves) compute(j, r, std::false_type{}, std::true_type{});
+    else
+      for (; j < n_full; j += kWaves) compute(j, r, std::false_type{}, std::false_type{});
+    const int first_tail = j;
+    for (; j < n_steps; j += kWaves) compute(j, r, std::true_type{}, std::false_type{});
+    if (!PAGE || all_see >= u.key_end || first_tail >= n_steps) break;
+    if (!again) {
+      float sum = 0.f;
 #pragma unroll
-          for (int b = 0; b < NB; b++) seen[b] = limit[b] < u.key_end ? limit[b] : u.key_end;
-          nan_to_rows<D, NB>(v, u.key_begin + KEYS * j + 16 * g, seen, st);
-        }
+      for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int d = 0; d < DB; d++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) sum += st.o[b][d][e];
+      again = __any(sum != sum);
+      if (!again) break;
+      continue;
+    }
+    for (j = first_tail; j < n_steps; j += kWaves)
+      if (hides(j)) {
+        const char* v = vbase + (uint64_t)pick(ids_of(j), g & 1, g & 2) * page_bytes;
+        int seen[NB];
+#pragma unroll
+        for (int b = 0; b < NB; b++) seen[b] = limit[b] < u.key_end ? limit[b] : u.key_end;
+        nan_to_rows<D, NB>(v, u.key_begin + KEYS * j + 16 * g, seen, st);
+      }
+    break;
   }
   finish<D, NB>(p, u, sm, st, PAGE ? 1.0f : p.v_scale[u.head], part_rows);
 }
