@@ -966,6 +966,14 @@ void add_rows(std::vector<RowsRequest>& reqs, int32_t qo_row, int32_t tokens, in
 // 13.6 / 15.8 / 20.7 / - / - / 18.3; 10 times 27 of 28/14/128 on 376 to 2651, fp8, 33 / 28 / 23 / 26.5 / - / 26.2.
 // Merges estimated at 10 us leave the last but one and 10 times 9 of 5/5/128 on 1193 to 1920 whole (18.7
 // and 14.3, now 14.7 and 10.7); at 5 us the 48 single queries are cut too.
+//
+// A plan that does not fit the kernel's arguments goes through a copy, which costs 5 to 7 us a call.
+// Fewer, longer ranges that fit are taken instead while the time that they are estimated to add stays
+// below that; the longest entry's partial results, which one workgroup merges one after the
+// other, count 0.09 us each (half of it for 64 dims) for the shorter ranges.  us a call with longer ranges in
+// the arguments / with the copy, 8/1/128 heads, page-scaled: 100 decodes on 200 and one on 131072
+// keys 31.7 / 46.8, 130 and one 42.3 / 47.4, 133 and one 249 / 48 (ranges of 52800 keys, for some 400:
+// what there is room for beside six words an entry); 134 on 100 to 30000 148 / 42.
 struct RowsPlan {
   std::vector<uint32_t> words;
   int64_t n_codes = 0, n_parts = 0;
@@ -980,38 +988,50 @@ RowsPlan make_rows_plan(const std::vector<RowsRequest>& reqs, int32_t Hkv, int32
     longest = std::max(longest, q.keys);
   }
   constexpr int64_t kSlots = 512;
-  constexpr double kMerge = 6.0, kBytesPerUs = 5.6e6;
+  constexpr double kMerge = 6.0, kBytesPerUs = 5.6e6, kCopy = 6.0, kMergeByte = 0.09 / 512;
   const double read = (double)total * key_bytes / kBytesPerUs, rate = bf16 ? 120.0 : 200.0;
+  auto done_by = [&](int64_t most) { return std::max((double)most / rate, read + 0.5 * (double)most / rate); };
   int64_t len = split_keys;
   if (split_keys == 0) {
     const int64_t share = ceil_div(total, kSlots);
     len = share <= 1024 ? std::max<int64_t>(384, share) : std::max<int64_t>(1024, share * blocks / 4);
-    auto done_by = [&](int64_t most) { return std::max((double)most / rate, read + 0.5 * (double)most / rate); };
     if (len < longest && done_by(longest) < 0.9 * (done_by(len) + kMerge)) len = longest;
   }
   auto len_of = [&](int64_t keys) {  // of an entry's ranges, all alike unless forced
     if (split_keys > 0) return len;
     return std::max(A, ceil_div(ceil_div(keys, std::max<int64_t>(1, ceil_div(keys, len))), A) * A);
   };
-  for (;;) {  // longer ranges: to bound the parts, and to keep a small batch's plan in the kernel arguments
-    int64_t parts = 0, most = 0, codes = 0;
-    for (const RowsRequest& q : reqs) {
-      const int64_t n = ceil_div(std::max<int64_t>(1, q.keys), len_of(q.keys));
-      if (n > 1) parts += n * Hkv;
-      most = std::max(most, n);
-      codes += n;
+  auto ranges_of = [&](int64_t keys) { return ceil_div(std::max<int64_t>(1, keys), len_of(keys)); };
+  struct Count {
+    int64_t parts = 0, most = 0, codes = 0, unit = 0;  // most: of an entry; unit: keys of the longest range
+  };
+  auto lengthen_until = [&](auto&& fits) {
+    for (;; len = ceil_div(len * 5 / 4, A) * A) {
+      Count c;
+      for (const RowsRequest& q : reqs) {
+        const int64_t n = ranges_of(q.keys);
+        if (n > 1) c.parts += n * Hkv;
+        c.most = std::max(c.most, n);
+        c.codes += n;
+        c.unit = std::max(c.unit, std::min(q.keys, len_of(q.keys)));
+      }
+      if (fits(c)) return c;
     }
-    const int64_t fit = kvx::kRowsWords - (int64_t)reqs.size() * kvx::kRowsEntryWords;
-    const bool tighten =
-        split_keys == 0 && total * key_bytes <= kStreamBytes && codes > fit && (int64_t)reqs.size() <= fit;
-    if (parts <= max_parts && most <= kMaxRanges && !tighten) break;
-    len = ceil_div(len * 5 / 4, A) * A;
+  };
+  const Count shortest = lengthen_until([&](const Count& c) { return c.parts <= max_parts && c.most <= kMaxRanges; });
+  const int64_t room = kvx::kRowsWords - (int64_t)reqs.size() * kvx::kRowsEntryWords;  // of codes in the arguments
+  if (split_keys == 0 && total * key_bytes <= kStreamBytes && shortest.codes > room && (int64_t)reqs.size() <= room) {
+    const int32_t row_bytes = key_bytes / (bf16 ? 4 : 2) * (int32_t)sizeof(float);  // of a partial result
+    auto cost = [&](const Count& c) { return done_by(c.unit) + (c.most > 1 ? (double)c.most * row_bytes * kMergeByte : 0.0); };
+    const int64_t with_copy = len;
+    const Count fitting = lengthen_until([&](const Count& c) { return c.codes <= room; });
+    if (cost(fitting) > cost(shortest) + kCopy) len = with_copy;
   }
   RowsPlan plan;
   std::vector<std::pair<int64_t, uint32_t>> codes;  // length, code
   for (size_t i = 0; i < reqs.size(); i++) {
     const RowsRequest& q = reqs[i];
-    const int64_t l = len_of(q.keys), n = ceil_div(std::max<int64_t>(1, q.keys), l);
+    const int64_t l = len_of(q.keys), n = ranges_of(q.keys);
     RowsEntry e{q.qo_row, q.ntok, q.page_base, (int32_t)q.keys, n > 1 ? (int32_t)plan.n_parts : -1,
                 (int32_t)std::min<int64_t>(l, INT32_MAX / A * A)};
     plan.words.resize(plan.words.size() + kvx::kRowsEntryWords);

@@ -6,6 +6,7 @@
 #include "kvx_host.cpp"
 #include "kvx_load.cpp"
 
+#include <cmath>
 #include <functional>
 #include <new>
 #include <string>
@@ -190,12 +191,77 @@ void messages() {
   CHECK(kv_pool_destroy(p) == KVX_OK);
 }
 
+// The ranges of a plan of few rows: longest unit and ranges of the longest entry; whether it fits
+// the kernel's arguments.
+struct Ranges {
+  int64_t longest = 0, of_longest = 0;
+  bool in_args = false;
+};
+Ranges ranges_of(const std::vector<RowsRequest>& reqs, int32_t heads, int32_t head_dim, bool bf16) {
+  const RowsPlan plan = make_rows_plan(reqs, heads, 1, 2 * head_dim * (bf16 ? 2 : 1), bf16, 0, kMaxParts);
+  Ranges r;
+  r.in_args = plan.words.size() <= (size_t)kvx::kRowsWords;
+  int64_t keys = 0, codes = 0;
+  for (size_t i = 0; i < reqs.size(); i++) {
+    RowsEntry e;
+    std::memcpy(&e, plan.words.data() + i * kvx::kRowsEntryWords, sizeof e);
+    CHECK(e.keys == reqs[i].keys && e.len > 0 && e.len % kvx::kDecodeChunkAlign == 0);
+    const int64_t n = e.keys > 0 ? (e.keys - 1) / e.len + 1 : 1;
+    r.longest = std::max<int64_t>(r.longest, std::min(e.keys, e.len));
+    if (e.keys > keys) {
+      keys = e.keys;
+      r.of_longest = n;
+    }
+    codes += n;
+  }
+  CHECK(plan.n_codes == codes && (int64_t)plan.words.size() == codes + (int64_t)reqs.size() * kvx::kRowsEntryWords);
+  return r;
+}
+
+// Ranges are lengthened for room in the kernel's arguments only where the longest unit's time, at 200 or 120 keys a
+// microsecond, grows by less than the copy and the merging that this saves; half of that growth
+// may pass where reading all keys takes longer.  With as many entries without keys as leave no room the
+// ranges are not lengthened.
+void ranges() {
+  std::vector<std::vector<int32_t>> lens;
+  for (const int n : {1, 60, 100, 130, 132, 133, 134, 135, 200})
+    for (const int32_t last : {3000, 30000, 100000, 131072, 262144}) {
+      lens.emplace_back((size_t)n, 200);
+      lens.back().push_back(last);
+    }
+  uint32_t rng = 12345;
+  auto next = [&]() { return (rng = rng * 1664525u + 1013904223u) >> 8; };
+  for (int trial = 0; trial < 400; trial++) {
+    lens.emplace_back();
+    for (int n = 1 + (int)(next() % 145); n > 0; n--)
+      lens.back().push_back((int32_t)std::exp(4.0 + (next() % 1000) / 1000.0 * (trial % 2 ? 6.3 : 4.0)));
+  }
+  bool fitted = false, copied = false;
+  for (const auto& l : lens)
+    for (const int32_t heads : {1, 4})
+      for (const int32_t head_dim : {64, 128})
+        for (const bool bf16 : {false, true}) {
+          std::vector<RowsRequest> reqs;
+          for (const int32_t keys : l) reqs.push_back(RowsRequest{0, 1, 0, keys});
+          const Ranges r = ranges_of(reqs, heads, head_dim, bf16);
+          reqs.resize(reqs.size() + 200, RowsRequest{0, 1, 0, 0});
+          const Ranges free = ranges_of(reqs, heads, head_dim, bf16);
+          const double rate = bf16 ? 120.0 : 200.0, saved = 6.0 + 0.09 * head_dim / 128.0 * (double)free.of_longest;
+          CHECK(!free.in_args && r.longest >= free.longest - kvx::kDecodeChunkAlign);
+          CHECK((double)(r.longest - free.longest) <= 2.0 * rate * saved + 2 * kvx::kDecodeChunkAlign);
+          fitted |= r.longest > free.longest + 64 && r.in_args;
+          copied |= !r.in_args && reqs.size() - 200 <= 130;
+        }
+  CHECK(fitted && copied);  // either choice is made
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
   const std::string what = argc > 1 ? argv[1] : "";
   if (what == "memory") memory();
   else if (what == "messages") messages();
+  else if (what == "ranges") ranges();
   else return 2;
   std::printf("%s passed\n", what.c_str());
   return 0;

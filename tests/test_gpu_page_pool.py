@@ -430,6 +430,17 @@ def test_drafts(setup, P, E, hkv, group, d):
     check_extend(s, held, q, 0.09, out, lse)
 
 
+@pytest.mark.parametrize("n", [100, 132, 133])
+def test_a_long_request_beside_many_short_ones(setup, n):
+    """A plan of few ranges for the kernel's arguments, and of many that go through a copy."""
+    P = [(7 * i) % 60 for i in range(n)] + [60000]
+    s = setup(P, [1] * (n + 1), 1, 64)
+    held = s.fill()
+    q = s.normal(s.T, 4, 64)
+    out, lse = attend(s, q, 4, 0.125)
+    check_extend(s, held, q, 0.125, out, lse)
+
+
 @pytest.mark.parametrize("e", [1, 3, 200])
 @pytest.mark.parametrize("split", [0, 64])
 def test_a_nan_query_stays_in_its_row(setup, e, split):

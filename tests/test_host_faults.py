@@ -1,6 +1,6 @@
-"""The KV pool's host code where host memory stays short, and what it says then, on the CPU over a
-stand-in for the HIP runtime (tests/sanitize/host_faults.cpp, built with AddressSanitizer and
-UndefinedBehaviorSanitizer)."""
+"""The KV pool's host code where host memory stays short and what it says then, and the lengths
+of key ranges in batches of few rows, on the CPU over a stand-in for the HIP runtime
+(tests/sanitize/host_faults.cpp, built with AddressSanitizer and UndefinedBehaviorSanitizer)."""
 
 import os
 import shutil
@@ -28,7 +28,7 @@ def driver(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("check", ["memory", "messages"])
+@pytest.mark.parametrize("check", ["memory", "messages", "ranges"])
 def test_host_calls(driver, check, tmp_path):
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
     run = subprocess.run([driver, check], capture_output=True, text=True, env=env, timeout=300, cwd=tmp_path)
