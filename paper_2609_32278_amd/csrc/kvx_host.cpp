@@ -930,8 +930,9 @@ struct RowsRequest {
 // tiles, requests of one size: 24 x 12/12/64 heads on 1200 keys, bf16 pool: 96 rows 38 / 51, 128 rows 44 / 53,
 // on 8000 keys 300 / 267; 8/8/128 heads, bf16: 64 rows 39 / 39, 96 rows 52 / 40; 8-bit pools, 128
 // rows: 12/12/64 heads 32 / 54, 8/8/128 38 / 45 (8000 keys 176 / 265, 214 / 258), 192 rows 8/8/128
-// 67 / 48.  Both kinds in one batch take two launches, which loses against either: 24 requests of
-// 3 to 224 rows of 12/12/64 heads on 700 to 1800 keys 53 / 40, both 61.
+// 67 / 48.  Both kinds in one batch take two launches, which loses against either on short keys: 24
+// requests of 3 to 224 rows of 12/12/64 heads on 700 to 1800 keys 53 / 40, both 61.  (Not on long ones: 40 times 1
+// query and 8 times 1200 of 32/8/128 heads on 6000, page-scaled, tiles 1015, both 950.)
 int64_t entries_per_tile(const kvx_pool* pool) {
   if (pool->kv_dtype != KVX_KV_BF16) return 4;
   return pool->head_dim == 64 ? 3 : 2;

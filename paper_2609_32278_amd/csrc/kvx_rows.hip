@@ -14,10 +14,10 @@
 // have read them.  The waves' results meet in LDS, 16 rows at a time; ranges of a split key range
 // by log-sum-exp in a second kernel.
 //
-// Kernel times: 24 agents of 16k to 131k tokens, 64/8/128 heads, page-scaled pool, 456 us
-// (6.2 TB/s); 48 single queries on 200 to 1500 tokens, 16/16/64 heads, bf16 pool, 21.3 us
+// Kernel times: 24 agents of 16k to 131k tokens, 64/8/128 heads, page-scaled pool, 454 us
+// (6.3 TB/s); 48 single queries on 200 to 1500 tokens, 16/16/64 heads, bf16 pool, 21.3 us
 // (5.4 TB/s); drafts of 1 to 5 tokens of 33 requests on 2k to 20k, 64/8/128 heads, page-scaled pool,
-// 114 us and the merge 5.4.  Each against what was measured in its place: 64 rows a unit (a
+// 112 us and the merge 5.  Each against what was measured in its place: 64 rows a unit (a
 // wave then has no registers for loads in flight) 160 us for those drafts against 120; 64 keys a step
 // of a bf16 pool 33 us for the single queries against 21; page ids read with the loads that need
 // them, not a step ahead, 31 against 21.
