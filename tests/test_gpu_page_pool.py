@@ -654,3 +654,52 @@ def test_a_turn_from_start_to_end(setup):
             o, _, to, _ = ref.attend(ref.f64(q[at:at + e[r]]), kr, vr, 0.09, seen=np.arange(lens[r] - e[r] + 1, lens[r] + 1))
             ref.check(ref.f64(out[at:at + e[r]]), o, to, f"step {step}, request {r}")
             at += e[r]
+
+
+# ------------------------------------------------------------------- a run of turns
+
+
+def test_agents_through_the_prefix_cache():
+    """Agents whose histories the round-robin prefix cache keeps in a page-scaled pool too small for all, with a
+    host tier: prefixes that stayed or come back with their scales are attended where they lie,
+    what was dropped is stored again."""
+    hkv, group, d, num_pages, host_pages = 2, 4, 64, 44, 8
+    pool = kvx.kv_pool_create(num_pages, 16, hkv, d, PAGE)
+    cache = kvx.kvx_cache_create_tiered(num_pages, host_pages, 16, 64, kvx.KVX_EVICT_RR)
+    host = torch.empty(host_pages * kvx.kv_pool_record_bytes(pool), dtype=torch.uint8, pin_memory=True)
+    g = torch.Generator(DEV).manual_seed(12)
+    rng = np.random.default_rng(12)
+    kv = [[torch.randn(700, hkv, d, device=DEV, generator=g, dtype=BF16) * 2.0 ** a for _ in range(2)] for a in (-3, 0, 2, 5)]
+    lens, reloaded, missed = [0] * 4, 0, 0
+    try:
+        for turn in range(6):
+            for agent in range(4):
+                before = lens[agent]
+                lens[agent] += int(rng.integers(1, 12) if turn % 2 else rng.integers(40, 110))
+                prefix, table, moves = kvx.kvx_cache_begin_turn_tiered(cache, agent, lens[agent])
+                if len(moves["spill_pages"]):
+                    kvx.kv_pool_spill(pool, moves["spill_pages"], moves["spill_slots"], host, host_pages)
+                if len(moves["reload_pages"]):
+                    kvx.kv_pool_reload(pool, moves["reload_pages"], moves["reload_slots"], host, host_pages)
+                reloaded += len(moves["reload_pages"])
+                missed += before - min(prefix, before) > 16
+                n, e = lens[agent], lens[agent] - prefix
+                k, v = kv[agent]
+                b = kvx.Batch([prefix], [e], [0, len(table)], torch.from_numpy(table).to(DEV))
+                kvx.store_kv(pool, b, k[prefix:n], v[prefix:n])
+                scale = 0.1 / float(k.float().std()) ** 2
+                q = torch.randn(e, hkv * group, d, device=DEV, generator=g, dtype=BF16) * float(k.float().std())
+                out = torch.empty_like(q)
+                kvx.extend_attention(pool, b, q, hkv * group, scale, out)
+                kvx.kvx_cache_end_turn(cache, agent)
+                # the whole history from its own rows, not from the pool
+                held = ref.PagePool(-(-n // 16), hkv, d)
+                held.store(lambda r: np.arange(-(-n // 16)), [0], [n], ref.f64(k[:n]), ref.f64(v[:n]))
+                rows = held.rows(np.arange(-(-n // 16)), 0, n)
+                o, _, tol, _ = ref.attend(ref.f64(q), *rows, scale, seen=np.arange(prefix + 1, n + 1))
+                ref.check(ref.f64(out), o, tol, f"turn {turn}, agent {agent}")
+        assert reloaded > 0 and missed > 0
+    finally:
+        torch.cuda.synchronize()
+        kvx.kvx_cache_destroy(cache)
+        kvx.kv_pool_destroy(pool)
