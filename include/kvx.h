@@ -269,6 +269,8 @@ int store_kv_rope(kvx_pool *pool, const kvx_batch *batch, const kvx_rope *rope, 
  *   out          device bf16 [T, num_q_heads, head_dim] (round to nearest even)
  *   lse          device fp32 [T, num_q_heads] natural-log sum of exp of the scaled
  *                scores, or NULL
+ * A row with a NaN among its scores gives NaN in out and lse; the decode kernel of bf16 pools and of
+ * fp8 pools with a scale a head gives zeros and -inf there.
  * A decode step -- every request has at most one suffix token, and at most 16
  * query heads share a KV head -- runs a dedicated decode kernel (key chunks of
  * each request and KV head streamed from HBM); the result is the same operation.

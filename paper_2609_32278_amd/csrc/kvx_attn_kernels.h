@@ -534,7 +534,7 @@ __device__ __forceinline__ void write_result(const AttnParams& p, const Rows& r,
   using G = Geom<D>;
   const float l_tot = pair_sum(l_run);
   const float inv = l_tot > 0.0f ? vscale / l_tot : 0.0f;
-  const float lse_val = l_tot > 0.0f ? (m_run + __log2f(l_tot)) * kLn2 : -INFINITY;
+  const float lse_val = (m_run + __log2f(l_tot)) * kLn2;  // -inf of a sum of 0, NaN of a NaN
   if (r.u.part < 0) {
     if (r.valid) {
       uint16_t* dst = p.out + ((size_t)(r.u.qo_row0 + r.tok) * p.num_q_heads + r.hq) * D;

@@ -71,7 +71,7 @@ struct CombineShared {
 // Lane (n, g) holds dims 16 b + 4 g + i of row n, relative to its row maximum m_run
 // (log2 units), and the part l_run of the row sum over its own keys.  A row whose sum is a
 // NaN (a NaN or an infinite score) is written as zeros, and as NaN with NANS, which is
-// what a prefill tile gives: one-token requests beside longer ones keep that.  They also
+// what a prefill tile gives: one-token requests beside longer ones keep that, in the lse too.  They also
 // get a tile's `none` where no score is above -inf: 0, on an fp8 pool NaN.
 template <int D, int NW, bool NANS>
 __device__ __forceinline__ void combine_waves(const DecodeArgs& p, const DecodeUnit& u, CombineShared<D, NW> sm,
@@ -104,7 +104,7 @@ __device__ __forceinline__ void combine_waves(const DecodeArgs& p, const DecodeU
       }
     }
     const float val = wsum > 0.f ? acc * vscale / wsum : !NANS ? 0.f : wsum == 0.f ? none : acc * 0.f;
-    const float lse_v = wsum > 0.f ? (M + __log2f(wsum)) * kLn2 : -INFINITY;
+    const float lse_v = NANS || wsum > 0.f ? (M + __log2f(wsum)) * kLn2 : -INFINITY;  // log2(0) = -inf, NaN stays
     if (u.part < 0) {
       const size_t orow = (size_t)u.qo_row * p.num_q_heads + u.head * G + row;
       p.out[orow * D + d] = __builtin_bit_cast(uint16_t, (__bf16)val);

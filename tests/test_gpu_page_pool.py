@@ -491,6 +491,60 @@ def test_a_nan_token_of_a_draft_reaches_no_token_before_it(setup, group, d, e, s
         assert torch.isnan(lse[seen]).all() and torch.equal(lse[~seen], good_lse[~seen])
 
 
+@pytest.mark.parametrize("scaled_q", [0, 1])
+@pytest.mark.parametrize("split", [0, 128])
+@pytest.mark.parametrize("dtype", [PAGE, kvx.KVX_KV_BF16])
+def test_a_nan_token_in_a_tile(setup, dtype, split, scaled_q):
+    """NaN in K of a suffix token: the rows that see it, and no other.  In V: those, and at most the rows of
+    the same tile (256 / 4 tokens) before it."""
+    P, E, hkv, group, d, t = [70, 33], [200, 180], 2, 4, 128, 150
+    outs = []
+    for of_k, bad in ((False, 0.0), (True, float("nan")), (False, float("nan"))):
+        s = setup(P, E, hkv, d, dtype)
+        kv = [s.normal(sum(P) + sum(E), hkv, d), s.normal(sum(P) + sum(E), hkv, d)]
+        kv[0][P[0] + t, 1, :4] = kv[1][P[0] + t, 1, :4] = 0.0
+        kv[0 if of_k else 1][P[0] + t, 1, :4] = bad
+        s.fill(seed_rows=kv)
+        kvx.kv_pool_set_split_keys(s.pool, split)
+        kvx.kv_pool_set_scaled_q(s.pool, scaled_q)
+        outs.append(attend(s, s.normal(s.T, hkv * group, d), hkv * group, 0.09))
+    (good, good_lse), (k_out, k_lse), (v_out, v_lse) = outs
+    sees = torch.zeros(s.T, hkv * group, dtype=torch.bool, device=DEV)
+    sees[t:E[0], group:] = True
+    assert torch.isnan(k_out[sees]).all() and torch.isnan(k_lse[sees]).all()
+    assert torch.equal(k_out[~sees], good[~sees]) and torch.equal(k_lse[~sees], good_lse[~sees])
+    assert torch.isnan(v_out[sees][:, :4]).all() and torch.equal(v_out[..., 4:], good[..., 4:])
+    may = sees.clone()
+    may[t // 64 * 64:t, group:] = True
+    assert torch.equal(v_out[~may], good[~may]) and torch.equal(v_lse, good_lse)
+
+
+@pytest.mark.parametrize("split", [0, 128])
+@pytest.mark.parametrize("dtype", [PAGE, kvx.KVX_KV_BF16, kvx.KVX_KV_FP8_E4M3])
+@pytest.mark.parametrize("P,E,cross", [
+    ([70, 33], [200, 180], False),           # tiles
+    ([3000, 500, 900], [1, 1, 300], False),  # decode units beside tiles
+    ([300, 90], [3, 2], False),              # few rows on a page-scaled pool, else tiles
+    ([900, 40], [200, 150], True),
+    ([700, 90], [1, 2], True),
+])
+def test_a_nan_score_makes_the_lse_nan(setup, P, E, cross, dtype, split):
+    """An lse of -inf would say that a row saw no key, and a join by lse would leave it out."""
+    hkv, group, d = 2, 4, 64
+    s = setup(P, E, hkv, d, dtype, cross=cross)
+    s.fill(P if cross else None)
+    kvx.kv_pool_set_split_keys(s.pool, split)
+    q = s.normal(s.T, hkv * group, d)
+    call = kvx.cross_attention if cross else kvx.extend_attention
+    good, good_lse = attend(s, q, hkv * group, 0.09, call)
+    q[0, 3, 5] = q[-1, 6, 0] = float("nan")
+    out, lse = attend(s, q, hkv * group, 0.09, call)
+    want = torch.zeros_like(lse, dtype=torch.bool)
+    want[0, 3] = want[-1, 6] = True
+    assert torch.equal(torch.isnan(lse), want) and torch.equal(torch.isnan(out), want[..., None].expand_as(out))
+    assert torch.equal(out[~want], good[~want]) and torch.equal(lse[~want], good_lse[~want])
+
+
 def gpu_attend(q, k, v, scale):
     """One query [Hq, d] over k, v [n, Hkv, d] in float64 on the GPU: output and its bound (page_ref.attend)."""
     Hq, d = q.shape
