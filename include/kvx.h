@@ -270,7 +270,8 @@ int store_kv_rope(kvx_pool *pool, const kvx_batch *batch, const kvx_rope *rope, 
  *   lse          device fp32 [T, num_q_heads] natural-log sum of exp of the scaled
  *                scores, or NULL
  * A row with a NaN among its scores gives NaN in out and lse; the decode kernel of bf16 pools and of
- * fp8 pools with a scale a head gives zeros and -inf there.
+ * fp8 pools with a scale a head takes the key range with that score as one without keys (zeros and
+ * -inf where it is the only one).
  * A decode step -- every request has at most one suffix token, and at most 16
  * query heads share a KV head -- runs a dedicated decode kernel (key chunks of
  * each request and KV head streamed from HBM); the result is the same operation.
